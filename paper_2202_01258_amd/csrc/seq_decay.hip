@@ -1,0 +1,504 @@
+// seq_decay.hip -- linear attention with a decay for each head: by chunks
+// (forward and backward) and the recurrent single-token step.  The C ABI is in
+// include/qd_seq.h.
+//
+// One recurrence serves every direction.  With rows x, y of DK and z of DV elements,
+//   M_i = a M_{i-1} + y_i^T z_i,   out_i = factor x_i M_i:
+//   o:  (x, y, z) = (q, k, v),   M the state S;
+//   dq: (do, v, k),              M = S^T;
+//   dv: (k, q, do), rows reversed, M = R = sum a^(t-s) q_t^T do_t + the state's gradient;
+//   dk: (v, do, q), rows reversed, M = R^T.
+// A chunk of 64 rows is
+//   out = ((x y^T) . a^(i-j) [j <= i]) z + a^(i+1) x M,   M <- a^64 M + (a^(63-j) y)^T z,
+// all products on the matrix cores, the state in registers.  By its bytes (each
+// row read and written once) the recurrence is bound by memory.
+#include "seq_common.hpp"
+
+namespace seq {
+namespace {
+
+constexpr int kChunk = 64;
+
+__device__ inline float decay_power(float lambda, int n) { return n == 0 ? 1.0f : fast_exp2(lambda * (float)n); }
+
+// One direction of the recurrence.
+struct Role {
+  View x, y, z, out;
+  const float* init;     // the state before the first row [b][h][dim_k][dim_v] of the caller's sides, or null
+  float* last;           // the state after the last row, or null
+  float* states;         // [b][h][segment][DK][DV]: each segment's own sum, then the state before it
+  float factor;          // of the outputs
+  float init_factor, last_factor;
+  bool reversed;         // rows from the last to the first
+  bool swapped;          // init and last are [dim_z][dim_x] (the transpose of M)
+};
+
+struct DecayArgs {
+  Role role[3];
+  const int32_t* lengths;
+  const float* log_decay;
+  int32_t batch, length, heads, dim_x, dim_z;
+  int32_t segments, segment_rows;     // segment_rows: a multiple of 64
+};
+
+__device__ inline int rows_of(const DecayArgs& a, int b) {
+  if (!a.lengths) return a.length;
+  return min(max(a.lengths[b], 0), a.length);
+}
+
+// Columns dt * 32 + l % 32 of a tile as rows (or columns) of an operand whose k
+// are the tile's rows row0 + 8 (l / 32) + e.
+template <class T, int DP> __device__ inline x8<T> tile_columns_straight(const T* lds, int row0, int dt) {
+  const int l = threadIdx.x & 63;
+  const int row = row0 + 8 * (l >> 5) + ((l & 15) >> 2);
+  const int col = dt * 32 + ((l >> 4) & 1) * 16 + (l & 3) * 4;
+  const x4<T> a = lds_read_transposed(lds + tile_at<DP>(row, col >> 3) + (col & 7));
+  const x4<T> b = lds_read_transposed(lds + tile_at<DP>(row + 4, col >> 3) + (col & 7));
+  return join8<T>(a, b);
+}
+// Rows row0 + l % 32 of a tile; k are the columns 16 u + 8 (e / 4) + 4 (l / 32) + e % 4,
+// the order in which a C tile holds its rows.
+template <class T, int DP> __device__ inline x8<T> tile_rows_as_c(const T* lds, int row0, int u) {
+  const int l = threadIdx.x & 63, row = row0 + (l & 31), in = 4 * (l >> 5);
+  const u32x2 a = *reinterpret_cast<const u32x2*>(lds + tile_at<DP>(row, 2 * u) + in);
+  const u32x2 b = *reinterpret_cast<const u32x2*>(lds + tile_at<DP>(row, 2 * u + 1) + in);
+  return __builtin_bit_cast(x8<T>, u32x4{a[0], a[1], b[0], b[1]});
+}
+
+// The state of one wave: all DK rows of 32 columns.  In memory [rows][cols], or transposed.
+template <int DK> struct State {
+  f32x16 m[DK / 32];
+  __device__ void zero() {
+#pragma unroll
+    for (int t = 0; t < DK / 32; ++t) m[t] = f32x16{};
+  }
+  __device__ void load(const float* p, int rows, int cols, int col, bool swapped, float factor) {
+#pragma unroll
+    for (int t = 0; t < DK / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int row = t * 32 + c_row(i);
+        m[t][i] = row < rows && col < cols ? factor * (swapped ? p[col * rows + row] : p[row * cols + col]) : 0.0f;
+      }
+  }
+  __device__ void store(float* p, int rows, int cols, int col, bool swapped, float factor) const {
+#pragma unroll
+    for (int t = 0; t < DK / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int row = t * 32 + c_row(i);
+        if (row < rows && col < cols) p[swapped ? col * rows + row : row * cols + col] = factor * m[t][i];
+      }
+  }
+};
+
+// How many numbers of 16 bits carry an fp32 one: the state is fp32, so its
+// summands a^(63-j) y_j z_j keep 24 bits (y is exact; z a^(63-j) is split).
+template <class T> struct Terms;
+template <> struct Terms<bf16> { static constexpr int n = 3; };
+template <> struct Terms<half> { static constexpr int n = 2; };
+
+// A workgroup has one batch element and head, and one segment of its rows; a wave
+// has 32 columns of the state and of the outputs.  Where there are too few heads
+// to fill the card, a sequence is cut into segments: with OUT false a segment
+// only forms its own sum, k_decay_scan turns the sums into the states before
+// the segments, and a second launch with OUT true starts from those.
+template <class T, int DK, int DV, bool OUT>
+__global__ __launch_bounds__(2 * DV, 1) void k_decay_chunks(DecayArgs a) {
+  constexpr int BLOCK = 2 * DV, WAVES = DV / 32;
+  SEQ_SHARED T sx[OUT ? kChunk * DK : 8], sy[kChunk * DK], sz[kChunk * DV];
+  SEQ_SHARED T sp[OUT ? kChunk * kChunk : 8];
+  SEQ_SHARED float s_age[kChunk];            // a^(rows - 1 - j) of the chunk's rows
+  const Role& role = a.role[blockIdx.z];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads;
+  const int n = rows_of(a, b);
+  const int first = blockIdx.y * a.segment_rows, end = min(first + a.segment_rows, n);
+  const float lambda = a.log_decay[h] * kLog2e;
+  const int64_t list = (int64_t)b * a.heads + h;
+  const int64_t turn = role.reversed ? n - 1 : 0, sign = role.reversed ? -1 : 1;
+  const T* xp = at<T>(role.x, b, turn, h);
+  const T* yp = at<T>(role.y, b, turn, h);
+  const T* zp = at<T>(role.z, b, turn, h);
+  const int64_t xs = sign * role.x.t, ys = sign * role.y.t, zs = sign * role.z.t;
+  const int col = wave * 32 + (lane & 31);
+
+  State<DK> st;
+  float* mine = role.states + (list * a.segments + blockIdx.y) * (DK * DV);
+  if (OUT && a.segments > 1)
+    st.load(mine, DK, DV, col, false, 1.0f);
+  else if (OUT && role.init)
+    st.load(role.init + list * a.dim_x * a.dim_z, a.dim_x, a.dim_z, col, role.swapped, role.init_factor);
+  else
+    st.zero();
+
+  if (first < end) {
+    Staged<T, DK, BLOCK> rx, ry;
+    Staged<T, DV, BLOCK> rz;
+    if (OUT) rx.load(xp, xs, first, end, a.dim_x);
+    ry.load(yp, ys, first, end, a.dim_x);
+    rz.load(zp, zs, first, end, a.dim_z);
+    for (int row0 = first; row0 < end; row0 += kChunk) {
+      const int count = min(kChunk, end - row0);
+      // the gradient of the last state meets the last row without a decay
+      const int less = role.reversed && row0 == 0 ? 1 : 0;
+      if (OUT) rx.store(sx);
+      ry.store(sy);
+      rz.store(sz);
+      if (threadIdx.x < kChunk)
+        s_age[threadIdx.x] = (int)threadIdx.x < count ? decay_power(lambda, count - 1 - threadIdx.x) : 0.0f;
+      __syncthreads();
+      if (row0 + kChunk < end) {
+        if (OUT) rx.load(xp, xs, row0 + kChunk, end, a.dim_x);
+        ry.load(yp, ys, row0 + kChunk, end, a.dim_x);
+        rz.load(zp, zs, row0 + kChunk, end, a.dim_z);
+      }
+      if (OUT) {
+        // Quarters (0, 0), (1, 0), (1, 1) of the products of rows, transposed (columns are i), one or two a wave.
+        for (int quarter = wave; quarter < 3; quarter += WAVES) {
+          const int ib = quarter > 0, jb = quarter > 1;
+          f32x16 s = f32x16{};
+#pragma unroll
+          for (int ks = 0; ks < DK / 16; ++ks)
+            s = mfma32(tile_rows<T, DK>(sy, jb * 32, ks), tile_rows<T, DK>(sx, ib * 32, ks), s);
+          const int i = ib * 32 + (lane & 31);
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            float p[4];
+            const int j = jb * 32 + 8 * r4 + 4 * (lane >> 5);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              p[e] = j + e <= i ? s[4 * r4 + e] * decay_power(lambda, i - j - e) : 0.0f;
+            *reinterpret_cast<u32x2*>(sp + tile_at<64>(i, j >> 3) + (j & 7)) =
+                __builtin_bit_cast(u32x2, pack4<T>(p[0], p[1], p[2], p[3]));
+          }
+        }
+        __syncthreads();
+      }
+      x8<T> z[4];
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) z[ks] = tile_columns_straight<T, DV>(sz, 16 * ks, wave);
+      if (OUT) {
+        // The products of rows and the state are rounded to the tensors' type for the
+        // output's products: as much as the output's own rounding.
+#pragma unroll
+        for (int ib = 0; ib < 2; ++ib) {
+          f32x16 o = f32x16{};
+#pragma unroll
+          for (int t = 0; t < DK / 32; ++t)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              float m[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) m[e] = st.m[t][8 * u + e];
+              o = mfma32(pack8<T>(m), tile_rows_as_c<T, DK>(sx, ib * 32, 2 * t + u), o);
+            }
+          const int i = ib * 32 + (lane & 31);
+          o *= decay_power(lambda, i + 1 - less);
+#pragma unroll
+          for (int ks = 0; ks < 2 * (ib + 1); ++ks) o = mfma32(z[ks], tile_rows<T, 64>(sp, ib * 32, ks), o);
+          if (i < count) {
+            const int64_t row = turn + sign * (row0 + i);
+            store_column<T>(at<T>(role.out, b, row, h), wave, o, role.factor, a.dim_z);
+          }
+        }
+      }
+      const float age = decay_power(lambda, count - less);
+#pragma unroll
+      for (int t = 0; t < DK / 32; ++t) st.m[t] *= age;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        x8<T> part[Terms<T>::n];
+        const int j = 16 * ks + 8 * (lane >> 5);
+        const f32x4 w0 = *reinterpret_cast<const f32x4*>(s_age + j), w1 = *reinterpret_cast<const f32x4*>(s_age + j + 4);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (float)z[ks][e] * (e < 4 ? w0[e & 3] : w1[e & 3]);
+#pragma unroll
+        for (int p = 0; p < Terms<T>::n; ++p) {
+          part[p] = pack8<T>(v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] -= (float)part[p][e];
+        }
+#pragma unroll
+        for (int t = 0; t < DK / 32; ++t) {
+          const x8<T> y = tile_columns_straight<T, DK>(sy, 16 * ks, t);
+#pragma unroll
+          for (int p = Terms<T>::n - 1; p >= 0; --p) st.m[t] = mfma32(y, part[p], st.m[t]);
+        }
+      }
+      __syncthreads();
+    }
+  }
+  if (!OUT) {
+    st.store(mine, DK, DV, col, false, 1.0f);
+    return;
+  }
+  if (a.segments == 1 && role.last) {
+    const float f = role.last_factor * (role.reversed && n > 0 ? decay_power(lambda, 1) : 1.0f);
+    st.store(role.last + list * a.dim_x * a.dim_z, a.dim_x, a.dim_z, col, role.swapped, f);
+  }
+  // rows past the end
+  const int stop = min(first + a.segment_rows, a.length);
+  const int packs = a.dim_z / 8;
+  for (int64_t x = threadIdx.x; x < (int64_t)(stop - max(first, n)) * packs; x += BLOCK) {
+    T* row = at<T>(role.out, b, max(first, n) + x / packs, h);
+    *reinterpret_cast<u32x4*>(row + x % packs * 8) = u32x4{0, 0, 0, 0};
+  }
+}
+
+// From each segment's own sum to the state before it; one element of M per thread.
+template <int DK, int DV> __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a) {
+  const Role& role = a.role[blockIdx.z];
+  const int64_t list = blockIdx.x / (DK * DV / 256);
+  const int e = blockIdx.x % (DK * DV / 256) * 256 + threadIdx.x, row = e / DV, col = e % DV;
+  const int b = (int)(list / a.heads), h = (int)(list % a.heads);
+  const int n = rows_of(a, b);
+  const float lambda = a.log_decay[h] * kLog2e;
+  const bool real = row < a.dim_x && col < a.dim_z;
+  const int64_t outer = list * a.dim_x * a.dim_z + (role.swapped ? col * a.dim_x + row : row * a.dim_z + col);
+  float m = role.init && real ? role.init_factor * role.init[outer] : 0.0f;
+  float* p = role.states + list * a.segments * (DK * DV) + e;
+#pragma unroll 4
+  for (int s = 0; s < a.segments; ++s, p += DK * DV) {
+    const int count = max(0, min(n - s * a.segment_rows, a.segment_rows));
+    const int less = role.reversed && s == 0 && count > 0 ? 1 : 0;
+    const float own = *p;
+    *p = m;
+    m = fmaf(m, decay_power(lambda, count - less), own);
+  }
+  if (role.last && real)
+    role.last[outer] = m * role.last_factor * (role.reversed && n > 0 ? decay_power(lambda, 1) : 1.0f);
+}
+
+// ---------------------------------------------------------------------------
+// Single-token step
+// ---------------------------------------------------------------------------
+struct StepArgs {
+  View q, k, v, o;
+  const float *log_decay, *state_in;
+  float* state_out;
+  int32_t heads, dim_k, dim_v;
+  float scale;
+};
+
+// Bound by reading and writing the states.  A workgroup has one state; a thread
+// has four columns of every (1024 / DV)-th row, so a wave's loads are contiguous.
+template <class T, int DK, int DV> __global__ __launch_bounds__(256) void k_decay_step(StepArgs a) {
+  constexpr int LANES = DV / 4, ROWS = 256 / LANES, N = DK / ROWS;
+  SEQ_SHARED float part[ROWS][DV];
+  const int col = threadIdx.x % LANES * 4, sub = threadIdx.x / LANES;
+  const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads;
+  const int64_t base = (int64_t)blockIdx.x * a.dim_k * a.dim_v;
+  const T *q = at<T>(a.q, b, 0, h), *k = at<T>(a.k, b, 0, h), *v = at<T>(a.v, b, 0, h);
+  const bool in_col = col < a.dim_v;
+  f32x4 s[N];
+  float qr[N], kr[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int row = i * ROWS + sub;
+    const bool real = row < a.dim_k && in_col;
+    s[i] = real ? *reinterpret_cast<const f32x4*>(a.state_in + base + (int64_t)row * a.dim_v + col) : f32x4{};
+    qr[i] = real ? (float)q[row] : 0.0f;
+    kr[i] = real ? (float)k[row] : 0.0f;
+  }
+  f32x4 vv = f32x4{};
+  if (in_col) {
+    const x4<T> raw = __builtin_bit_cast(x4<T>, *reinterpret_cast<const u32x2*>(v + col));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) vv[e] = (float)raw[e];
+  }
+  const float decay = fast_exp2(a.log_decay[h] * kLog2e);
+  f32x4 o = f32x4{};
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int row = i * ROWS + sub;
+    s[i] = s[i] * decay + vv * kr[i];
+    o += s[i] * qr[i];
+    if (row < a.dim_k && in_col) *reinterpret_cast<f32x4*>(a.state_out + base + (int64_t)row * a.dim_v + col) = s[i];
+  }
+  *reinterpret_cast<f32x4*>(&part[sub][col]) = o;
+  __syncthreads();
+  if ((int)threadIdx.x < a.dim_v) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) sum += part[r][threadIdx.x];
+    at<T>(a.o, b, 0, h)[threadIdx.x] = (T)(sum * a.scale);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------
+qds_status validate(const qds_decay_config* c) {
+  if (!c || c->abi_version != QDS_ABI_VERSION) return QDS_ERR_INVALID_ARG;
+  if (c->dtype != QDS_BF16 && c->dtype != QDS_F16)
+    return c->dtype == QDS_F32 ? QDS_ERR_UNSUPPORTED : QDS_ERR_INVALID_ARG;
+  if (c->batch < 0 || c->length < 0 || c->length >= (1 << 30) || c->heads < 1) return QDS_ERR_INVALID_ARG;
+  if (c->dim_k < 1 || c->dim_v < 1) return QDS_ERR_INVALID_ARG;
+  if (c->dim_k % 8 || c->dim_v % 8 || c->dim_k > 128 || c->dim_v > 128) return QDS_ERR_UNSUPPORTED;
+  if (!(c->scale > 0.0f) || c->scale > 3.0e38f) return QDS_ERR_INVALID_ARG;
+  if ((int64_t)c->batch * c->heads > (1 << 24)) return QDS_ERR_UNSUPPORTED;
+  return QDS_OK;
+}
+
+int pad(int dim) { return dim <= 64 ? 64 : 128; }
+
+struct SegmentPlan {
+  int32_t segments, rows;
+};
+// Segments only where there are too few states to fill the card, and of no less
+// than 256 rows: a segment's state is written and read twice, 4 DK DV bytes
+// against its rows' 2 (2 DK + 2 DV).
+SegmentPlan segment_plan(const qds_decay_config* c, int roles) {
+  const int64_t lists = (int64_t)c->batch * c->heads * roles;
+  int64_t want = lists > 0 ? ceil_div(kFill, lists) : 1;
+  const int64_t most = ceil_div(c->length, 256);
+  if (want > most) want = most;
+  if (want < 1) want = 1;
+  SegmentPlan p;
+  p.rows = (int32_t)(ceil_div(ceil_div(c->length, want), kChunk) * kChunk);
+  if (p.rows < kChunk) p.rows = kChunk;
+  p.segments = (int32_t)ceil_div(c->length, p.rows);
+  if (p.segments < 1) p.segments = 1;
+  return p;
+}
+uint64_t state_bytes(const qds_decay_config* c, int segments) {
+  if (segments == 1) return 0;
+  return align_up((uint64_t)c->batch * c->heads * segments * pad(c->dim_k) * pad(c->dim_v) * sizeof(float));
+}
+
+template <class T, int DK, int DV> void run_roles(const DecayArgs& a, int roles, hipStream_t s) {
+  const uint32_t lists = (uint32_t)a.batch * a.heads;
+  if (a.segments > 1) {
+    k_decay_chunks<T, DK, DV, false><<<dim3(lists, a.segments, roles), 2 * DV, 0, s>>>(a);
+    k_decay_scan<DK, DV><<<dim3(lists * (DK * DV / 256), 1, roles), 256, 0, s>>>(a);
+  }
+  k_decay_chunks<T, DK, DV, true><<<dim3(lists, a.segments, roles), 2 * DV, 0, s>>>(a);
+}
+template <class T> void run_dims(const DecayArgs& a, int roles, hipStream_t s) {
+  const int dk = pad(a.dim_x), dv = pad(a.dim_z);
+  if (dk == 64 && dv == 64) run_roles<T, 64, 64>(a, roles, s);
+  else if (dk == 64) run_roles<T, 64, 128>(a, roles, s);
+  else if (dv == 64) run_roles<T, 128, 64>(a, roles, s);
+  else run_roles<T, 128, 128>(a, roles, s);
+}
+void run(const qds_decay_config* c, const DecayArgs& a, int roles, void* stream) {
+  if (c->dtype == QDS_BF16) run_dims<bf16>(a, roles, (hipStream_t)stream);
+  else run_dims<half>(a, roles, (hipStream_t)stream);
+}
+
+DecayArgs decay_args(const qds_decay_config* c, const SegmentPlan& p, const int32_t* lengths, const float* log_decay) {
+  DecayArgs a{};
+  a.lengths = lengths;
+  a.log_decay = log_decay;
+  a.batch = c->batch;
+  a.length = c->length;
+  a.heads = c->heads;
+  a.dim_x = c->dim_k;
+  a.dim_z = c->dim_v;
+  a.segments = p.segments;
+  a.segment_rows = p.rows;
+  return a;
+}
+
+}  // namespace
+}  // namespace seq
+
+using namespace seq;
+
+extern "C" qds_status qds_decay_forward_workspace(const qds_decay_config* c, uint64_t* bytes) {
+  const qds_status st = validate(c);
+  if (st != QDS_OK) return st;
+  if (!bytes) return QDS_ERR_INVALID_ARG;
+  *bytes = state_bytes(c, segment_plan(c, 1).segments);
+  return QDS_OK;
+}
+
+extern "C" qds_status qds_decay_forward(const qds_decay_config* c, qds_view q, qds_view k, qds_view v,
+                                        const float* log_decay, const float* state_in,
+                                        const int32_t* lengths, qds_view o, float* state_out,
+                                        void* workspace, uint64_t workspace_bytes, void* stream) {
+  uint64_t need = 0;
+  const qds_status st = qds_decay_forward_workspace(c, &need);
+  if (st != QDS_OK) return st;
+  if (c->batch == 0) return QDS_OK;
+  if (!log_decay) return QDS_ERR_INVALID_ARG;
+  if (c->length > 0 && (!usable(q) || !usable(k) || !usable(v) || !usable(o))) return QDS_ERR_INVALID_ARG;
+  if (need && (!workspace || ((uintptr_t)workspace & 255))) return QDS_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
+  DecayArgs a = decay_args(c, segment_plan(c, 1), lengths, log_decay);
+  a.role[0] = Role{view(q), view(k), view(v), view(o), state_in, state_out, (float*)workspace, c->scale, 1.0f, 1.0f, false, false};
+  run(c, a, 1, stream);
+  return launch_status();
+}
+
+extern "C" qds_status qds_decay_backward_workspace(const qds_decay_config* c, uint64_t* bytes) {
+  const qds_status st = validate(c);
+  if (st != QDS_OK) return st;
+  if (!bytes) return QDS_ERR_INVALID_ARG;
+  *bytes = 3 * state_bytes(c, segment_plan(c, 3).segments);
+  return QDS_OK;
+}
+
+extern "C" qds_status qds_decay_backward(const qds_decay_config* c, qds_view dout, qds_view q, qds_view k,
+                                         qds_view v, const float* log_decay, const float* state_in,
+                                         const float* dstate_out, const int32_t* lengths, qds_view dq,
+                                         qds_view dk, qds_view dv, float* dstate_in, void* workspace,
+                                         uint64_t workspace_bytes, void* stream) {
+  uint64_t need = 0;
+  const qds_status st = qds_decay_backward_workspace(c, &need);
+  if (st != QDS_OK) return st;
+  if (c->batch == 0) return QDS_OK;
+  if (!log_decay) return QDS_ERR_INVALID_ARG;
+  if (c->length > 0 && (!usable(dout) || !usable(q) || !usable(k) || !usable(v) || !usable(dq) ||
+                        !usable(dk) || !usable(dv)))
+    return QDS_ERR_INVALID_ARG;
+  if (need && (!workspace || ((uintptr_t)workspace & 255))) return QDS_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
+  const SegmentPlan p = segment_plan(c, 3);
+  const uint64_t each = state_bytes(c, p.segments) / sizeof(float);
+  float* ws = (float*)workspace;
+  // R is formed without the scale; the state's gradient enters it divided by the scale.
+  const float back = 1.0f / c->scale;
+  const Role rq{view(dout), view(v), view(k), view(dq), state_in, nullptr, ws, c->scale, 1.0f, 1.0f, false, true};
+  const Role rk{view(v), view(dout), view(q), view(dk), dstate_out, nullptr, ws + each, c->scale, back, 1.0f, true, true};
+  const Role rv{view(k), view(q), view(dout), view(dv), dstate_out, dstate_in, ws + 2 * each, c->scale, back, c->scale, true, false};
+  DecayArgs a = decay_args(c, p, lengths, log_decay);
+  if (c->dim_k == c->dim_v) {
+    a.role[0] = rq, a.role[1] = rk, a.role[2] = rv;
+    run(c, a, 3, stream);
+  } else {
+    a.role[0] = rv;
+    run(c, a, 1, stream);
+    a.dim_x = c->dim_v, a.dim_z = c->dim_k;
+    a.role[0] = rq, a.role[1] = rk;
+    run(c, a, 2, stream);
+  }
+  return launch_status();
+}
+
+extern "C" qds_status qds_decay_step(const qds_decay_config* c, qds_view q, qds_view k, qds_view v,
+                                     const float* log_decay, const float* state_in, qds_view o,
+                                     float* state_out, void* stream) {
+  const qds_status st = validate(c);
+  if (st != QDS_OK) return st;
+  if (c->batch == 0) return QDS_OK;
+  if (!usable(q, false) || !usable(k, false) || !usable(v, false) || !usable(o, false) || !log_decay ||
+      !state_in || !state_out || !aligned16(state_in) || !aligned16(state_out))
+    return QDS_ERR_INVALID_ARG;
+  const StepArgs a{view(q), view(k), view(v), view(o), log_decay, state_in, state_out, c->heads, c->dim_k, c->dim_v, c->scale};
+  const uint32_t grid = (uint32_t)c->batch * c->heads;
+  hipStream_t s = (hipStream_t)stream;
+  const int dk = pad(c->dim_k), dv = pad(c->dim_v);
+  auto go = [&](auto t) {
+    using T = decltype(t);
+    if (dk == 64 && dv == 64) k_decay_step<T, 64, 64><<<grid, 256, 0, s>>>(a);
+    else if (dk == 64) k_decay_step<T, 64, 128><<<grid, 256, 0, s>>>(a);
+    else if (dv == 64) k_decay_step<T, 128, 64><<<grid, 256, 0, s>>>(a);
+    else k_decay_step<T, 128, 128><<<grid, 256, 0, s>>>(a);
+  };
+  if (c->dtype == QDS_BF16) go(bf16{});
+  else go(half{});
+  return launch_status();
+}

@@ -1,0 +1,561 @@
+// seq_norm.hip -- root-mean-square norm with the residual's addition: forward,
+// forward with an 8-bit output, backward.  The C ABI is in include/qd_seq.h.
+//
+// All three are bound by memory: 8 bytes (16-bit types) move per element
+// forward and again backward, against some ten operations.  A row is read once
+// and stays in registers between its sum and its use: one wave holds a row of up
+// to 64 lanes * 32 elements, four waves one of up to four times that.
+#include "seq_common.hpp"
+
+namespace seq {
+namespace {
+
+constexpr int kBlock = 256;
+constexpr float kFp8Max = 448.0f;
+constexpr float kFp8Floor = 0x1p-100f;   // a smaller maximum would make 448 / maximum overflow
+constexpr int kBackwardBlocks = 512;     // two workgroups per compute unit, each with its own dweight
+
+template <class T> __device__ inline float to_f32(T x) { return (float)x; }
+template <class T> __device__ inline T from_f32(float x) { return (T)x; }
+
+// VEC consecutive elements (16 bytes, or one element).
+template <class T, int VEC> struct Pack { T v[VEC]; };
+
+template <class T, int VEC> __device__ inline void load(float* out, const T* p) {
+  if constexpr (VEC == 1) {
+    out[0] = to_f32(*p);
+  } else {
+    const u32x4 raw = *reinterpret_cast<const u32x4*>(p);
+    const auto e = __builtin_bit_cast(Pack<T, VEC>, raw);
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) out[i] = to_f32(e.v[i]);
+  }
+}
+template <class T, int VEC> __device__ inline void store(T* p, const float* in) {
+  if constexpr (VEC == 1) {
+    *p = from_f32<T>(in[0]);
+  } else {
+    Pack<T, VEC> e;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) e.v[i] = from_f32<T>(in[i]);
+    *reinterpret_cast<u32x4*>(p) = __builtin_bit_cast(u32x4, e);
+  }
+}
+// The weight is fp32 or of the tensors' type.
+template <class T, int VEC> __device__ inline void load_weight(float* out, const void* w, bool w32, int col) {
+  if (w32) {
+    const float* p = (const float*)w + col;
+    if constexpr (VEC == 8) {
+      load<float, 4>(out, p);
+      load<float, 4>(out + 4, p + 4);
+    } else {
+      load<float, VEC>(out, p);
+    }
+  } else {
+    load<T, VEC>(out, (const T*)w + col);
+  }
+}
+
+// Sum over the lanes that share a row: a wave, or the whole workgroup.  `part`
+// has a place per wave; two calls that follow each other use different ones.
+template <int TPR> __device__ inline float row_sum(float x, float* part) {
+  x = wave_sum(x);
+  if constexpr (TPR > 64) {
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = (part[0] + part[1]) + (part[2] + part[3]);
+  }
+  return x;
+}
+template <int TPR> __device__ inline float row_max(float x, float* part) {
+  x = wave_max(x);
+  if constexpr (TPR > 64) {
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+    __syncthreads();
+    x = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+  }
+  return x;
+}
+
+__device__ inline float fp8_scale(float top) {
+  return top == 0.0f ? 1.0f : fmaxf(top, kFp8Floor) * (1.0f / kFp8Max);
+}
+// Clamped to the largest e4m3 number (what is beyond it by rounding would turn
+// into not-a-number); not-a-number stays.
+__device__ inline float fp8_clamp(float x) {
+  x = x > kFp8Max ? kFp8Max : x;
+  return x < -kFp8Max ? -kFp8Max : x;
+}
+__device__ inline uint32_t fp8_pack4(const float* v) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(fp8_clamp(v[0]), fp8_clamp(v[1]), 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(fp8_clamp(v[2]), fp8_clamp(v[3]), r, true);
+}
+__device__ inline uint8_t fp8_one(float v) {
+  return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(fp8_clamp(v), 0.0f, 0, false);
+}
+
+struct ForwardArgs {
+  const void *x, *r, *w;
+  void *y, *h;
+  float* rstd;      // or the scales of an 8-bit output
+  int64_t x_stride, r_stride, rows;
+  int32_t width;
+  float eps;
+  bool w32;
+};
+
+enum { kPlain = 0, kFp8Row = 1, kFp8Group = 2 };
+
+// One pass.  TPR lanes hold a row, each NV packs of VEC elements, pack j at
+// column (j TPR + lane) VEC: every load of a wave is one contiguous piece.
+template <class T, int VEC, int NV, int TPR, int MODE>
+__global__ __launch_bounds__(kBlock) void k_norm(ForwardArgs a) {
+  __shared__ float part[8];
+  constexpr int ROWS = kBlock / TPR;
+  const int lane = threadIdx.x % TPR;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+  if (TPR == 64 && row >= a.rows) return;      // whole waves; no barrier below for them
+  const T* x = (const T*)a.x + row * a.x_stride;
+  const T* r = a.r ? (const T*)a.r + row * a.r_stride : nullptr;
+  float h[NV][VEC];
+  float sum = 0.0f;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int col = (j * TPR + lane) * VEC;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) h[j][i] = 0.0f;
+    if (col < a.width) {
+      load<T, VEC>(h[j], x + col);
+      if (r) {
+        float t[VEC];
+        load<T, VEC>(t, r + col);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) h[j][i] += t[i];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) sum = fmaf(h[j][i], h[j][i], sum);
+  }
+  sum = row_sum<TPR>(sum, part);
+  const float rstd = rsqrtf(sum / (float)a.width + a.eps);
+  float top = 0.0f;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int col = (j * TPR + lane) * VEC;
+    if (col < a.width) {
+      store<T, VEC>((T*)a.h + row * a.width + col, h[j]);
+      float w[VEC];
+      load_weight<T, VEC>(w, a.w, a.w32, col);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) h[j][i] = h[j][i] * rstd * w[i];
+      if constexpr (MODE == kPlain) store<T, VEC>((T*)a.y + row * a.width + col, h[j]);
+      if constexpr (MODE == kFp8Row) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) top = fmaxf(top, fabsf(h[j][i]));
+      }
+    }
+  }
+  if constexpr (MODE == kPlain) {
+    if (lane == 0) a.rstd[row] = rstd;
+  } else if constexpr (MODE == kFp8Row) {
+    top = row_max<TPR>(top, part + 4);
+    const float scale = fp8_scale(top), inv = 1.0f / scale;
+    if (lane == 0) a.rstd[row] = scale;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int col = (j * TPR + lane) * VEC;
+      if (col >= a.width) continue;
+      uint8_t* q = (uint8_t*)a.y + row * a.width + col;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) h[j][i] *= inv;
+      if constexpr (VEC == 1) {
+        *q = fp8_one(h[j][0]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < VEC; i += 4) *reinterpret_cast<uint32_t*>(q + i) = fp8_pack4(h[j] + i);
+      }
+    }
+  } else {
+    // 128 columns are 128 / VEC neighbouring lanes (all 16 or 32 of them, as 128 divides the width).
+    static_assert(MODE == kPlain || VEC > 1, "groups need packs");
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int col = (j * TPR + lane) * VEC;
+      float t = 0.0f;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) t = fmaxf(t, fabsf(h[j][i]));
+#pragma unroll
+      for (int m = 1; m < 128 / VEC; m <<= 1) t = fmaxf(t, shfl_xor(t, m));
+      if (col >= a.width) continue;
+      const float scale = fp8_scale(t), inv = 1.0f / scale;
+      if (lane % (128 / VEC) == 0) a.rstd[row * (a.width / 128) + col / 128] = scale;
+      uint8_t* q = (uint8_t*)a.y + row * a.width + col;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) h[j][i] *= inv;
+#pragma unroll
+      for (int i = 0; i < VEC; i += 4) *reinterpret_cast<uint32_t*>(q + i) = fp8_pack4(h[j] + i);
+    }
+  }
+}
+
+// Rows of any width and alignment, read again for each use (from the caches): a
+// workgroup per row.
+template <class T, int MODE>
+__global__ __launch_bounds__(kBlock) void k_norm_any(ForwardArgs a) {
+  __shared__ float part[8];
+  const int64_t row = blockIdx.x;
+  const T* x = (const T*)a.x + row * a.x_stride;
+  const T* r = a.r ? (const T*)a.r + row * a.r_stride : nullptr;
+  auto at = [&](int c) { return to_f32(x[c]) + (r ? to_f32(r[c]) : 0.0f); };
+  float sum = 0.0f;
+  for (int c = threadIdx.x; c < a.width; c += kBlock) {
+    const float h = at(c);
+    sum = fmaf(h, h, sum);
+  }
+  sum = row_sum<kBlock>(sum, part);
+  const float rstd = rsqrtf(sum / (float)a.width + a.eps);
+  auto out = [&](int c, float h) {
+    float w;
+    load_weight<T, 1>(&w, a.w, a.w32, c);
+    return h * rstd * w;
+  };
+  if constexpr (MODE == kPlain) {
+    if (threadIdx.x == 0) a.rstd[row] = rstd;
+    for (int c = threadIdx.x; c < a.width; c += kBlock) {
+      const float h = at(c);
+      ((T*)a.h)[row * a.width + c] = from_f32<T>(h);
+      ((T*)a.y)[row * a.width + c] = from_f32<T>(out(c, h));
+    }
+  } else if constexpr (MODE == kFp8Row) {
+    float top = 0.0f;
+    for (int c = threadIdx.x; c < a.width; c += kBlock) {
+      const float h = at(c);
+      ((T*)a.h)[row * a.width + c] = from_f32<T>(h);
+      top = fmaxf(top, fabsf(out(c, h)));
+    }
+    top = row_max<kBlock>(top, part + 4);
+    const float scale = fp8_scale(top), inv = 1.0f / scale;
+    if (threadIdx.x == 0) a.rstd[row] = scale;
+    for (int c = threadIdx.x; c < a.width; c += kBlock)
+      ((uint8_t*)a.y)[row * a.width + c] = fp8_one(out(c, at(c)) * inv);
+  } else {
+    const int lane = threadIdx.x & 63;
+    for (int g = threadIdx.x >> 6; g < a.width / 128; g += kBlock / 64) {
+      const int c = g * 128 + lane;
+      const float h0 = at(c), h1 = at(c + 64);
+      ((T*)a.h)[row * a.width + c] = from_f32<T>(h0);
+      ((T*)a.h)[row * a.width + c + 64] = from_f32<T>(h1);
+      const float y0 = out(c, h0), y1 = out(c + 64, h1);
+      const float scale = fp8_scale(wave_max(fmaxf(fabsf(y0), fabsf(y1)))), inv = 1.0f / scale;
+      if (lane == 0) a.rstd[row * (a.width / 128) + g] = scale;
+      ((uint8_t*)a.y)[row * a.width + c] = fp8_one(y0 * inv);
+      ((uint8_t*)a.y)[row * a.width + c + 64] = fp8_one(y1 * inv);
+    }
+  }
+}
+
+struct BackwardArgs {
+  const void *dy, *dh, *h, *w;
+  const float* rstd;
+  void *dx, *dw;
+  float* partial;   // [blocks][width]
+  int64_t dy_stride, dh_stride, h_stride, rows;
+  int32_t width, blocks;
+  bool w32;
+};
+
+// g = dy w;  dx = dh + rstd (g - h rstd^2 mean(g h));  dw = sum over rows of dy h rstd.
+// A workgroup takes rows blockIdx.x, + gridDim.x, ... (four at a time where a
+// wave holds a row) and keeps its share of dw in registers; k_norm_dweight adds
+// the workgroups' shares in a fixed order.
+template <class T, int VEC, int NV, int TPR>
+__global__ __launch_bounds__(kBlock) void k_norm_backward(BackwardArgs a) {
+  __shared__ float part[8];
+  __shared__ float shares[TPR == 64 ? 3 * 64 * VEC * NV : 1];
+  constexpr int ROWS = kBlock / TPR;
+  const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
+  float dw[NV][VEC], w[NV][VEC];
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int col = (j * TPR + lane) * VEC;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) dw[j][i] = w[j][i] = 0.0f;
+    if (col < a.width) load_weight<T, VEC>(w[j], a.w, a.w32, col);
+  }
+  int turn = 0;
+  for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.rows; first += (int64_t)gridDim.x * ROWS) {
+    const int64_t row = first + sub;
+    if (TPR == 64 && row >= a.rows) break;     // a wave of its own; no barrier inside the loop for them
+    const float rstd = a.rstd[row];
+    float g[NV][VEC], h[NV][VEC];
+    float dot = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int col = (j * TPR + lane) * VEC;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) g[j][i] = h[j][i] = 0.0f;
+      if (col < a.width) {
+        load<T, VEC>(g[j], (const T*)a.dy + row * a.dy_stride + col);
+        load<T, VEC>(h[j], (const T*)a.h + row * a.h_stride + col);
+      }
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        h[j][i] *= rstd;
+        dw[j][i] = fmaf(g[j][i], h[j][i], dw[j][i]);
+        g[j][i] *= w[j][i];
+        dot = fmaf(g[j][i], h[j][i], dot);
+      }
+    }
+    dot = row_sum<TPR>(dot, part + 4 * (turn & 1)) / (float)a.width;
+    turn ^= 1;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int col = (j * TPR + lane) * VEC;
+      if (col >= a.width) continue;
+      float d[VEC];
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) d[i] = 0.0f;
+      if (a.dh) load<T, VEC>(d, (const T*)a.dh + row * a.dh_stride + col);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) d[i] += rstd * (g[j][i] - h[j][i] * dot);
+      store<T, VEC>((T*)a.dx + row * a.width + col, d);
+    }
+  }
+  if constexpr (TPR == 64) {
+    // the four waves' shares, added in the order of the waves
+    if (sub > 0) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) shares[((sub - 1) * NV * VEC + j * VEC + i) * 64 + lane] = dw[j][i];
+    }
+    __syncthreads();
+    if (sub > 0) return;
+#pragma unroll
+    for (int s = 0; s < 3; ++s)
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) dw[j][i] += shares[(s * NV * VEC + j * VEC + i) * 64 + lane];
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int col = (j * TPR + lane) * VEC;
+    if (col >= a.width) continue;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) a.partial[(int64_t)blockIdx.x * a.width + col + i] = dw[j][i];
+  }
+}
+
+// Rows of any width, read again for each use; dw goes through memory that only
+// this thread touches.
+template <class T> __global__ __launch_bounds__(kBlock) void k_norm_backward_any(BackwardArgs a) {
+  __shared__ float part[8];
+  float* mine = a.partial + (int64_t)blockIdx.x * a.width;
+  for (int c = threadIdx.x; c < a.width; c += kBlock) mine[c] = 0.0f;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const float rstd = a.rstd[row];
+    const T* dy = (const T*)a.dy + row * a.dy_stride;
+    const T* hp = (const T*)a.h + row * a.h_stride;
+    float dot = 0.0f;
+    for (int c = threadIdx.x; c < a.width; c += kBlock) {
+      const float d = to_f32(dy[c]), h = to_f32(hp[c]) * rstd;
+      float w;
+      load_weight<T, 1>(&w, a.w, a.w32, c);
+      mine[c] = fmaf(d, h, mine[c]);
+      dot = fmaf(d * w, h, dot);
+    }
+    dot = row_sum<kBlock>(dot, part + 4 * (turn & 1)) / (float)a.width;
+    turn ^= 1;
+    for (int c = threadIdx.x; c < a.width; c += kBlock) {
+      float w;
+      load_weight<T, 1>(&w, a.w, a.w32, c);
+      float d = a.dh ? to_f32(((const T*)a.dh)[row * a.dh_stride + c]) : 0.0f;
+      d += rstd * (to_f32(dy[c]) * w - to_f32(hp[c]) * rstd * dot);
+      ((T*)a.dx)[row * a.width + c] = from_f32<T>(d);
+    }
+  }
+}
+
+// 64 columns per workgroup: four waves each add every fourth share.
+template <class T> __global__ __launch_bounds__(kBlock) void k_norm_dweight(BackwardArgs a) {
+  __shared__ float part[kBlock];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int col = blockIdx.x * 64 + lane;
+  float sum = 0.0f;
+  if (col < a.width) {
+#pragma unroll 8
+    for (int b = wave; b < a.blocks; b += 4) sum += a.partial[(int64_t)b * a.width + col];
+  }
+  part[threadIdx.x] = sum;
+  __syncthreads();
+  if (wave == 0 && col < a.width) {
+    sum = (part[lane] + part[64 + lane]) + (part[128 + lane] + part[192 + lane]);
+    if (a.w32)
+      ((float*)a.dw)[col] = sum;
+    else
+      ((T*)a.dw)[col] = from_f32<T>(sum);
+  }
+}
+
+qds_status validate(const qds_norm_config* c) {
+  if (!c || c->abi_version != QDS_ABI_VERSION) return QDS_ERR_INVALID_ARG;
+  if (c->dtype < QDS_F32 || c->dtype > QDS_F16) return QDS_ERR_INVALID_ARG;
+  if (c->weight_dtype != QDS_F32 && c->weight_dtype != c->dtype) return QDS_ERR_INVALID_ARG;
+  if (c->width < 1 || c->width > (1 << 20)) return QDS_ERR_INVALID_ARG;
+  if (c->rows < 0 || c->rows > 0x7fffffff) return QDS_ERR_INVALID_ARG;
+  if (!(c->eps >= 0.0f)) return QDS_ERR_INVALID_ARG;
+  if (c->group != 0 && (c->group != 128 || c->width % 128 != 0)) return QDS_ERR_INVALID_ARG;
+  return QDS_OK;
+}
+
+// Elements per 16 bytes.
+int pack_of(int dtype) { return dtype == QDS_F32 ? 4 : 8; }
+
+// Whether rows may be read in packs of 16 bytes.
+bool packs(const qds_norm_config* c, std::initializer_list<const void*> pointers,
+           std::initializer_list<int64_t> strides) {
+  const int v = pack_of(c->dtype);
+  if (c->width % v) return false;
+  for (const void* p : pointers)
+    if (!aligned16(p)) return false;
+  for (int64_t s : strides)
+    if (s % v) return false;
+  return true;
+}
+
+// Calls f(VEC, NV, TPR) as compile-time values for the least that holds a row
+// in registers; returns false where nothing does.  A wave holds rows of up to
+// 32 elements a lane, so that loads of a whole row are in flight at once; four
+// waves hold wider ones.
+template <int V> using Int = std::integral_constant<int, V>;
+template <class T, class F> bool with_shape(int width, bool vec, F&& f) {
+  constexpr int V = 16 / sizeof(T);
+  if (vec) {
+    if (width <= 64 * V) f(Int<V>{}, Int<1>{}, Int<64>{});
+    else if (width <= 128 * V) f(Int<V>{}, Int<2>{}, Int<64>{});
+    else if (width <= 256 * V) f(Int<V>{}, Int<4>{}, Int<64>{});
+    else if (width <= 512 * V) f(Int<V>{}, Int<2>{}, Int<256>{});
+    else if (width <= 1024 * V) f(Int<V>{}, Int<4>{}, Int<256>{});
+    else return false;
+  } else {
+    if (width <= 256) f(Int<1>{}, Int<4>{}, Int<64>{});
+    else if (width <= 1024) f(Int<1>{}, Int<16>{}, Int<64>{});
+    else if (width <= 4096) f(Int<1>{}, Int<16>{}, Int<256>{});
+    else return false;
+  }
+  return true;
+}
+
+template <class T, int MODE> void forward(const ForwardArgs& a, bool vec, hipStream_t s) {
+  const bool held = with_shape<T>(a.width, vec, [&](auto V, auto NV, auto TPR) {
+    constexpr int v = decltype(V)::value, nv = decltype(NV)::value, tpr = decltype(TPR)::value;
+    if constexpr (MODE != kFp8Group || v > 1)
+      k_norm<T, v, nv, tpr, MODE><<<ceil_div(a.rows, kBlock / tpr), kBlock, 0, s>>>(a);
+    else
+      k_norm_any<T, MODE><<<a.rows, kBlock, 0, s>>>(a);
+  });
+  if (!held) k_norm_any<T, MODE><<<a.rows, kBlock, 0, s>>>(a);
+}
+
+template <int MODE> qds_status run_forward(const qds_norm_config* c, const ForwardArgs& a, bool vec, void* stream) {
+  if (c->rows == 0) return QDS_OK;
+  hipStream_t s = (hipStream_t)stream;
+  if (c->dtype == QDS_F32) forward<float, MODE>(a, vec, s);
+  else if (c->dtype == QDS_BF16) forward<bf16, MODE>(a, vec, s);
+  else forward<half, MODE>(a, vec, s);
+  return launch_status();
+}
+
+// Workgroups of the backward pass: enough to fill the card, no more than rows.
+int backward_blocks(const qds_norm_config* c) {
+  return (int)(c->rows < kBackwardBlocks ? (c->rows > 0 ? c->rows : 1) : kBackwardBlocks);
+}
+
+template <class T> void backward(BackwardArgs a, bool vec, hipStream_t s) {
+  if (a.rows > 0) {
+    const bool held = with_shape<T>(a.width, vec, [&](auto V, auto NV, auto TPR) {
+      constexpr int v = decltype(V)::value, nv = decltype(NV)::value, tpr = decltype(TPR)::value;
+      k_norm_backward<T, v, nv, tpr><<<a.blocks, kBlock, 0, s>>>(a);
+    });
+    if (!held) k_norm_backward_any<T><<<a.blocks, kBlock, 0, s>>>(a);
+  } else {
+    a.blocks = 0;
+  }
+  k_norm_dweight<T><<<ceil_div(a.width, 64), kBlock, 0, s>>>(a);
+}
+
+}  // namespace
+}  // namespace seq
+
+using namespace seq;
+
+extern "C" qds_status qds_residual_norm(const qds_norm_config* c, const void* x, int64_t x_stride,
+                                        const void* residual, int64_t residual_stride,
+                                        const void* weight, void* y, void* h, float* rstd,
+                                        void* stream) {
+  const qds_status st = validate(c);
+  if (st != QDS_OK) return st;
+  if (c->group != 0) return QDS_ERR_INVALID_ARG;
+  if (c->rows > 0 && (!x || !weight || !y || !h || !rstd)) return QDS_ERR_INVALID_ARG;
+  const ForwardArgs a{x, residual, weight, y, h, rstd, x_stride, residual_stride, c->rows,
+                      c->width, c->eps, c->weight_dtype == QDS_F32};
+  const bool vec = packs(c, {x, residual, weight, y, h}, {x_stride, residual ? residual_stride : 0});
+  return run_forward<kPlain>(c, a, vec, stream);
+}
+
+extern "C" qds_status qds_residual_norm_fp8(const qds_norm_config* c, const void* x,
+                                            int64_t x_stride, const void* residual,
+                                            int64_t residual_stride, const void* weight, void* q,
+                                            float* scale, void* h, void* stream) {
+  const qds_status st = validate(c);
+  if (st != QDS_OK) return st;
+  if (c->rows > 0 && (!x || !weight || !q || !scale || !h)) return QDS_ERR_INVALID_ARG;
+  const ForwardArgs a{x, residual, weight, q, h, scale, x_stride, residual_stride, c->rows,
+                      c->width, c->eps, c->weight_dtype == QDS_F32};
+  const bool vec = packs(c, {x, residual, weight, q, h}, {x_stride, residual ? residual_stride : 0});
+  return c->group ? run_forward<kFp8Group>(c, a, vec, stream) : run_forward<kFp8Row>(c, a, vec, stream);
+}
+
+extern "C" qds_status qds_residual_norm_backward_workspace(const qds_norm_config* c, uint64_t* bytes) {
+  const qds_status st = validate(c);
+  if (st != QDS_OK) return st;
+  if (!bytes) return QDS_ERR_INVALID_ARG;
+  *bytes = align_up((uint64_t)backward_blocks(c) * c->width * sizeof(float));
+  return QDS_OK;
+}
+
+extern "C" qds_status qds_residual_norm_backward(const qds_norm_config* c, const void* dy,
+                                                 int64_t dy_stride, const void* dh,
+                                                 int64_t dh_stride, const void* h, int64_t h_stride,
+                                                 const float* rstd, const void* weight, void* dx,
+                                                 void* dweight, void* workspace,
+                                                 uint64_t workspace_bytes, void* stream) {
+  uint64_t need = 0;
+  const qds_status st = qds_residual_norm_backward_workspace(c, &need);
+  if (st != QDS_OK) return st;
+  if (c->group != 0 || !dweight || !workspace || !weight || ((uintptr_t)workspace & 255))
+    return QDS_ERR_INVALID_ARG;
+  if (c->rows > 0 && (!dy || !h || !rstd || !dx)) return QDS_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
+  const BackwardArgs a{dy, dh, h, weight, rstd, dx, dweight, (float*)workspace, dy_stride, dh_stride,
+                       h_stride, c->rows, c->width, backward_blocks(c), c->weight_dtype == QDS_F32};
+  const bool vec = packs(c, {dy, dh, h, weight, dx}, {dy_stride, dh ? dh_stride : 0, h_stride});
+  hipStream_t s = (hipStream_t)stream;
+  if (c->dtype == QDS_F32) backward<float>(a, vec, s);
+  else if (c->dtype == QDS_BF16) backward<bf16>(a, vec, s);
+  else backward<half>(a, vec, s);
+  return launch_status();
+}
+
+extern "C" const char* qds_status_str(qds_status status) {
+  switch (status) {
+    case QDS_OK: return "ok";
+    case QDS_ERR_INVALID_ARG: return "invalid argument";
+    case QDS_ERR_WORKSPACE_TOO_SMALL: return "workspace too small";
+    case QDS_ERR_UNSUPPORTED: return "unsupported configuration";
+    case QDS_ERR_HIP: return "HIP runtime or launch error";
+  }
+  return "unknown status";
+}

@@ -1,0 +1,906 @@
+// seq_window.hip -- attention over a sliding window whose first tokens stay
+// visible: forward, backward, the single-token step over a ring cache, and the
+// cache's filling from a prompt.  The C ABI is in include/qd_seq.h.
+//
+// Row i of an episode of n rows sees j <= i < n with i - j < window or j < sinks.
+// Scores are kept in units of log 2: p = 2^(c s - m) with c = scale log2(e).
+#include "seq_common.hpp"
+
+namespace seq {
+namespace {
+
+constexpr int kBlock = 256;
+constexpr int kWaves = 4;
+constexpr float kNoMax = -3.0e38f;     // below every score; finite, so that differences are no not-a-number
+struct WindowArgs {
+  View q, k, v, o, dout, dq, dk, dv;
+  const int32_t* lengths;
+  float *lse, *delta;
+  int32_t batch, length, heads, kv_heads, dim, window, sinks;
+  float scale;
+};
+
+__device__ inline int rows_of(const WindowArgs& a, int b) {
+  if (!a.lengths) return a.length;
+  return min(max(a.lengths[b], 0), a.length);
+}
+
+// One row per lane l % 32 as an operand of the 32x32x16 product (k along the row).
+template <class T, int DP> __device__ inline void load_rows(x8<T>* f, const T* row, bool valid, int dim) {
+  const int half = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int s = 0; s < DP / 16; ++s) {
+    const int c = s * 2 + half;
+    f[s] = zero8<T>();
+    if (valid && c * 8 < dim) f[s] = __builtin_bit_cast(x8<T>, *reinterpret_cast<const u32x4*>(row + c * 8));
+  }
+}
+// The tiles of 64 keys that rows i0 .. i0 + rows - 1 can see: those of the first
+// tokens that are not in the band, then the band's.
+struct KeyTiles {
+  int first, band, count;   // tiles of first tokens; first tile of the band; all
+  __device__ KeyTiles(const WindowArgs& a, int i0, int rows, int n) {
+    const int lo = max(0, i0 - a.window + 1) / 64, hi = min(i0 + rows, n) - 1;
+    band = lo;
+    first = min((a.sinks + 63) / 64, lo);
+    count = first + hi / 64 - lo + 1;
+  }
+  __device__ int row(int t) const { return (t < first ? t : band + t - first) * 64; }
+};
+
+// ---------------------------------------------------------------------------
+// Forward
+// ---------------------------------------------------------------------------
+// A workgroup has 128 query rows of one head, a wave 32 of them.  Scores are
+// formed transposed (keys are rows of the C tile, queries its columns), so a
+// query's maximum and sum are over a lane's own registers and one exchange with
+// lane l ^ 32, and the weights are the B operand of o^T = v^T p^T as they are.
+constexpr int kForwardRows = 32 * kWaves;
+
+template <class T, int DP>
+__global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int q_blocks) {
+  SEQ_SHARED T sk[2][64 * DP], sv[2][64 * DP];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int group = a.heads / a.kv_heads;
+  int id = xcd_order(blockIdx.x, gridDim.x);
+  const int g = id % group;
+  id /= group;
+  // late blocks first: they have the most keys where the window is long
+  const int block = q_blocks - 1 - id % q_blocks;
+  id /= q_blocks;
+  const int hk = id % a.kv_heads, b = id / a.kv_heads;
+  const int h = hk * group + g;
+  const int n = rows_of(a, b);
+  const int i0 = block * kForwardRows, w0 = i0 + 32 * wave;
+  const int i = w0 + (lane & 31);
+  T* o_row = at<T>(a.o, b, i, h);
+  float* lse = a.lse + ((int64_t)b * a.heads + h) * a.length + i;
+
+  f32x16 o[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) o[d] = f32x16{};
+  if (i0 < n) {
+    const float c = a.scale * kLog2e;
+    x8<T> q[DP / 16];
+    load_rows<T, DP>(q, at<T>(a.q, b, i, h), i < n, a.dim);
+    const T* kp = at<T>(a.k, b, 0, hk);
+    const T* vp = at<T>(a.v, b, 0, hk);
+    const KeyTiles tiles(a, i0, kForwardRows, n);
+    Staged<T, DP, kBlock> rk, rv;
+    rk.load(kp, a.k.t, tiles.row(0), n, a.dim);
+    rv.load(vp, a.v.t, tiles.row(0), n, a.dim);
+    rk.store(sk[0]);
+    rv.store(sv[0]);
+    float m = kNoMax, sum = 0.0f;
+    for (int t = 0; t < tiles.count; ++t) {
+      __syncthreads();
+      const int j0 = tiles.row(t);
+      const bool more = t + 1 < tiles.count;
+      if (more) {
+        rk.load(kp, a.k.t, tiles.row(t + 1), n, a.dim);
+        rv.load(vp, a.v.t, tiles.row(t + 1), n, a.dim);
+      }
+      const T *tk = sk[t & 1], *tv = sv[t & 1];
+      const bool none = j0 > w0 + 31 || (w0 - (j0 + 63) >= a.window && j0 >= a.sinks);
+      if (!none) {
+        f32x16 s[2];
+#pragma unroll
+        for (int jb = 0; jb < 2; ++jb) {
+          s[jb] = f32x16{};
+#pragma unroll
+          for (int ks = 0; ks < DP / 16; ++ks) s[jb] = mfma32(tile_rows<T, DP>(tk, jb * 32, ks), q[ks], s[jb]);
+        }
+        const bool all = j0 + 63 <= w0 && (w0 + 31 - j0 < a.window || j0 + 63 < a.sinks);
+        float top = kNoMax;
+#pragma unroll
+        for (int jb = 0; jb < 2; ++jb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            if (!all) {
+              const int j = j0 + jb * 32 + c_row(r);
+              const bool seen = j <= i && (i - j < a.window || j < a.sinks);
+              s[jb][r] = seen ? s[jb][r] : -INFINITY;
+            }
+            top = fmaxf(top, s[jb][r]);
+          }
+        top = max_halves(top) * c;
+        // The maximum is moved only where a weight would pass 2^8: any reference
+        // gives the same quotient, and most tiles then need no rescaling.
+        if (__any(top > m + 8.0f)) {
+          const float to = fmaxf(m, top), alpha = fast_exp2(m - to);
+          m = to;
+          sum *= alpha;
+#pragma unroll
+          for (int d = 0; d < DP / 32; ++d) o[d] *= alpha;
+        }
+#pragma unroll
+        for (int jb = 0; jb < 2; ++jb) {
+          float p[16];
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            p[r] = fast_exp2(fmaf(s[jb][r], c, -m));
+            sum += p[r];
+          }
+          // The weights are rounded to the tensors' type for the matrix product
+          // (their sum is not): 2^-9 or 2^-12 of each, less than o's own rounding.
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const x8<T> pb = pack8<T>(p + 8 * u);
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+              o[d] = mfma32(tile_columns<T, DP>(tv, jb * 32 + 16 * u, d), pb, o[d]);
+          }
+        }
+      }
+      if (more) {
+        rk.store(sk[(t + 1) & 1]);
+        rv.store(sv[(t + 1) & 1]);
+      }
+    }
+    sum = sum_halves(sum);
+    if (i < n) {
+      const float inv = 1.0f / sum;
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) store_column<T>(o_row, d, o[d], inv, a.dim);
+      if (lane < 32) *lse = (m + fast_log2(sum)) * kLn2;
+    }
+  }
+  if (i >= n && i < a.length) {
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) store_column<T>(o_row, d, f32x16{}, 0.0f, a.dim);
+    if (lane < 32) *lse = -INFINITY;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Backward
+// ---------------------------------------------------------------------------
+// With p = 2^(c s - lse), delta_i = do_i . o_i, ds = p (do v^T - delta):
+//   dq = scale ds k,  dk = scale ds^T q,  dv = p^T do.
+// Two kernels, one over queries and one over keys, each forming p again; sums
+// are then over a workgroup's own loop, in a fixed order.
+
+// dq of 128 rows of one head, as the forward pass; also writes delta.
+template <class T, int DP>
+__global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dq(WindowArgs a, int q_blocks) {
+  SEQ_SHARED T sk[2][64 * DP], sv[2][64 * DP];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int group = a.heads / a.kv_heads;
+  int id = xcd_order(blockIdx.x, gridDim.x);
+  const int g = id % group;
+  id /= group;
+  const int block = q_blocks - 1 - id % q_blocks;
+  id /= q_blocks;
+  const int hk = id % a.kv_heads, b = id / a.kv_heads;
+  const int h = hk * group + g;
+  const int n = rows_of(a, b);
+  const int i0 = block * kForwardRows, w0 = i0 + 32 * wave;
+  const int i = w0 + (lane & 31);
+  const int64_t flat = ((int64_t)b * a.heads + h) * a.length + i;
+
+  f32x16 dq[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) dq[d] = f32x16{};
+  if (i0 < n) {
+    const float c = a.scale * kLog2e;
+    x8<T> q[DP / 16], go[DP / 16];
+    load_rows<T, DP>(q, at<T>(a.q, b, i, h), i < n, a.dim);
+    load_rows<T, DP>(go, at<T>(a.dout, b, i, h), i < n, a.dim);
+    float delta = 0.0f;
+    {
+      x8<T> o[DP / 16];
+      load_rows<T, DP>(o, at<T>(a.o, b, i, h), i < n, a.dim);
+#pragma unroll
+      for (int s = 0; s < DP / 16; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) delta = fmaf((float)o[s][e], (float)go[s][e], delta);
+    }
+    delta = sum_halves(delta);
+    if (lane < 32 && i < n) a.delta[flat] = delta;
+    const float lse = i < n ? a.lse[flat] * kLog2e : INFINITY;   // rows past the end: p = 0
+    const T* kp = at<T>(a.k, b, 0, hk);
+    const T* vp = at<T>(a.v, b, 0, hk);
+    const KeyTiles tiles(a, i0, kForwardRows, n);
+    Staged<T, DP, kBlock> rk, rv;
+    rk.load(kp, a.k.t, tiles.row(0), n, a.dim);
+    rv.load(vp, a.v.t, tiles.row(0), n, a.dim);
+    rk.store(sk[0]);
+    rv.store(sv[0]);
+    for (int t = 0; t < tiles.count; ++t) {
+      __syncthreads();
+      const int j0 = tiles.row(t);
+      const bool more = t + 1 < tiles.count;
+      if (more) {
+        rk.load(kp, a.k.t, tiles.row(t + 1), n, a.dim);
+        rv.load(vp, a.v.t, tiles.row(t + 1), n, a.dim);
+      }
+      const T *tk = sk[t & 1], *tv = sv[t & 1];
+      const bool none = j0 > w0 + 31 || (w0 - (j0 + 63) >= a.window && j0 >= a.sinks);
+      if (!none) {
+        const bool all = j0 + 63 <= w0 && (w0 + 31 - j0 < a.window || j0 + 63 < a.sinks);
+#pragma unroll
+        for (int jb = 0; jb < 2; ++jb) {
+          f32x16 s = f32x16{}, dp = f32x16{};
+#pragma unroll
+          for (int ks = 0; ks < DP / 16; ++ks) s = mfma32(tile_rows<T, DP>(tk, jb * 32, ks), q[ks], s);
+#pragma unroll
+          for (int ks = 0; ks < DP / 16; ++ks) dp = mfma32(tile_rows<T, DP>(tv, jb * 32, ks), go[ks], dp);
+          float ds[16];
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            float p = fast_exp2(fmaf(s[r], c, -lse));
+            if (!all) {
+              const int j = j0 + jb * 32 + c_row(r);
+              const bool seen = j <= i && (i - j < a.window || j < a.sinks);
+              p = seen ? p : 0.0f;
+            }
+            ds[r] = p * (dp[r] - delta);
+          }
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            const x8<T> db = pack8<T>(ds + 8 * u);
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+              dq[d] = mfma32(tile_columns<T, DP>(tk, jb * 32 + 16 * u, d), db, dq[d]);
+          }
+        }
+      }
+      if (more) {
+        rk.store(sk[(t + 1) & 1]);
+        rv.store(sv[(t + 1) & 1]);
+      }
+    }
+  }
+  if (i < a.length) {
+    T* row = at<T>(a.dq, b, i, h);
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d) store_column<T>(row, d, dq[d], i < n ? a.scale : 0.0f, a.dim);
+  }
+}
+
+// How the key blocks' work is cut.  A block of first tokens is seen by every
+// later row, one of the band by about window + 128 rows of each head of the
+// group: the former are cut into more pieces, so that no workgroup has far more
+// to do than the others; both into more where there are few blocks.  Pieces of
+// one block leave fp32 sums that k_window_dkdv_join adds in their order.
+constexpr int kKeyRows = 32 * kWaves;
+struct KeyPlan {
+  int32_t blocks, first;            // key blocks per key head; those that hold first tokens
+  int32_t first_cut, band_cut;      // pieces of each kind
+  int32_t items;                    // workgroups per key head
+};
+
+struct KeyItem {
+  int block, piece, cut;
+};
+__device__ inline KeyItem key_item(const KeyPlan& p, int x) {
+  if (x < p.first * p.first_cut) return {x / p.first_cut, x % p.first_cut, p.first_cut};
+  x -= p.first * p.first_cut;
+  return {p.first + x / p.band_cut, x % p.band_cut, p.band_cut};
+}
+
+template <class T, int DP>
+__global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dkdv(WindowArgs a, KeyPlan plan, float* parts) {
+  SEQ_SHARED T sq[2][64 * DP], sg[2][64 * DP];
+  SEQ_SHARED float s_lse[2][64], s_delta[2][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int group = a.heads / a.kv_heads;
+  const int id = xcd_order(blockIdx.x, gridDim.x);
+  const int head = id / plan.items;           // b * kv_heads + hk
+  const KeyItem item = key_item(plan, id % plan.items);
+  const int hk = head % a.kv_heads, b = head / a.kv_heads;
+  const int n = rows_of(a, b);
+  const int j0 = item.block * kKeyRows, w0 = j0 + 32 * wave;
+  const int j = w0 + (lane & 31);
+  const float c = a.scale * kLog2e;
+
+  f32x16 dk[DP / 32], dv[DP / 32];
+#pragma unroll
+  for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = f32x16{};
+  // the rows that see this block, in tiles of 64, for each head of the group
+  int unit = 0, stop = 0, q0 = 0, per_head = 1;
+  if (j0 < n) {
+    const int64_t last = j0 < a.sinks ? n - 1 : min((int64_t)n - 1, (int64_t)j0 + kKeyRows - 1 + a.window - 1);
+    q0 = j0 / 64;
+    per_head = (int)(last / 64) - q0 + 1;
+    const int64_t units = (int64_t)per_head * group;
+    unit = (int)(units * item.piece / item.cut);
+    stop = (int)(units * (item.piece + 1) / item.cut);
+  }
+  if (unit < stop) {
+    x8<T> k[DP / 16], v[DP / 16];
+    load_rows<T, DP>(k, at<T>(a.k, b, j, hk), j < n, a.dim);
+    load_rows<T, DP>(v, at<T>(a.v, b, j, hk), j < n, a.dim);
+    Staged<T, DP, kBlock> rq, rg;
+    float r_lse = 0.0f, r_delta = 0.0f;
+    auto fetch = [&](int u) {
+      const int h = hk * group + u / per_head, row0 = (q0 + u % per_head) * 64;
+      rq.load(at<T>(a.q, b, 0, h), a.q.t, row0, n, a.dim);
+      rg.load(at<T>(a.dout, b, 0, h), a.dout.t, row0, n, a.dim);
+      if (threadIdx.x < 64) {
+        const int i = row0 + threadIdx.x;
+        const int64_t flat = ((int64_t)b * a.heads + h) * a.length + i;
+        r_lse = i < n ? a.lse[flat] * kLog2e : INFINITY;     // rows past the end: p = 0
+        r_delta = i < n ? a.delta[flat] : 0.0f;
+      }
+    };
+    auto put = [&](int buf) {
+      rq.store(sq[buf]);
+      rg.store(sg[buf]);
+      if (threadIdx.x < 64) {
+        s_lse[buf][threadIdx.x] = r_lse;
+        s_delta[buf][threadIdx.x] = r_delta;
+      }
+    };
+    fetch(unit);
+    put(0);
+    for (int buf = 0; unit < stop; ++unit, buf ^= 1) {
+      __syncthreads();
+      if (unit + 1 < stop) fetch(unit + 1);
+      const int row0 = (q0 + unit % per_head) * 64;
+      const T *tq = sq[buf], *tg = sg[buf];
+#pragma unroll
+      for (int ib = 0; ib < 2; ++ib) {
+        const int r0 = row0 + ib * 32;
+        const bool none = r0 + 31 < w0 || (r0 - (w0 + 31) >= a.window && w0 >= a.sinks) || r0 >= n;
+        if (none) continue;
+        const bool all = r0 >= w0 + 31 && (r0 + 31 - w0 < a.window || w0 + 31 < a.sinks);
+        f32x16 s = f32x16{}, dp = f32x16{};
+#pragma unroll
+        for (int ks = 0; ks < DP / 16; ++ks) s = mfma32(tile_rows<T, DP>(tq, ib * 32, ks), k[ks], s);
+#pragma unroll
+        for (int ks = 0; ks < DP / 16; ++ks) dp = mfma32(tile_rows<T, DP>(tg, ib * 32, ks), v[ks], dp);
+        float p[16], ds[16];
+#pragma unroll
+        for (int r4 = 0; r4 < 4; ++r4) {
+          const int at4 = ib * 32 + 8 * r4 + 4 * (lane >> 5);
+          const f32x4 lse = *reinterpret_cast<const f32x4*>(&s_lse[buf][at4]);
+          const f32x4 delta = *reinterpret_cast<const f32x4*>(&s_delta[buf][at4]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int r = 4 * r4 + e;
+            p[r] = fast_exp2(fmaf(s[r], c, -lse[e]));
+            if (!all) {
+              const int i = r0 + c_row(r);
+              const bool seen = j <= i && (i - j < a.window || j < a.sinks);
+              p[r] = seen ? p[r] : 0.0f;
+            }
+            ds[r] = p[r] * (dp[r] - delta[e]);
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const x8<T> pb = pack8<T>(p + 8 * u), db = pack8<T>(ds + 8 * u);
+#pragma unroll
+          for (int d = 0; d < DP / 32; ++d) {
+            dv[d] = mfma32(tile_columns<T, DP>(tg, ib * 32 + 16 * u, d), pb, dv[d]);
+            dk[d] = mfma32(tile_columns<T, DP>(tq, ib * 32 + 16 * u, d), db, dk[d]);
+          }
+        }
+      }
+      if (unit + 1 < stop) put(buf ^ 1);
+    }
+  }
+  if (item.cut == 1) {
+    if (j < a.length) {
+      T* rk = at<T>(a.dk, b, j, hk);
+      T* rv = at<T>(a.dv, b, j, hk);
+#pragma unroll
+      for (int d = 0; d < DP / 32; ++d) {
+        store_column<T>(rk, d, dk[d], a.scale, a.dim);
+        store_column<T>(rv, d, dv[d], 1.0f, a.dim);
+      }
+    }
+  } else {
+    // [item][dk, dv][row][DP]
+    float* to = parts + (int64_t)id * (2 * kKeyRows * DP) + (wave * 32 + (lane & 31)) * DP;
+#pragma unroll
+    for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        const int col = d * 32 + 8 * r4 + 4 * (lane >> 5);
+        *reinterpret_cast<f32x4*>(to + col) =
+            f32x4{dk[d][4 * r4], dk[d][4 * r4 + 1], dk[d][4 * r4 + 2], dk[d][4 * r4 + 3]};
+        *reinterpret_cast<f32x4*>(to + kKeyRows * DP + col) =
+            f32x4{dv[d][4 * r4], dv[d][4 * r4 + 1], dv[d][4 * r4 + 2], dv[d][4 * r4 + 3]};
+      }
+  }
+}
+
+// Adds the pieces of cut blocks: a thread has four columns of a row of dk and of dv.
+template <class T, int DP>
+__global__ __launch_bounds__(kBlock) void k_window_dkdv_join(WindowArgs a, KeyPlan plan, int per_head, const float* parts) {
+  constexpr int ROWS = kBlock * 4 / DP;
+  const int head = blockIdx.x / per_head, x = blockIdx.x % per_head;
+  const int hk = head % a.kv_heads, b = head / a.kv_heads;
+  const int from = plan.first_cut > 1 ? 0 : plan.first;       // the cut blocks
+  const int block = from + x / (kKeyRows / ROWS);
+  const int row = (x % (kKeyRows / ROWS)) * ROWS + threadIdx.x / (DP / 4);
+  const int col = threadIdx.x % (DP / 4) * 4;
+  const int j = block * kKeyRows + row;
+  if (j >= a.length || col >= a.dim) return;
+  const bool is_first = block < plan.first;
+  const int cut = is_first ? plan.first_cut : plan.band_cut;
+  const int item = is_first ? block * plan.first_cut
+                            : plan.first * plan.first_cut + (block - plan.first) * plan.band_cut;
+  const float* p = parts + ((int64_t)head * plan.items + item) * (2 * kKeyRows * DP) + row * DP + col;
+  f32x4 dk = f32x4{}, dv = f32x4{};
+#pragma unroll 4
+  for (int s = 0; s < cut; ++s) {
+    dk += *reinterpret_cast<const f32x4*>(p);
+    dv += *reinterpret_cast<const f32x4*>(p + kKeyRows * DP);
+    p += 2 * kKeyRows * DP;
+  }
+  dk *= a.scale;
+  *reinterpret_cast<u32x2*>(at<T>(a.dk, b, j, hk) + col) = __builtin_bit_cast(u32x2, pack4<T>(dk[0], dk[1], dk[2], dk[3]));
+  *reinterpret_cast<u32x2*>(at<T>(a.dv, b, j, hk) + col) = __builtin_bit_cast(u32x2, pack4<T>(dv[0], dv[1], dv[2], dv[3]));
+}
+
+// ---------------------------------------------------------------------------
+// Single-token step
+// ---------------------------------------------------------------------------
+// Bound by reading the cache once.  Up to 16 query heads that share a key head
+// are the columns of one matrix product, so that its keys and values are read
+// once for all of them.  A workgroup has a range of slots, its waves take strips
+// of 32 slots in turn and keep running maxima and sums of their own; ranges and
+// waves are joined at the end.  Keys go from memory to the matrix operand, values
+// through 8 KB of LDS per wave that turns them.
+constexpr int kStrip = 32;
+
+struct StepArgs {
+  View q, k, v, o;
+  void *k_cache, *v_cache;
+  const int32_t* pos;
+  float* parts;            // [item][16]: maxima, then sums, then o [item][16][DP]
+  int32_t batch, heads, kv_heads, dim, window, sinks, tiles, cut, range;
+  float scale;
+};
+
+__device__ inline int slot_of(int p, int window, int sinks) { return p < sinks ? p : sinks + (p - sinks) % window; }
+
+template <class T, int DP>
+__global__ __launch_bounds__(kBlock, 2) void k_window_step(StepArgs a) {
+  constexpr int OUT = DP + 4;                       // padded, so that 16 heads spread over the banks
+  constexpr int kStage = kWaves * kStrip * DP * 2, kOut = kWaves * 16 * OUT * 4;
+  SEQ_SHARED char lds[kStage > kOut ? kStage : kOut];
+  __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int group = a.heads / a.kv_heads, slots = a.window + a.sinks;
+  const int tile = blockIdx.x % a.tiles, head = blockIdx.x / a.tiles;
+  const int hk = head % a.kv_heads, b = head / a.kv_heads;
+  const int pos = a.pos[b];
+  const int seen = pos < 0 ? 0 : min(pos, slots - 1) + 1;
+  const int fresh = pos < 0 ? -1 : slot_of(pos, a.window, a.sinks);
+  const int begin = blockIdx.y * a.range, end = min(begin + a.range, seen);
+  T* kc = (T*)a.k_cache + (int64_t)head * slots * a.dim;
+  T* vc = (T*)a.v_cache + (int64_t)head * slots * a.dim;
+  const T* k_new = at<T>(a.k, b, 0, hk);
+  const T* v_new = at<T>(a.v, b, 0, hk);
+
+  // The new row is read from k and v wherever it is needed, and written by one workgroup.
+  if (tile == 0 && fresh >= begin && fresh < end && threadIdx.x < DP / 8 && threadIdx.x * 8 < a.dim) {
+    const int c = threadIdx.x * 8;
+    *reinterpret_cast<u32x4*>(kc + (int64_t)fresh * a.dim + c) = *reinterpret_cast<const u32x4*>(k_new + c);
+    *reinterpret_cast<u32x4*>(vc + (int64_t)fresh * a.dim + c) = *reinterpret_cast<const u32x4*>(v_new + c);
+  }
+
+  const float c = a.scale * kLog2e;
+  const int g = tile * 16 + (lane & 15), quad = lane >> 4;
+  x8<T> q[DP / 32];
+#pragma unroll
+  for (int s = 0; s < DP / 32; ++s) {
+    const int col = (s * 4 + quad) * 8;
+    q[s] = zero8<T>();
+    if (g < group && col < a.dim)
+      q[s] = __builtin_bit_cast(x8<T>, *reinterpret_cast<const u32x4*>(at<T>(a.q, b, 0, hk * group + g) + col));
+  }
+
+  constexpr int NV = kStrip * DP / 8 / 64;
+  u32x4 rk[2][DP / 32], rv[NV];
+  auto fetch = [&](int s0) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int slot = s0 + 16 * t + (lane & 15);
+      const T* p = slot == fresh ? k_new : kc + (int64_t)slot * a.dim;
+#pragma unroll
+      for (int s = 0; s < DP / 32; ++s) {
+        const int col = (s * 4 + quad) * 8;
+        rk[t][s] = u32x4{0, 0, 0, 0};
+        if (slot < end && col < a.dim) rk[t][s] = *reinterpret_cast<const u32x4*>(p + col);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int id = lane + 64 * i, slot = s0 + id / (DP / 8), col = id % (DP / 8) * 8;
+      const T* p = slot == fresh ? v_new : vc + (int64_t)slot * a.dim;
+      rv[i] = u32x4{0, 0, 0, 0};
+      if (slot < end && col < a.dim) rv[i] = *reinterpret_cast<const u32x4*>(p + col);
+    }
+  };
+
+  f32x4 o[DP / 16];
+#pragma unroll
+  for (int d = 0; d < DP / 16; ++d) o[d] = f32x4{};
+  float m = kNoMax, sum = 0.0f;
+  T* stage = (T*)lds + wave * kStrip * DP;
+  int s0 = begin + wave * kStrip;
+  if (s0 < end) fetch(s0);
+  for (; s0 < end; s0 += kWaves * kStrip) {
+    x8<T> kf[2][DP / 32];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int s = 0; s < DP / 32; ++s) kf[t][s] = __builtin_bit_cast(x8<T>, rk[t][s]);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int id = lane + 64 * i;
+      *reinterpret_cast<u32x4*>(stage + tile_at<DP>(id / (DP / 8), id % (DP / 8))) = rv[i];
+    }
+    if (s0 + kWaves * kStrip < end) fetch(s0 + kWaves * kStrip);
+    f32x4 s[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      s[t] = f32x4{};
+#pragma unroll
+      for (int ks = 0; ks < DP / 32; ++ks) s[t] = mfma16(kf[t][ks], q[ks], s[t]);
+    }
+    float top = kNoMax;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int slot = s0 + 16 * t + 4 * quad + r;
+        s[t][r] = slot < end ? s[t][r] * c : -INFINITY;
+        top = fmaxf(top, s[t][r]);
+      }
+    top = fmaxf(top, shfl_xor(top, 16));
+    top = fmaxf(top, shfl_xor(top, 32));
+    if (__any(top > m)) {
+      const float to = fmaxf(m, top), alpha = fast_exp2(m - to);
+      m = to;
+      sum *= alpha;
+#pragma unroll
+      for (int d = 0; d < DP / 16; ++d) o[d] *= alpha;
+    }
+    float p[8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        p[4 * t + r] = fast_exp2(s[t][r] - m);
+        sum += p[4 * t + r];
+      }
+    const x8<T> pb = pack8<T>(p);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // the wave's own writes to its stage
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int d = 0; d < DP / 16; ++d) {
+      const int row = 4 * quad + ((lane & 15) >> 2), col = d * 16 + (lane & 3) * 4;
+      const x4<T> lo = lds_read_transposed(stage + tile_at<DP>(row, col >> 3) + (col & 7));
+      const x4<T> hi = lds_read_transposed(stage + tile_at<DP>(row + 16, col >> 3) + (col & 7));
+      o[d] = mfma16(join8<T>(lo, hi), pb, o[d]);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  sum += shfl_xor(sum, 16);
+  sum += shfl_xor(sum, 32);
+
+  // The waves' shares, added in their order.
+  __syncthreads();
+  float* out = (float*)lds;
+  if (lane < 16) {
+    s_m[wave][lane] = m;
+    s_l[wave][lane] = sum;
+  }
+#pragma unroll
+  for (int d = 0; d < DP / 16; ++d)
+    *reinterpret_cast<f32x4*>(out + (wave * 16 + (lane & 15)) * OUT + d * 16 + 4 * quad) = o[d];
+  __syncthreads();
+  const int heads_here = min(16, group - tile * 16);
+  const int64_t item = (int64_t)blockIdx.x * a.cut + blockIdx.y, items = (int64_t)gridDim.x * a.cut;
+  for (int x = threadIdx.x; x < heads_here * (DP / 4); x += kBlock) {
+    const int hh = x / (DP / 4), d = x % (DP / 4) * 4;
+    float top = s_m[0][hh];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, s_m[w][hh]);
+    f32x4 r = f32x4{};
+    float l = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = fast_exp2(s_m[w][hh] - top);
+      l = fmaf(s_l[w][hh], f, l);
+      r += *reinterpret_cast<const f32x4*>(out + (w * 16 + hh) * OUT + d) * f;
+    }
+    if (a.cut == 1) {
+      const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
+      if (d < a.dim)
+        *reinterpret_cast<u32x2*>(at<T>(a.o, b, 0, hk * group + tile * 16 + hh) + d) =
+            __builtin_bit_cast(u32x2, pack4<T>(r[0] * inv, r[1] * inv, r[2] * inv, r[3] * inv));
+    } else {
+      if (d == 0) {
+        a.parts[item * 16 + hh] = top;
+        a.parts[(items + item) * 16 + hh] = l;
+      }
+      *reinterpret_cast<f32x4*>(a.parts + items * 32 + (item * 16 + hh) * DP + d) = r;
+    }
+  }
+}
+
+// Joins the ranges of one head: a wave per head, DP / 64 columns a lane.
+template <class T, int DP> __global__ __launch_bounds__(64) void k_window_step_join(StepArgs a) {
+  const int lane = threadIdx.x;
+  const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads, group = a.heads / a.kv_heads;
+  const int g = h % group;
+  const int64_t first = (((int64_t)b * a.kv_heads + h / group) * a.tiles + g / 16) * a.cut;
+  const int64_t items = (int64_t)a.batch * a.kv_heads * a.tiles * a.cut;
+  float top = kNoMax;
+  for (int s = lane; s < a.cut; s += 64) top = fmaxf(top, a.parts[(first + s) * 16 + g % 16]);
+  top = wave_max(top);
+  float l = 0.0f, r[DP / 64];
+#pragma unroll
+  for (int d = 0; d < DP / 64; ++d) r[d] = 0.0f;
+#pragma unroll 4
+  for (int s = 0; s < a.cut; ++s) {
+    const int64_t at16 = (first + s) * 16 + g % 16;
+    const float f = fast_exp2(a.parts[at16] - top);
+    l = fmaf(a.parts[items * 16 + at16], f, l);
+#pragma unroll
+    for (int d = 0; d < DP / 64; ++d) r[d] = fmaf(a.parts[items * 32 + at16 * DP + d * 64 + lane], f, r[d]);
+  }
+  const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
+#pragma unroll
+  for (int d = 0; d < DP / 64; ++d)
+    if (d * 64 + lane < a.dim) at<T>(a.o, b, 0, h)[d * 64 + lane] = (T)(r[d] * inv);
+}
+
+// Slot by slot: the latest position below n that belongs in it.
+template <class T>
+__global__ __launch_bounds__(kBlock) void k_window_fill(WindowArgs a, T* k_cache, T* v_cache) {
+  const int64_t slots = (int64_t)a.window + a.sinks, packs = a.dim / 8;
+  const int64_t all = slots * packs * a.kv_heads * a.batch;
+  for (int64_t x = (int64_t)blockIdx.x * kBlock + threadIdx.x; x < all; x += (int64_t)gridDim.x * kBlock) {
+    const int col = (int)(x % packs) * 8;
+    const int slot = (int)(x / packs % slots);
+    const int64_t list = x / packs / slots;
+    const int hk = (int)(list % a.kv_heads), b = (int)(list / a.kv_heads);
+    const int last = rows_of(a, b) - 1;
+    if (last < slot) continue;                 // nothing has come this far
+    const int p = slot < a.sinks ? slot : last - (last - slot) % a.window;
+    *reinterpret_cast<u32x4*>(k_cache + x * 8) = *reinterpret_cast<const u32x4*>(at<T>(a.k, b, p, hk) + col);
+    *reinterpret_cast<u32x4*>(v_cache + x * 8) = *reinterpret_cast<const u32x4*>(at<T>(a.v, b, p, hk) + col);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------
+qds_status validate(const qds_window_config* c) {
+  if (!c || c->abi_version != QDS_ABI_VERSION) return QDS_ERR_INVALID_ARG;
+  if (c->dtype != QDS_BF16 && c->dtype != QDS_F16)
+    return c->dtype == QDS_F32 ? QDS_ERR_UNSUPPORTED : QDS_ERR_INVALID_ARG;
+  if (c->batch < 0 || c->length < 0 || c->heads < 1 || c->kv_heads < 1 || c->heads % c->kv_heads)
+    return QDS_ERR_INVALID_ARG;
+  if (c->dim < 1) return QDS_ERR_INVALID_ARG;
+  if (c->dim % 8 || c->dim > 128) return QDS_ERR_UNSUPPORTED;
+  if (c->window < 1 || c->sinks < 0 || (int64_t)c->window + c->sinks >= (1 << 30) || c->length >= (1 << 30))
+    return QDS_ERR_INVALID_ARG;
+  if (!(c->scale > 0.0f) || c->scale > 3.0e38f) return QDS_ERR_INVALID_ARG;
+  // the kernels' grids and their item numbers stay below 2^31
+  if ((int64_t)c->batch * c->heads > (1 << 24) ||
+      (int64_t)c->batch * c->heads * (ceil_div(c->length, 64) + 1) > (1ll << 30))
+    return QDS_ERR_UNSUPPORTED;
+  return QDS_OK;
+}
+
+WindowArgs window_args(const qds_window_config* c, const int32_t* lengths) {
+  WindowArgs a{};
+  a.lengths = lengths;
+  a.batch = c->batch;
+  a.length = c->length;
+  a.heads = c->heads;
+  a.kv_heads = c->kv_heads;
+  a.dim = c->dim;
+  a.window = c->window;
+  a.sinks = c->sinks;
+  a.scale = c->scale;
+  return a;
+}
+
+// Calls f with the tensors' type and the padded head dimension.
+template <class F> void with_type(int dtype, int dim, F&& f) {
+  using D64 = std::integral_constant<int, 64>;
+  using D128 = std::integral_constant<int, 128>;
+  if (dtype == QDS_BF16) {
+    if (dim <= 64) f(bf16{}, D64{});
+    else f(bf16{}, D128{});
+  } else {
+    if (dim <= 64) f(half{}, D64{});
+    else f(half{}, D128{});
+  }
+}
+
+KeyPlan key_plan(const qds_window_config* c) {
+  KeyPlan p{};
+  const int64_t group = c->heads / c->kv_heads, lists = (int64_t)c->batch * c->kv_heads;
+  const int64_t sinks = c->sinks < c->length ? c->sinks : c->length;
+  p.blocks = (int32_t)ceil_div(c->length, kKeyRows);
+  p.first = (int32_t)ceil_div(sinks, kKeyRows);
+  const int64_t all = ceil_div(c->length, 64);                                        // tiles that see a first block
+  int64_t band = ceil_div((int64_t)c->window + kKeyRows, 64) + 1;                     // ... and one of the band
+  if (band > all) band = all;
+  // pieces of equal size that give about kFill workgroups, but of no less than eight tiles
+  const int64_t total = (p.first * all + (p.blocks - p.first) * band) * group * lists;
+  int64_t piece = ceil_div(total, kFill);
+  if (piece < 8) piece = 8;
+  if (piece > band * group) piece = band * group;
+  p.first_cut = (int32_t)ceil_div(all * group, piece);
+  p.band_cut = (int32_t)ceil_div(band * group, piece);
+  p.items = p.first * p.first_cut + (p.blocks - p.first) * p.band_cut;
+  return p;
+}
+uint64_t key_parts(const qds_window_config* c, const KeyPlan& p) {
+  if (p.first_cut == 1 && p.band_cut == 1) return 0;
+  const uint64_t dp = c->dim <= 64 ? 64 : 128;
+  return (uint64_t)c->batch * c->kv_heads * p.items * 2 * kKeyRows * dp * sizeof(float);
+}
+
+struct StepPlan {
+  int32_t tiles, cut, range;
+};
+// Slots are cut into ranges where there are fewer heads than workgroups that
+// fill the card; a range has at least four strips for each wave.
+StepPlan step_plan(const qds_window_config* c) {
+  StepPlan p{};
+  p.tiles = (int32_t)ceil_div(c->heads / c->kv_heads, 16);
+  const int64_t lists = (int64_t)c->batch * c->kv_heads * p.tiles, slots = (int64_t)c->window + c->sinks;
+  constexpr int64_t strip = kWaves * kStrip;
+  int64_t cut = lists > 0 ? ceil_div(kFill, lists) : 1;
+  const int64_t most = ceil_div(slots, 4 * strip);
+  if (cut > most) cut = most;
+  p.range = (int32_t)(ceil_div(ceil_div(slots, cut), strip) * strip);
+  p.cut = (int32_t)ceil_div(slots, p.range);
+  return p;
+}
+
+}  // namespace
+}  // namespace seq
+
+using namespace seq;
+
+extern "C" qds_status qds_window_forward(const qds_window_config* c, qds_view q, qds_view k,
+                                         qds_view v, const int32_t* lengths, qds_view o, float* lse,
+                                         void* stream) {
+  const qds_status st = validate(c);
+  if (st != QDS_OK) return st;
+  if (c->batch == 0 || c->length == 0) return QDS_OK;
+  if (!usable(q) || !usable(k) || !usable(v) || !usable(o) || !lse) return QDS_ERR_INVALID_ARG;
+  WindowArgs a = window_args(c, lengths);
+  a.q = view(q), a.k = view(k), a.v = view(v), a.o = view(o), a.lse = lse;
+  const int blocks = (int)ceil_div(c->length, kForwardRows);
+  const int grid = c->batch * c->heads * blocks;
+  with_type(c->dtype, c->dim, [&](auto t, auto d) {
+    k_window_forward<decltype(t), decltype(d)::value><<<grid, kBlock, 0, (hipStream_t)stream>>>(a, blocks);
+  });
+  return launch_status();
+}
+
+extern "C" qds_status qds_window_backward_workspace(const qds_window_config* c, uint64_t* bytes) {
+  const qds_status st = validate(c);
+  if (st != QDS_OK) return st;
+  if (!bytes) return QDS_ERR_INVALID_ARG;
+  const uint64_t delta = align_up((uint64_t)c->batch * c->heads * c->length * sizeof(float));
+  *bytes = delta + align_up(key_parts(c, key_plan(c)));
+  return QDS_OK;
+}
+
+extern "C" qds_status qds_window_backward(const qds_window_config* c, qds_view dout, qds_view q,
+                                          qds_view k, qds_view v, qds_view o, const float* lse,
+                                          const int32_t* lengths, qds_view dq, qds_view dk,
+                                          qds_view dv, void* workspace, uint64_t workspace_bytes,
+                                          void* stream) {
+  uint64_t need = 0;
+  const qds_status st = qds_window_backward_workspace(c, &need);
+  if (st != QDS_OK) return st;
+  if (c->batch == 0 || c->length == 0) return QDS_OK;
+  if (!usable(dout) || !usable(q) || !usable(k) || !usable(v) || !usable(o) || !usable(dq) ||
+      !usable(dk) || !usable(dv) || !lse || !workspace || ((uintptr_t)workspace & 255))
+    return QDS_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
+  WindowArgs a = window_args(c, lengths);
+  a.q = view(q), a.k = view(k), a.v = view(v), a.o = view(o), a.dout = view(dout);
+  a.dq = view(dq), a.dk = view(dk), a.dv = view(dv), a.lse = const_cast<float*>(lse);
+  a.delta = (float*)workspace;
+  float* parts = (float*)((char*)workspace + align_up((uint64_t)c->batch * c->heads * c->length * sizeof(float)));
+  const KeyPlan plan = key_plan(c);
+  const int blocks = (int)ceil_div(c->length, kForwardRows);
+  const int lists = c->batch * c->kv_heads;
+  if ((int64_t)lists * plan.items > 0x7fffffff) return QDS_ERR_UNSUPPORTED;
+  hipStream_t s = (hipStream_t)stream;
+  with_type(c->dtype, c->dim, [&](auto t, auto d) {
+    using T = decltype(t);
+    constexpr int DP = decltype(d)::value;
+    k_window_dq<T, DP><<<c->batch * c->heads * blocks, kBlock, 0, s>>>(a, blocks);
+    k_window_dkdv<T, DP><<<lists * plan.items, kBlock, 0, s>>>(a, plan, parts);
+    const int from = plan.first_cut > 1 ? 0 : plan.first, to = plan.band_cut > 1 ? plan.blocks : plan.first;
+    if (to > from) {
+      const int per_head = (to - from) * (kKeyRows / (kBlock * 4 / DP));
+      k_window_dkdv_join<T, DP><<<(uint32_t)lists * per_head, kBlock, 0, s>>>(a, plan, per_head, parts);
+    }
+  });
+  return launch_status();
+}
+
+extern "C" qds_status qds_window_step_workspace(const qds_window_config* c, uint64_t* bytes) {
+  const qds_status st = validate(c);
+  if (st != QDS_OK) return st;
+  if (!bytes) return QDS_ERR_INVALID_ARG;
+  const StepPlan p = step_plan(c);
+  const uint64_t items = (uint64_t)c->batch * c->kv_heads * p.tiles * p.cut, dp = c->dim <= 64 ? 64 : 128;
+  *bytes = p.cut == 1 ? 0 : align_up(items * 16 * (2 + dp) * sizeof(float));
+  return QDS_OK;
+}
+
+extern "C" qds_status qds_window_step(const qds_window_config* c, qds_view q, qds_view k, qds_view v,
+                                      void* k_cache, void* v_cache, const int32_t* pos, qds_view o,
+                                      void* workspace, uint64_t workspace_bytes, void* stream) {
+  uint64_t need = 0;
+  const qds_status st = qds_window_step_workspace(c, &need);
+  if (st != QDS_OK) return st;
+  if (c->batch == 0) return QDS_OK;
+  if (!usable(q, false) || !usable(k, false) || !usable(v, false) || !usable(o, false) || !k_cache ||
+      !v_cache || !aligned16(k_cache) || !aligned16(v_cache) || !pos)
+    return QDS_ERR_INVALID_ARG;
+  if (need && (!workspace || ((uintptr_t)workspace & 255))) return QDS_ERR_INVALID_ARG;
+  if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
+  const StepPlan p = step_plan(c);
+  StepArgs a{view(q), view(k), view(v), view(o), k_cache, v_cache, pos, (float*)workspace,
+             c->batch, c->heads, c->kv_heads, c->dim, c->window, c->sinks, p.tiles, p.cut, p.range, c->scale};
+  hipStream_t s = (hipStream_t)stream;
+  with_type(c->dtype, c->dim, [&](auto t, auto d) {
+    using T = decltype(t);
+    constexpr int DP = decltype(d)::value;
+    k_window_step<T, DP><<<dim3(c->batch * c->kv_heads * p.tiles, p.cut), kBlock, 0, s>>>(a);
+    if (p.cut > 1) k_window_step_join<T, DP><<<c->batch * c->heads, 64, 0, s>>>(a);
+  });
+  return launch_status();
+}
+
+extern "C" qds_status qds_window_cache_fill(const qds_window_config* c, qds_view k, qds_view v,
+                                            const int32_t* lengths, void* k_cache, void* v_cache,
+                                            void* stream) {
+  const qds_status st = validate(c);
+  if (st != QDS_OK) return st;
+  if (c->batch == 0 || c->length == 0) return QDS_OK;
+  if (!usable(k) || !usable(v) || !k_cache || !v_cache || !aligned16(k_cache) || !aligned16(v_cache))
+    return QDS_ERR_INVALID_ARG;
+  WindowArgs a = window_args(c, lengths);
+  a.k = view(k), a.v = view(v);
+  const int64_t packs = ((int64_t)c->window + c->sinks) * (c->dim / 8) * c->kv_heads * c->batch;
+  const int64_t most = 8 * kFill, blocks = ceil_div(packs, kBlock);
+  const uint32_t grid = (uint32_t)(blocks < most ? blocks : most);
+  hipStream_t s = (hipStream_t)stream;
+  if (c->dtype == QDS_BF16) k_window_fill<bf16><<<grid, kBlock, 0, s>>>(a, (bf16*)k_cache, (bf16*)v_cache);
+  else k_window_fill<half><<<grid, kBlock, 0, s>>>(a, (half*)k_cache, (half*)v_cache);
+  return launch_status();
+}
