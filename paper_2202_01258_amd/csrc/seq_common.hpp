@@ -114,11 +114,13 @@ template <class T> __device__ inline x4<T> lds_read_transposed(const T* p) {
 }
 
 // Tiles in LDS: rows of DP 16-bit values in chunks of 8 (16 bytes), chunk c of
-// row r at place c ^ swizzle(r), so that lanes that read the same chunk of
-// consecutive rows spread over all banks (256 bytes: two rows of 64 values, or
-// one of 128).
+// row r at place c ^ swizzle(r).  LDS has 64 banks (256 bytes): 16 lanes that read
+// one chunk of consecutive rows, an operand's rows, are to meet 16 different places,
+// and 32 lanes that read four neighbouring chunks of four rows, a transposed read,
+// four different quarters.  (Counted: with r itself for the swizzle half of all LDS
+// cycles were conflicts of the transposed reads.)
 template <int DP> __device__ inline int swizzle(int row) {
-  return DP == 64 ? (row >> 1) & 7 : row & 15;
+  return DP == 64 ? ((row & 2) << 1) | ((row >> 2) & 3) : ((row & 3) << 2) | ((row >> 2) & 3);
 }
 template <int DP> __device__ inline int tile_at(int row, int chunk) {
   return row * DP + ((chunk ^ swizzle<DP>(row)) << 3);
@@ -143,47 +145,98 @@ inline bool usable(const qds_view& v, bool rows = true) {
   return v.data && aligned16(v.data) && v.stride[0] % 8 == 0 && v.stride[2] % 8 == 0 &&
          (!rows || v.stride[1] % 8 == 0);
 }
+// Tiles of 64 rows are addressed with 31 bits from their first row.
+inline bool near_rows(const qds_view& v) {
+  return v.stride[1] < (1 << 23) && v.stride[1] > -(1 << 23);
+}
 
 // 64 rows of a tensor in the registers of a workgroup of BLOCK threads (to be
 // written to LDS): rows from `end` on and columns from `dim` on are zero and
-// are not read.
+// are not read.  Buffer loads: the address is a scalar base per tile, a lane's
+// offset that never changes and a scalar offset per load, and an offset past the
+// buffer's size loads zero, so a load costs two vector instructions and no branch.
+constexpr uint32_t kBufferSize = 0x7fffffffu, kOutside = 0x80000000u;
+constexpr int kBufferFlags = 0x00027000;           // raw buffer of 32-bit data
 template <class T, int DP, int BLOCK> struct Staged {
-  static constexpr int N = 64 * DP / 8 / BLOCK;
+  static constexpr int N = 64 * DP / 8 / BLOCK, STEP = BLOCK / (DP / 8);   // loads; rows between two of a thread's
   u32x4 r[N];
-  __device__ void load(const T* p, int64_t stride, int row0, int end, int dim) {
+  const T* base;
+  int64_t stride;
+  uint32_t offset, step;       // bytes: of the thread's first piece in a tile, and from one to the next
+  int place;                   // its row, or one that no tensor has for columns that are not real
+  // A stride below 0 counts the tile's rows from its last one.
+  __device__ void init(const T* p, int64_t row_stride, int dim) {
+    base = p;
+    stride = row_stride;
+    const int c = threadIdx.x % (DP / 8), row = threadIdx.x / (DP / 8);
+    const uint32_t bytes = (uint32_t)(stride < 0 ? -stride : stride) * 2;
+    step = STEP * bytes;
+    offset = (stride < 0 ? 63 - row : row) * bytes + c * 16;
+    place = c * 8 < dim ? row : 1 << 30;
+  }
+  __device__ void load(int row0, int end) {
+    const T* first = base + (int64_t)(stride < 0 ? row0 + 63 : row0) * stride;
+    const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, kBufferSize, kBufferFlags);
+    const uint32_t down = stride < 0 ? step : 0, up = stride < 0 ? 0 : step;
+    const int rows = end - row0;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int id = threadIdx.x + i * BLOCK, row = id / (DP / 8), c = id % (DP / 8);
-      r[i] = u32x4{0, 0, 0, 0};
-      if (row0 + row < end && c * 8 < dim)
-        r[i] = *reinterpret_cast<const u32x4*>(p + (int64_t)(row0 + row) * stride + c * 8);
+      const uint32_t at = place < rows - i * STEP ? offset - i * down : kOutside;
+      r[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer, at, i * up, 0);
     }
   }
   __device__ void store(T* lds) const {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int id = threadIdx.x + i * BLOCK, row = id / (DP / 8), c = id % (DP / 8);
-      *reinterpret_cast<u32x4*>(lds + tile_at<DP>(row, c)) = r[i];
-    }
+    for (int i = 0; i < N; ++i)
+      *reinterpret_cast<u32x4*>(lds + tile_at<DP>(threadIdx.x / (DP / 8) + i * STEP, threadIdx.x % (DP / 8))) = r[i];
   }
 };
 
-// Rows row0 + l % 32 of a tile, the s-th 16 columns.
-template <class T, int DP> __device__ inline x8<T> tile_rows(const T* lds, int row0, int s) {
-  const int l = threadIdx.x & 63;
-  return __builtin_bit_cast(x8<T>, *reinterpret_cast<const u32x4*>(lds + tile_at<DP>(row0 + (l & 31), s * 2 + (l >> 5))));
+// Where a lane reads a tile's operands: byte offsets for the tile's first piece.  The
+// other pieces are at these with some of the bits 4..7 (the place of a chunk) flipped
+// and a multiple of 8 rows added, both known at compile time.
+template <int DP> struct Lanes {
+  static constexpr int ROW = DP * 2;
+  uint32_t rows, columns, straight, ordered;
+  __device__ Lanes() {
+    const int l = threadIdx.x & 63, half = l >> 5, r = l & 31, quad = (l & 15) >> 2;
+    // of a transposed read: 16 columns for each group of 16 lanes, in pieces of 4
+    const int piece = l & 3, turned = (piece >> 1) | ((piece & 1) << 1), group = ((l >> 4) & 1) * 2;
+    rows = r * ROW + ((half ^ swizzle<DP>(r)) << 4);
+    columns = (4 * half + quad) * ROW + (((group + (piece >> 1)) ^ swizzle<DP>(4 * half + quad)) << 4) + (piece & 1) * 8;
+    straight = (8 * half + quad) * ROW + (((group + (piece >> 1)) ^ swizzle<DP>(8 * half + quad)) << 4) + (piece & 1) * 8;
+    ordered = (8 * half + quad) * ROW + (((group + (turned >> 1)) ^ swizzle<DP>(8 * half + quad)) << 4) + (turned & 1) * 8;
+  }
+  // Makes the compiler form the other pieces' offsets again (an instruction each)
+  // where it would otherwise keep them all in registers that a kernel lacks.
+  __device__ void forget() { asm volatile("" : "+v"(rows), "+v"(columns), "+v"(straight), "+v"(ordered)); }
+};
+template <class T> __device__ inline const T* tile_byte(const T* lds, uint32_t offset) {
+  return (const T*)((const char*)lds + offset);
 }
-// Columns dt * 32 + l % 32 of a tile as rows of an operand whose k are the
+
+// Rows row0 + l % 32 of a tile, the s-th 16 columns (row0: a multiple of 32).
+template <class T, int DP> __device__ inline x8<T> tile_rows(const T* lds, const Lanes<DP>& at, int row0, int s) {
+  return __builtin_bit_cast(x8<T>, *reinterpret_cast<const u32x4*>(tile_byte(lds, (at.rows ^ (s << 5)) + row0 * DP * 2)));
+}
+// Columns dt * 32 + l % 32 of a tile as rows (or columns) of an operand whose k are the
 // tile's rows row0 + 8 (e / 4) + 4 (l / 32) + e % 4, e = 0..7: the order in
-// which a C tile holds its rows.
-template <class T, int DP> __device__ inline x8<T> tile_columns(const T* lds, int row0, int dt) {
-  const int l = threadIdx.x & 63;
-  const int row = row0 + 4 * (l >> 5) + ((l & 15) >> 2);
-  const int col = dt * 32 + ((l >> 4) & 1) * 16 + (l & 3) * 4;
-  const x4<T> a = lds_read_transposed(lds + tile_at<DP>(row, col >> 3) + (col & 7));
-  const x4<T> b = lds_read_transposed(lds + tile_at<DP>(row + 8, col >> 3) + (col & 7));
+// which a C tile holds its rows (row0: a multiple of 16).
+template <class T, int DP> __device__ inline x8<T> tile_columns(const T* lds, const Lanes<DP>& at, int row0, int dt) {
+  const uint32_t first = at.columns ^ (dt << 6), second = first ^ 32;       // swizzle(r + 8)
+  const x4<T> a = lds_read_transposed(tile_byte(lds, first + row0 * DP * 2));
+  const x4<T> b = lds_read_transposed(tile_byte(lds, second + (row0 + 8) * DP * 2));
   return join8<T>(a, b);
 }
+// The same with k the tile's rows row0 + 8 (l / 32) + e.
+template <class T, int DP> __device__ inline x8<T> tile_columns_straight(const T* lds, uint32_t lane_at, int row0, int dt) {
+  const uint32_t first = lane_at ^ (dt << 6), second = first ^ 16;      // swizzle(r + 4)
+  const x4<T> a = lds_read_transposed(tile_byte(lds, first + row0 * DP * 2));
+  const x4<T> b = lds_read_transposed(tile_byte(lds, second + (row0 + 4) * DP * 2));
+  return join8<T>(a, b);
+}
+// The wave's number in its workgroup, as a scalar (so that what depends on it branches for the whole wave).
+__device__ inline int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 // Row of register i of a 32x32 C tile.
 __device__ inline int c_row(int i) { return (i & 3) + 8 * (i >> 2) + 4 * ((threadIdx.x & 63) >> 5); }
 

@@ -19,7 +19,10 @@ namespace {
 
 constexpr int kChunk = 64;
 
-__device__ inline float decay_power(float lambda, int n) { return n == 0 ? 1.0f : fast_exp2(lambda * (float)n); }
+// a^n for lambda = log2(a).  `lambda` is kept finite (decay_rate), so that a^0 is 1
+// for a = 0, too; below the bound a^1 is 0 already.
+__device__ inline float decay_power(float lambda, float n) { return fast_exp2(lambda * n); }
+__device__ inline float decay_rate(const float* log_decay, int h) { return fmaxf(log_decay[h] * kLog2e, -1.0e4f); }
 
 // One direction of the recurrence.
 struct Role {
@@ -46,28 +49,13 @@ __device__ inline int rows_of(const DecayArgs& a, int b) {
   return min(max(a.lengths[b], 0), a.length);
 }
 
-// Columns dt * 32 + l % 32 of a tile as rows (or columns) of an operand whose k
-// are the tile's rows row0 + 8 (l / 32) + e.
-template <class T, int DP> __device__ inline x8<T> tile_columns_straight(const T* lds, int row0, int dt) {
-  const int l = threadIdx.x & 63;
-  const int row = row0 + 8 * (l >> 5) + ((l & 15) >> 2);
-  const int col = dt * 32 + ((l >> 4) & 1) * 16 + (l & 3) * 4;
-  const x4<T> a = lds_read_transposed(lds + tile_at<DP>(row, col >> 3) + (col & 7));
-  const x4<T> b = lds_read_transposed(lds + tile_at<DP>(row + 4, col >> 3) + (col & 7));
-  return join8<T>(a, b);
-}
-// Rows row0 + l % 32 of a tile; k are the columns 16 u + 8 (e / 4) + 4 (l / 32) + e % 4,
-// the order in which a C tile holds its rows.
-template <class T, int DP> __device__ inline x8<T> tile_rows_as_c(const T* lds, int row0, int u) {
-  const int l = threadIdx.x & 63, row = row0 + (l & 31), in = 4 * (l >> 5);
-  const u32x2 a = *reinterpret_cast<const u32x2*>(lds + tile_at<DP>(row, 2 * u) + in);
-  const u32x2 b = *reinterpret_cast<const u32x2*>(lds + tile_at<DP>(row, 2 * u + 1) + in);
-  return __builtin_bit_cast(x8<T>, u32x4{a[0], a[1], b[0], b[1]});
-}
-
 // The state of one wave: all DK rows of 32 columns.  In memory [rows][cols], or transposed.
+// Its products' left operand has its rows in an order (`ordered` reads) that puts
+// 8 neighbouring rows of the state into registers 8 u .. 8 u + 7 of a tile, so that
+// they are an operand of the output's product against plain rows of x.
 template <int DK> struct State {
   f32x16 m[DK / 32];
+  static __device__ int row_of(int t, int i) { return t * 32 + 16 * (i >> 3) + 8 * ((threadIdx.x & 63) >> 5) + (i & 7); }
   __device__ void zero() {
 #pragma unroll
     for (int t = 0; t < DK / 32; ++t) m[t] = f32x16{};
@@ -77,7 +65,7 @@ template <int DK> struct State {
     for (int t = 0; t < DK / 32; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int row = t * 32 + c_row(i);
+        const int row = row_of(t, i);
         m[t][i] = row < rows && col < cols ? factor * (swapped ? p[col * rows + row] : p[row * cols + col]) : 0.0f;
       }
   }
@@ -86,7 +74,7 @@ template <int DK> struct State {
     for (int t = 0; t < DK / 32; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int row = t * 32 + c_row(i);
+        const int row = row_of(t, i);
         if (row < rows && col < cols) p[swapped ? col * rows + row : row * cols + col] = factor * m[t][i];
       }
   }
@@ -104,25 +92,24 @@ template <> struct Terms<half> { static constexpr int n = 2; };
 // only forms its own sum, k_decay_scan turns the sums into the states before
 // the segments, and a second launch with OUT true starts from those.
 template <class T, int DK, int DV, bool OUT>
-__global__ __launch_bounds__(2 * DV, 1) void k_decay_chunks(DecayArgs a) {
+__global__ __launch_bounds__(2 * DV, DK == 128 && DV == 64 ? 1 : 2) void k_decay_chunks(DecayArgs a) {
   constexpr int BLOCK = 2 * DV, WAVES = DV / 32;
   SEQ_SHARED T sx[OUT ? kChunk * DK : 8], sy[kChunk * DK], sz[kChunk * DV];
   SEQ_SHARED T sp[OUT ? kChunk * kChunk : 8];
   SEQ_SHARED float s_age[kChunk];            // a^(rows - 1 - j) of the chunk's rows
   const Role& role = a.role[blockIdx.z];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = wave_index();
   const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads;
   const int n = rows_of(a, b);
   const int first = blockIdx.y * a.segment_rows, end = min(first + a.segment_rows, n);
-  const float lambda = a.log_decay[h] * kLog2e;
+  const float lambda = decay_rate(a.log_decay, h);
   const int64_t list = (int64_t)b * a.heads + h;
   const int64_t turn = role.reversed ? n - 1 : 0, sign = role.reversed ? -1 : 1;
-  const T* xp = at<T>(role.x, b, turn, h);
-  const T* yp = at<T>(role.y, b, turn, h);
-  const T* zp = at<T>(role.z, b, turn, h);
-  const int64_t xs = sign * role.x.t, ys = sign * role.y.t, zs = sign * role.z.t;
   const int col = wave * 32 + (lane & 31);
 
+  Lanes<DK> at_k;
+  Lanes<DV> at_v;
+  Lanes<64> at_p;
   State<DK> st;
   float* mine = role.states + (list * a.segments + blockIdx.y) * (DK * DV);
   if (OUT && a.segments > 1)
@@ -135,11 +122,15 @@ __global__ __launch_bounds__(2 * DV, 1) void k_decay_chunks(DecayArgs a) {
   if (first < end) {
     Staged<T, DK, BLOCK> rx, ry;
     Staged<T, DV, BLOCK> rz;
-    if (OUT) rx.load(xp, xs, first, end, a.dim_x);
-    ry.load(yp, ys, first, end, a.dim_x);
-    rz.load(zp, zs, first, end, a.dim_z);
+    if (OUT) rx.init(at<T>(role.x, b, turn, h), sign * role.x.t, a.dim_x);
+    ry.init(at<T>(role.y, b, turn, h), sign * role.y.t, a.dim_x);
+    rz.init(at<T>(role.z, b, turn, h), sign * role.z.t, a.dim_z);
+    if (OUT) rx.load(first, end);
+    ry.load(first, end);
+    rz.load(first, end);
     for (int row0 = first; row0 < end; row0 += kChunk) {
       const int count = min(kChunk, end - row0);
+      if (DK == 128) at_k.forget();
       // the gradient of the last state meets the last row without a decay
       const int less = role.reversed && row0 == 0 ? 1 : 0;
       if (OUT) rx.store(sx);
@@ -148,11 +139,6 @@ __global__ __launch_bounds__(2 * DV, 1) void k_decay_chunks(DecayArgs a) {
       if (threadIdx.x < kChunk)
         s_age[threadIdx.x] = (int)threadIdx.x < count ? decay_power(lambda, count - 1 - threadIdx.x) : 0.0f;
       __syncthreads();
-      if (row0 + kChunk < end) {
-        if (OUT) rx.load(xp, xs, row0 + kChunk, end, a.dim_x);
-        ry.load(yp, ys, row0 + kChunk, end, a.dim_x);
-        rz.load(zp, zs, row0 + kChunk, end, a.dim_z);
-      }
       if (OUT) {
         // Quarters (0, 0), (1, 0), (1, 1) of the products of rows, transposed (columns are i), one or two a wave.
         for (int quarter = wave; quarter < 3; quarter += WAVES) {
@@ -160,15 +146,16 @@ __global__ __launch_bounds__(2 * DV, 1) void k_decay_chunks(DecayArgs a) {
           f32x16 s = f32x16{};
 #pragma unroll
           for (int ks = 0; ks < DK / 16; ++ks)
-            s = mfma32(tile_rows<T, DK>(sy, jb * 32, ks), tile_rows<T, DK>(sx, ib * 32, ks), s);
+            s = mfma32(tile_rows<T, DK>(sy, at_k, jb * 32, ks), tile_rows<T, DK>(sx, at_k, ib * 32, ks), s);
           const int i = ib * 32 + (lane & 31);
 #pragma unroll
           for (int r4 = 0; r4 < 4; ++r4) {
             float p[4];
             const int j = jb * 32 + 8 * r4 + 4 * (lane >> 5);
+            const float gap = (float)(i - j);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              p[e] = j + e <= i ? s[4 * r4 + e] * decay_power(lambda, i - j - e) : 0.0f;
+              p[e] = j + e <= i ? s[4 * r4 + e] * decay_power(lambda, gap - (float)e) : 0.0f;
             *reinterpret_cast<u32x2*>(sp + tile_at<64>(i, j >> 3) + (j & 7)) =
                 __builtin_bit_cast(u32x2, pack4<T>(p[0], p[1], p[2], p[3]));
           }
@@ -177,7 +164,7 @@ __global__ __launch_bounds__(2 * DV, 1) void k_decay_chunks(DecayArgs a) {
       }
       x8<T> z[4];
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) z[ks] = tile_columns_straight<T, DV>(sz, 16 * ks, wave);
+      for (int ks = 0; ks < 4; ++ks) z[ks] = tile_columns_straight<T, DV>(sz, at_v.straight, 16 * ks, wave);
       if (OUT) {
         // The products of rows and the state are rounded to the tensors' type for the
         // output's products: as much as the output's own rounding.
@@ -191,17 +178,25 @@ __global__ __launch_bounds__(2 * DV, 1) void k_decay_chunks(DecayArgs a) {
               float m[8];
 #pragma unroll
               for (int e = 0; e < 8; ++e) m[e] = st.m[t][8 * u + e];
-              o = mfma32(pack8<T>(m), tile_rows_as_c<T, DK>(sx, ib * 32, 2 * t + u), o);
+              o = mfma32(pack8<T>(m), tile_rows<T, DK>(sx, at_k, ib * 32, 2 * t + u), o);
             }
           const int i = ib * 32 + (lane & 31);
           o *= decay_power(lambda, i + 1 - less);
 #pragma unroll
-          for (int ks = 0; ks < 2 * (ib + 1); ++ks) o = mfma32(z[ks], tile_rows<T, 64>(sp, ib * 32, ks), o);
+          for (int ks = 0; ks < 2 * (ib + 1); ++ks) o = mfma32(z[ks], tile_rows<T, 64>(sp, at_p, ib * 32, ks), o);
           if (i < count) {
             const int64_t row = turn + sign * (row0 + i);
             store_column<T>(at<T>(role.out, b, row, h), wave, o, role.factor, a.dim_z);
           }
         }
+      }
+      // The next rows' loads are under way during the state's products alone: with the
+      // output's in between as well, the registers that they fill would not fit.
+      __builtin_amdgcn_sched_barrier(0);
+      if (row0 + kChunk < end) {
+        if (OUT) rx.load(row0 + kChunk, end);
+        ry.load(row0 + kChunk, end);
+        rz.load(row0 + kChunk, end);
       }
       const float age = decay_power(lambda, count - less);
 #pragma unroll
@@ -222,7 +217,7 @@ __global__ __launch_bounds__(2 * DV, 1) void k_decay_chunks(DecayArgs a) {
         }
 #pragma unroll
         for (int t = 0; t < DK / 32; ++t) {
-          const x8<T> y = tile_columns_straight<T, DK>(sy, 16 * ks, t);
+          const x8<T> y = tile_columns_straight<T, DK>(sy, at_k.ordered, 16 * ks, t);
 #pragma unroll
           for (int p = Terms<T>::n - 1; p >= 0; --p) st.m[t] = mfma32(y, part[p], st.m[t]);
         }
@@ -254,7 +249,7 @@ template <int DK, int DV> __global__ __launch_bounds__(256) void k_decay_scan(De
   const int e = blockIdx.x % (DK * DV / 256) * 256 + threadIdx.x, row = e / DV, col = e % DV;
   const int b = (int)(list / a.heads), h = (int)(list % a.heads);
   const int n = rows_of(a, b);
-  const float lambda = a.log_decay[h] * kLog2e;
+  const float lambda = decay_rate(a.log_decay, h);
   const bool real = row < a.dim_x && col < a.dim_z;
   const int64_t outer = list * a.dim_x * a.dim_z + (role.swapped ? col * a.dim_x + row : row * a.dim_z + col);
   float m = role.init && real ? role.init_factor * role.init[outer] : 0.0f;
@@ -308,7 +303,7 @@ template <class T, int DK, int DV> __global__ __launch_bounds__(256) void k_deca
 #pragma unroll
     for (int e = 0; e < 4; ++e) vv[e] = (float)raw[e];
   }
-  const float decay = fast_exp2(a.log_decay[h] * kLog2e);
+  const float decay = decay_power(decay_rate(a.log_decay, h), 1.0f);
   f32x4 o = f32x4{};
 #pragma unroll
   for (int i = 0; i < N; ++i) {
@@ -427,6 +422,7 @@ extern "C" qds_status qds_decay_forward(const qds_decay_config* c, qds_view q, q
   if (c->length > 0 && (!usable(q) || !usable(k) || !usable(v) || !usable(o))) return QDS_ERR_INVALID_ARG;
   if (need && (!workspace || ((uintptr_t)workspace & 255))) return QDS_ERR_INVALID_ARG;
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
+  if (c->length > 0 && (!near_rows(q) || !near_rows(k) || !near_rows(v))) return QDS_ERR_UNSUPPORTED;
   DecayArgs a = decay_args(c, segment_plan(c, 1), lengths, log_decay);
   a.role[0] = Role{view(q), view(k), view(v), view(o), state_in, state_out, (float*)workspace, c->scale, 1.0f, 1.0f, false, false};
   run(c, a, 1, stream);
@@ -456,6 +452,7 @@ extern "C" qds_status qds_decay_backward(const qds_decay_config* c, qds_view dou
     return QDS_ERR_INVALID_ARG;
   if (need && (!workspace || ((uintptr_t)workspace & 255))) return QDS_ERR_INVALID_ARG;
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
+  if (c->length > 0 && (!near_rows(dout) || !near_rows(q) || !near_rows(k) || !near_rows(v))) return QDS_ERR_UNSUPPORTED;
   const SegmentPlan p = segment_plan(c, 3);
   const uint64_t each = state_bytes(c, p.segments) / sizeof(float);
   float* ws = (float*)workspace;

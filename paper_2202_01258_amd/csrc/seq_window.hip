@@ -48,6 +48,10 @@ struct KeyTiles {
   __device__ int row(int t) const { return (t < first ? t : band + t - first) * 64; }
 };
 
+// How far back key j is seen.  Row i sees it where i - j, taken as unsigned, is below
+// this: one comparison, without the branches that && and || would make of every element.
+__device__ inline uint32_t reach_of(int window, int sinks, int j) { return j < sinks ? 0x40000000u : (uint32_t)window; }
+
 // ---------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------
@@ -60,7 +64,8 @@ constexpr int kForwardRows = 32 * kWaves;
 template <class T, int DP>
 __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int q_blocks) {
   SEQ_SHARED T sk[2][64 * DP], sv[2][64 * DP];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = wave_index();
+  Lanes<DP> place;
   const int group = a.heads / a.kv_heads;
   int id = xcd_order(blockIdx.x, gridDim.x);
   const int g = id % group;
@@ -70,7 +75,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
   id /= q_blocks;
   const int hk = id % a.kv_heads, b = id / a.kv_heads;
   const int h = hk * group + g;
-  const int n = rows_of(a, b);
+  const int n = rows_of(a, b), window = a.window, sinks = a.sinks;
   const int i0 = block * kForwardRows, w0 = i0 + 32 * wave;
   const int i = w0 + (lane & 31);
   T* o_row = at<T>(a.o, b, i, h);
@@ -83,12 +88,12 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
     const float c = a.scale * kLog2e;
     x8<T> q[DP / 16];
     load_rows<T, DP>(q, at<T>(a.q, b, i, h), i < n, a.dim);
-    const T* kp = at<T>(a.k, b, 0, hk);
-    const T* vp = at<T>(a.v, b, 0, hk);
     const KeyTiles tiles(a, i0, kForwardRows, n);
     Staged<T, DP, kBlock> rk, rv;
-    rk.load(kp, a.k.t, tiles.row(0), n, a.dim);
-    rv.load(vp, a.v.t, tiles.row(0), n, a.dim);
+    rk.init(at<T>(a.k, b, 0, hk), a.k.t, a.dim);
+    rv.init(at<T>(a.v, b, 0, hk), a.v.t, a.dim);
+    rk.load(tiles.row(0), n);
+    rv.load(tiles.row(0), n);
     rk.store(sk[0]);
     rv.store(sv[0]);
     float m = kNoMax, sum = 0.0f;
@@ -97,32 +102,34 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
       const int j0 = tiles.row(t);
       const bool more = t + 1 < tiles.count;
       if (more) {
-        rk.load(kp, a.k.t, tiles.row(t + 1), n, a.dim);
-        rv.load(vp, a.v.t, tiles.row(t + 1), n, a.dim);
+        rk.load(tiles.row(t + 1), n);
+        rv.load(tiles.row(t + 1), n);
       }
       const T *tk = sk[t & 1], *tv = sv[t & 1];
-      const bool none = j0 > w0 + 31 || (w0 - (j0 + 63) >= a.window && j0 >= a.sinks);
+      const bool none = j0 > w0 + 31 || (w0 - (j0 + 63) >= window && j0 >= sinks);
       if (!none) {
         f32x16 s[2];
 #pragma unroll
         for (int jb = 0; jb < 2; ++jb) {
           s[jb] = f32x16{};
 #pragma unroll
-          for (int ks = 0; ks < DP / 16; ++ks) s[jb] = mfma32(tile_rows<T, DP>(tk, jb * 32, ks), q[ks], s[jb]);
+          for (int ks = 0; ks < DP / 16; ++ks) s[jb] = mfma32(tile_rows<T, DP>(tk, place, jb * 32, ks), q[ks], s[jb]);
         }
-        const bool all = j0 + 63 <= w0 && (w0 + 31 - j0 < a.window || j0 + 63 < a.sinks);
+        const bool all = j0 + 63 <= w0 && (w0 + 31 - j0 < window || j0 + 63 < sinks);
+        if (!all) {
+#pragma unroll
+          for (int jb = 0; jb < 2; ++jb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int j = j0 + jb * 32 + c_row(r);
+              s[jb][r] = (uint32_t)(i - j) < reach_of(window, sinks, j) ? s[jb][r] : -INFINITY;
+            }
+        }
         float top = kNoMax;
 #pragma unroll
         for (int jb = 0; jb < 2; ++jb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            if (!all) {
-              const int j = j0 + jb * 32 + c_row(r);
-              const bool seen = j <= i && (i - j < a.window || j < a.sinks);
-              s[jb][r] = seen ? s[jb][r] : -INFINITY;
-            }
-            top = fmaxf(top, s[jb][r]);
-          }
+          for (int r = 0; r < 16; ++r) top = fmaxf(top, s[jb][r]);
         top = max_halves(top) * c;
         // The maximum is moved only where a weight would pass 2^8: any reference
         // gives the same quotient, and most tiles then need no rescaling.
@@ -148,7 +155,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
             const x8<T> pb = pack8<T>(p + 8 * u);
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d)
-              o[d] = mfma32(tile_columns<T, DP>(tv, jb * 32 + 16 * u, d), pb, o[d]);
+              o[d] = mfma32(tile_columns<T, DP>(tv, place, jb * 32 + 16 * u, d), pb, o[d]);
           }
         }
       }
@@ -182,9 +189,10 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
 
 // dq of 128 rows of one head, as the forward pass; also writes delta.
 template <class T, int DP>
-__global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dq(WindowArgs a, int q_blocks) {
+__global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blocks) {
   SEQ_SHARED T sk[2][64 * DP], sv[2][64 * DP];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = wave_index();
+  Lanes<DP> place;
   const int group = a.heads / a.kv_heads;
   int id = xcd_order(blockIdx.x, gridDim.x);
   const int g = id % group;
@@ -193,7 +201,7 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dq(WindowAr
   id /= q_blocks;
   const int hk = id % a.kv_heads, b = id / a.kv_heads;
   const int h = hk * group + g;
-  const int n = rows_of(a, b);
+  const int n = rows_of(a, b), window = a.window, sinks = a.sinks;
   const int i0 = block * kForwardRows, w0 = i0 + 32 * wave;
   const int i = w0 + (lane & 31);
   const int64_t flat = ((int64_t)b * a.heads + h) * a.length + i;
@@ -218,12 +226,12 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dq(WindowAr
     delta = sum_halves(delta);
     if (lane < 32 && i < n) a.delta[flat] = delta;
     const float lse = i < n ? a.lse[flat] * kLog2e : INFINITY;   // rows past the end: p = 0
-    const T* kp = at<T>(a.k, b, 0, hk);
-    const T* vp = at<T>(a.v, b, 0, hk);
     const KeyTiles tiles(a, i0, kForwardRows, n);
     Staged<T, DP, kBlock> rk, rv;
-    rk.load(kp, a.k.t, tiles.row(0), n, a.dim);
-    rv.load(vp, a.v.t, tiles.row(0), n, a.dim);
+    rk.init(at<T>(a.k, b, 0, hk), a.k.t, a.dim);
+    rv.init(at<T>(a.v, b, 0, hk), a.v.t, a.dim);
+    rk.load(tiles.row(0), n);
+    rv.load(tiles.row(0), n);
     rk.store(sk[0]);
     rv.store(sv[0]);
     for (int t = 0; t < tiles.count; ++t) {
@@ -231,37 +239,38 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dq(WindowAr
       const int j0 = tiles.row(t);
       const bool more = t + 1 < tiles.count;
       if (more) {
-        rk.load(kp, a.k.t, tiles.row(t + 1), n, a.dim);
-        rv.load(vp, a.v.t, tiles.row(t + 1), n, a.dim);
+        rk.load(tiles.row(t + 1), n);
+        rv.load(tiles.row(t + 1), n);
       }
       const T *tk = sk[t & 1], *tv = sv[t & 1];
-      const bool none = j0 > w0 + 31 || (w0 - (j0 + 63) >= a.window && j0 >= a.sinks);
+      const bool none = j0 > w0 + 31 || (w0 - (j0 + 63) >= window && j0 >= sinks);
+      if (DP == 128) place.forget();
       if (!none) {
-        const bool all = j0 + 63 <= w0 && (w0 + 31 - j0 < a.window || j0 + 63 < a.sinks);
+        const bool all = j0 + 63 <= w0 && (w0 + 31 - j0 < window || j0 + 63 < sinks);
 #pragma unroll
         for (int jb = 0; jb < 2; ++jb) {
+          __builtin_amdgcn_sched_barrier(0);       // one half's products at a time: both would not fit the registers
           f32x16 s = f32x16{}, dp = f32x16{};
 #pragma unroll
-          for (int ks = 0; ks < DP / 16; ++ks) s = mfma32(tile_rows<T, DP>(tk, jb * 32, ks), q[ks], s);
+          for (int ks = 0; ks < DP / 16; ++ks) s = mfma32(tile_rows<T, DP>(tk, place, jb * 32, ks), q[ks], s);
 #pragma unroll
-          for (int ks = 0; ks < DP / 16; ++ks) dp = mfma32(tile_rows<T, DP>(tv, jb * 32, ks), go[ks], dp);
+          for (int ks = 0; ks < DP / 16; ++ks) dp = mfma32(tile_rows<T, DP>(tv, place, jb * 32, ks), go[ks], dp);
+          if (!all) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int j = j0 + jb * 32 + c_row(r);
+              s[r] = (uint32_t)(i - j) < reach_of(window, sinks, j) ? s[r] : -INFINITY;
+            }
+          }
           float ds[16];
 #pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            float p = fast_exp2(fmaf(s[r], c, -lse));
-            if (!all) {
-              const int j = j0 + jb * 32 + c_row(r);
-              const bool seen = j <= i && (i - j < a.window || j < a.sinks);
-              p = seen ? p : 0.0f;
-            }
-            ds[r] = p * (dp[r] - delta);
-          }
+          for (int r = 0; r < 16; ++r) ds[r] = fast_exp2(fmaf(s[r], c, -lse)) * (dp[r] - delta);
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const x8<T> db = pack8<T>(ds + 8 * u);
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d)
-              dq[d] = mfma32(tile_columns<T, DP>(tk, jb * 32 + 16 * u, d), db, dq[d]);
+              dq[d] = mfma32(tile_columns<T, DP>(tk, place, jb * 32 + 16 * u, d), db, dq[d]);
           }
         }
       }
@@ -303,16 +312,18 @@ template <class T, int DP>
 __global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dkdv(WindowArgs a, KeyPlan plan, float* parts) {
   SEQ_SHARED T sq[2][64 * DP], sg[2][64 * DP];
   SEQ_SHARED float s_lse[2][64], s_delta[2][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = wave_index();
+  Lanes<DP> place;
   const int group = a.heads / a.kv_heads;
   const int id = xcd_order(blockIdx.x, gridDim.x);
   const int head = id / plan.items;           // b * kv_heads + hk
   const KeyItem item = key_item(plan, id % plan.items);
   const int hk = head % a.kv_heads, b = head / a.kv_heads;
-  const int n = rows_of(a, b);
+  const int n = rows_of(a, b), window = a.window, sinks = a.sinks;
   const int j0 = item.block * kKeyRows, w0 = j0 + 32 * wave;
   const int j = w0 + (lane & 31);
   const float c = a.scale * kLog2e;
+  const uint32_t reach = reach_of(window, sinks, j);
 
   f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
@@ -320,7 +331,7 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dkdv(Window
   // the rows that see this block, in tiles of 64, for each head of the group
   int unit = 0, stop = 0, q0 = 0, per_head = 1;
   if (j0 < n) {
-    const int64_t last = j0 < a.sinks ? n - 1 : min((int64_t)n - 1, (int64_t)j0 + kKeyRows - 1 + a.window - 1);
+    const int64_t last = j0 < sinks ? n - 1 : min((int64_t)n - 1, (int64_t)j0 + kKeyRows - 1 + window - 1);
     q0 = j0 / 64;
     per_head = (int)(last / 64) - q0 + 1;
     const int64_t units = (int64_t)per_head * group;
@@ -332,11 +343,15 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dkdv(Window
     load_rows<T, DP>(k, at<T>(a.k, b, j, hk), j < n, a.dim);
     load_rows<T, DP>(v, at<T>(a.v, b, j, hk), j < n, a.dim);
     Staged<T, DP, kBlock> rq, rg;
+    rq.init(nullptr, a.q.t, a.dim);
+    rg.init(nullptr, a.dout.t, a.dim);
     float r_lse = 0.0f, r_delta = 0.0f;
     auto fetch = [&](int u) {
       const int h = hk * group + u / per_head, row0 = (q0 + u % per_head) * 64;
-      rq.load(at<T>(a.q, b, 0, h), a.q.t, row0, n, a.dim);
-      rg.load(at<T>(a.dout, b, 0, h), a.dout.t, row0, n, a.dim);
+      rq.base = at<T>(a.q, b, 0, h);
+      rg.base = at<T>(a.dout, b, 0, h);
+      rq.load(row0, n);
+      rg.load(row0, n);
       if (threadIdx.x < 64) {
         const int i = row0 + threadIdx.x;
         const int64_t flat = ((int64_t)b * a.heads + h) * a.length + i;
@@ -362,14 +377,18 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dkdv(Window
 #pragma unroll
       for (int ib = 0; ib < 2; ++ib) {
         const int r0 = row0 + ib * 32;
-        const bool none = r0 + 31 < w0 || (r0 - (w0 + 31) >= a.window && w0 >= a.sinks) || r0 >= n;
+        const bool none = r0 + 31 < w0 || (r0 - (w0 + 31) >= window && w0 >= sinks) || r0 >= n;
         if (none) continue;
-        const bool all = r0 >= w0 + 31 && (r0 + 31 - w0 < a.window || w0 + 31 < a.sinks);
+        const bool all = r0 >= w0 + 31 && (r0 + 31 - w0 < window || w0 + 31 < sinks);
         f32x16 s = f32x16{}, dp = f32x16{};
 #pragma unroll
-        for (int ks = 0; ks < DP / 16; ++ks) s = mfma32(tile_rows<T, DP>(tq, ib * 32, ks), k[ks], s);
+        for (int ks = 0; ks < DP / 16; ++ks) s = mfma32(tile_rows<T, DP>(tq, place, ib * 32, ks), k[ks], s);
 #pragma unroll
-        for (int ks = 0; ks < DP / 16; ++ks) dp = mfma32(tile_rows<T, DP>(tg, ib * 32, ks), v[ks], dp);
+        for (int ks = 0; ks < DP / 16; ++ks) dp = mfma32(tile_rows<T, DP>(tg, place, ib * 32, ks), v[ks], dp);
+        if (!all) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] = (uint32_t)(r0 + c_row(r) - j) < reach ? s[r] : -INFINITY;
+        }
         float p[16], ds[16];
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
@@ -380,11 +399,6 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dkdv(Window
           for (int e = 0; e < 4; ++e) {
             const int r = 4 * r4 + e;
             p[r] = fast_exp2(fmaf(s[r], c, -lse[e]));
-            if (!all) {
-              const int i = r0 + c_row(r);
-              const bool seen = j <= i && (i - j < a.window || j < a.sinks);
-              p[r] = seen ? p[r] : 0.0f;
-            }
             ds[r] = p[r] * (dp[r] - delta[e]);
           }
         }
@@ -393,8 +407,8 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dkdv(Window
           const x8<T> pb = pack8<T>(p + 8 * u), db = pack8<T>(ds + 8 * u);
 #pragma unroll
           for (int d = 0; d < DP / 32; ++d) {
-            dv[d] = mfma32(tile_columns<T, DP>(tg, ib * 32 + 16 * u, d), pb, dv[d]);
-            dk[d] = mfma32(tile_columns<T, DP>(tq, ib * 32 + 16 * u, d), db, dk[d]);
+            dv[d] = mfma32(tile_columns<T, DP>(tg, place, ib * 32 + 16 * u, d), pb, dv[d]);
+            dk[d] = mfma32(tile_columns<T, DP>(tq, place, ib * 32 + 16 * u, d), db, dk[d]);
           }
         }
       }
@@ -484,7 +498,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_step(StepArgs a) {
   constexpr int kStage = kWaves * kStrip * DP * 2, kOut = kWaves * 16 * OUT * 4;
   SEQ_SHARED char lds[kStage > kOut ? kStage : kOut];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = wave_index();
   const int group = a.heads / a.kv_heads, slots = a.window + a.sinks;
   const int tile = blockIdx.x % a.tiles, head = blockIdx.x / a.tiles;
   const int hk = head % a.kv_heads, b = head / a.kv_heads;
@@ -795,6 +809,7 @@ extern "C" qds_status qds_window_forward(const qds_window_config* c, qds_view q,
   if (st != QDS_OK) return st;
   if (c->batch == 0 || c->length == 0) return QDS_OK;
   if (!usable(q) || !usable(k) || !usable(v) || !usable(o) || !lse) return QDS_ERR_INVALID_ARG;
+  if (!near_rows(k) || !near_rows(v)) return QDS_ERR_UNSUPPORTED;
   WindowArgs a = window_args(c, lengths);
   a.q = view(q), a.k = view(k), a.v = view(v), a.o = view(o), a.lse = lse;
   const int blocks = (int)ceil_div(c->length, kForwardRows);
@@ -827,6 +842,7 @@ extern "C" qds_status qds_window_backward(const qds_window_config* c, qds_view d
       !usable(dk) || !usable(dv) || !lse || !workspace || ((uintptr_t)workspace & 255))
     return QDS_ERR_INVALID_ARG;
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
+  if (!near_rows(q) || !near_rows(k) || !near_rows(v) || !near_rows(dout)) return QDS_ERR_UNSUPPORTED;
   WindowArgs a = window_args(c, lengths);
   a.q = view(q), a.k = view(k), a.v = view(v), a.o = view(o), a.dout = view(dout);
   a.dq = view(dq), a.dk = view(dk), a.dv = view(dv), a.lse = const_cast<float*>(lse);
