@@ -18,6 +18,7 @@ namespace seq {
 namespace {
 
 constexpr int kChunk = 64;
+constexpr int kEarly = 128;
 
 // a^n for lambda = log2(a).  `lambda` is kept finite (decay_rate), so that a^0 is 1
 // for a = 0, too; below the bound a^1 is 0 already.
@@ -125,9 +126,20 @@ __global__ __launch_bounds__(2 * DV, DK == 128 && DV == 64 ? 1 : 2) void k_decay
     if (OUT) rx.init(at<T>(role.x, b, turn, h), sign * role.x.t, a.dim_x);
     ry.init(at<T>(role.y, b, turn, h), sign * role.y.t, a.dim_x);
     rz.init(at<T>(role.z, b, turn, h), sign * role.z.t, a.dim_z);
-    if (OUT) rx.load(first, end);
-    ry.load(first, end);
-    rz.load(first, end);
+    // factor a^(i-j) of a wave's products of rows, 0 for j > i: the same in every chunk
+    float fade[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int gap = (wave == 1 ? 32 : 0) + (lane & 31) - c_row(r);
+      fade[r] = gap >= 0 ? role.factor * decay_power(lambda, gap) : 0.0f;
+    }
+    auto fetch = [&](int row0) {
+      if (row0 >= end) return;
+      if (OUT) rx.load(row0, end);
+      ry.load(row0, end);
+      rz.load(row0, end);
+    };
+    fetch(first);
     for (int row0 = first; row0 < end; row0 += kChunk) {
       const int count = min(kChunk, end - row0);
       if (DK == 128) at_k.forget();
@@ -139,10 +151,11 @@ __global__ __launch_bounds__(2 * DV, DK == 128 && DV == 64 ? 1 : 2) void k_decay
       if (threadIdx.x < kChunk)
         s_age[threadIdx.x] = (int)threadIdx.x < count ? decay_power(lambda, count - 1 - threadIdx.x) : 0.0f;
       __syncthreads();
+      if (DK + DV <= kEarly) fetch(row0 + kChunk);
       if (OUT) {
         // Quarters (0, 0), (1, 0), (1, 1) of the products of rows, transposed (columns are i), one or two a wave.
         for (int quarter = wave; quarter < 3; quarter += WAVES) {
-          const int ib = quarter > 0, jb = quarter > 1;
+          const int ib = quarter > 0, jb = quarter > 1;      // with two waves, one has both on the diagonal
           f32x16 s = f32x16{};
 #pragma unroll
           for (int ks = 0; ks < DK / 16; ++ks)
@@ -150,14 +163,10 @@ __global__ __launch_bounds__(2 * DV, DK == 128 && DV == 64 ? 1 : 2) void k_decay
           const int i = ib * 32 + (lane & 31);
 #pragma unroll
           for (int r4 = 0; r4 < 4; ++r4) {
-            float p[4];
             const int j = jb * 32 + 8 * r4 + 4 * (lane >> 5);
-            const float gap = (float)(i - j);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              p[e] = j + e <= i ? s[4 * r4 + e] * decay_power(lambda, gap - (float)e) : 0.0f;
-            *reinterpret_cast<u32x2*>(sp + tile_at<64>(i, j >> 3) + (j & 7)) =
-                __builtin_bit_cast(u32x2, pack4<T>(p[0], p[1], p[2], p[3]));
+            const float* f = fade + 4 * r4;
+            *reinterpret_cast<u32x2*>(sp + tile_at<64>(i, j >> 3) + (j & 7)) = __builtin_bit_cast(
+                u32x2, pack4<T>(s[4 * r4] * f[0], s[4 * r4 + 1] * f[1], s[4 * r4 + 2] * f[2], s[4 * r4 + 3] * f[3]));
           }
         }
         __syncthreads();
@@ -181,22 +190,20 @@ __global__ __launch_bounds__(2 * DV, DK == 128 && DV == 64 ? 1 : 2) void k_decay
               o = mfma32(pack8<T>(m), tile_rows<T, DK>(sx, at_k, ib * 32, 2 * t + u), o);
             }
           const int i = ib * 32 + (lane & 31);
-          o *= decay_power(lambda, i + 1 - less);
+          o *= role.factor * decay_power(lambda, i + 1 - less);
 #pragma unroll
           for (int ks = 0; ks < 2 * (ib + 1); ++ks) o = mfma32(z[ks], tile_rows<T, 64>(sp, at_p, ib * 32, ks), o);
           if (i < count) {
             const int64_t row = turn + sign * (row0 + i);
-            store_column<T>(at<T>(role.out, b, row, h), wave, o, role.factor, a.dim_z);
+            store_column<T>(at<T>(role.out, b, row, h), wave, o, 1.0f, a.dim_z);
           }
         }
       }
       // The next rows' loads are under way during the state's products alone: with the
       // output's in between as well, the registers that they fill would not fit.
-      __builtin_amdgcn_sched_barrier(0);
-      if (row0 + kChunk < end) {
-        if (OUT) rx.load(row0 + kChunk, end);
-        ry.load(row0 + kChunk, end);
-        rz.load(row0 + kChunk, end);
+      if (DK + DV > kEarly) {
+        __builtin_amdgcn_sched_barrier(0);
+        fetch(row0 + kChunk);
       }
       const float age = decay_power(lambda, count - less);
 #pragma unroll
