@@ -150,15 +150,15 @@ inline bool near_rows(const qds_view& v) {
   return v.stride[1] < (1 << 23) && v.stride[1] > -(1 << 23);
 }
 
-// 64 rows of a tensor in the registers of a workgroup of BLOCK threads (to be
+// ROWS rows of a tensor in the registers of a workgroup of BLOCK threads (to be
 // written to LDS): rows from `end` on and columns from `dim` on are zero and
 // are not read.  Buffer loads: the address is a scalar base per tile, a lane's
 // offset that never changes and a scalar offset per load, and an offset past the
 // buffer's size loads zero, so a load costs two vector instructions and no branch.
 constexpr uint32_t kBufferSize = 0x7fffffffu, kOutside = 0x80000000u;
 constexpr int kBufferFlags = 0x00027000;           // raw buffer of 32-bit data
-template <class T, int DP, int BLOCK> struct Staged {
-  static constexpr int N = 64 * DP / 8 / BLOCK, STEP = BLOCK / (DP / 8);   // loads; rows between two of a thread's
+template <class T, int DP, int BLOCK, int ROWS = 64> struct Staged {
+  static constexpr int N = ROWS * DP / 8 / BLOCK, STEP = BLOCK / (DP / 8);   // loads; rows between two of a thread's
   u32x4 r[N];
   const T* base;
   int64_t stride;
@@ -171,11 +171,11 @@ template <class T, int DP, int BLOCK> struct Staged {
     const int c = threadIdx.x % (DP / 8), row = threadIdx.x / (DP / 8);
     const uint32_t bytes = (uint32_t)(stride < 0 ? -stride : stride) * 2;
     step = STEP * bytes;
-    offset = (stride < 0 ? 63 - row : row) * bytes + c * 16;
+    offset = (stride < 0 ? ROWS - 1 - row : row) * bytes + c * 16;
     place = c * 8 < dim ? row : 1 << 30;
   }
   __device__ void load(int row0, int end) {
-    const T* first = base + (int64_t)(stride < 0 ? row0 + 63 : row0) * stride;
+    const T* first = base + (int64_t)(stride < 0 ? row0 + ROWS - 1 : row0) * stride;
     const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, kBufferSize, kBufferFlags);
     const uint32_t down = stride < 0 ? step : 0, up = stride < 0 ? 0 : step;
     const int rows = end - row0;
@@ -235,6 +235,20 @@ template <class T, int DP> __device__ inline x8<T> tile_columns_straight(const T
   const x4<T> b = lds_read_transposed(tile_byte(lds, second + (row0 + 4) * DP * 2));
   return join8<T>(a, b);
 }
+// Asks the compiler to keep LDS reads AHEAD products in front of the N products
+// that use them (READS reads each) in the code before it, up to the last branch.
+// Left alone it reads each operand right before its product, and every product
+// then waits for LDS (some 100 cycles against 32).
+template <int N, int READS, int AHEAD> __device__ inline void reads_ahead() {
+  __builtin_amdgcn_sched_group_barrier(0x100, READS * AHEAD, 0);
+#pragma unroll
+  for (int i = 0; i < N - AHEAD; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
+}
+
 // The wave's number in its workgroup, as a scalar (so that what depends on it branches for the whole wave).
 __device__ inline int wave_index() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 // Row of register i of a 32x32 C tile.

@@ -115,6 +115,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
 #pragma unroll
           for (int ks = 0; ks < DP / 16; ++ks) s[jb] = mfma32(tile_rows<T, DP>(tk, place, jb * 32, ks), q[ks], s[jb]);
         }
+        reads_ahead<DP / 8, 1, 4>();
         const bool all = j0 + 63 <= w0 && (w0 + 31 - j0 < window || j0 + 63 < sinks);
         if (!all) {
 #pragma unroll
@@ -308,10 +309,17 @@ __device__ inline KeyItem key_item(const KeyPlan& p, int x) {
   return {p.first + x / p.band_cut, x % p.band_cut, p.band_cut};
 }
 
+// A wave has 32 keys, a unit is 32 query rows of one head.  Scores have queries as
+// rows and keys as columns of the C tile, so that both the weights and the score
+// gradients are operands of the sums over queries as they are.  Keys stay in
+// registers; values do for 64 columns, and are read from LDS for 128, where the
+// registers that two waves on a SIMD leave each other are 160 for keys and sums.
 template <class T, int DP>
-__global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dkdv(WindowArgs a, KeyPlan plan, float* parts) {
-  SEQ_SHARED T sq[2][64 * DP], sg[2][64 * DP];
-  SEQ_SHARED float s_lse[2][64], s_delta[2][64];
+__global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan plan, float* parts) {
+  constexpr int QT = 32;
+  constexpr bool V_LDS = DP == 128;
+  SEQ_SHARED T sq[2][QT * DP], sg[2][QT * DP], sv[V_LDS ? kKeyRows * DP : 8];
+  SEQ_SHARED float s_lse[2][QT], s_delta[2][QT];
   const int lane = threadIdx.x & 63, wave = wave_index();
   Lanes<DP> place;
   const int group = a.heads / a.kv_heads;
@@ -328,63 +336,78 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dkdv(Window
   f32x16 dk[DP / 32], dv[DP / 32];
 #pragma unroll
   for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = f32x16{};
-  // the rows that see this block, in tiles of 64, for each head of the group
-  int unit = 0, stop = 0, q0 = 0, per_head = 1;
+  // the rows that see this block, in tiles of 32, for each head of the group
+  int unit = 0, stop = 0, per_head = 1;
   if (j0 < n) {
     const int64_t last = j0 < sinks ? n - 1 : min((int64_t)n - 1, (int64_t)j0 + kKeyRows - 1 + window - 1);
-    q0 = j0 / 64;
-    per_head = (int)(last / 64) - q0 + 1;
+    per_head = (int)((last - j0) / QT) + 1;
     const int64_t units = (int64_t)per_head * group;
     unit = (int)(units * item.piece / item.cut);
     stop = (int)(units * (item.piece + 1) / item.cut);
   }
   if (unit < stop) {
-    x8<T> k[DP / 16], v[DP / 16];
+    x8<T> k[DP / 16], v[V_LDS ? 1 : DP / 16];
     load_rows<T, DP>(k, at<T>(a.k, b, j, hk), j < n, a.dim);
-    load_rows<T, DP>(v, at<T>(a.v, b, j, hk), j < n, a.dim);
-    Staged<T, DP, kBlock> rq, rg;
+    if constexpr (V_LDS) {
+      Staged<T, DP, kBlock> rv;
+      rv.init(at<T>(a.v, b, 0, hk), a.v.t, a.dim);
+#pragma unroll
+      for (int half = 0; half < kKeyRows / 64; ++half) {
+        rv.load(j0 + half * 64, n);
+        rv.store(sv + half * 64 * DP);
+      }
+    } else {
+      load_rows<T, DP>(v, at<T>(a.v, b, j, hk), j < n, a.dim);
+    }
+    Staged<T, DP, kBlock, QT> rq, rg;
     rq.init(nullptr, a.q.t, a.dim);
     rg.init(nullptr, a.dout.t, a.dim);
     float r_lse = 0.0f, r_delta = 0.0f;
-    auto fetch = [&](int u) {
-      const int h = hk * group + u / per_head, row0 = (q0 + u % per_head) * 64;
+    int u_head = unit / per_head, u_row = unit % per_head;        // of the unit that is fetched next
+    int row_fetched = 0;
+    auto fetch = [&] {
+      const int h = hk * group + u_head;
+      row_fetched = j0 + u_row * QT;
       rq.base = at<T>(a.q, b, 0, h);
       rg.base = at<T>(a.dout, b, 0, h);
-      rq.load(row0, n);
-      rg.load(row0, n);
-      if (threadIdx.x < 64) {
-        const int i = row0 + threadIdx.x;
-        const int64_t flat = ((int64_t)b * a.heads + h) * a.length + i;
-        r_lse = i < n ? a.lse[flat] * kLog2e : INFINITY;     // rows past the end: p = 0
-        r_delta = i < n ? a.delta[flat] : 0.0f;
+      rq.load(row_fetched, n);
+      rg.load(row_fetched, n);
+      if (wave == 0) {
+        const int64_t flat = ((int64_t)b * a.heads + h) * a.length + min(row_fetched + (lane & 31), n - 1);
+        r_lse = a.lse[flat];
+        r_delta = a.delta[flat];
       }
+      if (++u_row == per_head) u_row = 0, ++u_head;
     };
     auto put = [&](int buf) {
       rq.store(sq[buf]);
       rg.store(sg[buf]);
-      if (threadIdx.x < 64) {
-        s_lse[buf][threadIdx.x] = r_lse;
+      if (threadIdx.x < QT) {
+        // rows past the end: p = 0
+        s_lse[buf][threadIdx.x] = row_fetched + (int)threadIdx.x < n ? r_lse * kLog2e : INFINITY;
         s_delta[buf][threadIdx.x] = r_delta;
       }
     };
-    fetch(unit);
+    fetch();
     put(0);
     for (int buf = 0; unit < stop; ++unit, buf ^= 1) {
       __syncthreads();
-      if (unit + 1 < stop) fetch(unit + 1);
-      const int row0 = (q0 + unit % per_head) * 64;
+      const int r0 = row_fetched;
+      if (unit + 1 < stop) fetch();
+      const bool none = r0 + 31 < w0 || (r0 - (w0 + 31) >= window && w0 >= sinks);
+      const bool all = r0 >= w0 + 31 && (r0 + 31 - w0 < window || w0 + 31 < sinks);
       const T *tq = sq[buf], *tg = sg[buf];
-#pragma unroll
-      for (int ib = 0; ib < 2; ++ib) {
-        const int r0 = row0 + ib * 32;
-        const bool none = r0 + 31 < w0 || (r0 - (w0 + 31) >= window && w0 >= sinks) || r0 >= n;
-        if (none) continue;
-        const bool all = r0 >= w0 + 31 && (r0 + 31 - w0 < window || w0 + 31 < sinks);
+      if (DP == 128) place.forget();
+      if (!none) {
         f32x16 s = f32x16{}, dp = f32x16{};
 #pragma unroll
-        for (int ks = 0; ks < DP / 16; ++ks) s = mfma32(tile_rows<T, DP>(tq, place, ib * 32, ks), k[ks], s);
+        for (int ks = 0; ks < DP / 16; ++ks) s = mfma32(tile_rows<T, DP>(tq, place, 0, ks), k[ks], s);
 #pragma unroll
-        for (int ks = 0; ks < DP / 16; ++ks) dp = mfma32(tile_rows<T, DP>(tg, place, ib * 32, ks), v[ks], dp);
+        for (int ks = 0; ks < DP / 16; ++ks) {
+          const x8<T> vf = V_LDS ? tile_rows<T, DP>(sv + 32 * DP * wave, place, 0, ks) : v[V_LDS ? 0 : ks];
+          dp = mfma32(tile_rows<T, DP>(tg, place, 0, ks), vf, dp);
+        }
+        reads_ahead<DP / 16, 1, 4>();
         if (!all) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = (uint32_t)(r0 + c_row(r) - j) < reach ? s[r] : -INFINITY;
@@ -392,7 +415,7 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dkdv(Window
         float p[16], ds[16];
 #pragma unroll
         for (int r4 = 0; r4 < 4; ++r4) {
-          const int at4 = ib * 32 + 8 * r4 + 4 * (lane >> 5);
+          const int at4 = 8 * r4 + 4 * (lane >> 5);
           const f32x4 lse = *reinterpret_cast<const f32x4*>(&s_lse[buf][at4]);
           const f32x4 delta = *reinterpret_cast<const f32x4*>(&s_delta[buf][at4]);
 #pragma unroll
@@ -407,8 +430,8 @@ __global__ __launch_bounds__(kBlock, DP == 64 ? 2 : 1) void k_window_dkdv(Window
           const x8<T> pb = pack8<T>(p + 8 * u), db = pack8<T>(ds + 8 * u);
 #pragma unroll
           for (int d = 0; d < DP / 32; ++d) {
-            dv[d] = mfma32(tile_columns<T, DP>(tg, place, ib * 32 + 16 * u, d), pb, dv[d]);
-            dk[d] = mfma32(tile_columns<T, DP>(tq, place, ib * 32 + 16 * u, d), db, dk[d]);
+            dv[d] = mfma32(tile_columns<T, DP>(tg, place, 16 * u, d), pb, dv[d]);
+            dk[d] = mfma32(tile_columns<T, DP>(tq, place, 16 * u, d), db, dk[d]);
           }
         }
       }
@@ -760,13 +783,13 @@ KeyPlan key_plan(const qds_window_config* c) {
   const int64_t sinks = c->sinks < c->length ? c->sinks : c->length;
   p.blocks = (int32_t)ceil_div(c->length, kKeyRows);
   p.first = (int32_t)ceil_div(sinks, kKeyRows);
-  const int64_t all = ceil_div(c->length, 64);                                        // tiles that see a first block
-  int64_t band = ceil_div((int64_t)c->window + kKeyRows, 64) + 1;                     // ... and one of the band
+  const int64_t all = ceil_div(c->length, 32);                                        // tiles that see a first block
+  int64_t band = ceil_div((int64_t)c->window + kKeyRows, 32);                         // ... and one of the band
   if (band > all) band = all;
-  // pieces of equal size that give about kFill workgroups, but of no less than eight tiles
+  // pieces of equal size that give about kFill workgroups, but of no less than 16 tiles
   const int64_t total = (p.first * all + (p.blocks - p.first) * band) * group * lists;
   int64_t piece = ceil_div(total, kFill);
-  if (piece < 8) piece = 8;
+  if (piece < 16) piece = 16;
   if (piece > band * group) piece = band * group;
   p.first_cut = (int32_t)ceil_div(all * group, piece);
   p.band_cut = (int32_t)ceil_div(band * group, piece);
