@@ -52,6 +52,24 @@ struct KeyTiles {
 // this: one comparison, without the branches that && and || would make of every element.
 __device__ inline uint32_t reach_of(int window, int sinks, int j) { return j < sinks ? 0x40000000u : (uint32_t)window; }
 
+// Hides what row i does not see of a tile of scores (keys j0 .. j0 + 31 as its rows).
+// Most masked tiles need one side of the band only: two or three instructions an
+// element, where both at once take five.
+__device__ inline void hide(f32x16& s, int i, int j0, int window, int sinks, bool later, bool earlier) {
+  const int half = 4 * ((threadIdx.x & 63) >> 5);
+  if (later) {               // j <= i
+    const int last = i - j0 - half;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = (r & 3) + 8 * (r >> 2) <= last ? s[r] : -INFINITY;
+  }
+  if (earlier) {             // hidden: sinks <= j <= i - window
+    const int from = sinks - j0 - half;
+    const uint32_t count = (uint32_t)max(i - window - sinks + 1, 0);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = (uint32_t)((r & 3) + 8 * (r >> 2) - from) >= count ? s[r] : -INFINITY;
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------
@@ -116,16 +134,9 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
           for (int ks = 0; ks < DP / 16; ++ks) s[jb] = mfma32(tile_rows<T, DP>(tk, place, jb * 32, ks), q[ks], s[jb]);
         }
         reads_ahead<DP / 8, 1, 4>();
-        const bool all = j0 + 63 <= w0 && (w0 + 31 - j0 < window || j0 + 63 < sinks);
-        if (!all) {
+        const bool later = j0 + 63 > w0, earlier = w0 + 31 - j0 >= window && j0 + 63 >= sinks;
 #pragma unroll
-          for (int jb = 0; jb < 2; ++jb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int j = j0 + jb * 32 + c_row(r);
-              s[jb][r] = (uint32_t)(i - j) < reach_of(window, sinks, j) ? s[jb][r] : -INFINITY;
-            }
-        }
+        for (int jb = 0; jb < 2; ++jb) hide(s[jb], i, j0 + jb * 32, window, sinks, later, earlier);
         float top = kNoMax;
 #pragma unroll
         for (int jb = 0; jb < 2; ++jb)
@@ -247,7 +258,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blo
       const bool none = j0 > w0 + 31 || (w0 - (j0 + 63) >= window && j0 >= sinks);
       if (DP == 128) place.forget();
       if (!none) {
-        const bool all = j0 + 63 <= w0 && (w0 + 31 - j0 < window || j0 + 63 < sinks);
+        const bool later = j0 + 63 > w0, earlier = w0 + 31 - j0 >= window && j0 + 63 >= sinks;
 #pragma unroll
         for (int jb = 0; jb < 2; ++jb) {
           __builtin_amdgcn_sched_barrier(0);       // one half's products at a time: both would not fit the registers
@@ -256,13 +267,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blo
           for (int ks = 0; ks < DP / 16; ++ks) s = mfma32(tile_rows<T, DP>(tk, place, jb * 32, ks), q[ks], s);
 #pragma unroll
           for (int ks = 0; ks < DP / 16; ++ks) dp = mfma32(tile_rows<T, DP>(tv, place, jb * 32, ks), go[ks], dp);
-          if (!all) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int j = j0 + jb * 32 + c_row(r);
-              s[r] = (uint32_t)(i - j) < reach_of(window, sinks, j) ? s[r] : -INFINITY;
-            }
-          }
+          hide(s, i, j0 + jb * 32, window, sinks, later, earlier);
           float ds[16];
 #pragma unroll
           for (int r = 0; r < 16; ++r) ds[r] = fast_exp2(fmaf(s[r], c, -lse)) * (dp[r] - delta);
