@@ -267,13 +267,15 @@ template <class T> __device__ inline void store_column(T* row, int dt, const f32
   }
 }
 
-// Workgroups that follow each other go round the card's eight XCDs, each with
-// an L2 cache of its own.  This gives each XCD a contiguous piece of the work
-// items, so that items that read the same keys share a cache.
+// Workgroups that follow each other go round the card's eight XCDs, each with an L2
+// cache of its own.  This puts the `per_list` items of a list, which read the same
+// keys, on one XCD: lists are dealt to the XCDs in turn where their number allows
+// (so that episodes of different lengths even out), else in contiguous pieces.
 constexpr int kXcds = 8;
-__device__ inline int xcd_order(int id, int count) {
-  const int per = count / kXcds, rest = count % kXcds;
+__device__ inline int xcd_order(int id, int count, int per_list) {
   const int x = id % kXcds, y = id / kXcds;
+  if (count / per_list % kXcds == 0) return (y / per_list * kXcds + x) * per_list + y % per_list;
+  const int per = count / kXcds, rest = count % kXcds;
   return x * per + min(x, rest) + y;
 }
 

@@ -85,7 +85,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
   const int lane = threadIdx.x & 63, wave = wave_index();
   Lanes<DP> place;
   const int group = a.heads / a.kv_heads;
-  int id = xcd_order(blockIdx.x, gridDim.x);
+  int id = xcd_order(blockIdx.x, gridDim.x, group * q_blocks);
   const int g = id % group;
   id /= group;
   // late blocks first: they have the most keys where the window is long
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blo
   const int lane = threadIdx.x & 63, wave = wave_index();
   Lanes<DP> place;
   const int group = a.heads / a.kv_heads;
-  int id = xcd_order(blockIdx.x, gridDim.x);
+  int id = xcd_order(blockIdx.x, gridDim.x, group * q_blocks);
   const int g = id % group;
   id /= group;
   const int block = q_blocks - 1 - id % q_blocks;
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan
   const int lane = threadIdx.x & 63, wave = wave_index();
   Lanes<DP> place;
   const int group = a.heads / a.kv_heads;
-  const int id = xcd_order(blockIdx.x, gridDim.x);
+  const int id = xcd_order(blockIdx.x, gridDim.x, plan.items);
   const int head = id / plan.items;           // b * kv_heads + hk
   const KeyItem item = key_item(plan, id % plan.items);
   const int hk = head % a.kv_heads, b = head / a.kv_heads;
