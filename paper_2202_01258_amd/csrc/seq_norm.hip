@@ -287,17 +287,22 @@ __global__ __launch_bounds__(kBlock) void k_norm_backward(BackwardArgs a) {
     const int64_t row = first + sub;
     if (TPR == 64 && row >= a.rows) break;     // a wave of its own; no barrier inside the loop for them
     const float rstd = a.rstd[row];
-    float g[NV][VEC], h[NV][VEC];
+    float g[NV][VEC], h[NV][VEC], d[NV][VEC];
     float dot = 0.0f;
+    // all of the row's loads are under way before the first is used
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int col = (j * TPR + lane) * VEC;
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) g[j][i] = h[j][i] = 0.0f;
+      for (int i = 0; i < VEC; ++i) g[j][i] = h[j][i] = d[j][i] = 0.0f;
       if (col < a.width) {
         load<T, VEC>(g[j], (const T*)a.dy + row * a.dy_stride + col);
         load<T, VEC>(h[j], (const T*)a.h + row * a.h_stride + col);
+        if (a.dh) load<T, VEC>(d[j], (const T*)a.dh + row * a.dh_stride + col);
       }
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         h[j][i] *= rstd;
@@ -312,13 +317,9 @@ __global__ __launch_bounds__(kBlock) void k_norm_backward(BackwardArgs a) {
     for (int j = 0; j < NV; ++j) {
       const int col = (j * TPR + lane) * VEC;
       if (col >= a.width) continue;
-      float d[VEC];
 #pragma unroll
-      for (int i = 0; i < VEC; ++i) d[i] = 0.0f;
-      if (a.dh) load<T, VEC>(d, (const T*)a.dh + row * a.dh_stride + col);
-#pragma unroll
-      for (int i = 0; i < VEC; ++i) d[i] += rstd * (g[j][i] - h[j][i] * dot);
-      store<T, VEC>((T*)a.dx + row * a.width + col, d);
+      for (int i = 0; i < VEC; ++i) d[j][i] += rstd * (g[j][i] - h[j][i] * dot);
+      store<T, VEC>((T*)a.dx + row * a.width + col, d[j]);
     }
   }
   if constexpr (TPR == 64) {
@@ -378,20 +379,24 @@ template <class T> __global__ __launch_bounds__(kBlock) void k_norm_backward_any
   }
 }
 
-// 64 columns per workgroup: four waves each add every fourth share.
-template <class T> __global__ __launch_bounds__(kBlock) void k_norm_dweight(BackwardArgs a) {
-  __shared__ float part[kBlock];
+// 64 columns per workgroup: sixteen waves each add every sixteenth share (a column's
+// chain of loads is what takes the time: 7.6 us with four waves, 777 columns).
+constexpr int kJoinWaves = 16;
+template <class T> __global__ __launch_bounds__(64 * kJoinWaves) void k_norm_dweight(BackwardArgs a) {
+  __shared__ float part[64 * kJoinWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = blockIdx.x * 64 + lane;
   float sum = 0.0f;
   if (col < a.width) {
 #pragma unroll 8
-    for (int b = wave; b < a.blocks; b += 4) sum += a.partial[(int64_t)b * a.width + col];
+    for (int b = wave; b < a.blocks; b += kJoinWaves) sum += a.partial[(int64_t)b * a.width + col];
   }
   part[threadIdx.x] = sum;
   __syncthreads();
   if (wave == 0 && col < a.width) {
-    sum = (part[lane] + part[64 + lane]) + (part[128 + lane] + part[192 + lane]);
+    sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kJoinWaves; ++w) sum += part[w * 64 + lane];
     if (a.w32)
       ((float*)a.dw)[col] = sum;
     else
@@ -477,13 +482,15 @@ template <class T> void backward(BackwardArgs a, bool vec, hipStream_t s) {
   if (a.rows > 0) {
     const bool held = with_shape<T>(a.width, vec, [&](auto V, auto NV, auto TPR) {
       constexpr int v = decltype(V)::value, nv = decltype(NV)::value, tpr = decltype(TPR)::value;
+      const int64_t most = ceil_div(a.rows, kBlock / tpr);
+      if (a.blocks > most) a.blocks = (int)most;
       k_norm_backward<T, v, nv, tpr><<<a.blocks, kBlock, 0, s>>>(a);
     });
     if (!held) k_norm_backward_any<T><<<a.blocks, kBlock, 0, s>>>(a);
   } else {
     a.blocks = 0;
   }
-  k_norm_dweight<T><<<ceil_div(a.width, 64), kBlock, 0, s>>>(a);
+  k_norm_dweight<T><<<ceil_div(a.width, 64), 64 * kJoinWaves, 0, s>>>(a);
 }
 
 }  // namespace

@@ -27,6 +27,8 @@ from __future__ import annotations
 import ctypes as C
 import os
 
+import torch
+
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libqdseq.so")
 
@@ -44,7 +46,9 @@ EXPORTS = ["qds_residual_norm", "qds_residual_norm_fp8", "qds_residual_norm_back
 
 
 class QdsView(C.Structure):
-    _fields_ = [("data", C.c_void_p), ("stride", C.c_int64 * 3)]
+    # stride[0], stride[1], stride[2] of the C struct
+    _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_t", C.c_int64),
+                ("stride_h", C.c_int64)]
 
 
 class QdsNormConfig(C.Structure):
@@ -116,60 +120,64 @@ def _check(status: int, what: str):
 # ---------------------------------------------------------------------------
 # Marshalling
 # ---------------------------------------------------------------------------
-_CODES = {}
-
-
-def _codes():
-    import torch
-    if not _CODES:
-        _CODES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
-    return _CODES
-
-
-def _need(cond, message):
-    if not cond:
-        raise ValueError(message)
+# A rollout calls these operators once per step and layer, so the time of a call
+# counts: checks format their messages only when they fail, and a configuration
+# (with the size of its scratch memory) is made once for each set of sizes.
+_CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+_PLANS = 4096                                      # sets of sizes that are remembered
 
 
 def _code(t, name):
-    code = _codes().get(t.dtype)
-    _need(code is not None, f"{name}: float32, bfloat16 or float16, not {t.dtype}")
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: float32, bfloat16 or float16, not {t.dtype}")
     return code
 
 
-def _like(name, t, ref, shape=None, dtype=None):
+def _like(name, t, ref, shape, dtype=None):
     """Checks a tensor's device, type and shape against those of `ref`."""
-    _need(t.device == ref.device, f"{name} is on {t.device}, not on {ref.device}")
-    _need(t.dtype == (dtype or ref.dtype), f"{name} is {t.dtype}, not {dtype or ref.dtype}")
-    if shape is not None:
-        _need(tuple(t.shape) == tuple(shape), f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
+    if t.device != ref.device:
+        raise ValueError(f"{name} is on {t.device}, not on {ref.device}")
+    if t.dtype != (dtype or ref.dtype):
+        raise ValueError(f"{name} is {t.dtype}, not {dtype or ref.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} is {tuple(t.shape)}, not {tuple(shape)}")
 
 
 def _on_gpu(t, name):
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise RuntimeError(f"{name}: libqdseq needs tensors on a GPU, not on {t.device}")
 
 
 def _rows(t):
     """`t` with contiguous, 16-byte aligned rows: itself, or a copy."""
-    if t.stride(-1) == 1 and t.data_ptr() % 16 == 0 and not any(s % 8 for s in t.stride()[:-1]):
-        return t
-    import torch
+    s = t.stride()
+    if s[-1] == 1 and t.data_ptr() % 16 == 0:
+        for x in s[:-1]:
+            if x % 8:
+                break
+        else:
+            return t
     return t.clone(memory_format=torch.contiguous_format)
 
 
 def _view(t):
     """A [batch, rows, heads, dim] or [batch, heads, dim] tensor as a qds_view."""
     s = t.stride()
-    return QdsView(t.data_ptr(), (C.c_int64 * 3)(s[0], s[1] if len(s) == 4 else 0, s[-2]))
+    return QdsView(t.data_ptr(), s[0], s[1] if len(s) == 4 else 0, s[-2])
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+# The current stream's handle without a Stream object around it, where torch offers that.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(t):
-    import torch
+    if _raw_stream is not None:
+        return _raw_stream(t.device.index)
     return torch.cuda.current_stream(t.device).cuda_stream
 
 
@@ -177,7 +185,6 @@ class _on:
     """The tensors' device as the current one (cheap where it already is)."""
 
     def __init__(self, t):
-        import torch
         index = t.device.index
         self.guard = None if torch.cuda.current_device() == index else torch.cuda.device(index)
 
@@ -190,17 +197,33 @@ class _on:
             self.guard.__exit__(*exc)
 
 
-def _workspace(query, cfg, ref, what):
-    """Scratch memory of the size that `query` gives; torch's allocator keeps it
-    from other work on this stream until the call's work is done."""
-    import torch
-    n = C.c_uint64()
-    _check(query(C.byref(cfg), C.byref(n)), what)
-    return torch.empty(n.value, dtype=torch.uint8, device=ref.device), n.value
+_plans = {}
+
+
+def _plan(kind, query, key):
+    """The configuration of a set of sizes and the bytes of scratch memory that a
+    call with it needs (`query`: the library's function for that, or None)."""
+    got = _plans.get((query, key))
+    if got is None:
+        for x in key:
+            if isinstance(x, int) and not -1 << 31 <= x < 1 << 31:
+                raise ValueError(f"{x} is too large")      # ctypes would cut it to 32 bits
+        cfg, size = kind(ABI_VERSION, *key), C.c_uint64(0)
+        if query is not None:
+            _check(getattr(lib(), query)(C.byref(cfg), C.byref(size)), query)
+        if len(_plans) >= _PLANS:
+            _plans.clear()
+        got = _plans[(query, key)] = (cfg, C.byref(cfg), size.value)
+    return got
+
+
+def _scratch(size, ref):
+    """Scratch memory; torch's allocator keeps it from other work until this
+    stream's work on it is done."""
+    return torch.empty(size, dtype=torch.uint8, device=ref.device) if size else None
 
 
 def _lengths(lengths, batch, ref):
-    import torch
     if lengths is None:
         return None
     _like("lengths", lengths, ref, (batch,), torch.int32)
@@ -216,35 +239,36 @@ def _norm_rows(t, width):
     return t if t.stride(-1) == 1 or t.numel() == 0 else t.contiguous()
 
 
-def _norm_setup(x, residual, weight, eps, group):
+def _norm_setup(x, residual, weight, eps, group, query=None):
     _on_gpu(x, "x")
     code = _code(x, "x")
-    _need(x.dim() >= 1 and x.shape[-1] >= 1, "x has no columns")
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x has no columns")
     width = x.shape[-1]
     if residual is not None:
         _like("residual", residual, x, x.shape)
-    _need(weight.device == x.device and tuple(weight.shape) == (width,),
-          f"weight: [{width}] on {x.device}")
+    if weight.device != x.device or weight.shape != (width,):
+        raise ValueError(f"weight: [{width}] on {x.device}")
     wcode = _code(weight, "weight")
-    _need(wcode in (F32, code), f"weight is {weight.dtype}: float32 or x's {x.dtype}")
+    if wcode != F32 and wcode != code:
+        raise ValueError(f"weight is {weight.dtype}: float32 or x's {x.dtype}")
     x2 = _norm_rows(x, width)
     r2 = None if residual is None else _norm_rows(residual, width)
-    cfg = QdsNormConfig(ABI_VERSION, code, wcode, width, x2.shape[0], eps, group)
-    return cfg, x2, r2, weight.contiguous()
+    plan = _plan(QdsNormConfig, query, (code, wcode, width, x2.shape[0], eps, group))
+    return plan, x2, r2, weight.contiguous()
 
 
 def residual_norm_forward(x, residual, weight, eps: float = 1e-6):
     """h = x + residual, y = h (mean(h^2) + eps)^(-1/2) weight over the last
     dimension.  Returns y, h (x's type and shape) and rstd (float32, a value per
     row).  `residual` may be None; `weight` is float32 or of x's type."""
-    import torch
-    cfg, x2, r2, w = _norm_setup(x, residual, weight, eps, 0)
+    (_, cfg, _), x2, r2, w = _norm_setup(x, residual, weight, eps, 0)
     y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
     rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     with _on(x):
         _check(lib().qds_residual_norm(
-            C.byref(cfg), x2.data_ptr(), x2.stride(0), _ptr(r2), 0 if r2 is None else r2.stride(0),
+            cfg, x2.data_ptr(), x2.stride(0), _ptr(r2), 0 if r2 is None else r2.stride(0),
             w.data_ptr(), y.data_ptr(), h.data_ptr(), rstd.data_ptr(), _stream(x)),
             "qds_residual_norm")
     return y, h, rstd
@@ -254,17 +278,16 @@ def residual_norm_fp8(x, residual, weight, eps: float = 1e-6, group: int = 0):
     """The norm with its output in 8 bits: returns q (float8_e4m3fn, x's shape),
     scale (float32, [..., 1], or [..., width / 128] with `group` = 128) and h.
     q * scale is y; scale is the largest |y| of its columns / 448."""
-    import torch
-    cfg, x2, r2, w = _norm_setup(x, residual, weight, eps, group)
-    _need(group == 0 or (group == 128 and cfg.width % 128 == 0),
-          f"group: 0, or 128 where it divides the width ({cfg.width}), not {group}")
+    (c, cfg, _), x2, r2, w = _norm_setup(x, residual, weight, eps, group)
+    if group != 0 and (group != 128 or c.width % 128):
+        raise ValueError(f"group: 0, or 128 where it divides the width ({c.width}), not {group}")
     q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
     h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    scale = torch.empty((*x.shape[:-1], cfg.width // group if group else 1), dtype=torch.float32,
+    scale = torch.empty((*x.shape[:-1], c.width // group if group else 1), dtype=torch.float32,
                         device=x.device)
     with _on(x):
         _check(lib().qds_residual_norm_fp8(
-            C.byref(cfg), x2.data_ptr(), x2.stride(0), _ptr(r2), 0 if r2 is None else r2.stride(0),
+            cfg, x2.data_ptr(), x2.stride(0), _ptr(r2), 0 if r2 is None else r2.stride(0),
             w.data_ptr(), q.data_ptr(), scale.data_ptr(), h.data_ptr(), _stream(x)),
             "qds_residual_norm_fp8")
     return q, scale, h
@@ -273,24 +296,22 @@ def residual_norm_fp8(x, residual, weight, eps: float = 1e-6, group: int = 0):
 def residual_norm_backward(dy, dh, h, rstd, weight):
     """Gradients from those of y and of h (`dh` may be None): returns dx (also
     the residual's gradient) and dweight.  h and rstd are the forward call's."""
-    import torch
-    cfg, h2, _, w = _norm_setup(h, None, weight, 0.0, 0)
+    (c, cfg, size), h2, _, w = _norm_setup(h, None, weight, 0.0, 0, "qds_residual_norm_backward_workspace")
     _like("dy", dy, h, h.shape)
     _like("rstd", rstd, h, h.shape[:-1], torch.float32)
-    dy2, dh2 = _norm_rows(dy, cfg.width), None
+    dy2, dh2 = _norm_rows(dy, c.width), None
     if dh is not None:
         _like("dh", dh, h, h.shape)
-        dh2 = _norm_rows(dh, cfg.width)
+        dh2 = _norm_rows(dh, c.width)
     rstd = rstd.contiguous()
     with _on(h):
-        ws, size = _workspace(lib().qds_residual_norm_backward_workspace, cfg, h,
-                              "qds_residual_norm_backward_workspace")
+        ws = _scratch(size, h)
         dx = torch.empty(h.shape, dtype=h.dtype, device=h.device)
         dw = torch.empty(weight.shape, dtype=weight.dtype, device=h.device)
         _check(lib().qds_residual_norm_backward(
-            C.byref(cfg), dy2.data_ptr(), dy2.stride(0), _ptr(dh2),
+            cfg, dy2.data_ptr(), dy2.stride(0), _ptr(dh2),
             0 if dh2 is None else dh2.stride(0), h2.data_ptr(), h2.stride(0), rstd.data_ptr(),
-            w.data_ptr(), dx.data_ptr(), dw.data_ptr(), ws.data_ptr(), size, _stream(h)),
+            w.data_ptr(), dx.data_ptr(), dw.data_ptr(), _ptr(ws), size, _stream(h)),
             "qds_residual_norm_backward")
     return dx, dw
 
@@ -298,20 +319,22 @@ def residual_norm_backward(dy, dh, h, rstd, weight):
 # ---------------------------------------------------------------------------
 # Attention over a sliding window whose first tokens stay visible
 # ---------------------------------------------------------------------------
-def _window_setup(q, k, v, window, sinks, scale):
-    """Checks q, k, v [batch, rows, heads, dim] (or without rows) and makes the configuration."""
+def _window_setup(q, k, v, window, sinks, scale, rows, query=None):
+    """Checks q, k, v [batch, rows, heads, dim] (or without rows) and makes the plan."""
     _on_gpu(q, "q")
     code = _code(q, "q")
-    _need(q.dim() in (3, 4) and k.dim() == q.dim(), "q, k, v: [batch, rows, heads, dim]")
+    if q.dim() != (4 if rows else 3) or k.dim() != q.dim():
+        raise ValueError("q, k, v: [batch, rows, heads, dim]" if rows else "q, k, v: [batch, heads, dim]")
     batch, heads, dim = q.shape[0], q.shape[-2], q.shape[-1]
     kv_heads = k.shape[-2]
     _like("k", k, q, (*q.shape[:-2], kv_heads, dim))
     _like("v", v, q, k.shape)
-    _need(kv_heads >= 1 and heads % kv_heads == 0,
-          f"{heads} query heads are no multiple of {kv_heads} key heads")
-    _need(window >= 1 and sinks >= 0, f"window {window} >= 1 and sinks {sinks} >= 0")
-    return QdsWindowConfig(ABI_VERSION, code, batch, q.shape[1] if q.dim() == 4 else 0, heads,
-                           kv_heads, dim, window, sinks, dim ** -0.5 if scale is None else scale)
+    if kv_heads < 1 or heads % kv_heads:
+        raise ValueError(f"{heads} query heads are no multiple of {kv_heads} key heads")
+    if window < 1 or sinks < 0:
+        raise ValueError(f"window {window} >= 1 and sinks {sinks} >= 0")
+    return _plan(QdsWindowConfig, query, (code, batch, q.shape[1] if rows else 0, heads, kv_heads, dim,
+                                          window, sinks, dim ** -0.5 if scale is None else scale))
 
 
 def window_attention_forward(q, k, v, window: int, sinks: int = 0, lengths=None, scale=None):
@@ -326,15 +349,13 @@ def window_attention_forward(q, k, v, window: int, sinks: int = 0, lengths=None,
     weight of 0 times infinity), in the same batch element and head.
 
     Returns o (q's shape) and lse (float32 [batch, heads, rows])."""
-    import torch
-    _need(q.dim() == 4, "q, k, v: [batch, rows, heads, dim]")
-    cfg = _window_setup(q, k, v, window, sinks, scale)
-    lengths = _lengths(lengths, cfg.batch, q)
+    c, cfg, _ = _window_setup(q, k, v, window, sinks, scale, True)
+    lengths = _lengths(lengths, c.batch, q)
     q, k, v = _rows(q), _rows(k), _rows(v)
     o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty((cfg.batch, cfg.heads, cfg.length), dtype=torch.float32, device=q.device)
+    lse = torch.empty((c.batch, c.heads, c.length), dtype=torch.float32, device=q.device)
     with _on(q):
-        _check(lib().qds_window_forward(C.byref(cfg), _view(q), _view(k), _view(v), _ptr(lengths),
+        _check(lib().qds_window_forward(cfg, _view(q), _view(k), _view(v), _ptr(lengths),
                                         _view(o), lse.data_ptr(), _stream(q)), "qds_window_forward")
     return o, lse
 
@@ -342,50 +363,50 @@ def window_attention_forward(q, k, v, window: int, sinks: int = 0, lengths=None,
 def window_attention_backward(do, q, k, v, o, lse, window: int, sinks: int = 0, lengths=None,
                               scale=None):
     """Gradients dq, dk, dv from o's, with what the forward call saw and gave."""
-    import torch
-    _need(q.dim() == 4, "q, k, v: [batch, rows, heads, dim]")
-    cfg = _window_setup(q, k, v, window, sinks, scale)
+    c, cfg, size = _window_setup(q, k, v, window, sinks, scale, True, "qds_window_backward_workspace")
     _like("do", do, q, q.shape)
     _like("o", o, q, q.shape)
-    _like("lse", lse, q, (cfg.batch, cfg.heads, cfg.length), torch.float32)
-    lengths = _lengths(lengths, cfg.batch, q)
+    _like("lse", lse, q, (c.batch, c.heads, c.length), torch.float32)
+    lengths = _lengths(lengths, c.batch, q)
     do, q, k, v, o, lse = _rows(do), _rows(q), _rows(k), _rows(v), _rows(o), lse.contiguous()
     dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
     with _on(q):
-        ws, size = _workspace(lib().qds_window_backward_workspace, cfg, q,
-                              "qds_window_backward_workspace")
+        ws = _scratch(size, q)
         _check(lib().qds_window_backward(
-            C.byref(cfg), _view(do), _view(q), _view(k), _view(v), _view(o), lse.data_ptr(),
-            _ptr(lengths), _view(dq), _view(dk), _view(dv), ws.data_ptr(), size, _stream(q)),
+            cfg, _view(do), _view(q), _view(k), _view(v), _view(o), lse.data_ptr(),
+            _ptr(lengths), _view(dq), _view(dk), _view(dv), _ptr(ws), size, _stream(q)),
             "qds_window_backward")
     return dq, dk, dv
 
 
 def window_cache(batch: int, kv_heads: int, dim: int, window: int, sinks: int, dtype, device="cuda:0"):
     """An empty ring cache: k and v, each [batch, kv_heads, sinks + window, dim]."""
-    import torch
     shape = (batch, kv_heads, sinks + window, dim)
     return torch.zeros(shape, dtype=dtype, device=device), torch.zeros(shape, dtype=dtype, device=device)
 
 
-def _cache(cfg, q, k_cache, v_cache):
-    shape = (cfg.batch, cfg.kv_heads, cfg.sinks + cfg.window, cfg.dim)
-    for name, t in (("k_cache", k_cache), ("v_cache", v_cache)):
-        _like(name, t, q, shape)
-        _need(t.is_contiguous() and t.data_ptr() % 16 == 0, f"{name}: contiguous and 16-byte aligned")
+def _in_place(name, t, ref, shape, dtype=None):
+    _like(name, t, ref, shape, dtype)
+    if not t.is_contiguous() or t.data_ptr() % 16:
+        raise ValueError(f"{name}: contiguous and 16-byte aligned")
+
+
+def _cache(c, q, k_cache, v_cache):
+    shape = (c.batch, c.kv_heads, c.sinks + c.window, c.dim)
+    _in_place("k_cache", k_cache, q, shape)
+    _in_place("v_cache", v_cache, q, shape)
 
 
 def window_cache_fill(k, v, k_cache, v_cache, window: int, sinks: int = 0, lengths=None):
     """Writes the rows of a prompt (k, v as for window_attention) that later
     tokens can still see into the cache: after it, the token at position
     lengths[b] (or rows) is next."""
-    _need(k.dim() == 4, "k, v: [batch, rows, kv_heads, dim]")
-    cfg = _window_setup(k, k, v, window, sinks, 1.0)
-    _cache(cfg, k, k_cache, v_cache)
-    lengths = _lengths(lengths, cfg.batch, k)
+    c, cfg, _ = _window_setup(k, k, v, window, sinks, 1.0, True)
+    _cache(c, k, k_cache, v_cache)
+    lengths = _lengths(lengths, c.batch, k)
     k, v = _rows(k), _rows(v)
     with _on(k):
-        _check(lib().qds_window_cache_fill(C.byref(cfg), _view(k), _view(v), _ptr(lengths),
+        _check(lib().qds_window_cache_fill(cfg, _view(k), _view(v), _ptr(lengths),
                                            k_cache.data_ptr(), v_cache.data_ptr(), _stream(k)),
                "qds_window_cache_fill")
 
@@ -395,43 +416,40 @@ def window_attention_step(q, k, v, k_cache, v_cache, pos, window: int, sinks: in
     position pos[b] (int32) into the cache and attends with q [batch, heads,
     dim] to what that position sees.  pos[b] < 0: no token; the cache stays and
     the output is 0.  Returns o [batch, heads, dim]."""
-    import torch
-    _need(q.dim() == 3, "q, k, v: [batch, heads, dim]")
-    cfg = _window_setup(q, k, v, window, sinks, scale)
-    _cache(cfg, q, k_cache, v_cache)
-    _like("pos", pos, q, (cfg.batch,), torch.int32)
+    c, cfg, size = _window_setup(q, k, v, window, sinks, scale, False, "qds_window_step_workspace")
+    _cache(c, q, k_cache, v_cache)
+    _like("pos", pos, q, (c.batch,), torch.int32)
     pos = pos.contiguous()
     q, k, v = _rows(q), _rows(k), _rows(v)
     o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
     with _on(q):
-        ws, size = _workspace(lib().qds_window_step_workspace, cfg, q, "qds_window_step_workspace")
+        ws = _scratch(size, q)
         _check(lib().qds_window_step(
-            C.byref(cfg), _view(q), _view(k), _view(v), k_cache.data_ptr(), v_cache.data_ptr(),
-            pos.data_ptr(), _view(o), ws.data_ptr(), size, _stream(q)), "qds_window_step")
+            cfg, _view(q), _view(k), _view(v), k_cache.data_ptr(), v_cache.data_ptr(),
+            pos.data_ptr(), _view(o), _ptr(ws), size, _stream(q)), "qds_window_step")
     return o
 
 
 # ---------------------------------------------------------------------------
 # Linear attention with a decay for each head
 # ---------------------------------------------------------------------------
-def _decay_setup(q, k, v, log_decay, scale):
-    import torch
+def _decay_setup(q, k, v, log_decay, scale, rows, query=None):
     _on_gpu(q, "q")
     code = _code(q, "q")
-    _need(q.dim() in (3, 4) and v.dim() == q.dim(), "q, k, v: [batch, rows, heads, dim]")
+    if q.dim() != (4 if rows else 3) or v.dim() != q.dim():
+        raise ValueError("q, k, v: [batch, rows, heads, dim]" if rows else "q, k, v: [batch, heads, dim]")
+    heads, dim_k, dim_v = q.shape[-2], q.shape[-1], v.shape[-1]
     _like("k", k, q, q.shape)
-    _like("v", v, q, (*q.shape[:-1], v.shape[-1]))
-    _like("log_decay", log_decay, q, (q.shape[-2],), torch.float32)
-    dim_k, dim_v = q.shape[-1], v.shape[-1]
-    return QdsDecayConfig(ABI_VERSION, code, q.shape[0], q.shape[1] if q.dim() == 4 else 0,
-                          q.shape[-2], dim_k, dim_v, dim_k ** -0.5 if scale is None else scale)
+    _like("v", v, q, (*q.shape[:-1], dim_v))
+    _like("log_decay", log_decay, q, (heads,), torch.float32)
+    return _plan(QdsDecayConfig, query, (code, q.shape[0], q.shape[1] if rows else 0, heads, dim_k, dim_v,
+                                         dim_k ** -0.5 if scale is None else scale))
 
 
-def _state(name, t, cfg, ref):
-    import torch
+def _state(name, t, c, ref):
     if t is None:
         return None
-    _like(name, t, ref, (cfg.batch, cfg.heads, cfg.dim_k, cfg.dim_v), torch.float32)
+    _like(name, t, ref, (c.batch, c.heads, c.dim_k, c.dim_v), torch.float32)
     return t.contiguous()
 
 
@@ -443,9 +461,7 @@ def decay_attention_forward(q, k, v, log_decay, state=None, lengths=None, scale=
     before the first row, 0 if None; `lengths` as for window_attention.
 
     Returns o and the state after the last row."""
-    import torch
-    _need(q.dim() == 4, "q, k, v: [batch, rows, heads, dim]")
-    cfg = _decay_setup(q, k, v, log_decay, scale)
+    cfg, ref, size = _decay_setup(q, k, v, log_decay, scale, True, "qds_decay_forward_workspace")
     state = _state("state", state, cfg, q)
     lengths = _lengths(lengths, cfg.batch, q)
     log_decay = log_decay.contiguous()
@@ -453,10 +469,10 @@ def decay_attention_forward(q, k, v, log_decay, state=None, lengths=None, scale=
     o = torch.empty((*q.shape[:-1], cfg.dim_v), dtype=q.dtype, device=q.device)
     last = torch.empty((cfg.batch, cfg.heads, cfg.dim_k, cfg.dim_v), dtype=torch.float32, device=q.device)
     with _on(q):
-        ws, size = _workspace(lib().qds_decay_forward_workspace, cfg, q, "qds_decay_forward_workspace")
+        ws = _scratch(size, q)
         _check(lib().qds_decay_forward(
-            C.byref(cfg), _view(q), _view(k), _view(v), log_decay.data_ptr(), _ptr(state),
-            _ptr(lengths), _view(o), last.data_ptr(), ws.data_ptr(), size, _stream(q)),
+            ref, _view(q), _view(k), _view(v), log_decay.data_ptr(), _ptr(state),
+            _ptr(lengths), _view(o), last.data_ptr(), _ptr(ws), size, _stream(q)),
             "qds_decay_forward")
     return o, last
 
@@ -464,9 +480,7 @@ def decay_attention_forward(q, k, v, log_decay, state=None, lengths=None, scale=
 def decay_attention_backward(do, q, k, v, log_decay, state=None, dstate=None, lengths=None, scale=None):
     """Gradients dq, dk, dv and that of the first state from those of o and of
     the last state (`dstate`; None: 0)."""
-    import torch
-    _need(q.dim() == 4, "q, k, v: [batch, rows, heads, dim]")
-    cfg = _decay_setup(q, k, v, log_decay, scale)
+    cfg, ref, size = _decay_setup(q, k, v, log_decay, scale, True, "qds_decay_backward_workspace")
     _like("do", do, v, v.shape)
     state = _state("state", state, cfg, q)
     dstate = _state("dstate", dstate, cfg, q)
@@ -476,11 +490,11 @@ def decay_attention_backward(do, q, k, v, log_decay, state=None, dstate=None, le
     dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
     dfirst = torch.empty((cfg.batch, cfg.heads, cfg.dim_k, cfg.dim_v), dtype=torch.float32, device=q.device)
     with _on(q):
-        ws, size = _workspace(lib().qds_decay_backward_workspace, cfg, q, "qds_decay_backward_workspace")
+        ws = _scratch(size, q)
         _check(lib().qds_decay_backward(
-            C.byref(cfg), _view(do), _view(q), _view(k), _view(v), log_decay.data_ptr(), _ptr(state),
+            ref, _view(do), _view(q), _view(k), _view(v), log_decay.data_ptr(), _ptr(state),
             _ptr(dstate), _ptr(lengths), _view(dq), _view(dk), _view(dv), dfirst.data_ptr(),
-            ws.data_ptr(), size, _stream(q)), "qds_decay_backward")
+            _ptr(ws), size, _stream(q)), "qds_decay_backward")
     return dq, dk, dv, dfirst
 
 
@@ -488,18 +502,17 @@ def decay_attention_step(q, k, v, log_decay, state, scale=None, out_state=None):
     """One token: q, k [batch, heads, dim_k], v [batch, heads, dim_v].  Writes
     the new state into `out_state` (by default into `state` itself) and returns
     o [batch, heads, dim_v] and that state."""
-    import torch
-    _need(q.dim() == 3, "q, k, v: [batch, heads, dim]")
-    cfg = _decay_setup(q, k, v, log_decay, scale)
+    cfg, ref, _ = _decay_setup(q, k, v, log_decay, scale, False)
     out_state = state if out_state is None else out_state
-    for name, t in (("state", state), ("out_state", out_state)):
-        _like(name, t, q, (cfg.batch, cfg.heads, cfg.dim_k, cfg.dim_v), torch.float32)
-        _need(t.is_contiguous() and t.data_ptr() % 16 == 0, f"{name}: contiguous and 16-byte aligned")
+    shape = (cfg.batch, cfg.heads, cfg.dim_k, cfg.dim_v)
+    _in_place("state", state, q, shape, torch.float32)
+    if out_state is not state:
+        _in_place("out_state", out_state, q, shape, torch.float32)
     log_decay = log_decay.contiguous()
     q, k, v = _rows(q), _rows(k), _rows(v)
     o = torch.empty((*q.shape[:-1], cfg.dim_v), dtype=q.dtype, device=q.device)
     with _on(q):
-        _check(lib().qds_decay_step(C.byref(cfg), _view(q), _view(k), _view(v), log_decay.data_ptr(),
+        _check(lib().qds_decay_step(ref, _view(q), _view(k), _view(v), log_decay.data_ptr(),
                                     state.data_ptr(), _view(o), out_state.data_ptr(), _stream(q)),
                "qds_decay_step")
     return o, out_state
@@ -512,11 +525,10 @@ _functions = None
 
 
 def _autograd():
-    """The autograd functions (torch is imported on first use, as elsewhere in the package)."""
+    """The autograd functions, made on first use."""
     global _functions
     if _functions is not None:
         return _functions
-    import torch
 
     class ResidualNorm(torch.autograd.Function):
         @staticmethod
@@ -587,5 +599,6 @@ def window_attention(q, k, v, window: int, sinks: int = 0, lengths=None, scale=N
 
 def decay_attention(q, k, v, log_decay, state=None, lengths=None, scale=None):
     """decay_attention_forward under autograd: returns o and the last state."""
-    _need(not log_decay.requires_grad, "log_decay is a constant of the layer: it has no gradient")
+    if log_decay.requires_grad:
+        raise ValueError("log_decay is a constant of the layer: it has no gradient")
     return _autograd()[2].apply(q, k, v, log_decay, state, lengths, scale)

@@ -62,7 +62,7 @@ P = 1 << 20                                       # a pointer that nothing may f
 
 
 def view(p=P, strides=(8, 8, 8)):
-    return S.QdsView(p, (C.c_int64 * 3)(*strides))
+    return S.QdsView(p, *strides)
 
 
 def norm(**over):

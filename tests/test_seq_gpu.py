@@ -600,11 +600,10 @@ def test_decay_state_in_place():
     ld = torch.tensor([-0.01, -0.1], device="cuda")
     s = rand(1, 2, 64, 64, seed=2)
     o, last = S.decay_attention_forward(q, k, v, ld, s)
-    import ctypes as C
-    cfg = S._decay_setup(q, k, v, ld, None)
-    ws, size = S._workspace(S.lib().qds_decay_forward_workspace, cfg, q, "workspace")
+    _, cfg, size = S._decay_setup(q, k, v, ld, None, True, "qds_decay_forward_workspace")
+    ws = torch.empty(size, dtype=torch.uint8, device="cuda")
     o2, s2 = torch.empty_like(o), s.clone()
-    assert S.lib().qds_decay_forward(C.byref(cfg), S._view(q), S._view(k), S._view(v), ld.data_ptr(), s2.data_ptr(),
+    assert size > 0 and S.lib().qds_decay_forward(cfg, S._view(q), S._view(k), S._view(v), ld.data_ptr(), s2.data_ptr(),
                                      None, S._view(o2), s2.data_ptr(), ws.data_ptr(), size, S._stream(q)) == S.OK
     assert torch.equal(o, o2) and torch.equal(last, s2)
 
@@ -763,6 +762,8 @@ def test_refusals():
         S.window_attention_forward(q[:, :, :3], k, v, 4)
     with pytest.raises(ValueError, match="window"):
         S.window_attention_forward(q, k, v, 0)
+    with pytest.raises(ValueError, match="too large"):
+        S.window_attention_forward(q, k, v, (1 << 32) + 4)
     with pytest.raises(ValueError, match="lengths"):
         S.window_attention_forward(q, k, v, 4, lengths=torch.tensor([3, 4], device="cuda"))
     with pytest.raises(ValueError, match="lengths is on"):
