@@ -50,20 +50,24 @@ __device__ inline int rows_of(const DecayArgs& a, int b) {
   return min(max(a.lengths[b], 0), a.length);
 }
 
-// The state of one wave: all DK rows of 32 columns.  In memory [rows][cols], or transposed.
-// Its products' left operand has its rows in an order (`ordered` reads) that puts
-// 8 neighbouring rows of the state into registers 8 u .. 8 u + 7 of a tile, so that
-// they are an operand of the output's product against plain rows of x.
-template <int DK> struct State {
-  f32x16 m[DK / 32];
-  static __device__ int row_of(int t, int i) { return t * 32 + 16 * (i >> 3) + 8 * ((threadIdx.x & 63) >> 5) + (i & 7); }
+// N tiles of 32 rows of the state, 32 columns; the first is tile `first` of all.
+// In memory [rows][cols], or transposed.  The left operand of the products that
+// form it has its rows in an order (`ordered` reads) that puts 8 neighbouring rows
+// of the state into registers 8 u .. 8 u + 7 of a tile, so that they are an operand
+// of the output's product against plain rows of x.
+template <int N> struct State {
+  f32x16 m[N];
+  int first;
+  __device__ int row_of(int t, int i) const {
+    return (first + t) * 32 + 16 * (i >> 3) + 8 * ((threadIdx.x & 63) >> 5) + (i & 7);
+  }
   __device__ void zero() {
 #pragma unroll
-    for (int t = 0; t < DK / 32; ++t) m[t] = f32x16{};
+    for (int t = 0; t < N; ++t) m[t] = f32x16{};
   }
   __device__ void load(const float* p, int rows, int cols, int col, bool swapped, float factor) {
 #pragma unroll
-    for (int t = 0; t < DK / 32; ++t)
+    for (int t = 0; t < N; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int row = row_of(t, i);
@@ -72,7 +76,7 @@ template <int DK> struct State {
   }
   __device__ void store(float* p, int rows, int cols, int col, bool swapped, float factor) const {
 #pragma unroll
-    for (int t = 0; t < DK / 32; ++t)
+    for (int t = 0; t < N; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int row = row_of(t, i);
@@ -87,31 +91,43 @@ template <class T> struct Terms;
 template <> struct Terms<bf16> { static constexpr int n = 3; };
 template <> struct Terms<half> { static constexpr int n = 2; };
 
-// A workgroup has one batch element and head, and one segment of its rows; a wave
-// has 32 columns of the state and of the outputs.  Where there are too few heads
-// to fill the card, a sequence is cut into segments: with OUT false a segment
-// only forms its own sum, k_decay_scan turns the sums into the states before
-// the segments, and a second launch with OUT true starts from those.
+// Waves per 32 columns of the state.  With 128 columns four waves have a column
+// block each, with all rows.  With 64 columns two waves share a block: each holds
+// half of the state's rows and forms the outputs of half of the chunk's rows, and
+// they show each other their halves of the state (rounded, as the product wants
+// them) through LDS.  That halves the time that a chunk takes a workgroup, which
+// is what bounds few heads: chunks follow each other.
+template <int DV> constexpr int kShare = DV == 64 ? 2 : 1;
+template <int DV> constexpr int kDecayBlock = 2 * DV * kShare<DV>;
+
+// A workgroup has one batch element and head, and one segment of its rows.  Where
+// there are too few heads to fill the card, a sequence is cut into segments: with
+// OUT false a segment only forms its own sum, k_decay_scan turns the sums into the
+// states before the segments, and a second launch with OUT true starts from those.
 template <class T, int DK, int DV, bool OUT>
-__global__ __launch_bounds__(2 * DV, DK == 128 && DV == 64 ? 1 : 2) void k_decay_chunks(DecayArgs a) {
-  constexpr int BLOCK = 2 * DV, WAVES = DV / 32;
+__global__ __launch_bounds__(kDecayBlock<DV>, 2) void k_decay_chunks(DecayArgs a) {
+  constexpr int SHARE = kShare<DV>, BLOCK = kDecayBlock<DV>, WAVES = BLOCK / 64, SLICES = DV / 32;
+  constexpr int TILES = DK / 32, OWN = TILES / SHARE;
   SEQ_SHARED T sx[OUT ? kChunk * DK : 8], sy[kChunk * DK], sz[kChunk * DV];
   SEQ_SHARED T sp[OUT ? kChunk * kChunk : 8];
+  SEQ_SHARED T sm[OUT && SHARE == 2 ? WAVES * OWN * 2 * 64 * 8 : 8];
   SEQ_SHARED float s_age[kChunk];            // a^(rows - 1 - j) of the chunk's rows
   const Role& role = a.role[blockIdx.z];
   const int lane = threadIdx.x & 63, wave = wave_index();
+  const int slice = wave % SLICES, part = wave / SLICES;
   const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads;
   const int n = rows_of(a, b);
   const int first = blockIdx.y * a.segment_rows, end = min(first + a.segment_rows, n);
   const float lambda = decay_rate(a.log_decay, h);
   const int64_t list = (int64_t)b * a.heads + h;
   const int64_t turn = role.reversed ? n - 1 : 0, sign = role.reversed ? -1 : 1;
-  const int col = wave * 32 + (lane & 31);
+  const int col = slice * 32 + (lane & 31);
 
   Lanes<DK> at_k;
   Lanes<DV> at_v;
   Lanes<64> at_p;
-  State<DK> st;
+  State<OWN> st;
+  st.first = part * OWN;
   float* mine = role.states + (list * a.segments + blockIdx.y) * (DK * DV);
   if (OUT && a.segments > 1)
     st.load(mine, DK, DV, col, false, 1.0f);
@@ -150,12 +166,28 @@ __global__ __launch_bounds__(2 * DV, DK == 128 && DV == 64 ? 1 : 2) void k_decay
       rz.store(sz);
       if (threadIdx.x < kChunk)
         s_age[threadIdx.x] = (int)threadIdx.x < count ? decay_power(lambda, count - 1 - threadIdx.x) : 0.0f;
+      // The products of rows and the state are rounded to the tensors' type for the
+      // output's products: as much as the output's own rounding.
+      x8<T> packed[OUT ? OWN : 1][2];
+      if constexpr (OUT) {
+#pragma unroll
+        for (int t = 0; t < OWN; ++t)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            float m[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m[e] = st.m[t][8 * u + e];
+            packed[t][u] = pack8<T>(m);
+            if (SHARE == 2)
+              *reinterpret_cast<x8<T>*>(sm + (((wave * OWN + t) * 2 + u) * 64 + lane) * 8) = packed[t][u];
+          }
+      }
       __syncthreads();
       if (DK + DV <= kEarly) fetch(row0 + kChunk);
-      if (OUT) {
-        // Quarters (0, 0), (1, 0), (1, 1) of the products of rows, transposed (columns are i), one or two a wave.
-        for (int quarter = wave; quarter < 3; quarter += WAVES) {
-          const int ib = quarter > 0, jb = quarter > 1;      // with two waves, one has both on the diagonal
+      if constexpr (OUT) {
+        // Quarters (0, 0), (1, 0), (1, 1) of the products of rows, transposed (columns are i), a wave each.
+        if (wave < 3) {
+          const int ib = wave > 0, jb = wave > 1;
           f32x16 s = f32x16{};
 #pragma unroll
           for (int ks = 0; ks < DK / 16; ++ks)
@@ -173,30 +205,39 @@ __global__ __launch_bounds__(2 * DV, DK == 128 && DV == 64 ? 1 : 2) void k_decay
       }
       x8<T> z[4];
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) z[ks] = tile_columns_straight<T, DV>(sz, at_v.straight, 16 * ks, wave);
-      if (OUT) {
-        // The products of rows and the state are rounded to the tensors' type for the
-        // output's products: as much as the output's own rounding.
-#pragma unroll
-        for (int ib = 0; ib < 2; ++ib) {
+      for (int ks = 0; ks < 4; ++ks) z[ks] = tile_columns_straight<T, DV>(sz, at_v.straight, 16 * ks, slice);
+      if constexpr (OUT) {
+        auto output = [&](int ib) {
           f32x16 o = f32x16{};
 #pragma unroll
-          for (int t = 0; t < DK / 32; ++t)
+          for (int t = 0; t < TILES; ++t)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-              float m[8];
-#pragma unroll
-              for (int e = 0; e < 8; ++e) m[e] = st.m[t][8 * u + e];
-              o = mfma32(pack8<T>(m), tile_rows<T, DK>(sx, at_k, ib * 32, 2 * t + u), o);
+              x8<T> m;
+              if (SHARE == 1) {
+                m = packed[t % OWN][u];
+              } else {
+                // the halves in one order for both waves, so that sums do not depend on the wave
+                const int holder = slice + SLICES * (t / OWN);
+                m = *reinterpret_cast<const x8<T>*>(sm + (((holder * OWN + t % OWN) * 2 + u) * 64 + lane) * 8);
+              }
+              o = mfma32(m, tile_rows<T, DK>(sx, at_k, ib * 32, 2 * t + u), o);
             }
           const int i = ib * 32 + (lane & 31);
           o *= role.factor * decay_power(lambda, i + 1 - less);
 #pragma unroll
-          for (int ks = 0; ks < 2 * (ib + 1); ++ks) o = mfma32(z[ks], tile_rows<T, 64>(sp, at_p, ib * 32, ks), o);
+          for (int ks = 0; ks < 4; ++ks)
+            if (ks < 2 * (ib + 1)) o = mfma32(z[ks], tile_rows<T, 64>(sp, at_p, ib * 32, ks), o);
           if (i < count) {
             const int64_t row = turn + sign * (row0 + i);
-            store_column<T>(at<T>(role.out, b, row, h), wave, o, 1.0f, a.dim_z);
+            store_column<T>(at<T>(role.out, b, row, h), slice, o, 1.0f, a.dim_z);
           }
+        };
+        if (SHARE == 2) {
+          output(part);
+        } else {
+          output(0);
+          output(1);
         }
       }
       // The next rows' loads are under way during the state's products alone: with the
@@ -207,10 +248,10 @@ __global__ __launch_bounds__(2 * DV, DK == 128 && DV == 64 ? 1 : 2) void k_decay
       }
       const float age = decay_power(lambda, count - less);
 #pragma unroll
-      for (int t = 0; t < DK / 32; ++t) st.m[t] *= age;
+      for (int t = 0; t < OWN; ++t) st.m[t] *= age;
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) {
-        x8<T> part[Terms<T>::n];
+        x8<T> term[Terms<T>::n];
         const int j = 16 * ks + 8 * (lane >> 5);
         const f32x4 w0 = *reinterpret_cast<const f32x4*>(s_age + j), w1 = *reinterpret_cast<const f32x4*>(s_age + j + 4);
         float v[8];
@@ -218,15 +259,15 @@ __global__ __launch_bounds__(2 * DV, DK == 128 && DV == 64 ? 1 : 2) void k_decay
         for (int e = 0; e < 8; ++e) v[e] = (float)z[ks][e] * (e < 4 ? w0[e & 3] : w1[e & 3]);
 #pragma unroll
         for (int p = 0; p < Terms<T>::n; ++p) {
-          part[p] = pack8<T>(v);
+          term[p] = pack8<T>(v);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] -= (float)part[p][e];
+          for (int e = 0; e < 8; ++e) v[e] -= (float)term[p][e];
         }
 #pragma unroll
-        for (int t = 0; t < DK / 32; ++t) {
-          const x8<T> y = tile_columns_straight<T, DK>(sy, at_k.ordered, 16 * ks, t);
+        for (int t = 0; t < OWN; ++t) {
+          const x8<T> y = tile_columns_straight<T, DK>(sy, at_k.ordered, 16 * ks, st.first + t);
 #pragma unroll
-          for (int p = Terms<T>::n - 1; p >= 0; --p) st.m[t] = mfma32(y, part[p], st.m[t]);
+          for (int p = Terms<T>::n - 1; p >= 0; --p) st.m[t] = mfma32(y, term[p], st.m[t]);
         }
       }
       __syncthreads();
@@ -349,12 +390,12 @@ int pad(int dim) { return dim <= 64 ? 64 : 128; }
 struct SegmentPlan {
   int32_t segments, rows;
 };
-// Segments only where there are too few states to fill the card, and of no less
-// than 256 rows: a segment's state is written and read twice, 4 DK DV bytes
-// against its rows' 2 (2 DK + 2 DV).
+// Segments only where there are too few states to give each compute unit one, and
+// of no less than 256 rows: cutting reads y and z twice and moves 4 DK DV bytes of
+// state per segment four times (256 heads of 128, 4096 rows: 308 us whole, 408 us cut).
 SegmentPlan segment_plan(const qds_decay_config* c, int roles) {
   const int64_t lists = (int64_t)c->batch * c->heads * roles;
-  int64_t want = lists > 0 ? ceil_div(kFill, lists) : 1;
+  int64_t want = lists > 0 && lists < kFill / 2 ? ceil_div(kFill, lists) : 1;
   const int64_t most = ceil_div(c->length, 256);
   if (want > most) want = most;
   if (want < 1) want = 1;
@@ -373,10 +414,10 @@ uint64_t state_bytes(const qds_decay_config* c, int segments) {
 template <class T, int DK, int DV> void run_roles(const DecayArgs& a, int roles, hipStream_t s) {
   const uint32_t lists = (uint32_t)a.batch * a.heads;
   if (a.segments > 1) {
-    k_decay_chunks<T, DK, DV, false><<<dim3(lists, a.segments, roles), 2 * DV, 0, s>>>(a);
+    k_decay_chunks<T, DK, DV, false><<<dim3(lists, a.segments, roles), kDecayBlock<DV>, 0, s>>>(a);
     k_decay_scan<DK, DV><<<dim3(lists * (DK * DV / 256), 1, roles), 256, 0, s>>>(a);
   }
-  k_decay_chunks<T, DK, DV, true><<<dim3(lists, a.segments, roles), 2 * DV, 0, s>>>(a);
+  k_decay_chunks<T, DK, DV, true><<<dim3(lists, a.segments, roles), kDecayBlock<DV>, 0, s>>>(a);
 }
 template <class T> void run_dims(const DecayArgs& a, int roles, hipStream_t s) {
   const int dk = pad(a.dim_x), dv = pad(a.dim_z);
