@@ -124,40 +124,48 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
         rv.load(tiles.row(t + 1), n);
       }
       const T *tk = sk[t & 1], *tv = sv[t & 1];
-      const bool none = j0 > w0 + 31 || (w0 - (j0 + 63) >= window && j0 >= sinks);
-      if (!none) {
-        f32x16 s[2];
+      if (DP == 128) place.forget();
+      // Keys in steps of 32 for narrow heads, whose products are short against their
+      // weights: a step that no row of the wave sees is skipped (the half of a tile behind
+      // the diagonal, before the band, or behind the first tokens).  Wide heads take 64.
+      constexpr int STEP = DP == 64 ? 1 : 2;
 #pragma unroll
-        for (int jb = 0; jb < 2; ++jb) {
-          s[jb] = f32x16{};
+      for (int first = 0; first < 2; first += STEP) {
+        const int from = j0 + 32 * first, to = from + 32 * STEP - 1;
+        if (from > w0 + 31 || (w0 - to >= window && from >= sinks)) continue;
+        f32x16 s[STEP];
 #pragma unroll
-          for (int ks = 0; ks < DP / 16; ++ks) s[jb] = mfma32(tile_rows<T, DP>(tk, place, jb * 32, ks), q[ks], s[jb]);
+        for (int x = 0; x < STEP; ++x) {
+          s[x] = f32x16{};
+#pragma unroll
+          for (int ks = 0; ks < DP / 16; ++ks)
+            s[x] = mfma32(tile_rows<T, DP>(tk, place, (first + x) * 32, ks), q[ks], s[x]);
         }
-        reads_ahead<DP / 8, 1, 4>();
-        const bool later = j0 + 63 > w0, earlier = w0 + 31 - j0 >= window && j0 + 63 >= sinks;
+        if (STEP == 2) reads_ahead<DP / 8, 1, 4>();
+        const bool later = to > w0, earlier = w0 + 31 - from >= window && to >= sinks;
 #pragma unroll
-        for (int jb = 0; jb < 2; ++jb) hide(s[jb], i, j0 + jb * 32, window, sinks, later, earlier);
+        for (int x = 0; x < STEP; ++x) hide(s[x], i, from + x * 32, window, sinks, later, earlier);
         float top = kNoMax;
 #pragma unroll
-        for (int jb = 0; jb < 2; ++jb)
+        for (int x = 0; x < STEP; ++x)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) top = fmaxf(top, s[jb][r]);
+          for (int r = 0; r < 16; ++r) top = fmaxf(top, s[x][r]);
         top = max_halves(top) * c;
         // The maximum is moved only where a weight would pass 2^8: any reference
         // gives the same quotient, and most tiles then need no rescaling.
         if (__any(top > m + 8.0f)) {
-          const float to = fmaxf(m, top), alpha = fast_exp2(m - to);
-          m = to;
+          const float to_m = fmaxf(m, top), alpha = fast_exp2(m - to_m);
+          m = to_m;
           sum *= alpha;
 #pragma unroll
           for (int d = 0; d < DP / 32; ++d) o[d] *= alpha;
         }
 #pragma unroll
-        for (int jb = 0; jb < 2; ++jb) {
+        for (int x = 0; x < STEP; ++x) {
           float p[16];
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
-            p[r] = fast_exp2(fmaf(s[jb][r], c, -m));
+            p[r] = fast_exp2(fmaf(s[x][r], c, -m));
             sum += p[r];
           }
           // The weights are rounded to the tensors' type for the matrix product
@@ -167,7 +175,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
             const x8<T> pb = pack8<T>(p + 8 * u);
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d)
-              o[d] = mfma32(tile_columns<T, DP>(tv, place, jb * 32 + 16 * u, d), pb, o[d]);
+              o[d] = mfma32(tile_columns<T, DP>(tv, place, (first + x) * 32 + 16 * u, d), pb, o[d]);
           }
         }
       }
@@ -255,12 +263,13 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blo
         rv.load(tiles.row(t + 1), n);
       }
       const T *tk = sk[t & 1], *tv = sv[t & 1];
-      const bool none = j0 > w0 + 31 || (w0 - (j0 + 63) >= window && j0 >= sinks);
       if (DP == 128) place.forget();
-      if (!none) {
-        const bool later = j0 + 63 > w0, earlier = w0 + 31 - j0 >= window && j0 + 63 >= sinks;
+      {
 #pragma unroll
         for (int jb = 0; jb < 2; ++jb) {
+          const int from = j0 + 32 * jb;
+          if (from > w0 + 31 || (w0 - (from + 31) >= window && from >= sinks)) continue;
+          const bool later = from + 31 > w0, earlier = w0 + 31 - from >= window && from + 31 >= sinks;
           __builtin_amdgcn_sched_barrier(0);       // one half's products at a time: both would not fit the registers
           f32x16 s = f32x16{}, dp = f32x16{};
 #pragma unroll
