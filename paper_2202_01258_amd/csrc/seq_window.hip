@@ -532,7 +532,7 @@ __device__ inline int slot_of(int p, int window, int sinks) { return p < sinks ?
 template <class T, int DP>
 __global__ __launch_bounds__(kBlock, 2) void k_window_step(StepArgs a) {
   constexpr int OUT = DP + 4;                       // padded, so that 16 heads spread over the banks
-  constexpr int kStage = kWaves * kStrip * DP * 2, kOut = kWaves * 16 * OUT * 4;
+  constexpr int kStage = 2 * kWaves * kStrip * DP * 2, kOut = kWaves * 16 * OUT * 4;
   SEQ_SHARED char lds[kStage > kOut ? kStage : kOut];
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
   const int lane = threadIdx.x & 63, wave = wave_index();
@@ -566,26 +566,20 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_step(StepArgs a) {
       q[s] = __builtin_bit_cast(x8<T>, *reinterpret_cast<const u32x4*>(at<T>(a.q, b, 0, hk * group + g) + col));
   }
 
+  // Whole rows a load: a wave's lanes cover contiguous memory.
   constexpr int NV = kStrip * DP / 8 / 64;
-  u32x4 rk[2][DP / 32], rv[NV];
+  u32x4 rk[NV], rv[NV];
   auto fetch = [&](int s0) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int slot = s0 + 16 * t + (lane & 15);
-      const T* p = slot == fresh ? k_new : kc + (int64_t)slot * a.dim;
-#pragma unroll
-      for (int s = 0; s < DP / 32; ++s) {
-        const int col = (s * 4 + quad) * 8;
-        rk[t][s] = u32x4{0, 0, 0, 0};
-        if (slot < end && col < a.dim) rk[t][s] = *reinterpret_cast<const u32x4*>(p + col);
-      }
-    }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int id = lane + 64 * i, slot = s0 + id / (DP / 8), col = id % (DP / 8) * 8;
-      const T* p = slot == fresh ? v_new : vc + (int64_t)slot * a.dim;
-      rv[i] = u32x4{0, 0, 0, 0};
-      if (slot < end && col < a.dim) rv[i] = *reinterpret_cast<const u32x4*>(p + col);
+      const T* kr = slot == fresh ? k_new : kc + (int64_t)slot * a.dim;
+      const T* vr = slot == fresh ? v_new : vc + (int64_t)slot * a.dim;
+      rk[i] = rv[i] = u32x4{0, 0, 0, 0};
+      if (slot < end && col < a.dim) {
+        rk[i] = *reinterpret_cast<const u32x4*>(kr + col);
+        rv[i] = *reinterpret_cast<const u32x4*>(vr + col);
+      }
     }
   };
 
@@ -594,26 +588,29 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_step(StepArgs a) {
   for (int d = 0; d < DP / 16; ++d) o[d] = f32x4{};
   float m = kNoMax, sum = 0.0f;
   T* stage = (T*)lds + wave * kStrip * DP;
+  T* stage_k = (T*)lds + (kWaves + wave) * kStrip * DP;
   int s0 = begin + wave * kStrip;
   if (s0 < end) fetch(s0);
   for (; s0 < end; s0 += kWaves * kStrip) {
-    x8<T> kf[2][DP / 32];
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int s = 0; s < DP / 32; ++s) kf[t][s] = __builtin_bit_cast(x8<T>, rk[t][s]);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int id = lane + 64 * i;
-      *reinterpret_cast<u32x4*>(stage + tile_at<DP>(id / (DP / 8), id % (DP / 8))) = rv[i];
+      const int id = lane + 64 * i, place = tile_at<DP>(id / (DP / 8), id % (DP / 8));
+      *reinterpret_cast<u32x4*>(stage_k + place) = rk[i];
+      *reinterpret_cast<u32x4*>(stage + place) = rv[i];
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // the wave's own writes to its stages
+    __builtin_amdgcn_wave_barrier();
     if (s0 + kWaves * kStrip < end) fetch(s0 + kWaves * kStrip);
     f32x4 s[2];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       s[t] = f32x4{};
 #pragma unroll
-      for (int ks = 0; ks < DP / 32; ++ks) s[t] = mfma16(kf[t][ks], q[ks], s[t]);
+      for (int ks = 0; ks < DP / 32; ++ks) {
+        const x8<T> kf = __builtin_bit_cast(
+            x8<T>, *reinterpret_cast<const u32x4*>(stage_k + tile_at<DP>(16 * t + (lane & 15), ks * 4 + quad)));
+        s[t] = mfma16(kf, q[ks], s[t]);
+      }
     }
     float top = kNoMax;
 #pragma unroll
@@ -642,8 +639,6 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_step(StepArgs a) {
         sum += p[4 * t + r];
       }
     const x8<T> pb = pack8<T>(p);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");      // the wave's own writes to its stage
-    __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int d = 0; d < DP / 16; ++d) {
       const int row = 4 * quad + ((lane & 15) >> 2), col = d * 16 + (lane & 3) * 4;
