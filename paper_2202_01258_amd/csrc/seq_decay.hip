@@ -65,14 +65,21 @@ template <int N> struct State {
 #pragma unroll
     for (int t = 0; t < N; ++t) m[t] = f32x16{};
   }
+  // Buffer loads, all under way at once: an element outside is read as 0, without a branch
+  // (with one, each load was waited for by itself).
   __device__ void load(const float* p, int rows, int cols, int col, bool swapped, float factor) {
+    const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, kBufferSize, kBufferFlags);
+    const uint32_t step = swapped ? 4 : 4 * cols, base = swapped ? col * 4 * rows : col * 4;
 #pragma unroll
     for (int t = 0; t < N; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int row = row_of(t, i);
-        m[t][i] = row < rows && col < cols ? factor * (swapped ? p[col * rows + row] : p[row * cols + col]) : 0.0f;
+        const uint32_t at = row < rows && col < cols ? base + row * step : kOutside;
+        m[t][i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer, at, 0, 0));
       }
+#pragma unroll
+    for (int t = 0; t < N; ++t) m[t] *= factor;
   }
   __device__ void store(float* p, int rows, int cols, int col, bool swapped, float factor) const {
 #pragma unroll

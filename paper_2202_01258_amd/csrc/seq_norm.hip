@@ -18,28 +18,26 @@ constexpr int kBackwardBlocks = 512;     // two workgroups per compute unit, eac
 template <class T> __device__ inline float to_f32(T x) { return (float)x; }
 template <class T> __device__ inline T from_f32(float x) { return (T)x; }
 
-// VEC consecutive elements (16 bytes, or one element).
+// VEC consecutive elements: one access of up to 16 bytes.
 template <class T, int VEC> struct Pack { T v[VEC]; };
+template <int BYTES> struct Raw;
+template <> struct Raw<16> { using type = u32x4; };
+template <> struct Raw<8> { using type = u32x2; };
+template <> struct Raw<4> { using type = uint32_t; };
+template <> struct Raw<2> { using type = uint16_t; };
 
 template <class T, int VEC> __device__ inline void load(float* out, const T* p) {
-  if constexpr (VEC == 1) {
-    out[0] = to_f32(*p);
-  } else {
-    const u32x4 raw = *reinterpret_cast<const u32x4*>(p);
-    const auto e = __builtin_bit_cast(Pack<T, VEC>, raw);
+  using R = typename Raw<VEC * sizeof(T)>::type;
+  const auto e = __builtin_bit_cast(Pack<T, VEC>, *reinterpret_cast<const R*>(p));
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) out[i] = to_f32(e.v[i]);
-  }
+  for (int i = 0; i < VEC; ++i) out[i] = to_f32(e.v[i]);
 }
 template <class T, int VEC> __device__ inline void store(T* p, const float* in) {
-  if constexpr (VEC == 1) {
-    *p = from_f32<T>(in[0]);
-  } else {
-    Pack<T, VEC> e;
+  using R = typename Raw<VEC * sizeof(T)>::type;
+  Pack<T, VEC> e;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) e.v[i] = from_f32<T>(in[i]);
-    *reinterpret_cast<u32x4*>(p) = __builtin_bit_cast(u32x4, e);
-  }
+  for (int i = 0; i < VEC; ++i) e.v[i] = from_f32<T>(in[i]);
+  *reinterpret_cast<R*>(p) = __builtin_bit_cast(R, e);
 }
 // The weight is fp32 or of the tensors' type.
 template <class T, int VEC> __device__ inline void load_weight(float* out, const void* w, bool w32, int col) {
@@ -56,10 +54,11 @@ template <class T, int VEC> __device__ inline void load_weight(float* out, const
   }
 }
 
-// Sum over the lanes that share a row: a wave, or the whole workgroup.  `part`
-// has a place per wave; two calls that follow each other use different ones.
+// Sum over the lanes that share a row: part of a wave, a wave, or the workgroup.
+// `part` has a place per wave; two calls that follow each other use different ones.
 template <int TPR> __device__ inline float row_sum(float x, float* part) {
-  x = wave_sum(x);
+#pragma unroll
+  for (int m = 1; m < TPR && m < 64; m <<= 1) x += shfl_xor(x, m);
   if constexpr (TPR > 64) {
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
@@ -68,7 +67,8 @@ template <int TPR> __device__ inline float row_sum(float x, float* part) {
   return x;
 }
 template <int TPR> __device__ inline float row_max(float x, float* part) {
-  x = wave_max(x);
+#pragma unroll
+  for (int m = 1; m < TPR && m < 64; m <<= 1) x = fmaxf(x, shfl_xor(x, m));
   if constexpr (TPR > 64) {
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
@@ -89,6 +89,16 @@ __device__ inline float fp8_clamp(float x) {
 __device__ inline uint32_t fp8_pack4(const float* v) {
   int r = __builtin_amdgcn_cvt_pk_fp8_f32(fp8_clamp(v[0]), fp8_clamp(v[1]), 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(fp8_clamp(v[2]), fp8_clamp(v[3]), r, true);
+}
+template <int VEC> __device__ inline void fp8_store(uint8_t* q, const float* v) {
+  if constexpr (VEC == 1)
+    *q = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(fp8_clamp(v[0]), 0.0f, 0, false);
+  else if constexpr (VEC == 2)
+    *reinterpret_cast<uint16_t*>(q) =
+        (uint16_t)__builtin_amdgcn_cvt_pk_fp8_f32(fp8_clamp(v[0]), fp8_clamp(v[1]), 0, false);
+  else
+#pragma unroll
+    for (int i = 0; i < VEC; i += 4) *reinterpret_cast<uint32_t*>(q + i) = fp8_pack4(v + i);
 }
 __device__ inline uint8_t fp8_one(float v) {
   return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(fp8_clamp(v), 0.0f, 0, false);
@@ -114,7 +124,7 @@ __global__ __launch_bounds__(kBlock) void k_norm(ForwardArgs a) {
   constexpr int ROWS = kBlock / TPR;
   const int lane = threadIdx.x % TPR;
   const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
-  if (TPR == 64 && row >= a.rows) return;      // whole waves; no barrier below for them
+  if (TPR <= 64 && row >= a.rows) return;      // no barrier below for rows that waves hold
   const T* x = (const T*)a.x + row * a.x_stride;
   const T* r = a.r ? (const T*)a.r + row * a.r_stride : nullptr;
   float h[NV][VEC];
@@ -168,16 +178,11 @@ __global__ __launch_bounds__(kBlock) void k_norm(ForwardArgs a) {
       uint8_t* q = (uint8_t*)a.y + row * a.width + col;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) h[j][i] *= inv;
-      if constexpr (VEC == 1) {
-        *q = fp8_one(h[j][0]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < VEC; i += 4) *reinterpret_cast<uint32_t*>(q + i) = fp8_pack4(h[j] + i);
-      }
+      fp8_store<VEC>(q, h[j]);
     }
   } else {
-    // 128 columns are 128 / VEC neighbouring lanes (all 16 or 32 of them, as 128 divides the width).
-    static_assert(MODE == kPlain || VEC > 1, "groups need packs");
+    // 128 columns are 128 / VEC neighbouring lanes (all of them real, as 128 divides the width).
+    static_assert(MODE == kPlain || (VEC > 1 && TPR >= 128 / VEC), "a group is within a row's lanes");
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int col = (j * TPR + lane) * VEC;
@@ -192,8 +197,7 @@ __global__ __launch_bounds__(kBlock) void k_norm(ForwardArgs a) {
       uint8_t* q = (uint8_t*)a.y + row * a.width + col;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) h[j][i] *= inv;
-#pragma unroll
-      for (int i = 0; i < VEC; i += 4) *reinterpret_cast<uint32_t*>(q + i) = fp8_pack4(h[j] + i);
+      fp8_store<VEC>(q, h[j]);
     }
   }
 }
@@ -271,8 +275,8 @@ struct BackwardArgs {
 template <class T, int VEC, int NV, int TPR>
 __global__ __launch_bounds__(kBlock) void k_norm_backward(BackwardArgs a) {
   __shared__ float part[8];
-  __shared__ float shares[TPR == 64 ? 3 * 64 * VEC * NV : 1];
   constexpr int ROWS = kBlock / TPR;
+  __shared__ float shares[ROWS > 1 ? (ROWS - 1) * TPR * VEC * NV : 1];
   const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   float dw[NV][VEC], w[NV][VEC];
 #pragma unroll
@@ -285,7 +289,7 @@ __global__ __launch_bounds__(kBlock) void k_norm_backward(BackwardArgs a) {
   int turn = 0;
   for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.rows; first += (int64_t)gridDim.x * ROWS) {
     const int64_t row = first + sub;
-    if (TPR == 64 && row >= a.rows) break;     // a wave of its own; no barrier inside the loop for them
+    if (TPR <= 64 && row >= a.rows) break;     // no barrier inside the loop for rows that waves hold
     const float rstd = a.rstd[row];
     float g[NV][VEC], h[NV][VEC], d[NV][VEC];
     float dot = 0.0f;
@@ -322,22 +326,22 @@ __global__ __launch_bounds__(kBlock) void k_norm_backward(BackwardArgs a) {
       store<T, VEC>((T*)a.dx + row * a.width + col, d[j]);
     }
   }
-  if constexpr (TPR == 64) {
-    // the four waves' shares, added in the order of the waves
+  if constexpr (ROWS > 1) {
+    // the shares of the lanes that hold the same columns, added in their order
     if (sub > 0) {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) shares[((sub - 1) * NV * VEC + j * VEC + i) * 64 + lane] = dw[j][i];
+        for (int i = 0; i < VEC; ++i) shares[((sub - 1) * NV * VEC + j * VEC + i) * TPR + lane] = dw[j][i];
     }
     __syncthreads();
     if (sub > 0) return;
 #pragma unroll
-    for (int s = 0; s < 3; ++s)
+    for (int s = 0; s < ROWS - 1; ++s)
 #pragma unroll
       for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) dw[j][i] += shares[(s * NV * VEC + j * VEC + i) * 64 + lane];
+        for (int i = 0; i < VEC; ++i) dw[j][i] += shares[(s * NV * VEC + j * VEC + i) * TPR + lane];
   }
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
@@ -415,48 +419,56 @@ qds_status validate(const qds_norm_config* c) {
   return QDS_OK;
 }
 
-// Elements per 16 bytes.
-int pack_of(int dtype) { return dtype == QDS_F32 ? 4 : 8; }
-
-// Whether rows may be read in packs of 16 bytes.
-bool packs(const qds_norm_config* c, std::initializer_list<const void*> pointers,
-           std::initializer_list<int64_t> strides) {
-  const int v = pack_of(c->dtype);
-  if (c->width % v) return false;
-  for (const void* p : pointers)
-    if (!aligned16(p)) return false;
-  for (int64_t s : strides)
-    if (s % v) return false;
-  return true;
+// How many elements of a row may be read at once: 16 bytes, 2 elements, or 1, by
+// what the width, the strides and the addresses are multiples of.
+int pack_of(const qds_norm_config* c, const void* weight, std::initializer_list<const void*> pointers,
+            std::initializer_list<int64_t> strides) {
+  const int size = c->dtype == QDS_F32 ? 4 : 2, weight_size = c->weight_dtype == QDS_F32 ? 4 : 2;
+  for (int v : {16 / size, 2}) {
+    const uintptr_t bytes = v * size, weight_bytes = v * weight_size < 16 ? v * weight_size : 16;
+    bool ok = c->width % v == 0 && (uintptr_t)weight % weight_bytes == 0;
+    for (const void* p : pointers) ok = ok && (uintptr_t)p % bytes == 0;
+    for (int64_t s : strides) ok = ok && s % v == 0;
+    if (ok) return v;
+  }
+  return 1;
 }
 
 // Calls f(VEC, NV, TPR) as compile-time values for the least that holds a row
-// in registers; returns false where nothing does.  A wave holds rows of up to
-// 32 elements a lane, so that loads of a whole row are in flight at once; four
-// waves hold wider ones.
+// in registers; returns false where nothing does.  Up to 32 elements a lane, so that
+// loads of a whole row are in flight at once.  Few lanes for narrow rows: with a wave
+// for each, 127238 rows of 128 took 54 us; with 16 lanes, 26 us.
 template <int V> using Int = std::integral_constant<int, V>;
-template <class T, class F> bool with_shape(int width, bool vec, F&& f) {
+template <class T, class F> bool with_shape(int width, int pack, F&& f) {
   constexpr int V = 16 / sizeof(T);
-  if (vec) {
-    if (width <= 64 * V) f(Int<V>{}, Int<1>{}, Int<64>{});
+  if (pack == V) {
+    if (width <= 16 * V) f(Int<V>{}, Int<1>{}, Int<16>{});
+    else if (width <= 32 * V) f(Int<V>{}, Int<1>{}, Int<32>{});
+    else if (width <= 64 * V) f(Int<V>{}, Int<1>{}, Int<64>{});
     else if (width <= 128 * V) f(Int<V>{}, Int<2>{}, Int<64>{});
     else if (width <= 256 * V) f(Int<V>{}, Int<4>{}, Int<64>{});
     else if (width <= 512 * V) f(Int<V>{}, Int<2>{}, Int<256>{});
     else if (width <= 1024 * V) f(Int<V>{}, Int<4>{}, Int<256>{});
     else return false;
+  } else if (pack == 2) {
+    if (width <= 512) f(Int<2>{}, Int<4>{}, Int<64>{});
+    else if (width <= 2048) f(Int<2>{}, Int<16>{}, Int<64>{});
+    else if (width <= 8192) f(Int<2>{}, Int<16>{}, Int<256>{});
+    else return false;
   } else {
-    if (width <= 256) f(Int<1>{}, Int<4>{}, Int<64>{});
+    if (width <= 128) f(Int<1>{}, Int<4>{}, Int<32>{});
     else if (width <= 1024) f(Int<1>{}, Int<16>{}, Int<64>{});
     else if (width <= 4096) f(Int<1>{}, Int<16>{}, Int<256>{});
+    else if (width <= 8192) f(Int<1>{}, Int<32>{}, Int<256>{});
     else return false;
   }
   return true;
 }
 
-template <class T, int MODE> void forward(const ForwardArgs& a, bool vec, hipStream_t s) {
-  const bool held = with_shape<T>(a.width, vec, [&](auto V, auto NV, auto TPR) {
+template <class T, int MODE> void forward(const ForwardArgs& a, int pack, hipStream_t s) {
+  const bool held = with_shape<T>(a.width, pack, [&](auto V, auto NV, auto TPR) {
     constexpr int v = decltype(V)::value, nv = decltype(NV)::value, tpr = decltype(TPR)::value;
-    if constexpr (MODE != kFp8Group || v > 1)
+    if constexpr (MODE != kFp8Group || (v > 1 && tpr >= 128 / v))
       k_norm<T, v, nv, tpr, MODE><<<ceil_div(a.rows, kBlock / tpr), kBlock, 0, s>>>(a);
     else
       k_norm_any<T, MODE><<<a.rows, kBlock, 0, s>>>(a);
@@ -464,12 +476,12 @@ template <class T, int MODE> void forward(const ForwardArgs& a, bool vec, hipStr
   if (!held) k_norm_any<T, MODE><<<a.rows, kBlock, 0, s>>>(a);
 }
 
-template <int MODE> qds_status run_forward(const qds_norm_config* c, const ForwardArgs& a, bool vec, void* stream) {
+template <int MODE> qds_status run_forward(const qds_norm_config* c, const ForwardArgs& a, int pack, void* stream) {
   if (c->rows == 0) return QDS_OK;
   hipStream_t s = (hipStream_t)stream;
-  if (c->dtype == QDS_F32) forward<float, MODE>(a, vec, s);
-  else if (c->dtype == QDS_BF16) forward<bf16, MODE>(a, vec, s);
-  else forward<half, MODE>(a, vec, s);
+  if (c->dtype == QDS_F32) forward<float, MODE>(a, pack, s);
+  else if (c->dtype == QDS_BF16) forward<bf16, MODE>(a, pack, s);
+  else forward<half, MODE>(a, pack, s);
   return launch_status();
 }
 
@@ -478,9 +490,9 @@ int backward_blocks(const qds_norm_config* c) {
   return (int)(c->rows < kBackwardBlocks ? (c->rows > 0 ? c->rows : 1) : kBackwardBlocks);
 }
 
-template <class T> void backward(BackwardArgs a, bool vec, hipStream_t s) {
+template <class T> void backward(BackwardArgs a, int pack, hipStream_t s) {
   if (a.rows > 0) {
-    const bool held = with_shape<T>(a.width, vec, [&](auto V, auto NV, auto TPR) {
+    const bool held = with_shape<T>(a.width, pack, [&](auto V, auto NV, auto TPR) {
       constexpr int v = decltype(V)::value, nv = decltype(NV)::value, tpr = decltype(TPR)::value;
       const int64_t most = ceil_div(a.rows, kBlock / tpr);
       if (a.blocks > most) a.blocks = (int)most;
@@ -508,8 +520,8 @@ extern "C" qds_status qds_residual_norm(const qds_norm_config* c, const void* x,
   if (c->rows > 0 && (!x || !weight || !y || !h || !rstd)) return QDS_ERR_INVALID_ARG;
   const ForwardArgs a{x, residual, weight, y, h, rstd, x_stride, residual_stride, c->rows,
                       c->width, c->eps, c->weight_dtype == QDS_F32};
-  const bool vec = packs(c, {x, residual, weight, y, h}, {x_stride, residual ? residual_stride : 0});
-  return run_forward<kPlain>(c, a, vec, stream);
+  const int pack = pack_of(c, weight, {x, residual, y, h}, {x_stride, residual ? residual_stride : 0});
+  return run_forward<kPlain>(c, a, pack, stream);
 }
 
 extern "C" qds_status qds_residual_norm_fp8(const qds_norm_config* c, const void* x,
@@ -521,8 +533,8 @@ extern "C" qds_status qds_residual_norm_fp8(const qds_norm_config* c, const void
   if (c->rows > 0 && (!x || !weight || !q || !scale || !h)) return QDS_ERR_INVALID_ARG;
   const ForwardArgs a{x, residual, weight, q, h, scale, x_stride, residual_stride, c->rows,
                       c->width, c->eps, c->weight_dtype == QDS_F32};
-  const bool vec = packs(c, {x, residual, weight, q, h}, {x_stride, residual ? residual_stride : 0});
-  return c->group ? run_forward<kFp8Group>(c, a, vec, stream) : run_forward<kFp8Row>(c, a, vec, stream);
+  const int pack = pack_of(c, weight, {x, residual, q, h}, {x_stride, residual ? residual_stride : 0});
+  return c->group ? run_forward<kFp8Group>(c, a, pack, stream) : run_forward<kFp8Row>(c, a, pack, stream);
 }
 
 extern "C" qds_status qds_residual_norm_backward_workspace(const qds_norm_config* c, uint64_t* bytes) {
@@ -548,11 +560,11 @@ extern "C" qds_status qds_residual_norm_backward(const qds_norm_config* c, const
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
   const BackwardArgs a{dy, dh, h, weight, rstd, dx, dweight, (float*)workspace, dy_stride, dh_stride,
                        h_stride, c->rows, c->width, backward_blocks(c), c->weight_dtype == QDS_F32};
-  const bool vec = packs(c, {dy, dh, h, weight, dx}, {dy_stride, dh ? dh_stride : 0, h_stride});
+  const int pack = pack_of(c, weight, {dy, dh, h, dx}, {dy_stride, dh ? dh_stride : 0, h_stride});
   hipStream_t s = (hipStream_t)stream;
-  if (c->dtype == QDS_F32) backward<float>(a, vec, s);
-  else if (c->dtype == QDS_BF16) backward<bf16>(a, vec, s);
-  else backward<half>(a, vec, s);
+  if (c->dtype == QDS_F32) backward<float>(a, pack, s);
+  else if (c->dtype == QDS_BF16) backward<bf16>(a, pack, s);
+  else backward<half>(a, pack, s);
   return launch_status();
 }
 
