@@ -18,26 +18,25 @@ constexpr int kBackwardBlocks = 512;     // two workgroups per compute unit, eac
 template <class T> __device__ inline float to_f32(T x) { return (float)x; }
 template <class T> __device__ inline T from_f32(float x) { return (T)x; }
 
-// VEC consecutive elements: one access of up to 16 bytes.
+// VEC consecutive elements, 16 bytes, at any alignment: rows of odd widths start
+// anywhere.  Where VEC does not divide the width (TAIL), a row's last lane takes its
+// last VEC elements, some of which its neighbour has as well: both store the same
+// values, and only the neighbour counts them in sums.  That leaves no branch around
+// the accesses (a branch per element at the row's end let each load wait for the
+// one before: 32000 x 1024 then took 141 us in place of 95).
 template <class T, int VEC> struct Pack { T v[VEC]; };
-template <int BYTES> struct Raw;
-template <> struct Raw<16> { using type = u32x4; };
-template <> struct Raw<8> { using type = u32x2; };
-template <> struct Raw<4> { using type = uint32_t; };
-template <> struct Raw<2> { using type = uint16_t; };
 
 template <class T, int VEC> __device__ inline void load(float* out, const T* p) {
-  using R = typename Raw<VEC * sizeof(T)>::type;
-  const auto e = __builtin_bit_cast(Pack<T, VEC>, *reinterpret_cast<const R*>(p));
+  Pack<T, VEC> e;
+  __builtin_memcpy(&e, p, sizeof(e));
 #pragma unroll
   for (int i = 0; i < VEC; ++i) out[i] = to_f32(e.v[i]);
 }
 template <class T, int VEC> __device__ inline void store(T* p, const float* in) {
-  using R = typename Raw<VEC * sizeof(T)>::type;
   Pack<T, VEC> e;
 #pragma unroll
   for (int i = 0; i < VEC; ++i) e.v[i] = from_f32<T>(in[i]);
-  *reinterpret_cast<R*>(p) = __builtin_bit_cast(R, e);
+  __builtin_memcpy(p, &e, sizeof(e));
 }
 // The weight is fp32 or of the tensors' type.
 template <class T, int VEC> __device__ inline void load_weight(float* out, const void* w, bool w32, int col) {
@@ -52,6 +51,10 @@ template <class T, int VEC> __device__ inline void load_weight(float* out, const
   } else {
     load<T, VEC>(out, (const T*)w + col);
   }
+}
+// Where the pack of a lane at column `col` (inside the row) starts.
+template <int VEC, bool TAIL> __device__ inline int pack_at(int col, int width) {
+  return TAIL ? min(col, width - VEC) : col;
 }
 
 // Sum over the lanes that share a row: part of a wave, a wave, or the workgroup.
@@ -90,18 +93,15 @@ __device__ inline uint32_t fp8_pack4(const float* v) {
   int r = __builtin_amdgcn_cvt_pk_fp8_f32(fp8_clamp(v[0]), fp8_clamp(v[1]), 0, false);
   return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(fp8_clamp(v[2]), fp8_clamp(v[3]), r, true);
 }
-template <int VEC> __device__ inline void fp8_store(uint8_t* q, const float* v) {
-  if constexpr (VEC == 1)
-    *q = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(fp8_clamp(v[0]), 0.0f, 0, false);
-  else if constexpr (VEC == 2)
-    *reinterpret_cast<uint16_t*>(q) =
-        (uint16_t)__builtin_amdgcn_cvt_pk_fp8_f32(fp8_clamp(v[0]), fp8_clamp(v[1]), 0, false);
-  else
-#pragma unroll
-    for (int i = 0; i < VEC; i += 4) *reinterpret_cast<uint32_t*>(q + i) = fp8_pack4(v + i);
-}
 __device__ inline uint8_t fp8_one(float v) {
   return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(fp8_clamp(v), 0.0f, 0, false);
+}
+
+template <int VEC> __device__ inline void fp8_store(uint8_t* q, const float* v) {
+  uint32_t e[VEC / 4];
+#pragma unroll
+  for (int i = 0; i < VEC / 4; ++i) e[i] = fp8_pack4(v + 4 * i);
+  __builtin_memcpy(q, e, VEC);
 }
 
 struct ForwardArgs {
@@ -118,7 +118,7 @@ enum { kPlain = 0, kFp8Row = 1, kFp8Group = 2 };
 
 // One pass.  TPR lanes hold a row, each NV packs of VEC elements, pack j at
 // column (j TPR + lane) VEC: every load of a wave is one contiguous piece.
-template <class T, int VEC, int NV, int TPR, int MODE>
+template <class T, int VEC, int NV, int TPR, bool TAIL, int MODE>
 __global__ __launch_bounds__(kBlock) void k_norm(ForwardArgs a) {
   __shared__ float part[8];
   constexpr int ROWS = kBlock / TPR;
@@ -134,17 +134,21 @@ __global__ __launch_bounds__(kBlock) void k_norm(ForwardArgs a) {
     const int col = (j * TPR + lane) * VEC;
 #pragma unroll
     for (int i = 0; i < VEC; ++i) h[j][i] = 0.0f;
+    const int at = pack_at<VEC, TAIL>(col, a.width);
     if (col < a.width) {
-      load<T, VEC>(h[j], x + col);
+      load<T, VEC>(h[j], x + at);
       if (r) {
         float t[VEC];
-        load<T, VEC>(t, r + col);
+        load<T, VEC>(t, r + at);
 #pragma unroll
         for (int i = 0; i < VEC; ++i) h[j][i] += t[i];
       }
     }
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) sum = fmaf(h[j][i], h[j][i], sum);
+    for (int i = 0; i < VEC; ++i) {
+      const float own = TAIL && at + i < col ? 0.0f : h[j][i];
+      sum = fmaf(own, own, sum);
+    }
   }
   sum = row_sum<TPR>(sum, part);
   const float rstd = rsqrtf(sum / (float)a.width + a.eps);
@@ -153,12 +157,13 @@ __global__ __launch_bounds__(kBlock) void k_norm(ForwardArgs a) {
   for (int j = 0; j < NV; ++j) {
     const int col = (j * TPR + lane) * VEC;
     if (col < a.width) {
-      store<T, VEC>((T*)a.h + row * a.width + col, h[j]);
+      const int at = pack_at<VEC, TAIL>(col, a.width);
+      store<T, VEC>((T*)a.h + row * a.width + at, h[j]);
       float w[VEC];
-      load_weight<T, VEC>(w, a.w, a.w32, col);
+      load_weight<T, VEC>(w, a.w, a.w32, at);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) h[j][i] = h[j][i] * rstd * w[i];
-      if constexpr (MODE == kPlain) store<T, VEC>((T*)a.y + row * a.width + col, h[j]);
+      if constexpr (MODE == kPlain) store<T, VEC>((T*)a.y + row * a.width + at, h[j]);
       if constexpr (MODE == kFp8Row) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) top = fmaxf(top, fabsf(h[j][i]));
@@ -175,14 +180,13 @@ __global__ __launch_bounds__(kBlock) void k_norm(ForwardArgs a) {
     for (int j = 0; j < NV; ++j) {
       const int col = (j * TPR + lane) * VEC;
       if (col >= a.width) continue;
-      uint8_t* q = (uint8_t*)a.y + row * a.width + col;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) h[j][i] *= inv;
-      fp8_store<VEC>(q, h[j]);
+      fp8_store<VEC>((uint8_t*)a.y + row * a.width + pack_at<VEC, TAIL>(col, a.width), h[j]);
     }
   } else {
     // 128 columns are 128 / VEC neighbouring lanes (all of them real, as 128 divides the width).
-    static_assert(MODE == kPlain || (VEC > 1 && TPR >= 128 / VEC), "a group is within a row's lanes");
+    static_assert(MODE == kPlain || TPR >= 128 / VEC, "a group is within a row's lanes");
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int col = (j * TPR + lane) * VEC;
@@ -272,7 +276,7 @@ struct BackwardArgs {
 // A workgroup takes rows blockIdx.x, + gridDim.x, ... (four at a time where a
 // wave holds a row) and keeps its share of dw in registers; k_norm_dweight adds
 // the workgroups' shares in a fixed order.
-template <class T, int VEC, int NV, int TPR>
+template <class T, int VEC, int NV, int TPR, bool TAIL>
 __global__ __launch_bounds__(kBlock) void k_norm_backward(BackwardArgs a) {
   __shared__ float part[8];
   constexpr int ROWS = kBlock / TPR;
@@ -284,7 +288,7 @@ __global__ __launch_bounds__(kBlock) void k_norm_backward(BackwardArgs a) {
     const int col = (j * TPR + lane) * VEC;
 #pragma unroll
     for (int i = 0; i < VEC; ++i) dw[j][i] = w[j][i] = 0.0f;
-    if (col < a.width) load_weight<T, VEC>(w[j], a.w, a.w32, col);
+    if (col < a.width) load_weight<T, VEC>(w[j], a.w, a.w32, pack_at<VEC, TAIL>(col, a.width));
   }
   int turn = 0;
   for (int64_t first = (int64_t)blockIdx.x * ROWS; first < a.rows; first += (int64_t)gridDim.x * ROWS) {
@@ -299,20 +303,22 @@ __global__ __launch_bounds__(kBlock) void k_norm_backward(BackwardArgs a) {
       const int col = (j * TPR + lane) * VEC;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) g[j][i] = h[j][i] = d[j][i] = 0.0f;
+      const int at = pack_at<VEC, TAIL>(col, a.width);
       if (col < a.width) {
-        load<T, VEC>(g[j], (const T*)a.dy + row * a.dy_stride + col);
-        load<T, VEC>(h[j], (const T*)a.h + row * a.h_stride + col);
-        if (a.dh) load<T, VEC>(d[j], (const T*)a.dh + row * a.dh_stride + col);
+        load<T, VEC>(g[j], (const T*)a.dy + row * a.dy_stride + at);
+        load<T, VEC>(h[j], (const T*)a.h + row * a.h_stride + at);
+        if (a.dh) load<T, VEC>(d[j], (const T*)a.dh + row * a.dh_stride + at);
       }
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
+      const int col = (j * TPR + lane) * VEC, at = pack_at<VEC, TAIL>(col, a.width);
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         h[j][i] *= rstd;
         dw[j][i] = fmaf(g[j][i], h[j][i], dw[j][i]);
         g[j][i] *= w[j][i];
-        dot = fmaf(g[j][i], h[j][i], dot);
+        dot = fmaf(TAIL && at + i < col ? 0.0f : g[j][i], h[j][i], dot);
       }
     }
     dot = row_sum<TPR>(dot, part + 4 * (turn & 1)) / (float)a.width;
@@ -323,7 +329,7 @@ __global__ __launch_bounds__(kBlock) void k_norm_backward(BackwardArgs a) {
       if (col >= a.width) continue;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) d[j][i] += rstd * (g[j][i] - h[j][i] * dot);
-      store<T, VEC>((T*)a.dx + row * a.width + col, d[j]);
+      store<T, VEC>((T*)a.dx + row * a.width + pack_at<VEC, TAIL>(col, a.width), d[j]);
     }
   }
   if constexpr (ROWS > 1) {
@@ -348,7 +354,8 @@ __global__ __launch_bounds__(kBlock) void k_norm_backward(BackwardArgs a) {
     const int col = (j * TPR + lane) * VEC;
     if (col >= a.width) continue;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) a.partial[(int64_t)blockIdx.x * a.width + col + i] = dw[j][i];
+    for (int i = 0; i < VEC; ++i)
+      a.partial[(int64_t)blockIdx.x * a.width + pack_at<VEC, TAIL>(col, a.width) + i] = dw[j][i];
   }
 }
 
@@ -419,69 +426,47 @@ qds_status validate(const qds_norm_config* c) {
   return QDS_OK;
 }
 
-// How many elements of a row may be read at once: 16 bytes, 2 elements, or 1, by
-// what the width, the strides and the addresses are multiples of.
-int pack_of(const qds_norm_config* c, const void* weight, std::initializer_list<const void*> pointers,
-            std::initializer_list<int64_t> strides) {
-  const int size = c->dtype == QDS_F32 ? 4 : 2, weight_size = c->weight_dtype == QDS_F32 ? 4 : 2;
-  for (int v : {16 / size, 2}) {
-    const uintptr_t bytes = v * size, weight_bytes = v * weight_size < 16 ? v * weight_size : 16;
-    bool ok = c->width % v == 0 && (uintptr_t)weight % weight_bytes == 0;
-    for (const void* p : pointers) ok = ok && (uintptr_t)p % bytes == 0;
-    for (int64_t s : strides) ok = ok && s % v == 0;
-    if (ok) return v;
-  }
-  return 1;
-}
-
 // Calls f(VEC, NV, TPR) as compile-time values for the least that holds a row
 // in registers; returns false where nothing does.  Up to 32 elements a lane, so that
 // loads of a whole row are in flight at once.  Few lanes for narrow rows: with a wave
-// for each, 127238 rows of 128 took 54 us; with 16 lanes, 26 us.
+// for each, 127238 rows of 128 took 47 us; with 16 lanes, 20 us.
 template <int V> using Int = std::integral_constant<int, V>;
-template <class T, class F> bool with_shape(int width, int pack, F&& f) {
+template <class T, bool TAIL, class F> bool with_lanes(int width, F&& f) {
   constexpr int V = 16 / sizeof(T);
-  if (pack == V) {
-    if (width <= 16 * V) f(Int<V>{}, Int<1>{}, Int<16>{});
-    else if (width <= 32 * V) f(Int<V>{}, Int<1>{}, Int<32>{});
-    else if (width <= 64 * V) f(Int<V>{}, Int<1>{}, Int<64>{});
-    else if (width <= 128 * V) f(Int<V>{}, Int<2>{}, Int<64>{});
-    else if (width <= 256 * V) f(Int<V>{}, Int<4>{}, Int<64>{});
-    else if (width <= 512 * V) f(Int<V>{}, Int<2>{}, Int<256>{});
-    else if (width <= 1024 * V) f(Int<V>{}, Int<4>{}, Int<256>{});
-    else return false;
-  } else if (pack == 2) {
-    if (width <= 512) f(Int<2>{}, Int<4>{}, Int<64>{});
-    else if (width <= 2048) f(Int<2>{}, Int<16>{}, Int<64>{});
-    else if (width <= 8192) f(Int<2>{}, Int<16>{}, Int<256>{});
-    else return false;
-  } else {
-    if (width <= 128) f(Int<1>{}, Int<4>{}, Int<32>{});
-    else if (width <= 1024) f(Int<1>{}, Int<16>{}, Int<64>{});
-    else if (width <= 4096) f(Int<1>{}, Int<16>{}, Int<256>{});
-    else if (width <= 8192) f(Int<1>{}, Int<32>{}, Int<256>{});
-    else return false;
-  }
+  const Int<TAIL> tail{};
+  if (width < V) return false;
+  if (width <= 16 * V) f(Int<V>{}, Int<1>{}, Int<16>{}, tail);
+  else if (width <= 32 * V) f(Int<V>{}, Int<1>{}, Int<32>{}, tail);
+  else if (width <= 64 * V) f(Int<V>{}, Int<1>{}, Int<64>{}, tail);
+  else if (width <= 128 * V) f(Int<V>{}, Int<2>{}, Int<64>{}, tail);
+  else if (width <= 256 * V) f(Int<V>{}, Int<4>{}, Int<64>{}, tail);
+  else if (width <= 512 * V) f(Int<V>{}, Int<2>{}, Int<256>{}, tail);
+  else if (width <= 1024 * V) f(Int<V>{}, Int<4>{}, Int<256>{}, tail);
+  else return false;
   return true;
 }
+template <class T, class F> bool with_shape(int width, F&& f) {
+  return width % (16 / sizeof(T)) ? with_lanes<T, true>(width, f) : with_lanes<T, false>(width, f);
+}
 
-template <class T, int MODE> void forward(const ForwardArgs& a, int pack, hipStream_t s) {
-  const bool held = with_shape<T>(a.width, pack, [&](auto V, auto NV, auto TPR) {
+template <class T, int MODE> void forward(const ForwardArgs& a, hipStream_t s) {
+  const bool held = with_shape<T>(a.width, [&](auto V, auto NV, auto TPR, auto TAIL) {
     constexpr int v = decltype(V)::value, nv = decltype(NV)::value, tpr = decltype(TPR)::value;
-    if constexpr (MODE != kFp8Group || (v > 1 && tpr >= 128 / v))
-      k_norm<T, v, nv, tpr, MODE><<<ceil_div(a.rows, kBlock / tpr), kBlock, 0, s>>>(a);
+    constexpr bool tail = decltype(TAIL)::value;
+    if constexpr (MODE != kFp8Group || (tpr >= 128 / v && !tail))
+      k_norm<T, v, nv, tpr, tail, MODE><<<ceil_div(a.rows, kBlock / tpr), kBlock, 0, s>>>(a);
     else
       k_norm_any<T, MODE><<<a.rows, kBlock, 0, s>>>(a);
   });
   if (!held) k_norm_any<T, MODE><<<a.rows, kBlock, 0, s>>>(a);
 }
 
-template <int MODE> qds_status run_forward(const qds_norm_config* c, const ForwardArgs& a, int pack, void* stream) {
+template <int MODE> qds_status run_forward(const qds_norm_config* c, const ForwardArgs& a, void* stream) {
   if (c->rows == 0) return QDS_OK;
   hipStream_t s = (hipStream_t)stream;
-  if (c->dtype == QDS_F32) forward<float, MODE>(a, pack, s);
-  else if (c->dtype == QDS_BF16) forward<bf16, MODE>(a, pack, s);
-  else forward<half, MODE>(a, pack, s);
+  if (c->dtype == QDS_F32) forward<float, MODE>(a, s);
+  else if (c->dtype == QDS_BF16) forward<bf16, MODE>(a, s);
+  else forward<half, MODE>(a, s);
   return launch_status();
 }
 
@@ -490,13 +475,14 @@ int backward_blocks(const qds_norm_config* c) {
   return (int)(c->rows < kBackwardBlocks ? (c->rows > 0 ? c->rows : 1) : kBackwardBlocks);
 }
 
-template <class T> void backward(BackwardArgs a, int pack, hipStream_t s) {
+template <class T> void backward(BackwardArgs a, hipStream_t s) {
   if (a.rows > 0) {
-    const bool held = with_shape<T>(a.width, pack, [&](auto V, auto NV, auto TPR) {
+    const bool held = with_shape<T>(a.width, [&](auto V, auto NV, auto TPR, auto TAIL) {
       constexpr int v = decltype(V)::value, nv = decltype(NV)::value, tpr = decltype(TPR)::value;
+    constexpr bool tail = decltype(TAIL)::value;
       const int64_t most = ceil_div(a.rows, kBlock / tpr);
       if (a.blocks > most) a.blocks = (int)most;
-      k_norm_backward<T, v, nv, tpr><<<a.blocks, kBlock, 0, s>>>(a);
+      k_norm_backward<T, v, nv, tpr, tail><<<a.blocks, kBlock, 0, s>>>(a);
     });
     if (!held) k_norm_backward_any<T><<<a.blocks, kBlock, 0, s>>>(a);
   } else {
@@ -520,8 +506,7 @@ extern "C" qds_status qds_residual_norm(const qds_norm_config* c, const void* x,
   if (c->rows > 0 && (!x || !weight || !y || !h || !rstd)) return QDS_ERR_INVALID_ARG;
   const ForwardArgs a{x, residual, weight, y, h, rstd, x_stride, residual_stride, c->rows,
                       c->width, c->eps, c->weight_dtype == QDS_F32};
-  const int pack = pack_of(c, weight, {x, residual, y, h}, {x_stride, residual ? residual_stride : 0});
-  return run_forward<kPlain>(c, a, pack, stream);
+  return run_forward<kPlain>(c, a, stream);
 }
 
 extern "C" qds_status qds_residual_norm_fp8(const qds_norm_config* c, const void* x,
@@ -533,8 +518,7 @@ extern "C" qds_status qds_residual_norm_fp8(const qds_norm_config* c, const void
   if (c->rows > 0 && (!x || !weight || !q || !scale || !h)) return QDS_ERR_INVALID_ARG;
   const ForwardArgs a{x, residual, weight, q, h, scale, x_stride, residual_stride, c->rows,
                       c->width, c->eps, c->weight_dtype == QDS_F32};
-  const int pack = pack_of(c, weight, {x, residual, q, h}, {x_stride, residual ? residual_stride : 0});
-  return c->group ? run_forward<kFp8Group>(c, a, pack, stream) : run_forward<kFp8Row>(c, a, pack, stream);
+  return c->group ? run_forward<kFp8Group>(c, a, stream) : run_forward<kFp8Row>(c, a, stream);
 }
 
 extern "C" qds_status qds_residual_norm_backward_workspace(const qds_norm_config* c, uint64_t* bytes) {
@@ -560,11 +544,10 @@ extern "C" qds_status qds_residual_norm_backward(const qds_norm_config* c, const
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
   const BackwardArgs a{dy, dh, h, weight, rstd, dx, dweight, (float*)workspace, dy_stride, dh_stride,
                        h_stride, c->rows, c->width, backward_blocks(c), c->weight_dtype == QDS_F32};
-  const int pack = pack_of(c, weight, {dy, dh, h, dx}, {dy_stride, dh ? dh_stride : 0, h_stride});
   hipStream_t s = (hipStream_t)stream;
-  if (c->dtype == QDS_F32) backward<float>(a, pack, s);
-  else if (c->dtype == QDS_BF16) backward<bf16>(a, pack, s);
-  else backward<half>(a, pack, s);
+  if (c->dtype == QDS_F32) backward<float>(a, s);
+  else if (c->dtype == QDS_BF16) backward<bf16>(a, s);
+  else backward<half>(a, s);
   return launch_status();
 }
 
