@@ -121,8 +121,9 @@ def _check(status: int, what: str):
 # Marshalling
 # ---------------------------------------------------------------------------
 # A rollout calls these operators once per step and layer, so the time of a call
-# counts: checks format their messages only when they fail, and a configuration
-# (with the size of its scratch memory) is made once for each set of sizes.
+# counts: checks format their messages only when they fail, and what follows from
+# shapes, types and devices alone (their checks, the configuration, the size of its
+# scratch memory) is worked out once for each set of them.
 _CODES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 _PLANS = 4096                                      # sets of sizes that are remembered
 
@@ -181,46 +182,50 @@ def _stream(t):
     return torch.cuda.current_stream(t.device).cuda_stream
 
 
-class _on:
-    """The tensors' device as the current one (cheap where it already is)."""
-
-    def __init__(self, t):
-        index = t.device.index
-        self.guard = None if torch.cuda.current_device() == index else torch.cuda.device(index)
+class _Same:
+    """Stands for torch.cuda.device where the tensors' device is the current one."""
 
     def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
+        pass
 
     def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+        pass
+
+
+_same = _Same()
+
+
+def _on(t):
+    index = t.device.index
+    return _same if torch.cuda.current_device() == index else torch.cuda.device(index)
 
 
 _plans = {}
 
 
-def _plan(kind, query, key):
-    """The configuration of a set of sizes and the bytes of scratch memory that a
-    call with it needs (`query`: the library's function for that, or None)."""
-    got = _plans.get((query, key))
-    if got is None:
-        for x in key:
-            if isinstance(x, int) and not -1 << 31 <= x < 1 << 31:
-                raise ValueError(f"{x} is too large")      # ctypes would cut it to 32 bits
-        cfg, size = kind(ABI_VERSION, *key), C.c_uint64(0)
-        if query is not None:
-            _check(getattr(lib(), query)(C.byref(cfg), C.byref(size)), query)
-        if len(_plans) >= _PLANS:
-            _plans.clear()
-        got = _plans[(query, key)] = (cfg, C.byref(cfg), size.value)
-    return got
+def _remember(key, plan):
+    if len(_plans) >= _PLANS:
+        _plans.clear()
+    _plans[key] = plan
+    return plan
+
+
+def _plan(kind, query, *fields):
+    """A configuration, a pointer to it, and the bytes of scratch memory that a call
+    with it needs (`query`: the library's function for that, or None)."""
+    for x in fields:
+        if isinstance(x, int) and not -1 << 31 <= x < 1 << 31:
+            raise ValueError(f"{x} is too large")      # ctypes would cut it to 32 bits
+    cfg, size = kind(ABI_VERSION, *fields), C.c_uint64(0)
+    if query is not None:
+        _check(getattr(lib(), query)(C.byref(cfg), C.byref(size)), query)
+    return cfg, C.byref(cfg), size.value
 
 
 def _scratch(size, ref):
     """Scratch memory; torch's allocator keeps it from other work until this
     stream's work on it is done."""
-    return torch.empty(size, dtype=torch.uint8, device=ref.device) if size else None
+    return ref.new_empty(size, dtype=torch.uint8) if size else None
 
 
 def _lengths(lengths, batch, ref):
@@ -240,22 +245,25 @@ def _norm_rows(t, width):
 
 
 def _norm_setup(x, residual, weight, eps, group, query=None):
-    _on_gpu(x, "x")
-    code = _code(x, "x")
-    if x.dim() < 1 or x.shape[-1] < 1:
-        raise ValueError("x has no columns")
-    width = x.shape[-1]
-    if residual is not None:
-        _like("residual", residual, x, x.shape)
-    if weight.device != x.device or weight.shape != (width,):
-        raise ValueError(f"weight: [{width}] on {x.device}")
-    wcode = _code(weight, "weight")
-    if wcode != F32 and wcode != code:
-        raise ValueError(f"weight is {weight.dtype}: float32 or x's {x.dtype}")
-    x2 = _norm_rows(x, width)
-    r2 = None if residual is None else _norm_rows(residual, width)
-    plan = _plan(QdsNormConfig, query, (code, wcode, width, x2.shape[0], eps, group))
-    return plan, x2, r2, weight.contiguous()
+    key = (x.shape, x.dtype, x.device, weight.shape, weight.dtype, weight.device, eps, group, query) + (
+        () if residual is None else (residual.shape, residual.dtype, residual.device))
+    plan = _plans.get(key)
+    if plan is None:
+        _on_gpu(x, "x")
+        code = _code(x, "x")
+        if x.dim() < 1 or x.shape[-1] < 1:
+            raise ValueError("x has no columns")
+        width = x.shape[-1]
+        if residual is not None:
+            _like("residual", residual, x, x.shape)
+        if weight.device != x.device or weight.shape != (width,):
+            raise ValueError(f"weight: [{width}] on {x.device}")
+        wcode = _code(weight, "weight")
+        if wcode != F32 and wcode != code:
+            raise ValueError(f"weight is {weight.dtype}: float32 or x's {x.dtype}")
+        plan = _remember(key, _plan(QdsNormConfig, query, code, wcode, width, x.numel() // width, eps, group))
+    width = plan[0].width
+    return plan, _norm_rows(x, width), None if residual is None else _norm_rows(residual, width), weight.contiguous()
 
 
 def residual_norm_forward(x, residual, weight, eps: float = 1e-6):
@@ -263,9 +271,8 @@ def residual_norm_forward(x, residual, weight, eps: float = 1e-6):
     dimension.  Returns y, h (x's type and shape) and rstd (float32, a value per
     row).  `residual` may be None; `weight` is float32 or of x's type."""
     (_, cfg, _), x2, r2, w = _norm_setup(x, residual, weight, eps, 0)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    y, h = x.new_empty(x.shape), x.new_empty(x.shape)
+    rstd = x.new_empty(x.shape[:-1], dtype=torch.float32)
     with _on(x):
         _check(lib().qds_residual_norm(
             cfg, x2.data_ptr(), x2.stride(0), _ptr(r2), 0 if r2 is None else r2.stride(0),
@@ -281,10 +288,8 @@ def residual_norm_fp8(x, residual, weight, eps: float = 1e-6, group: int = 0):
     (c, cfg, _), x2, r2, w = _norm_setup(x, residual, weight, eps, group)
     if group != 0 and (group != 128 or c.width % 128):
         raise ValueError(f"group: 0, or 128 where it divides the width ({c.width}), not {group}")
-    q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
-    h = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    scale = torch.empty((*x.shape[:-1], c.width // group if group else 1), dtype=torch.float32,
-                        device=x.device)
+    q, h = x.new_empty(x.shape, dtype=torch.float8_e4m3fn), x.new_empty(x.shape)
+    scale = x.new_empty((*x.shape[:-1], c.width // group if group else 1), dtype=torch.float32)
     with _on(x):
         _check(lib().qds_residual_norm_fp8(
             cfg, x2.data_ptr(), x2.stride(0), _ptr(r2), 0 if r2 is None else r2.stride(0),
@@ -306,8 +311,7 @@ def residual_norm_backward(dy, dh, h, rstd, weight):
     rstd = rstd.contiguous()
     with _on(h):
         ws = _scratch(size, h)
-        dx = torch.empty(h.shape, dtype=h.dtype, device=h.device)
-        dw = torch.empty(weight.shape, dtype=weight.dtype, device=h.device)
+        dx, dw = h.new_empty(h.shape), weight.new_empty(weight.shape)
         _check(lib().qds_residual_norm_backward(
             cfg, dy2.data_ptr(), dy2.stride(0), _ptr(dh2),
             0 if dh2 is None else dh2.stride(0), h2.data_ptr(), h2.stride(0), rstd.data_ptr(),
@@ -321,6 +325,11 @@ def residual_norm_backward(dy, dh, h, rstd, weight):
 # ---------------------------------------------------------------------------
 def _window_setup(q, k, v, window, sinks, scale, rows, query=None):
     """Checks q, k, v [batch, rows, heads, dim] (or without rows) and makes the plan."""
+    key = (q.shape, q.dtype, q.device, k.shape, k.dtype, k.device, v.shape, v.dtype, v.device, window, sinks,
+           scale, rows, query)
+    plan = _plans.get(key)
+    if plan is not None:
+        return plan
     _on_gpu(q, "q")
     code = _code(q, "q")
     if q.dim() != (4 if rows else 3) or k.dim() != q.dim():
@@ -333,8 +342,8 @@ def _window_setup(q, k, v, window, sinks, scale, rows, query=None):
         raise ValueError(f"{heads} query heads are no multiple of {kv_heads} key heads")
     if window < 1 or sinks < 0:
         raise ValueError(f"window {window} >= 1 and sinks {sinks} >= 0")
-    return _plan(QdsWindowConfig, query, (code, batch, q.shape[1] if rows else 0, heads, kv_heads, dim,
-                                          window, sinks, dim ** -0.5 if scale is None else scale))
+    return _remember(key, _plan(QdsWindowConfig, query, code, batch, q.shape[1] if rows else 0, heads, kv_heads,
+                                dim, window, sinks, dim ** -0.5 if scale is None else scale))
 
 
 def window_attention_forward(q, k, v, window: int, sinks: int = 0, lengths=None, scale=None):
@@ -352,8 +361,8 @@ def window_attention_forward(q, k, v, window: int, sinks: int = 0, lengths=None,
     c, cfg, _ = _window_setup(q, k, v, window, sinks, scale, True)
     lengths = _lengths(lengths, c.batch, q)
     q, k, v = _rows(q), _rows(k), _rows(v)
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    lse = torch.empty((c.batch, c.heads, c.length), dtype=torch.float32, device=q.device)
+    o = q.new_empty(q.shape)
+    lse = q.new_empty((c.batch, c.heads, c.length), dtype=torch.float32)
     with _on(q):
         _check(lib().qds_window_forward(cfg, _view(q), _view(k), _view(v), _ptr(lengths),
                                         _view(o), lse.data_ptr(), _stream(q)), "qds_window_forward")
@@ -369,7 +378,7 @@ def window_attention_backward(do, q, k, v, o, lse, window: int, sinks: int = 0, 
     _like("lse", lse, q, (c.batch, c.heads, c.length), torch.float32)
     lengths = _lengths(lengths, c.batch, q)
     do, q, k, v, o, lse = _rows(do), _rows(q), _rows(k), _rows(v), _rows(o), lse.contiguous()
-    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
     with _on(q):
         ws = _scratch(size, q)
         _check(lib().qds_window_backward(
@@ -421,7 +430,7 @@ def window_attention_step(q, k, v, k_cache, v_cache, pos, window: int, sinks: in
     _like("pos", pos, q, (c.batch,), torch.int32)
     pos = pos.contiguous()
     q, k, v = _rows(q), _rows(k), _rows(v)
-    o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    o = q.new_empty(q.shape)
     with _on(q):
         ws = _scratch(size, q)
         _check(lib().qds_window_step(
@@ -434,6 +443,11 @@ def window_attention_step(q, k, v, k_cache, v_cache, pos, window: int, sinks: in
 # Linear attention with a decay for each head
 # ---------------------------------------------------------------------------
 def _decay_setup(q, k, v, log_decay, scale, rows, query=None):
+    key = (q.shape, q.dtype, q.device, k.shape, k.dtype, k.device, v.shape, v.dtype, v.device, log_decay.shape,
+           log_decay.dtype, log_decay.device, scale, rows, query)
+    plan = _plans.get(key)
+    if plan is not None:
+        return plan
     _on_gpu(q, "q")
     code = _code(q, "q")
     if q.dim() != (4 if rows else 3) or v.dim() != q.dim():
@@ -442,8 +456,8 @@ def _decay_setup(q, k, v, log_decay, scale, rows, query=None):
     _like("k", k, q, q.shape)
     _like("v", v, q, (*q.shape[:-1], dim_v))
     _like("log_decay", log_decay, q, (heads,), torch.float32)
-    return _plan(QdsDecayConfig, query, (code, q.shape[0], q.shape[1] if rows else 0, heads, dim_k, dim_v,
-                                         dim_k ** -0.5 if scale is None else scale))
+    return _remember(key, _plan(QdsDecayConfig, query, code, q.shape[0], q.shape[1] if rows else 0, heads, dim_k,
+                                dim_v, dim_k ** -0.5 if scale is None else scale))
 
 
 def _state(name, t, c, ref):
@@ -466,8 +480,8 @@ def decay_attention_forward(q, k, v, log_decay, state=None, lengths=None, scale=
     lengths = _lengths(lengths, cfg.batch, q)
     log_decay = log_decay.contiguous()
     q, k, v = _rows(q), _rows(k), _rows(v)
-    o = torch.empty((*q.shape[:-1], cfg.dim_v), dtype=q.dtype, device=q.device)
-    last = torch.empty((cfg.batch, cfg.heads, cfg.dim_k, cfg.dim_v), dtype=torch.float32, device=q.device)
+    o = v.new_empty(v.shape)
+    last = q.new_empty((cfg.batch, cfg.heads, cfg.dim_k, cfg.dim_v), dtype=torch.float32)
     with _on(q):
         ws = _scratch(size, q)
         _check(lib().qds_decay_forward(
@@ -487,8 +501,8 @@ def decay_attention_backward(do, q, k, v, log_decay, state=None, dstate=None, le
     lengths = _lengths(lengths, cfg.batch, q)
     log_decay = log_decay.contiguous()
     do, q, k, v = _rows(do), _rows(q), _rows(k), _rows(v)
-    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
-    dfirst = torch.empty((cfg.batch, cfg.heads, cfg.dim_k, cfg.dim_v), dtype=torch.float32, device=q.device)
+    dq, dk, dv = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
+    dfirst = q.new_empty((cfg.batch, cfg.heads, cfg.dim_k, cfg.dim_v), dtype=torch.float32)
     with _on(q):
         ws = _scratch(size, q)
         _check(lib().qds_decay_backward(
@@ -510,7 +524,7 @@ def decay_attention_step(q, k, v, log_decay, state, scale=None, out_state=None):
         _in_place("out_state", out_state, q, shape, torch.float32)
     log_decay = log_decay.contiguous()
     q, k, v = _rows(q), _rows(k), _rows(v)
-    o = torch.empty((*q.shape[:-1], cfg.dim_v), dtype=q.dtype, device=q.device)
+    o = v.new_empty(v.shape)
     with _on(q):
         _check(lib().qds_decay_step(ref, _view(q), _view(k), _view(v), log_decay.data_ptr(),
                                     state.data_ptr(), _view(o), out_state.data_ptr(), _stream(q)),
