@@ -111,6 +111,9 @@ template <int DV> constexpr int kDecayBlock = 2 * DV * kShare<DV>;
 // there are too few heads to fill the card, a sequence is cut into segments: with
 // OUT false a segment only forms its own sum, k_decay_scan turns the sums into the
 // states before the segments, and a second launch with OUT true starts from those.
+// Few heads are bound by their chunks' sequence: 32 x 1000 rows, 8 heads of 64 take 38 us
+// forward and 71 us back.  131072 rows, 16 heads of 128, in segments: 273 us for the
+// sums, 561 us for the outputs, at 3.9 and 3.8 TB/s.
 template <class T, int DK, int DV, bool OUT>
 __global__ __launch_bounds__(kDecayBlock<DV>, 2) void k_decay_chunks(DecayArgs a) {
   constexpr int SHARE = kShare<DV>, BLOCK = kDecayBlock<DV>, WAVES = BLOCK / 64, SLICES = DV / 32;
@@ -298,6 +301,7 @@ __global__ __launch_bounds__(kDecayBlock<DV>, 2) void k_decay_chunks(DecayArgs a
 }
 
 // From each segment's own sum to the state before it; one element of M per thread.
+// 17 us for 16 heads of 128 x 128 in 32 segments.
 template <int DK, int DV> __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a) {
   const Role& role = a.role[blockIdx.z];
   const int64_t list = blockIdx.x / (DK * DV / 256);
@@ -334,6 +338,7 @@ struct StepArgs {
 
 // Bound by reading and writing the states.  A workgroup has one state; a thread
 // has four columns of every (1024 / DV)-th row, so a wave's loads are contiguous.
+// 16384 states of 64 x 64: 98 us, 5.5 TB/s.
 template <class T, int DK, int DV> __global__ __launch_bounds__(256) void k_decay_step(StepArgs a) {
   constexpr int LANES = DV / 4, ROWS = 256 / LANES, N = DK / ROWS;
   SEQ_SHARED float part[ROWS][DV];

@@ -118,6 +118,8 @@ enum { kPlain = 0, kFp8Row = 1, kFp8Group = 2 };
 
 // One pass.  TPR lanes hold a row, each NV packs of VEC elements, pack j at
 // column (j TPR + lane) VEC: every load of a wave is one contiguous piece.
+// 32000 x 1024 bfloat16: 49 us, 5.3 TB/s.  131072 x 4096 with a scale per 128: 638 us,
+// 5.9 TB/s.  79133 rows of 73 halves, whose packs overlap: 17 us, 2.3 TB/s.
 template <class T, int VEC, int NV, int TPR, bool TAIL, int MODE>
 __global__ __launch_bounds__(kBlock) void k_norm(ForwardArgs a) {
   __shared__ float part[8];
@@ -275,7 +277,8 @@ struct BackwardArgs {
 // g = dy w;  dx = dh + rstd (g - h rstd^2 mean(g h));  dw = sum over rows of dy h rstd.
 // A workgroup takes rows blockIdx.x, + gridDim.x, ... (four at a time where a
 // wave holds a row) and keeps its share of dw in registers; k_norm_dweight adds
-// the workgroups' shares in a fixed order.
+// the workgroups' shares in a fixed order.  32000 x 1024 bfloat16: 48 us, 5.4 TB/s.
+// dw is formed from h as stored, so it carries h's rounding.
 template <class T, int VEC, int NV, int TPR, bool TAIL>
 __global__ __launch_bounds__(kBlock) void k_norm_backward(BackwardArgs a) {
   __shared__ float part[8];
@@ -391,7 +394,8 @@ template <class T> __global__ __launch_bounds__(kBlock) void k_norm_backward_any
 }
 
 // 64 columns per workgroup: sixteen waves each add every sixteenth share (a column's
-// chain of loads is what takes the time: 7.6 us with four waves, 777 columns).
+// chain of loads is what takes the time: 777 columns of fp32 take 7.9 us with four
+// waves, 3.9 with sixteen).
 constexpr int kJoinWaves = 16;
 template <class T> __global__ __launch_bounds__(64 * kJoinWaves) void k_norm_dweight(BackwardArgs a) {
   __shared__ float part[64 * kJoinWaves];
