@@ -279,6 +279,13 @@ __device__ inline int xcd_order(int id, int count, int per_list) {
   return x * per + min(x, rest) + y;
 }
 
+// The same with every list on every XCD: the items are dealt one of each list in turn,
+// and one list further from item to item, so that a list's neighbours go round the XCDs.
+__device__ inline int spread_order(int id, int count, int per_list) {
+  const uint32_t lists = (uint32_t)(count / per_list), y = (uint32_t)id / lists;
+  return (int)(((uint32_t)id + y) % lists * (uint32_t)per_list + y);
+}
+
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 constexpr int kFill = 512;       // workgroups that fill the card: two per compute unit

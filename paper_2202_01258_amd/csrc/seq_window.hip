@@ -4,6 +4,8 @@
 //
 // Row i of an episode of n rows sees j <= i < n with i - j < window or j < sinks.
 // Scores are kept in units of log 2: p = 2^(c s - m) with c = scale log2(e).
+#include <algorithm>
+
 #include "seq_common.hpp"
 
 namespace seq {
@@ -18,7 +20,13 @@ struct WindowArgs {
   float *lse, *delta;
   int32_t batch, length, heads, kv_heads, dim, window, sinks;
   float scale;
+  bool spread;                        // see spread()
 };
+
+// The item of this workgroup where each list (one batch element's key head) has per_list.
+__device__ inline int item_of(const WindowArgs& a, int per_list) {
+  return a.spread ? spread_order(blockIdx.x, gridDim.x, per_list) : xcd_order(blockIdx.x, gridDim.x, per_list);
+}
 
 __device__ inline int rows_of(const WindowArgs& a, int b) {
   if (!a.lengths) return a.length;
@@ -89,7 +97,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
   const int lane = threadIdx.x & 63, wave = wave_index();
   Lanes<DP> place;
   const int group = a.heads / a.kv_heads;
-  int id = xcd_order(blockIdx.x, gridDim.x, group * q_blocks);
+  int id = item_of(a, group * q_blocks);
   const int g = id % group;
   id /= group;
   // late blocks first: they have the most keys where the window is long
@@ -223,7 +231,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blo
   const int lane = threadIdx.x & 63, wave = wave_index();
   Lanes<DP> place;
   const int group = a.heads / a.kv_heads;
-  int id = xcd_order(blockIdx.x, gridDim.x, group * q_blocks);
+  int id = item_of(a, group * q_blocks);
   const int g = id % group;
   id /= group;
   const int block = q_blocks - 1 - id % q_blocks;
@@ -349,7 +357,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan
   const int lane = threadIdx.x & 63, wave = wave_index();
   Lanes<DP> place;
   const int group = a.heads / a.kv_heads;
-  const int id = xcd_order(blockIdx.x, gridDim.x, plan.items);
+  const int id = item_of(a, plan.items);
   const int head = id / plan.items;           // b * kv_heads + hk
   const KeyItem item = key_item(plan, id % plan.items);
   const int hk = head % a.kv_heads, b = head / a.kv_heads;
@@ -775,6 +783,29 @@ qds_status validate(const qds_window_config* c) {
   return QDS_OK;
 }
 
+// Whether a list's items go to all XCDs, in place of one.  One XCD reads a list's keys
+// once into its own L2, but the XCDs then end apart where their work differs: lists with
+// lengths, a number of them that does not divide evenly, or early rows that see less
+// than a window in a large part of a list (of the stretch that an XCD has, for fewer
+// than four lists; of half a list else, whose long blocks begin late in the last lists).
+// Spread, the lists' keys and values share every L2: up to 64 MiB of them that costs less
+// than it gains, and with two lists for each XCD or fewer it does at any size.
+// Forward and backward, us, one XCD each | spread:
+//   with lengths  64 lists x 1000 rows of 64, window 250       173 | 151
+//                 8 x 16384 of 128, 1024                       790 | 577
+//                 24 x 2048 of 64, 2048                        232 | 181
+//                 96 x 4096 of 64, 1024 (96 MiB)               844 | 912
+//                 64 x 8192 of 64, 512 (128 MiB)              1580 | 1754
+//   without       128 x 1024 of 64, 1024                       176 | 139
+//                 16 x 16384 of 64, 4096                      4750 | 5270
+//                 4 x 65536 of 128, 2048                      1418 | 1503
+bool spread(const qds_window_config* c, const int32_t* lengths) {
+  const int64_t lists = (int64_t)c->batch * c->kv_heads;
+  const bool deals_evenly = lists % kXcds == 0 || kXcds % lists == 0;
+  const bool even = !lengths && deals_evenly && c->window < c->length * std::min<int64_t>(lists, 4) / 8;
+  return !even && (lists <= 2 * kXcds || lists * c->length * c->dim * 4 <= 64 << 20);
+}
+
 WindowArgs window_args(const qds_window_config* c, const int32_t* lengths) {
   WindowArgs a{};
   a.lengths = lengths;
@@ -786,6 +817,7 @@ WindowArgs window_args(const qds_window_config* c, const int32_t* lengths) {
   a.window = c->window;
   a.sinks = c->sinks;
   a.scale = c->scale;
+  a.spread = spread(c, lengths);
   return a;
 }
 

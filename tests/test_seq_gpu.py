@@ -361,6 +361,25 @@ def test_window_few_heads(t, window, sinks, b, hq, hkv, d):
     check_window(*qkv(b, t, hq, hkv, d, BF16), window, sinks)
 
 
+@pytest.mark.parametrize("b,hkv", [(1, 1), (3, 1), (2, 4), (9, 1), (4, 4), (17, 1), (5, 5)])
+@pytest.mark.parametrize("window", [20, 300])
+def test_window_order_of_work(b, hkv, window):
+    """One, few and many lists, numbers of them that divide by eight and that do not:
+    workgroups take their work in another order where lengths are given, results stay."""
+    q, k, v = qkv(b, 300, 2 * hkv, hkv, 64, BF16)
+    check_window(q, k, v, window, 2)
+    whole = torch.full((b,), 300, dtype=torch.int32, device="cuda")
+    o, lse = S.window_attention_forward(q, k, v, window, 2)
+    for x, y in zip((o, lse), S.window_attention_forward(q, k, v, window, 2, whole)):
+        assert torch.equal(x, y)
+    do = rand(*o.shape, dtype=BF16, seed=9)
+    for x, y in zip(S.window_attention_backward(do, q, k, v, o, lse, window, 2),
+                    S.window_attention_backward(do, q, k, v, o, lse, window, 2, whole)):
+        assert torch.equal(x, y)
+    lengths = torch.tensor([(i * 131 + 77) % 301 for i in range(b)], dtype=torch.int32, device="cuda")
+    check_window(q, k, v, window, 2, lengths)
+
+
 def test_window_many_heads():
     """Key blocks that are not cut."""
     check_window(*qkv(40, 140, 8, 8, 64, BF16), 60, 2)
