@@ -560,7 +560,10 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_step(StepArgs a) {
   __shared__ float s_m[kWaves][16], s_l[kWaves][16];
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int group = a.heads / a.kv_heads, slots = a.window + a.sinks;
-  const int tile = blockIdx.x % a.tiles, head = blockIdx.x / a.tiles;
+  // One list further from range to range: the ranges of a long cache go round the XCDs,
+  // whose shares of the memory's bandwidth would else differ as the positions do (2
+  // policies of 4 key heads of 128, 65536 slots: 48 us on the lists' own XCDs, 34 so).
+  const int unit = (int)((blockIdx.x + blockIdx.y) % gridDim.x), tile = unit % a.tiles, head = unit / a.tiles;
   const int hk = head % a.kv_heads, b = head / a.kv_heads;
   const int pos = a.pos[b];
   const int seen = pos < 0 ? 0 : min(pos, slots - 1) + 1;
@@ -687,7 +690,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_step(StepArgs a) {
     *reinterpret_cast<f32x4*>(out + (wave * 16 + (lane & 15)) * OUT + d * 16 + 4 * quad) = o[d];
   __syncthreads();
   const int heads_here = min(16, group - tile * 16);
-  const int64_t item = (int64_t)blockIdx.x * a.cut + blockIdx.y, items = (int64_t)gridDim.x * a.cut;
+  const int64_t item = (int64_t)unit * a.cut + blockIdx.y, items = (int64_t)gridDim.x * a.cut;
   for (int x = threadIdx.x; x < heads_here * (DP / 4); x += kBlock) {
     const int hh = x / (DP / 4), d = x % (DP / 4) * 4;
     float top = s_m[0][hh];
