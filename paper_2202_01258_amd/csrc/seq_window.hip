@@ -537,7 +537,7 @@ __global__ __launch_bounds__(kBlock) void k_window_dkdv_join(WindowArgs a, KeyPl
 // of 32 slots in turn and keep running maxima and sums of their own; ranges and
 // waves are joined at the end.  Keys and values are loaded as whole rows and go
 // through LDS (8 KB a wave for 64 columns, 16 KB for 128), which turns them.
-// 8 policies of 4 key heads of 128 over 65552 slots, float16: 166 us, 5.4 TB/s; 256
+// 8 policies of 4 key heads of 128 over 65552 slots, float16: 164 us, 5.5 TB/s; 256
 // policies of 8 heads of 64 over 251 slots: 19.6 us.
 constexpr int kStrip = 32;
 
@@ -719,32 +719,50 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_step(StepArgs a) {
   }
 }
 
-// Joins the ranges of one head: a wave per head, DP / 64 columns a lane.  5.4 us for
-// the 256 heads of 8 policies, 16 ranges each.
-template <class T, int DP> __global__ __launch_bounds__(64) void k_window_step_join(StepArgs a) {
-  const int lane = threadIdx.x;
+// Joins the ranges of one head: DP / 64 columns a lane, every eighth range a wave, as
+// a range's sum waits for its loads.  One key head over 65536 slots, 128 ranges: a call takes
+// 18 us, with one wave 27; 8 policies of 32 heads, 16 ranges: 4.8 us beside the step's 164.
+constexpr int kStepJoinWaves = 8;
+template <class T, int DP>
+__global__ __launch_bounds__(64 * kStepJoinWaves) void k_window_step_join(StepArgs a) {
+  __shared__ float s_top[kStepJoinWaves], s_l[kStepJoinWaves], s_r[kStepJoinWaves][DP];
+  const int lane = threadIdx.x & 63, wave = wave_index();
   const int b = blockIdx.x / a.heads, h = blockIdx.x % a.heads, group = a.heads / a.kv_heads;
   const int g = h % group;
   const int64_t first = (((int64_t)b * a.kv_heads + h / group) * a.tiles + g / 16) * a.cut;
   const int64_t items = (int64_t)a.batch * a.kv_heads * a.tiles * a.cut;
   float top = kNoMax;
-  for (int s = lane; s < a.cut; s += 64) top = fmaxf(top, a.parts[(first + s) * 16 + g % 16]);
+  for (int s = threadIdx.x; s < a.cut; s += 64 * kStepJoinWaves) top = fmaxf(top, a.parts[(first + s) * 16 + g % 16]);
   top = wave_max(top);
+  if (lane == 0) s_top[wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kStepJoinWaves; ++w) top = fmaxf(top, s_top[w]);
   float l = 0.0f, r[DP / 64];
 #pragma unroll
   for (int d = 0; d < DP / 64; ++d) r[d] = 0.0f;
 #pragma unroll 4
-  for (int s = 0; s < a.cut; ++s) {
+  for (int s = wave; s < a.cut; s += kStepJoinWaves) {
     const int64_t at16 = (first + s) * 16 + g % 16;
     const float f = fast_exp2(a.parts[at16] - top);
     l = fmaf(a.parts[items * 16 + at16], f, l);
 #pragma unroll
     for (int d = 0; d < DP / 64; ++d) r[d] = fmaf(a.parts[items * 32 + at16 * DP + d * 64 + lane], f, r[d]);
   }
-  const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
+  if (lane == 0) s_l[wave] = l;
 #pragma unroll
-  for (int d = 0; d < DP / 64; ++d)
-    if (d * 64 + lane < a.dim) at<T>(a.o, b, 0, h)[d * 64 + lane] = (T)(r[d] * inv);
+  for (int d = 0; d < DP / 64; ++d) s_r[wave][d * 64 + lane] = r[d];
+  __syncthreads();
+  if (threadIdx.x >= a.dim) return;
+  l = 0.0f;
+  float sum = 0.0f;
+#pragma unroll
+  for (int w = 0; w < kStepJoinWaves; ++w) {
+    l += s_l[w];
+    sum += s_r[w][threadIdx.x];
+  }
+  const float inv = l > 0.0f ? 1.0f / l : (l == 0.0f ? 0.0f : l);
+  at<T>(a.o, b, 0, h)[threadIdx.x] = (T)(sum * inv);
 }
 
 // Slot by slot: the latest position below n that belongs in it.
@@ -870,9 +888,12 @@ uint64_t key_parts(const qds_window_config* c, const KeyPlan& p) {
 struct StepPlan {
   int32_t tiles, cut, range;
 };
-// Slots are cut into ranges where there are fewer heads than workgroups that
-// fill the card; a range has at least four strips for each wave (one key head over
-// 65536 slots: 26 us; with a strip for each, 36, as the join adds 512 ranges in turn).
+// Slots are cut into ranges where there are fewer heads than workgroups that fill the
+// card; a range has at least four strips for each wave (with one strip, a key head over
+// 65536 slots takes as long: 18.8 us, and 18.4 with four).  Short caches stay whole, as
+// a second launch costs more than a longer range: 4 policies of 8 key heads of 64, 516 and
+// 1016 slots, whole 6.8 and 9.4 us on the card, 12.2 and 12.1 a call; cut in two 8.0 and
+// 8.9, 16.2 and 15.7 a call.  At 2016 slots whole takes 15.8, cut 9.0.
 StepPlan step_plan(const qds_window_config* c) {
   StepPlan p{};
   p.tiles = (int32_t)ceil_div(c->heads / c->kv_heads, 16);
@@ -881,6 +902,7 @@ StepPlan step_plan(const qds_window_config* c) {
   int64_t cut = lists > 0 ? ceil_div(kFill, lists) : 1;
   const int64_t most = ceil_div(slots, 4 * strip);
   if (cut > most) cut = most;
+  if (slots * (c->dim <= 64 ? 64 : 128) <= 80 << 10) cut = 1;
   p.range = (int32_t)(ceil_div(ceil_div(slots, cut), strip) * strip);
   p.cut = (int32_t)ceil_div(slots, p.range);
   return p;
@@ -986,7 +1008,7 @@ extern "C" qds_status qds_window_step(const qds_window_config* c, qds_view q, qd
     using T = decltype(t);
     constexpr int DP = decltype(d)::value;
     k_window_step<T, DP><<<dim3(c->batch * c->kv_heads * p.tiles, p.cut), kBlock, 0, s>>>(a);
-    if (p.cut > 1) k_window_step_join<T, DP><<<c->batch * c->heads, 64, 0, s>>>(a);
+    if (p.cut > 1) k_window_step_join<T, DP><<<c->batch * c->heads, 64 * kStepJoinWaves, 0, s>>>(a);
   });
   return launch_status();
 }

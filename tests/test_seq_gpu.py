@@ -470,6 +470,32 @@ def test_window_steps_after_a_prompt(window, sinks, d, hq, hkv, dtype):
             assert torch.equal(kc[i, :, slot], k_all[i, p]) and torch.equal(vc[i, :, slot], v_all[i, p])
 
 
+@pytest.mark.parametrize("window,sinks,d,hq,hkv,dtype", [
+    (20000, 3, 128, 20, 1, BF16), (33000, 0, 64, 2, 1, F16), (6000, 70, 72, 4, 2, BF16), (1200, 81, 64, 3, 3, F16), (1199, 81, 64, 3, 3, F16)])
+def test_window_step_ranges(window, sinks, d, hq, hkv, dtype):
+    """Few heads over long caches, whose slots are cut into many ranges, most of them
+    empty for some positions; and the sizes on both sides of the first cut."""
+    slots = window + sinks
+    pos = [0, 511, 512, slots - 1, slots, 2 * slots + 5, -1]
+    b, t = len(pos), max(pos) + 1
+    k_all, v_all = rand(b, t, hkv, d, dtype=dtype, seed=3), rand(b, t, hkv, d, dtype=dtype, seed=4)
+    kc, vc = S.window_cache(b, hkv, d, window, sinks, dtype)
+    kc.fill_(float("nan"))
+    vc.fill_(float("nan"))
+    at = torch.tensor(pos, device="cuda")
+    S.window_cache_fill(k_all, v_all, kc, vc, window, sinks, at.clamp(min=0).to(torch.int32))
+    rows = torch.arange(b, device="cuda")
+    q = rand(b, hq, d, dtype=dtype, seed=50)
+    o = S.window_attention_step(q, k_all[rows, at], v_all[rows, at], kc, vc, at.to(torch.int32), window, sinks)
+    within(o, *step_exact(q, k_all, v_all, window, sinks, pos), "o")
+    assert (o[-1] == 0).all()
+    # one policy alone has the finest ranges
+    one = slice(5, 6)
+    alone = S.window_attention_step(q[one], k_all[rows, at][one], v_all[rows, at][one], kc[one], vc[one],
+                                    at[one].to(torch.int32), window, sinks)
+    within(alone, *step_exact(q[one], k_all[one], v_all[one], window, sinks, pos[5:6]), "o alone")
+
+
 def test_window_step_reads_what_forward_sees():
     """A whole episode token by token gives the rows of one forward call."""
     b, t, hq, hkv, d, window, sinks = 3, 60, 4, 2, 64, 11, 2
