@@ -434,6 +434,8 @@ qds_status validate(const qds_norm_config* c) {
 // in registers; returns false where nothing does.  Up to 32 elements a lane, so that
 // loads of a whole row are in flight at once.  Few lanes for narrow rows: with a wave
 // for each, 127238 rows of 128 took 47 us; with 16 lanes, 20 us.
+// fp32 rows beyond 4096 take eight packs of four: 9947 x 4697 forward and backward
+// 299 us, read again for each use 668.
 template <int V> using Int = std::integral_constant<int, V>;
 template <class T, bool TAIL, class F> bool with_lanes(int width, F&& f) {
   constexpr int V = 16 / sizeof(T);
@@ -446,6 +448,7 @@ template <class T, bool TAIL, class F> bool with_lanes(int width, F&& f) {
   else if (width <= 256 * V) f(Int<V>{}, Int<4>{}, Int<64>{}, tail);
   else if (width <= 512 * V) f(Int<V>{}, Int<2>{}, Int<256>{}, tail);
   else if (width <= 1024 * V) f(Int<V>{}, Int<4>{}, Int<256>{}, tail);
+  else if (V == 4 && width <= 2048 * V) f(Int<V>{}, Int<V == 4 ? 8 : 4>{}, Int<256>{}, tail);
   else return false;
   return true;
 }
