@@ -402,13 +402,18 @@ int pad(int dim) { return dim <= 64 ? 64 : 128; }
 struct SegmentPlan {
   int32_t segments, rows;
 };
-// Segments only where there are too few states to give each compute unit one, and
-// of no less than 256 rows: cutting reads y and z twice and moves 4 DK DV bytes of
-// state per segment four times (256 heads of 128, 4096 rows: 308 us whole, 408 us cut).
+// Segments only where there are too few states for half of the compute units: cutting
+// reads y and z twice and moves 4 DK DV bytes of state per segment four times.  Forward, us,
+// whole | cut: 80 states of 64, 8000 rows 201 | 118;  120 states of 64, 8000 rows 204 | 184;
+// 192 states of 64, 8000 rows 205 | 292;  240 of 128, 1000 rows 72 | 121.
+// Short sequences stay whole, as two more launches cost more than eight chunks of 64 columns or
+// four of 128: 32 states of 64, 512 rows 18.5 | 22.  A segment has two chunks or more: 32 states
+// of 64 x 128, 819 rows 26 us with 128 rows, 29 with 256, 28 with 64.
 SegmentPlan segment_plan(const qds_decay_config* c, int roles) {
   const int64_t lists = (int64_t)c->batch * c->heads * roles;
-  int64_t want = lists > 0 && lists < kFill / 2 ? ceil_div(kFill, lists) : 1;
-  const int64_t most = ceil_div(c->length, 256);
+  int64_t want = lists > 0 && lists < kFill / 4 ? ceil_div(kFill, lists) : 1;
+  const int64_t columns = pad(c->dim_k > c->dim_v ? c->dim_k : c->dim_v);
+  const int64_t most = c->length * columns <= 1 << 15 ? 1 : ceil_div(c->length, 2 * kChunk);
   if (want > most) want = most;
   if (want < 1) want = 1;
   SegmentPlan p;

@@ -616,6 +616,14 @@ def test_decay_ragged():
     check_decay(4, 900, 1, 64, 128, BF16, lengths=lengths)
 
 
+@pytest.mark.parametrize("t,dk,dv", [(512, 64, 64), (513, 64, 64), (256, 128, 64), (257, 64, 128), (700, 128, 128)])
+def test_decay_ragged_segments(t, dk, dv):
+    """Around the rows from which sequences are cut: episodes that end before, at and
+    behind a segment's first row."""
+    lengths = [t, 0, 1, 127, 128, 129, t - 1]
+    check_decay(len(lengths), t, 2, dk, dv, BF16, lengths=torch.tensor(lengths, dtype=torch.int32, device="cuda"))
+
+
 def test_decay_none_and_all():
     """No decay, and one that forgets everything at once."""
     check_decay(1, 150, 2, 64, 64, F16, torch.tensor([0.0, -math.inf], device="cuda"), with_state=False, with_dstate=False)
