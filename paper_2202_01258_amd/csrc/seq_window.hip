@@ -21,6 +21,7 @@ struct WindowArgs {
   int32_t batch, length, heads, kv_heads, dim, window, sinks;
   float scale;
   bool spread;                        // see spread()
+  int32_t share;                      // log2 of the query heads of a group that a workgroup has; see shared_heads()
 };
 
 // The item of this workgroup where each list (one batch element's key head) has per_list.
@@ -81,7 +82,8 @@ __device__ inline void hide(f32x16& s, int i, int j0, int window, int sinks, boo
 // ---------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------
-// A workgroup has 128 query rows of one head, a wave 32 of them.  Scores are
+// A workgroup has 128 query rows (of one head, or of up to four heads of a group), a
+// wave 32 of one head.  Scores are
 // formed transposed (keys are rows of the C tile, queries its columns), so a
 // query's maximum and sum are over a lane's own registers and one exchange with
 // lane l ^ 32, and the weights are the B operand of o^T = v^T p^T as they are.
@@ -97,16 +99,17 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
   const int lane = threadIdx.x & 63, wave = wave_index();
   Lanes<DP> place;
   const int group = a.heads / a.kv_heads;
-  int id = item_of(a, group * q_blocks);
-  const int g = id % group;
-  id /= group;
+  const int per_block = group >> a.share;
+  int id = item_of(a, per_block * q_blocks);
+  const int g = ((id % per_block) << a.share) + (wave & ((1 << a.share) - 1));
+  id /= per_block;
   // late blocks first: they have the most keys where the window is long
   const int block = q_blocks - 1 - id % q_blocks;
   id /= q_blocks;
   const int hk = id % a.kv_heads, b = id / a.kv_heads;
   const int h = hk * group + g;
   const int n = rows_of(a, b), window = a.window, sinks = a.sinks;
-  const int i0 = block * kForwardRows, w0 = i0 + 32 * wave;
+  const int rows = kForwardRows >> a.share, i0 = block * rows, w0 = i0 + 32 * (wave >> a.share);
   const int i = w0 + (lane & 31);
   T* o_row = at<T>(a.o, b, i, h);
   float* lse = a.lse + ((int64_t)b * a.heads + h) * a.length + i;
@@ -118,7 +121,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
     const float c = a.scale * kLog2e;
     x8<T> q[DP / 16];
     load_rows<T, DP>(q, at<T>(a.q, b, i, h), i < n, a.dim);
-    const KeyTiles tiles(a, i0, kForwardRows, n);
+    const KeyTiles tiles(a, i0, rows, n);
     Staged<T, DP, kBlock> rk, rv;
     rk.init(at<T>(a.k, b, 0, hk), a.k.t, a.dim);
     rv.init(at<T>(a.v, b, 0, hk), a.v.t, a.dim);
@@ -219,7 +222,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
 // Two kernels, one over queries and one over keys, each forming p again; sums
 // are then over a workgroup's own loop, in a fixed order.
 
-// dq of 128 rows of one head, as the forward pass; also writes delta.  2 x 8192 rows,
+// dq of the same rows as the forward pass has; also writes delta.  2 x 8192 rows,
 // 16 heads of 128, window 1024, bfloat16: 261 us (the forward pass takes 198).
 //
 // delta is formed from o as stored, so it carries o's rounding; the score gradients
@@ -231,15 +234,16 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blo
   const int lane = threadIdx.x & 63, wave = wave_index();
   Lanes<DP> place;
   const int group = a.heads / a.kv_heads;
-  int id = item_of(a, group * q_blocks);
-  const int g = id % group;
-  id /= group;
+  const int per_block = group >> a.share;
+  int id = item_of(a, per_block * q_blocks);
+  const int g = ((id % per_block) << a.share) + (wave & ((1 << a.share) - 1));
+  id /= per_block;
   const int block = q_blocks - 1 - id % q_blocks;
   id /= q_blocks;
   const int hk = id % a.kv_heads, b = id / a.kv_heads;
   const int h = hk * group + g;
   const int n = rows_of(a, b), window = a.window, sinks = a.sinks;
-  const int i0 = block * kForwardRows, w0 = i0 + 32 * wave;
+  const int rows = kForwardRows >> a.share, i0 = block * rows, w0 = i0 + 32 * (wave >> a.share);
   const int i = w0 + (lane & 31);
   const int64_t flat = ((int64_t)b * a.heads + h) * a.length + i;
 
@@ -263,7 +267,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blo
     delta = sum_halves(delta);
     if (lane < 32 && i < n) a.delta[flat] = delta;
     const float lse = i < n ? a.lse[flat] * kLog2e : INFINITY;   // rows past the end: p = 0
-    const KeyTiles tiles(a, i0, kForwardRows, n);
+    const KeyTiles tiles(a, i0, rows, n);
     Staged<T, DP, kBlock> rk, rv;
     rk.init(at<T>(a.k, b, 0, hk), a.k.t, a.dim);
     rv.init(at<T>(a.v, b, 0, hk), a.v.t, a.dim);
@@ -827,6 +831,17 @@ bool spread(const qds_window_config* c, const int32_t* lengths) {
   return !even && (lists <= 2 * kXcds || lists * c->length * c->dim * 4 <= 64 << 20);
 }
 
+// How many query heads of a group share a workgroup of the kernels over queries, whose four
+// waves then have 32 or 64 rows of several heads in place of 128 of one: the same keys are
+// loaded for as many products, but fewer tiles of them by rows that others cannot see.  Two
+// or four where that divides the group.  Forward, us, one head | four: 4 x 3994 rows of 128,
+// 32 heads over 4, window 113: 134 | 125;  15 x 1374 of 64, 64 over 8, window 37: 152 | 132;
+// 13 x 776 of 80, 32 over 4, 104: 80 | 65;  long windows the same.
+int shared_heads(const qds_window_config* c) {
+  const int group = c->heads / c->kv_heads;
+  return group % 4 == 0 ? 2 : group % 2 == 0 ? 1 : 0;
+}
+
 WindowArgs window_args(const qds_window_config* c, const int32_t* lengths) {
   WindowArgs a{};
   a.lengths = lengths;
@@ -839,6 +854,7 @@ WindowArgs window_args(const qds_window_config* c, const int32_t* lengths) {
   a.sinks = c->sinks;
   a.scale = c->scale;
   a.spread = spread(c, lengths);
+  a.share = shared_heads(c);
   return a;
 }
 
@@ -923,8 +939,8 @@ extern "C" qds_status qds_window_forward(const qds_window_config* c, qds_view q,
   if (!near_rows(k) || !near_rows(v)) return QDS_ERR_UNSUPPORTED;
   WindowArgs a = window_args(c, lengths);
   a.q = view(q), a.k = view(k), a.v = view(v), a.o = view(o), a.lse = lse;
-  const int blocks = (int)ceil_div(c->length, kForwardRows);
-  const int grid = c->batch * c->heads * blocks;
+  const int blocks = (int)ceil_div(c->length, kForwardRows >> a.share);
+  const int grid = c->batch * (c->heads >> a.share) * blocks;
   with_type(c->dtype, c->dim, [&](auto t, auto d) {
     k_window_forward<decltype(t), decltype(d)::value><<<grid, kBlock, 0, (hipStream_t)stream>>>(a, blocks);
   });
@@ -960,14 +976,14 @@ extern "C" qds_status qds_window_backward(const qds_window_config* c, qds_view d
   a.delta = (float*)workspace;
   float* parts = (float*)((char*)workspace + align_up((uint64_t)c->batch * c->heads * c->length * sizeof(float)));
   const KeyPlan plan = key_plan(c);
-  const int blocks = (int)ceil_div(c->length, kForwardRows);
+  const int blocks = (int)ceil_div(c->length, kForwardRows >> a.share);
   const int lists = c->batch * c->kv_heads;
   if ((int64_t)lists * plan.items > 0x7fffffff) return QDS_ERR_UNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
   with_type(c->dtype, c->dim, [&](auto t, auto d) {
     using T = decltype(t);
     constexpr int DP = decltype(d)::value;
-    k_window_dq<T, DP><<<c->batch * c->heads * blocks, kBlock, 0, s>>>(a, blocks);
+    k_window_dq<T, DP><<<c->batch * (c->heads >> a.share) * blocks, kBlock, 0, s>>>(a, blocks);
     k_window_dkdv<T, DP><<<lists * plan.items, kBlock, 0, s>>>(a, plan, parts);
     const int from = plan.first_cut > 1 ? 0 : plan.first, to = plan.band_cut > 1 ? plan.blocks : plan.first;
     if (to > from) {

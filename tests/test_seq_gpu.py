@@ -324,6 +324,15 @@ def test_window_heads_and_dims(d, hq, hkv, dtype):
     check_window(*qkv(2, 150, hq, hkv, d, dtype), 40, 5)
 
 
+@pytest.mark.parametrize("hq,hkv", [(4, 1), (6, 1), (6, 2), (12, 3), (8, 1), (16, 2)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_window_head_groups(hq, hkv, d):
+    """Groups of 2, 3, 4, 6 and 8 heads: one, two or four of them share a workgroup."""
+    q, k, v = qkv(3, 170, hq, hkv, d, BF16)
+    check_window(q, k, v, 37, 2)
+    check_window(q, k, v, 1000, 0, torch.tensor([170, 33, 96], dtype=torch.int32, device="cuda"))
+
+
 @pytest.mark.parametrize("layout", ["plain", "heads", "time", "odd"])
 @pytest.mark.parametrize("d", [64, 128])
 def test_window_layouts(layout, d):
