@@ -82,13 +82,12 @@ __device__ inline void hide(f32x16& s, int i, int j0, int window, int sinks, boo
 // ---------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------
-// A workgroup has 128 query rows (of one head, or of up to four heads of a group), a
-// wave 32 of one head.  Scores are
-// formed transposed (keys are rows of the C tile, queries its columns), so a
-// query's maximum and sum are over a lane's own registers and one exchange with
+// A workgroup has 128 query rows (of one head, or 64 or 32 rows of heads of a group), a
+// wave 32 of them.  Scores are formed transposed (keys are rows of the C tile, queries
+// its columns), so a query's maximum and sum are over a lane's own registers and one exchange with
 // lane l ^ 32, and the weights are the B operand of o^T = v^T p^T as they are.
 // Bound by the issue of matrix and vector instructions together: 32768 rows, 16 heads
-// of 128 over 4 key heads, window 4096, bfloat16 take 1.12 ms, 940 TFLOP/s.  The next
+// of 128 over 4 key heads, window 4096, bfloat16 take 1.09 to 1.14 ms, 920 to 970 TFLOP/s.  The next
 // tile's scores beside this tile's weights do not fit the registers of two waves on a
 // SIMD (292 spills), and with one wave took 2.11 ms beside 1.07.
 constexpr int kForwardRows = 32 * kWaves;
@@ -223,7 +222,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
 // are then over a workgroup's own loop, in a fixed order.
 
 // dq of the same rows as the forward pass has; also writes delta.  2 x 8192 rows,
-// 16 heads of 128, window 1024, bfloat16: 261 us (the forward pass takes 198).
+// 16 heads of 128, window 1024, bfloat16: 255 us (the forward pass takes 193).
 //
 // delta is formed from o as stored, so it carries o's rounding; the score gradients
 // are rounded to the tensors' type for their product, relative to each of them.  In
@@ -350,7 +349,7 @@ __device__ inline KeyItem key_item(const KeyPlan& p, int x) {
 // registers; values do for 64 columns, and are read from LDS for 128, where the
 // registers that two waves on a SIMD leave each other are 160 for keys and sums.
 // Two waves with values in LDS take 400 us where one with all in registers takes 490
-// (2 x 8192 rows, 16 heads of 128, window 1024, bfloat16; 397 now).  The weights and
+// (2 x 8192 rows, 16 heads of 128, window 1024, bfloat16; 388 now).  The weights and
 // the score gradients are rounded as in the other two kernels.
 template <class T, int DP>
 __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan plan, float* parts) {
