@@ -34,11 +34,15 @@ __device__ inline int rows_of(const WindowArgs& a, int b) {
   return min(max(a.lengths[b], 0), a.length);
 }
 
+// Tiles in LDS have rows of 64 or 128 columns; products are formed of the first DC of
+// them: 32, 64, 96 or 128, the least that holds the head.
+constexpr int padded(int columns) { return columns <= 64 ? 64 : 128; }
+
 // One row per lane l % 32 as an operand of the 32x32x16 product (k along the row).
-template <class T, int DP> __device__ inline void load_rows(x8<T>* f, const T* row, bool valid, int dim) {
+template <class T, int DC> __device__ inline void load_rows(x8<T>* f, const T* row, bool valid, int dim) {
   const int half = (threadIdx.x & 63) >> 5;
 #pragma unroll
-  for (int s = 0; s < DP / 16; ++s) {
+  for (int s = 0; s < DC / 16; ++s) {
     const int c = s * 2 + half;
     f[s] = zero8<T>();
     if (valid && c * 8 < dim) f[s] = __builtin_bit_cast(x8<T>, *reinterpret_cast<const u32x4*>(row + c * 8));
@@ -92,8 +96,9 @@ __device__ inline void hide(f32x16& s, int i, int j0, int window, int sinks, boo
 // SIMD (292 spills), and with one wave took 2.11 ms beside 1.07.
 constexpr int kForwardRows = 32 * kWaves;
 
-template <class T, int DP>
+template <class T, int DC>
 __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int q_blocks) {
+  constexpr int DP = padded(DC);
   SEQ_SHARED T sk[2][64 * DP], sv[2][64 * DP];
   const int lane = threadIdx.x & 63, wave = wave_index();
   Lanes<DP> place;
@@ -113,13 +118,13 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
   T* o_row = at<T>(a.o, b, i, h);
   float* lse = a.lse + ((int64_t)b * a.heads + h) * a.length + i;
 
-  f32x16 o[DP / 32];
+  f32x16 o[DC / 32];
 #pragma unroll
-  for (int d = 0; d < DP / 32; ++d) o[d] = f32x16{};
+  for (int d = 0; d < DC / 32; ++d) o[d] = f32x16{};
   if (i0 < n) {
     const float c = a.scale * kLog2e;
-    x8<T> q[DP / 16];
-    load_rows<T, DP>(q, at<T>(a.q, b, i, h), i < n, a.dim);
+    x8<T> q[DC / 16];
+    load_rows<T, DC>(q, at<T>(a.q, b, i, h), i < n, a.dim);
     const KeyTiles tiles(a, i0, rows, n);
     Staged<T, DP, kBlock> rk, rv;
     rk.init(at<T>(a.k, b, 0, hk), a.k.t, a.dim);
@@ -152,10 +157,10 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
         for (int x = 0; x < STEP; ++x) {
           s[x] = f32x16{};
 #pragma unroll
-          for (int ks = 0; ks < DP / 16; ++ks)
+          for (int ks = 0; ks < DC / 16; ++ks)
             s[x] = mfma32(tile_rows<T, DP>(tk, place, (first + x) * 32, ks), q[ks], s[x]);
         }
-        if (STEP == 2) reads_ahead<DP / 8, 1, 4>();
+        if (STEP == 2) reads_ahead<DC / 8, 1, 4>();
         const bool later = to > w0, earlier = w0 + 31 - from >= window && to >= sinks;
 #pragma unroll
         for (int x = 0; x < STEP; ++x) hide(s[x], i, from + x * 32, window, sinks, later, earlier);
@@ -172,7 +177,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
           m = to_m;
           sum *= alpha;
 #pragma unroll
-          for (int d = 0; d < DP / 32; ++d) o[d] *= alpha;
+          for (int d = 0; d < DC / 32; ++d) o[d] *= alpha;
         }
 #pragma unroll
         for (int x = 0; x < STEP; ++x) {
@@ -188,7 +193,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
           for (int u = 0; u < 2; ++u) {
             const x8<T> pb = pack8<T>(p + 8 * u);
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d)
+            for (int d = 0; d < DC / 32; ++d)
               o[d] = mfma32(tile_columns<T, DP>(tv, place, (first + x) * 32 + 16 * u, d), pb, o[d]);
           }
         }
@@ -202,13 +207,13 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
     if (i < n) {
       const float inv = 1.0f / sum;
 #pragma unroll
-      for (int d = 0; d < DP / 32; ++d) store_column<T>(o_row, d, o[d], inv, a.dim);
+      for (int d = 0; d < DC / 32; ++d) store_column<T>(o_row, d, o[d], inv, a.dim);
       if (lane < 32) *lse = (m + fast_log2(sum)) * kLn2;
     }
   }
   if (i >= n && i < a.length) {
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d) store_column<T>(o_row, d, f32x16{}, 0.0f, a.dim);
+    for (int d = 0; d < DC / 32; ++d) store_column<T>(o_row, d, f32x16{}, 0.0f, a.dim);
     if (lane < 32) *lse = -INFINITY;
   }
 }
@@ -227,8 +232,9 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
 // delta is formed from o as stored, so it carries o's rounding; the score gradients
 // are rounded to the tensors' type for their product, relative to each of them.  In
 // float16 those below 2^-24 vanish: a loss is scaled there as for any float16 gradient.
-template <class T, int DP>
+template <class T, int DC>
 __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blocks) {
+  constexpr int DP = padded(DC);
   SEQ_SHARED T sk[2][64 * DP], sv[2][64 * DP];
   const int lane = threadIdx.x & 63, wave = wave_index();
   Lanes<DP> place;
@@ -246,20 +252,20 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blo
   const int i = w0 + (lane & 31);
   const int64_t flat = ((int64_t)b * a.heads + h) * a.length + i;
 
-  f32x16 dq[DP / 32];
+  f32x16 dq[DC / 32];
 #pragma unroll
-  for (int d = 0; d < DP / 32; ++d) dq[d] = f32x16{};
+  for (int d = 0; d < DC / 32; ++d) dq[d] = f32x16{};
   if (i0 < n) {
     const float c = a.scale * kLog2e;
-    x8<T> q[DP / 16], go[DP / 16];
-    load_rows<T, DP>(q, at<T>(a.q, b, i, h), i < n, a.dim);
-    load_rows<T, DP>(go, at<T>(a.dout, b, i, h), i < n, a.dim);
+    x8<T> q[DC / 16], go[DC / 16];
+    load_rows<T, DC>(q, at<T>(a.q, b, i, h), i < n, a.dim);
+    load_rows<T, DC>(go, at<T>(a.dout, b, i, h), i < n, a.dim);
     float delta = 0.0f;
     {
-      x8<T> o[DP / 16];
-      load_rows<T, DP>(o, at<T>(a.o, b, i, h), i < n, a.dim);
+      x8<T> o[DC / 16];
+      load_rows<T, DC>(o, at<T>(a.o, b, i, h), i < n, a.dim);
 #pragma unroll
-      for (int s = 0; s < DP / 16; ++s)
+      for (int s = 0; s < DC / 16; ++s)
 #pragma unroll
         for (int e = 0; e < 8; ++e) delta = fmaf((float)o[s][e], (float)go[s][e], delta);
     }
@@ -293,9 +299,9 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blo
           __builtin_amdgcn_sched_barrier(0);       // one half's products at a time: both would not fit the registers
           f32x16 s = f32x16{}, dp = f32x16{};
 #pragma unroll
-          for (int ks = 0; ks < DP / 16; ++ks) s = mfma32(tile_rows<T, DP>(tk, place, jb * 32, ks), q[ks], s);
+          for (int ks = 0; ks < DC / 16; ++ks) s = mfma32(tile_rows<T, DP>(tk, place, jb * 32, ks), q[ks], s);
 #pragma unroll
-          for (int ks = 0; ks < DP / 16; ++ks) dp = mfma32(tile_rows<T, DP>(tv, place, jb * 32, ks), go[ks], dp);
+          for (int ks = 0; ks < DC / 16; ++ks) dp = mfma32(tile_rows<T, DP>(tv, place, jb * 32, ks), go[ks], dp);
           hide(s, i, j0 + jb * 32, window, sinks, later, earlier);
           float ds[16];
 #pragma unroll
@@ -304,7 +310,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blo
           for (int u = 0; u < 2; ++u) {
             const x8<T> db = pack8<T>(ds + 8 * u);
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d)
+            for (int d = 0; d < DC / 32; ++d)
               dq[d] = mfma32(tile_columns<T, DP>(tk, place, jb * 32 + 16 * u, d), db, dq[d]);
           }
         }
@@ -318,7 +324,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blo
   if (i < a.length) {
     T* row = at<T>(a.dq, b, i, h);
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d) store_column<T>(row, d, dq[d], i < n ? a.scale : 0.0f, a.dim);
+    for (int d = 0; d < DC / 32; ++d) store_column<T>(row, d, dq[d], i < n ? a.scale : 0.0f, a.dim);
   }
 }
 
@@ -351,8 +357,9 @@ __device__ inline KeyItem key_item(const KeyPlan& p, int x) {
 // Two waves with values in LDS take 400 us where one with all in registers takes 490
 // (2 x 8192 rows, 16 heads of 128, window 1024, bfloat16; 388 now).  The weights and
 // the score gradients are rounded as in the other two kernels.
-template <class T, int DP>
+template <class T, int DC>
 __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan plan, float* parts) {
+  constexpr int DP = padded(DC);
   constexpr int QT = 32;
   constexpr bool V_LDS = DP == 128;
   SEQ_SHARED T sq[2][QT * DP], sg[2][QT * DP], sv[V_LDS ? kKeyRows * DP : 8];
@@ -370,9 +377,9 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan
   const float c = a.scale * kLog2e;
   const uint32_t reach = reach_of(window, sinks, j);
 
-  f32x16 dk[DP / 32], dv[DP / 32];
+  f32x16 dk[DC / 32], dv[DC / 32];
 #pragma unroll
-  for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = f32x16{};
+  for (int d = 0; d < DC / 32; ++d) dk[d] = dv[d] = f32x16{};
   // the rows that see this block, in tiles of 32, for each head of the group
   int unit = 0, stop = 0, per_head = 1;
   if (j0 < n) {
@@ -383,8 +390,8 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan
     stop = (int)(units * (item.piece + 1) / item.cut);
   }
   if (unit < stop) {
-    x8<T> k[DP / 16], v[V_LDS ? 1 : DP / 16];
-    load_rows<T, DP>(k, at<T>(a.k, b, j, hk), j < n, a.dim);
+    x8<T> k[DC / 16], v[V_LDS ? 1 : DC / 16];
+    load_rows<T, DC>(k, at<T>(a.k, b, j, hk), j < n, a.dim);
     if constexpr (V_LDS) {
       Staged<T, DP, kBlock> rv;
       rv.init(at<T>(a.v, b, 0, hk), a.v.t, a.dim);
@@ -394,7 +401,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan
         rv.store(sv + half * 64 * DP);
       }
     } else {
-      load_rows<T, DP>(v, at<T>(a.v, b, j, hk), j < n, a.dim);
+      load_rows<T, DC>(v, at<T>(a.v, b, j, hk), j < n, a.dim);
     }
     Staged<T, DP, kBlock, QT> rq, rg;
     rq.init(nullptr, a.q.t, a.dim);
@@ -438,13 +445,13 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan
       if (!none) {
         f32x16 s = f32x16{}, dp = f32x16{};
 #pragma unroll
-        for (int ks = 0; ks < DP / 16; ++ks) s = mfma32(tile_rows<T, DP>(tq, place, 0, ks), k[ks], s);
+        for (int ks = 0; ks < DC / 16; ++ks) s = mfma32(tile_rows<T, DP>(tq, place, 0, ks), k[ks], s);
 #pragma unroll
-        for (int ks = 0; ks < DP / 16; ++ks) {
+        for (int ks = 0; ks < DC / 16; ++ks) {
           const x8<T> vf = V_LDS ? tile_rows<T, DP>(sv + 32 * DP * wave, place, 0, ks) : v[V_LDS ? 0 : ks];
           dp = mfma32(tile_rows<T, DP>(tg, place, 0, ks), vf, dp);
         }
-        reads_ahead<DP / 16, 1, 4>();
+        reads_ahead<DC / 16, 1, 4>();
         if (!all) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) s[r] = (uint32_t)(r0 + c_row(r) - j) < reach ? s[r] : -INFINITY;
@@ -466,7 +473,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan
         for (int u = 0; u < 2; ++u) {
           const x8<T> pb = pack8<T>(p + 8 * u), db = pack8<T>(ds + 8 * u);
 #pragma unroll
-          for (int d = 0; d < DP / 32; ++d) {
+          for (int d = 0; d < DC / 32; ++d) {
             dv[d] = mfma32(tile_columns<T, DP>(tg, place, 16 * u, d), pb, dv[d]);
             dk[d] = mfma32(tile_columns<T, DP>(tq, place, 16 * u, d), db, dk[d]);
           }
@@ -480,7 +487,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan
       T* rk = at<T>(a.dk, b, j, hk);
       T* rv = at<T>(a.dv, b, j, hk);
 #pragma unroll
-      for (int d = 0; d < DP / 32; ++d) {
+      for (int d = 0; d < DC / 32; ++d) {
         store_column<T>(rk, d, dk[d], a.scale, a.dim);
         store_column<T>(rv, d, dv[d], 1.0f, a.dim);
       }
@@ -489,7 +496,7 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan
     // [item][dk, dv][row][DP]
     float* to = parts + (int64_t)id * (2 * kKeyRows * DP) + (wave * 32 + (lane & 31)) * DP;
 #pragma unroll
-    for (int d = 0; d < DP / 32; ++d)
+    for (int d = 0; d < DC / 32; ++d)
 #pragma unroll
       for (int r4 = 0; r4 < 4; ++r4) {
         const int col = d * 32 + 8 * r4 + 4 * (lane >> 5);
@@ -857,17 +864,19 @@ WindowArgs window_args(const qds_window_config* c, const int32_t* lengths) {
   return a;
 }
 
-// Calls f with the tensors' type and the padded head dimension.
+// Calls f with the tensors' type and the columns of the head that products are formed of.
+// Forward and backward, us, with products of all 64 or 128 columns | so: 10514 rows, 32 heads
+// of 80 over 8, window 3652: 2490 | 2090;  4 x 4096, 8 of 96 over 2, 2000: 558 | 480;
+// 2 x 2355, 32 of 32 over 8, 289: 132 | 96.
+template <class T, class F> void with_columns(int dim, F&& f) {
+  if (dim <= 32) f(T{}, std::integral_constant<int, 32>{});
+  else if (dim <= 64) f(T{}, std::integral_constant<int, 64>{});
+  else if (dim <= 96) f(T{}, std::integral_constant<int, 96>{});
+  else f(T{}, std::integral_constant<int, 128>{});
+}
 template <class F> void with_type(int dtype, int dim, F&& f) {
-  using D64 = std::integral_constant<int, 64>;
-  using D128 = std::integral_constant<int, 128>;
-  if (dtype == QDS_BF16) {
-    if (dim <= 64) f(bf16{}, D64{});
-    else f(bf16{}, D128{});
-  } else {
-    if (dim <= 64) f(half{}, D64{});
-    else f(half{}, D128{});
-  }
+  if (dtype == QDS_BF16) with_columns<bf16>(dim, f);
+  else with_columns<half>(dim, f);
 }
 
 KeyPlan key_plan(const qds_window_config* c) {
@@ -981,9 +990,9 @@ extern "C" qds_status qds_window_backward(const qds_window_config* c, qds_view d
   hipStream_t s = (hipStream_t)stream;
   with_type(c->dtype, c->dim, [&](auto t, auto d) {
     using T = decltype(t);
-    constexpr int DP = decltype(d)::value;
-    k_window_dq<T, DP><<<c->batch * (c->heads >> a.share) * blocks, kBlock, 0, s>>>(a, blocks);
-    k_window_dkdv<T, DP><<<lists * plan.items, kBlock, 0, s>>>(a, plan, parts);
+    constexpr int DC = decltype(d)::value, DP = padded(DC);
+    k_window_dq<T, DC><<<c->batch * (c->heads >> a.share) * blocks, kBlock, 0, s>>>(a, blocks);
+    k_window_dkdv<T, DC><<<lists * plan.items, kBlock, 0, s>>>(a, plan, parts);
     const int from = plan.first_cut > 1 ? 0 : plan.first, to = plan.band_cut > 1 ? plan.blocks : plan.first;
     if (to > from) {
       const int per_head = (to - from) * (kKeyRows / (kBlock * 4 / DP));
@@ -1021,7 +1030,7 @@ extern "C" qds_status qds_window_step(const qds_window_config* c, qds_view q, qd
   hipStream_t s = (hipStream_t)stream;
   with_type(c->dtype, c->dim, [&](auto t, auto d) {
     using T = decltype(t);
-    constexpr int DP = decltype(d)::value;
+    constexpr int DP = padded(decltype(d)::value);
     k_window_step<T, DP><<<dim3(c->batch * c->kv_heads * p.tiles, p.cut), kBlock, 0, s>>>(a);
     if (p.cut > 1) k_window_step_join<T, DP><<<c->batch * c->heads, 64 * kStepJoinWaves, 0, s>>>(a);
   });

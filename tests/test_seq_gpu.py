@@ -324,6 +324,14 @@ def test_window_heads_and_dims(d, hq, hkv, dtype):
     check_window(*qkv(2, 150, hq, hkv, d, dtype), 40, 5)
 
 
+@pytest.mark.parametrize("d", [16, 24, 56, 88, 96, 104, 120])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_window_widths_around_a_step(d, dtype):
+    """Products are formed of 32, 64, 96 or 128 columns, whichever hold the head."""
+    check_window(*qkv(2, 140, 4, 2, d, dtype), 45, 3)
+    check_window(*qkv(1, 700, 2, 1, d, dtype, "odd"), 700, 0, torch.tensor([650], dtype=torch.int32, device="cuda"))
+
+
 @pytest.mark.parametrize("hq,hkv", [(4, 1), (6, 1), (6, 2), (12, 3), (8, 1), (16, 2)])
 @pytest.mark.parametrize("d", [64, 128])
 def test_window_head_groups(hq, hkv, d):
