@@ -300,28 +300,58 @@ __global__ __launch_bounds__(kDecayBlock<DV>, 2) void k_decay_chunks(DecayArgs a
   }
 }
 
-// From each segment's own sum to the state before it; one element of M per thread.
-// 17 us for 16 heads of 128 x 128 in 32 segments.
-template <int DK, int DV> __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a) {
+// From each segment's own sum to the state before it.  A thread has one element of M and
+// one of PARTS parts of the segments: it adds their sums, the parts' sums give where each
+// part starts, and it goes through its segments again from there (one part starts at
+// once).  All sums are in a fixed order.
+// Eight parts where there are more than 64 segments: a thread's chain of 505 took 63 of
+// 106 us (129161 rows, one head of 64 x 128), in parts the call takes 76; 64 segments of
+// 8 heads of 128 x 128 take 57 in one part, 61 in eight.
+template <int DK, int DV, int PARTS> __global__ __launch_bounds__(256) void k_decay_scan(DecayArgs a) {
+  constexpr int M = DK * DV, ELEMENTS = 256 / PARTS, BLOCKS = M / ELEMENTS, AHEAD = 8;
+  __shared__ float sums[PARTS][ELEMENTS];
   const Role& role = a.role[blockIdx.z];
-  const int64_t list = blockIdx.x / (DK * DV / 256);
-  const int e = blockIdx.x % (DK * DV / 256) * 256 + threadIdx.x, row = e / DV, col = e % DV;
+  const int64_t list = blockIdx.x / BLOCKS;
+  const int part = threadIdx.x / ELEMENTS, lane = threadIdx.x % ELEMENTS;
+  const int e = blockIdx.x % BLOCKS * ELEMENTS + lane, row = e / DV, col = e % DV;
   const int b = (int)(list / a.heads), h = (int)(list % a.heads);
   const int n = rows_of(a, b);
   const float lambda = decay_rate(a.log_decay, h);
   const bool real = row < a.dim_x && col < a.dim_z;
   const int64_t outer = list * a.dim_x * a.dim_z + (role.swapped ? col * a.dim_x + row : row * a.dim_z + col);
   float m = role.init && real ? role.init_factor * role.init[outer] : 0.0f;
-  float* p = role.states + list * a.segments * (DK * DV) + e;
-#pragma unroll 4
-  for (int s = 0; s < a.segments; ++s, p += DK * DV) {
-    const int count = max(0, min(n - s * a.segment_rows, a.segment_rows));
-    const int less = role.reversed && s == 0 && count > 0 ? 1 : 0;
-    const float own = *p;
-    *p = m;
-    m = fmaf(m, decay_power(lambda, count - less), own);
+  const int per = (a.segments + PARTS - 1) / PARTS;
+  // rows of segments s .. s + many - 1; one less where the first of reversed rows is among them
+  auto fade = [&](int s, int many) {
+    const int64_t left = (int64_t)n - (int64_t)s * a.segment_rows, all = (int64_t)many * a.segment_rows;
+    const int count = left <= 0 ? 0 : (int)(left < all ? left : all);
+    return decay_power(lambda, count - (role.reversed && s == 0 && count > 0 ? 1 : 0));
+  };
+  const int first = min(part * per, a.segments), end = min(first + per, a.segments);
+  float* p = role.states + (list * a.segments) * M + e;
+  if constexpr (PARTS > 1) {
+    float sum = 0.0f;
+#pragma unroll 8
+    for (int s = first; s < end; ++s) sum = fmaf(sum, fade(s, 1), p[(int64_t)s * M]);
+    sums[part][lane] = sum;
+    __syncthreads();
+    for (int q = 0; q < part; ++q) {
+      const int from = min(q * per, a.segments);
+      m = fmaf(m, fade(from, min(from + per, a.segments) - from), sums[q][lane]);
+    }
   }
-  if (role.last && real)
+  for (int s0 = first; s0 < end; s0 += AHEAD) {
+    float own[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) own[i] = s0 + i < end ? p[(int64_t)(s0 + i) * M] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (s0 + i >= end) break;
+      p[(int64_t)(s0 + i) * M] = m;
+      m = fmaf(m, fade(s0 + i, 1), own[i]);
+    }
+  }
+  if (role.last && real && part == PARTS - 1)
     role.last[outer] = m * role.last_factor * (role.reversed && n > 0 ? decay_power(lambda, 1) : 1.0f);
 }
 
@@ -432,7 +462,10 @@ template <class T, int DK, int DV> void run_roles(const DecayArgs& a, int roles,
   const uint32_t lists = (uint32_t)a.batch * a.heads;
   if (a.segments > 1) {
     k_decay_chunks<T, DK, DV, false><<<dim3(lists, a.segments, roles), kDecayBlock<DV>, 0, s>>>(a);
-    k_decay_scan<DK, DV><<<dim3(lists * (DK * DV / 256), 1, roles), 256, 0, s>>>(a);
+    if (a.segments <= 64)
+      k_decay_scan<DK, DV, 1><<<dim3(lists * (DK * DV / 256), 1, roles), 256, 0, s>>>(a);
+    else
+      k_decay_scan<DK, DV, 8><<<dim3(lists * (DK * DV / 32), 1, roles), 256, 0, s>>>(a);
   }
   k_decay_chunks<T, DK, DV, true><<<dim3(lists, a.segments, roles), kDecayBlock<DV>, 0, s>>>(a);
 }

@@ -633,6 +633,14 @@ def test_decay_ragged():
     check_decay(4, 900, 1, 64, 128, BF16, lengths=lengths)
 
 
+@pytest.mark.parametrize("t,dk,dv,dtype", [(8192, 64, 64, BF16), (8193, 64, 64, BF16), (8704, 40, 72, F16), (9001, 128, 64, BF16)])
+def test_decay_many_segments(t, dk, dv, dtype):
+    """64 segments, one more, and numbers of them that eight parts do not share evenly."""
+    check_decay(1, t, 1, dk, dv, dtype, torch.tensor([math.log(0.9999)], device="cuda"))
+    lengths = torch.tensor([t - 200], dtype=torch.int32, device="cuda")
+    check_decay(1, t, 1, dk, dv, dtype, torch.tensor([math.log(0.99)], device="cuda"), lengths=lengths, with_dstate=False)
+
+
 @pytest.mark.parametrize("t,dk,dv", [(512, 64, 64), (513, 64, 64), (256, 128, 64), (257, 64, 128), (700, 128, 128)])
 def test_decay_ragged_segments(t, dk, dv):
     """Around the rows from which sequences are cut: episodes that end before, at and
