@@ -112,8 +112,8 @@ template <int DV> constexpr int kDecayBlock = 2 * DV * kShare<DV>;
 // OUT false a segment only forms its own sum, k_decay_scan turns the sums into the
 // states before the segments, and a second launch with OUT true starts from those.
 // Few heads are bound by their chunks' sequence: 32 x 1000 rows, 8 heads of 64 take 38 us
-// forward and 71 us back.  131072 rows, 16 heads of 128, in segments: 273 us for the
-// sums, 561 us for the outputs, at 3.9 and 3.8 TB/s.
+// forward and 71 us back.  131072 rows, 16 heads of 128, in segments: 273 to
+// 293 us for the sums, 561 to 589 us for the outputs, at 3.7 to 3.9 TB/s.
 template <class T, int DK, int DV, bool OUT>
 __global__ __launch_bounds__(kDecayBlock<DV>, 2) void k_decay_chunks(DecayArgs a) {
   constexpr int SHARE = kShare<DV>, BLOCK = kDecayBlock<DV>, WAVES = BLOCK / 64, SLICES = DV / 32;
