@@ -898,6 +898,7 @@ KeyPlan key_plan(const qds_window_config* c) {
   int64_t piece = ceil_div(total, kFill);
   if (piece < 16) piece = 16;
   if (piece > band * group) piece = band * group;
+  if (piece < 1) piece = 1;                                                           // no rows: nothing to cut
   p.first_cut = (int32_t)ceil_div(all * group, piece);
   p.band_cut = (int32_t)ceil_div(band * group, piece);
   p.items = p.first * p.first_cut + (p.blocks - p.first) * p.band_cut;

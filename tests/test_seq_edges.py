@@ -1,0 +1,82 @@
+"""libqdseq.so on the CPU: empty calls, the sizes that it accepts, and the
+scratch memory and work items that it plans."""
+import ctypes as C
+import os
+import subprocess
+import sys
+
+import pytest
+
+from paper_2202_01258_amd import seq as S
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P = 1 << 20                                       # a pointer that nothing may follow
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(S.LIB_PATH):
+        pytest.skip("libqdseq.so not built")
+    return S.lib()
+
+
+def view(p=P, strides=(8, 8, 8)):
+    return S.QdsView(p, *strides)
+
+
+def norm(**over):
+    f = dict(abi_version=S.ABI_VERSION, dtype=S.BF16, weight_dtype=S.BF16, width=128, rows=4, eps=1e-6, group=0)
+    f.update(over)
+    return S.QdsNormConfig(*[f[n] for n, _ in S.QdsNormConfig._fields_])
+
+
+def window(**over):
+    f = dict(abi_version=S.ABI_VERSION, dtype=S.BF16, batch=2, length=100, heads=4, kv_heads=2, dim=64,
+             window=10, sinks=1, scale=0.125)
+    f.update(over)
+    return S.QdsWindowConfig(*[f[n] for n, _ in S.QdsWindowConfig._fields_])
+
+
+def decay(**over):
+    f = dict(abi_version=S.ABI_VERSION, dtype=S.BF16, batch=2, length=100, heads=4, dim_k=64, dim_v=64, scale=0.125)
+    f.update(over)
+    return S.QdsDecayConfig(*[f[n] for n, _ in S.QdsDecayConfig._fields_])
+
+
+def bytes_of(fn, cfg):
+    n = C.c_uint64()
+    return fn(C.byref(cfg), C.byref(n)), n.value
+
+
+# -- no rows, no batch: every query answers, and a call without outputs launches nothing.
+# In a process of its own, as a fault here would end the test runner.
+EMPTY = """
+import sys
+sys.path[:0] = [{root!r}, {tests!r}]
+import ctypes as C
+from paper_2202_01258_amd import seq as S
+import test_seq_edges as T
+lib, none = S.lib(), T.view(None)
+for over in (dict(length=0), dict(batch=0), dict(length=0, sinks=0), dict(length=0, window=1 << 20, sinks=1 << 20)):
+    st, need = T.bytes_of(lib.qds_window_backward_workspace, T.window(**over))
+    assert (st, need) == (S.OK, 0), (over, st, need)
+    assert T.bytes_of(lib.qds_window_step_workspace, T.window(**over))[0] == S.OK
+    c = T.window(**over)
+    assert lib.qds_window_forward(C.byref(c), none, none, none, None, none, None, None) == S.OK
+    assert lib.qds_window_backward(C.byref(c), *[none] * 5, None, None, *[none] * 3, None, 0, None) == S.OK
+    assert lib.qds_window_cache_fill(C.byref(c), none, none, None, None, None, None) == S.OK
+for over in (dict(length=0), dict(batch=0)):
+    for query in (lib.qds_decay_forward_workspace, lib.qds_decay_backward_workspace):
+        assert T.bytes_of(query, T.decay(**over)) == (S.OK, 0)
+c = T.decay(batch=0)
+assert lib.qds_decay_forward(C.byref(c), none, none, none, None, None, None, none, None, None, 0, None) == S.OK
+assert lib.qds_decay_backward(C.byref(c), *[none] * 4, None, None, None, None, *[none] * 3, None, None, 0, None) == S.OK
+assert T.bytes_of(lib.qds_residual_norm_backward_workspace, T.norm(rows=0))[0] == S.OK
+print("all answered")
+"""
+
+
+def test_empty_calls(lib):
+    done = subprocess.run([sys.executable, "-c", EMPTY.format(root=ROOT, tests=os.path.join(ROOT, "tests"))],
+                          capture_output=True, text=True)
+    assert done.returncode == 0 and "all answered" in done.stdout, (done.returncode, done.stderr)
