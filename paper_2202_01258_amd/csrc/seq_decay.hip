@@ -93,10 +93,24 @@ template <int N> struct State {
 };
 
 // How many numbers of 16 bits carry an fp32 one: the state is fp32, so its
-// summands a^(63-j) y_j z_j keep 24 bits (y is exact; z a^(63-j) is split).
+// summands a^(63-j) y_j z_j keep 24 bits in bfloat16, 22 in float16 (y is exact;
+// z a^(63-j) is split).
 template <class T> struct Terms;
 template <> struct Terms<bf16> { static constexpr int n = 3; };
 template <> struct Terms<half> { static constexpr int n = 2; };
+
+// float16 ends at 65504 and in steps of 2^-24.  What it carries for an fp32 sum is first
+// brought to its upper end by a power of two, `up`, that takes the largest of the numbers
+// that share it to 2^14 .. 2^15; `down` = 1 / up takes the products back.  Numbers below 2^-29 of
+// that largest keep fewer bits, those below 2^-40 none.  bfloat16 has fp32's range.
+template <class T> constexpr bool kScaled = std::is_same<T, half>::value;
+struct Power {
+  float up, down;
+};
+__device__ inline Power to_upper_end(float largest) {
+  const uint32_t e = min(max(__float_as_uint(largest) >> 23, 15u), 254u);      // both powers are normal numbers
+  return {__uint_as_float((268 - e) << 23), __uint_as_float((e - 14) << 23)};
+}
 
 // Waves per 32 columns of the state.  With 128 columns four waves have a column
 // block each, with all rows.  With 64 columns two waves share a block: each holds
@@ -259,25 +273,64 @@ __global__ __launch_bounds__(kDecayBlock<DV>, 2) void k_decay_chunks(DecayArgs a
       const float age = decay_power(lambda, count - less);
 #pragma unroll
       for (int t = 0; t < OWN; ++t) st.m[t] *= age;
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        x8<T> term[Terms<T>::n];
+      // z a^(63-j) of a lane's 8 rows in step ks
+      auto summand = [&](int ks, float* v) {
         const int j = 16 * ks + 8 * (lane >> 5);
         const f32x4 w0 = *reinterpret_cast<const f32x4*>(s_age + j), w1 = *reinterpret_cast<const f32x4*>(s_age + j + 4);
-        float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = (float)z[ks][e] * (e < 4 ? w0[e & 3] : w1[e & 3]);
+      };
+      auto split = [&](x8<T>* term, float* v) {
 #pragma unroll
         for (int p = 0; p < Terms<T>::n; ++p) {
           term[p] = pack8<T>(v);
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] -= (float)term[p][e];
         }
+      };
+      if constexpr (kScaled<T>) {
+        // a power of two for each of the state's columns, which is a column of z: in the lane and lane ^ 32
+        float top = 0.0f, v[8];
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          summand(ks, v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
+        }
+        const Power power = to_upper_end(max_halves(top));
+        x8<T> term[4][Terms<T>::n];
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          summand(ks, v);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] *= power.up;
+          split(term[ks], v);
+        }
 #pragma unroll
         for (int t = 0; t < OWN; ++t) {
-          const x8<T> y = tile_columns_straight<T, DK>(sy, at_k.ordered, 16 * ks, st.first + t);
+          f32x16 sum = f32x16{};
 #pragma unroll
-          for (int p = Terms<T>::n - 1; p >= 0; --p) st.m[t] = mfma32(y, term[p], st.m[t]);
+          for (int ks = 0; ks < 4; ++ks) {
+            const x8<T> y = tile_columns_straight<T, DK>(sy, at_k.ordered, 16 * ks, st.first + t);
+#pragma unroll
+            for (int p = Terms<T>::n - 1; p >= 0; --p) sum = mfma32(y, term[ks][p], sum);
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) st.m[t][r] = fmaf(sum[r], power.down, st.m[t][r]);
+        }
+      } else {
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          x8<T> term[Terms<T>::n];
+          float v[8];
+          summand(ks, v);
+          split(term, v);
+#pragma unroll
+          for (int t = 0; t < OWN; ++t) {
+            const x8<T> y = tile_columns_straight<T, DK>(sy, at_k.ordered, 16 * ks, st.first + t);
+#pragma unroll
+            for (int p = Terms<T>::n - 1; p >= 0; --p) st.m[t] = mfma32(y, term[p], st.m[t]);
+          }
         }
       }
       __syncthreads();

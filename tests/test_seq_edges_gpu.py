@@ -41,3 +41,56 @@ def test_training_on_nothing(b, t):
     y, h = S.residual_norm(x, None, w)
     (y.sum() + h.sum()).backward()
     assert x.grad.shape == x.shape and (w.grad == 0).all()
+
+
+# ---------------------------------------------------------------------------
+# Decay attention in float16: values far from 1
+# ---------------------------------------------------------------------------
+def check_half_decay(b, t, h, dk, dv, log_decay, lengths=None, scale=None, q=1.0, k=1.0, v=1.0, g=1.0, state=None, dstate=None,
+                     only=("o", "state", "dq", "dk", "dv", "dstate")):
+    """Inputs of the given magnitudes.  States keep fp32's accuracy at any of them.  In the
+    other results products of rows and the state are rounded relative to their own size
+    (a power of two brings each column's or row's largest to float16's upper end), so
+    float16's smallest step counts once, where the result itself is rounded."""
+    Q, K = (rand(b, t, h, dk, dtype=F16, seed=t + i, scale=x) for i, x in enumerate((q, k)))
+    V, G = (rand(b, t, h, dv, dtype=F16, seed=t + 2 + i, scale=x) for i, x in enumerate((v, g)))
+    s0, d0 = ((None if x is None else rand(b, h, dk, dv, seed=5 + i, scale=x)) for i, x in enumerate((state, dstate)))
+    log_decay = torch.tensor(log_decay, device="cuda")
+    o, last = S.decay_attention_forward(Q, K, V, log_decay, s0, lengths, scale)
+    grads = S.decay_attention_backward(G, Q, K, V, log_decay, s0, d0, lengths, scale)
+    got = dict(zip(("o", "state", "dq", "dk", "dv", "dstate"), (o, last) + grads))
+    u = U[F16]
+    for i in range(b):
+        n = t if lengths is None else int(lengths[i])
+        one = lambda x: None if x is None else x[i:i + 1]  # noqa: E731
+        want = decay_exact(Q[i:i + 1, :n], K[i:i + 1, :n], V[i:i + 1, :n], log_decay, one(s0), G[i:i + 1, :n], one(d0), scale)
+        for name in only:
+            (x, size), y = want[name], got[name][i:i + 1]
+            if name in ("state", "dstate"):
+                within(y, x, SINGLE * size, name)
+            else:
+                assert n == 0 or float(x.abs().amax()) < 60000, f"{name}: the case is beyond float16"
+                within(y[:, :n], x, u * x.abs() + (u + SINGLE) * size + TINY[F16], name)
+
+
+HALF_DIMS = [(64, 64), (128, 128), (64, 128), (128, 64), (40, 72)]
+
+
+@pytest.mark.parametrize("dk,dv", HALF_DIMS)
+@pytest.mark.parametrize("small", [2.0 ** -10, 2.0 ** -16])
+def test_half_decay_sums_of_small_values(dk, dv, small):
+    """Values and gradients as small as training has them: the states that they are summed into are fp32."""
+    sums = ("state", "dstate")
+    check_half_decay(2, 200, 2, dk, dv, [-0.1, -0.002], v=small, g=small, only=sums)
+    check_half_decay(1, 1100, 1, dk, dv, [-0.002], v=small, g=small, state=small, dstate=small, only=sums)
+
+
+def test_half_decay_small_columns_beside_large():
+    """A column of small values keeps its accuracy beside columns of large ones."""
+    q, k, v = (rand(1, 150, 1, 64, dtype=F16, seed=i) for i in range(3))
+    v = (v.float() * 2.0 ** -torch.arange(0, 16, 0.25, device="cuda")).to(F16)
+    ld = torch.tensor([-0.02], device="cuda")
+    o, last = S.decay_attention_forward(q, k, v, ld)
+    want = decay_exact(q, k, v, ld, None)
+    within(last, want["state"][0], SINGLE * want["state"][1], "state")
+    within(o, want["o"][0], U[F16] * want["o"][0].abs() + (U[F16] + SINGLE) * want["o"][1] + TINY[F16], "o")
