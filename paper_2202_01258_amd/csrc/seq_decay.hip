@@ -100,17 +100,16 @@ template <> struct Terms<bf16> { static constexpr int n = 3; };
 template <> struct Terms<half> { static constexpr int n = 2; };
 
 // float16 ends at 65504 and in steps of 2^-24.  What it carries for an fp32 sum is first
-// brought to its upper end by a power of two, `up`, that takes the largest of the numbers
-// that share it to 2^14 .. 2^15; `down` = 1 / up takes the products back.  Numbers below 2^-29 of
+// brought to its upper end by a power of two that takes the largest of the numbers that
+// share it to 2^14 .. 2^15; its inverse takes the products back.  Numbers below 2^-29 of
 // that largest keep fewer bits, those below 2^-40 none.  bfloat16 has fp32's range.
+// LEAST bounds the power to 2^(141 - LEAST).
 template <class T> constexpr bool kScaled = std::is_same<T, half>::value;
-struct Power {
-  float up, down;
-};
-__device__ inline Power to_upper_end(float largest) {
-  const uint32_t e = min(max(__float_as_uint(largest) >> 23, 15u), 254u);      // both powers are normal numbers
-  return {__uint_as_float((268 - e) << 23), __uint_as_float((e - 14) << 23)};
+template <uint32_t LEAST = 15> __device__ inline float to_upper_end(float largest) {
+  const uint32_t e = min(max(__float_as_uint(largest) >> 23, LEAST), 254u);      // the power and its inverse are normal numbers
+  return __uint_as_float((268 - e) << 23);
 }
+__device__ inline float inverse(float power) { return __uint_as_float(0x7f000000u - __float_as_uint(power)); }
 
 // Waves per 32 columns of the state.  With 128 columns four waves have a column
 // block each, with all rows.  With 64 columns two waves share a block: each holds
@@ -126,16 +125,19 @@ template <int DV> constexpr int kDecayBlock = 2 * DV * kShare<DV>;
 // OUT false a segment only forms its own sum, k_decay_scan turns the sums into the
 // states before the segments, and a second launch with OUT true starts from those.
 // Few heads are bound by their chunks' sequence: 32 x 1000 rows, 8 heads of 64 take 38 us
-// forward and 71 us back.  131072 rows, 16 heads of 128, in segments: 273 to
+// forward and 71 us back (float16, with its powers of two, 49 and 84; 47 and 97 with two
+// waves on a SIMD in place of three).  131072 rows, 16 heads of 128, in segments: 273 to
 // 293 us for the sums, 561 to 589 us for the outputs, at 3.7 to 3.9 TB/s.
 template <class T, int DK, int DV, bool OUT>
-__global__ __launch_bounds__(kDecayBlock<DV>, 2) void k_decay_chunks(DecayArgs a) {
+__global__ __launch_bounds__(kDecayBlock<DV>, kScaled<T> && DK + DV <= kEarly ? 3 : 2) void k_decay_chunks(DecayArgs a) {
   constexpr int SHARE = kShare<DV>, BLOCK = kDecayBlock<DV>, WAVES = BLOCK / 64, SLICES = DV / 32;
   constexpr int TILES = DK / 32, OWN = TILES / SHARE;
   SEQ_SHARED T sx[OUT ? kChunk * DK : 8], sy[kChunk * DK], sz[kChunk * DV];
   SEQ_SHARED T sp[OUT ? kChunk * kChunk : 8];
   SEQ_SHARED T sm[OUT && SHARE == 2 ? WAVES * OWN * 2 * 64 * 8 : 8];
   SEQ_SHARED float s_age[kChunk];            // a^(rows - 1 - j) of the chunk's rows
+  // what takes products with the state back (each share's columns), and the powers of products of rows (each row's halves)
+  SEQ_SHARED float s_state[OUT && kScaled<T> ? SHARE * DV : 4], s_rows[OUT && kScaled<T> ? 2 * kChunk : 4];
   const Role& role = a.role[blockIdx.z];
   const int lane = threadIdx.x & 63, wave = wave_index();
   const int slice = wave % SLICES, part = wave / SLICES;
@@ -191,16 +193,28 @@ __global__ __launch_bounds__(kDecayBlock<DV>, 2) void k_decay_chunks(DecayArgs a
       if (threadIdx.x < kChunk)
         s_age[threadIdx.x] = (int)threadIdx.x < count ? decay_power(lambda, count - 1 - threadIdx.x) : 0.0f;
       // The products of rows and the state are rounded to the tensors' type for the
-      // output's products: as much as the output's own rounding.
+      // output's products: as much as the output's own rounding.  Float16 also brings each
+      // column of the state, and each row of a quarter of the products of rows, to its
+      // upper end: states grow beyond 65504 and gradients are small where outputs are neither.
       x8<T> packed[OUT ? OWN : 1][2];
       if constexpr (OUT) {
+        float up = 1.0f;
+        if constexpr (kScaled<T>) {
+          float top = 0.0f;
+#pragma unroll
+          for (int t = 0; t < OWN; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(st.m[t][r]));
+          up = to_upper_end(max_halves(top));
+          if (lane < 32) s_state[part * DV + col] = inverse(up);
+        }
 #pragma unroll
         for (int t = 0; t < OWN; ++t)
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             float m[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) m[e] = st.m[t][8 * u + e];
+            for (int e = 0; e < 8; ++e) m[e] = kScaled<T> ? st.m[t][8 * u + e] * up : st.m[t][8 * u + e];
             packed[t][u] = pack8<T>(m);
             if (SHARE == 2)
               *reinterpret_cast<x8<T>*>(sm + (((wave * OWN + t) * 2 + u) * 64 + lane) * 8) = packed[t][u];
@@ -218,11 +232,23 @@ __global__ __launch_bounds__(kDecayBlock<DV>, 2) void k_decay_chunks(DecayArgs a
             s = mfma32(tile_rows<T, DK>(sy, at_k, jb * 32, ks), tile_rows<T, DK>(sx, at_k, ib * 32, ks), s);
           const int i = ib * 32 + (lane & 31);
 #pragma unroll
+          for (int r = 0; r < 16; ++r) s[r] *= fade[r];
+          if constexpr (kScaled<T>) {
+            // up to 2^40: below that, products are nothing in a float16 output, and the output in
+            // fp32 is multiplied with the power, too
+            float top = 0.0f;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(s[r]));
+            const float up = to_upper_end<101>(max_halves(top));
+            if (lane < 32) s_rows[jb * kChunk + i] = up;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] *= up;
+          }
+#pragma unroll
           for (int r4 = 0; r4 < 4; ++r4) {
             const int j = jb * 32 + 8 * r4 + 4 * (lane >> 5);
-            const float* f = fade + 4 * r4;
-            *reinterpret_cast<u32x2*>(sp + tile_at<64>(i, j >> 3) + (j & 7)) = __builtin_bit_cast(
-                u32x2, pack4<T>(s[4 * r4] * f[0], s[4 * r4 + 1] * f[1], s[4 * r4 + 2] * f[2], s[4 * r4 + 3] * f[3]));
+            *reinterpret_cast<u32x2*>(sp + tile_at<64>(i, j >> 3) + (j & 7)) =
+                __builtin_bit_cast(u32x2, pack4<T>(s[4 * r4], s[4 * r4 + 1], s[4 * r4 + 2], s[4 * r4 + 3]));
           }
         }
         __syncthreads();
@@ -231,27 +257,54 @@ __global__ __launch_bounds__(kDecayBlock<DV>, 2) void k_decay_chunks(DecayArgs a
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) z[ks] = tile_columns_straight<T, DV>(sz, at_v.straight, 16 * ks, slice);
       if constexpr (OUT) {
+        auto state_of = [&](int t, int u) {
+          if (SHARE == 1) return packed[t % OWN][u];
+          const int holder = slice + SLICES * (t / OWN);
+          return *reinterpret_cast<const x8<T>*>(sm + (((holder * OWN + t % OWN) * 2 + u) * 64 + lane) * 8);
+        };
         auto output = [&](int ib) {
-          f32x16 o = f32x16{};
-#pragma unroll
-          for (int t = 0; t < TILES; ++t)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              x8<T> m;
-              if (SHARE == 1) {
-                m = packed[t % OWN][u];
-              } else {
-                // the halves in one order for both waves, so that sums do not depend on the wave
-                const int holder = slice + SLICES * (t / OWN);
-                m = *reinterpret_cast<const x8<T>*>(sm + (((holder * OWN + t % OWN) * 2 + u) * 64 + lane) * 8);
-              }
-              o = mfma32(m, tile_rows<T, DK>(sx, at_k, ib * 32, 2 * t + u), o);
-            }
           const int i = ib * 32 + (lane & 31);
-          o *= role.factor * decay_power(lambda, i + 1 - less);
+          const float reach = role.factor * decay_power(lambda, i + 1 - less);
+          f32x16 o = f32x16{};
+          if constexpr (kScaled<T>) {
+            // Each share and each half has powers of its own.
 #pragma unroll
-          for (int ks = 0; ks < 4; ++ks)
-            if (ks < 2 * (ib + 1)) o = mfma32(z[ks], tile_rows<T, 64>(sp, at_p, ib * 32, ks), o);
+            for (int q = 0; q < SHARE; ++q) {
+              f32x16 sum = f32x16{};
+#pragma unroll
+              for (int t = q * OWN; t < (q + 1) * OWN; ++t)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) sum = mfma32(state_of(t, u), tile_rows<T, DK>(sx, at_k, ib * 32, 2 * t + u), sum);
+#pragma unroll
+              for (int r4 = 0; r4 < 4; ++r4) {
+                const f32x4 down = *reinterpret_cast<const f32x4*>(s_state + q * DV + slice * 32 + 8 * r4 + 4 * (lane >> 5));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                  const float part_sum = sum[4 * r4 + e] * (down[e] * reach);
+                  o[4 * r4 + e] = q == 0 ? part_sum : o[4 * r4 + e] + part_sum;
+                }
+              }
+            }
+#pragma unroll
+            for (int jb = 0; jb < 2; ++jb) {
+              if (jb > ib) break;
+              const float up = s_rows[jb * kChunk + i];
+              o *= up;
+#pragma unroll
+              for (int ks = 2 * jb; ks < 2 * jb + 2; ++ks) o = mfma32(z[ks], tile_rows<T, 64>(sp, at_p, ib * 32, ks), o);
+              o *= inverse(up);
+            }
+          } else {
+            // the halves in one order for both waves, so that sums do not depend on the wave
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+#pragma unroll
+              for (int u = 0; u < 2; ++u) o = mfma32(state_of(t, u), tile_rows<T, DK>(sx, at_k, ib * 32, 2 * t + u), o);
+            o *= reach;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+              if (ks < 2 * (ib + 1)) o = mfma32(z[ks], tile_rows<T, 64>(sp, at_p, ib * 32, ks), o);
+          }
           if (i < count) {
             const int64_t row = turn + sign * (row0 + i);
             store_column<T>(at<T>(role.out, b, row, h), slice, o, 1.0f, a.dim_z);
@@ -261,6 +314,7 @@ __global__ __launch_bounds__(kDecayBlock<DV>, 2) void k_decay_chunks(DecayArgs a
           output(part);
         } else {
           output(0);
+          if (kScaled<T>) __builtin_amdgcn_sched_barrier(0);       // both at once would not fit the registers
           output(1);
         }
       }
@@ -297,13 +351,13 @@ __global__ __launch_bounds__(kDecayBlock<DV>, 2) void k_decay_chunks(DecayArgs a
 #pragma unroll
           for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(v[e]));
         }
-        const Power power = to_upper_end(max_halves(top));
+        const float up = to_upper_end(max_halves(top)), down = inverse(up);
         x8<T> term[4][Terms<T>::n];
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks) {
           summand(ks, v);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] *= power.up;
+          for (int e = 0; e < 8; ++e) v[e] *= up;
           split(term[ks], v);
         }
 #pragma unroll
@@ -316,7 +370,7 @@ __global__ __launch_bounds__(kDecayBlock<DV>, 2) void k_decay_chunks(DecayArgs a
             for (int p = Terms<T>::n - 1; p >= 0; --p) sum = mfma32(y, term[ks][p], sum);
           }
 #pragma unroll
-          for (int r = 0; r < 16; ++r) st.m[t][r] = fmaf(sum[r], power.down, st.m[t][r]);
+          for (int r = 0; r < 16; ++r) st.m[t][r] = fmaf(sum[r], down, st.m[t][r]);
         }
       } else {
 #pragma unroll

@@ -94,3 +94,69 @@ def test_half_decay_small_columns_beside_large():
     want = decay_exact(q, k, v, ld, None)
     within(last, want["state"][0], SINGLE * want["state"][1], "state")
     within(o, want["o"][0], U[F16] * want["o"][0].abs() + (U[F16] + SINGLE) * want["o"][1] + TINY[F16], "o")
+
+
+@pytest.mark.parametrize("dk,dv", HALF_DIMS)
+@pytest.mark.parametrize("small", [2.0 ** -10, 2.0 ** -16])
+def test_half_decay_small_values(dk, dv, small):
+    """Values and gradients as small as training has them, also in what is not a sum."""
+    check_half_decay(2, 200, 2, dk, dv, [-0.1, -0.002], v=small, g=small)
+    check_half_decay(2, 130, 2, dk, dv, [-0.1, -0.002], v=small, g=small, state=small, dstate=small)
+
+
+def test_half_decay_small_values_in_segments():
+    check_half_decay(1, 1100, 2, 64, 64, [-0.05, -0.001], v=2.0 ** -14, g=2.0 ** -14)
+    check_half_decay(1, 1100, 1, 128, 128, [-0.001], k=2.0 ** -12, g=2.0 ** -14)
+    lengths = torch.tensor([700, 0, 129, 1], dtype=torch.int32, device="cuda")
+    check_half_decay(4, 700, 1, 64, 128, [-0.01], lengths=lengths, v=2.0 ** -14, g=2.0 ** -14)
+
+
+@pytest.mark.parametrize("dk,dv", HALF_DIMS)
+@pytest.mark.parametrize("log_decay", [[0.0, 0.0], [-0.01, -0.5]])
+def test_half_decay_large_states(dk, dv, log_decay):
+    """States beyond float16's range in front of and behind the rows; their products with small rows are within it."""
+    small = 2.0 ** -7
+    check_half_decay(2, 130, 2, dk, dv, log_decay, q=small, k=small, v=small, g=small, state=1e5, dstate=1e5)
+    check_half_decay(1, 700, 2, dk, dv, log_decay, q=small, k=small, v=small, g=small, state=3e5)
+
+
+def test_half_decay_large_state_of_unread_rows():
+    """A state's entry that no row reads leaves the outputs as they are, however large it is."""
+    q, k, v = (rand(2, 100, 2, 64, dtype=F16, seed=i) for i in range(3))
+    q[..., 5] = 0
+    ld = torch.tensor([0.0, -0.1], device="cuda")
+    s = rand(2, 2, 64, 64, seed=4)
+    want = decay_exact(q, k, v, ld, torch.where(torch.arange(64, device="cuda")[:, None] == 5, 0.0, s))["o"]
+    for large in (1e5, 1e30):
+        s[:, :, 5, 9] = large
+        o, last = S.decay_attention_forward(q, k, v, ld, s)
+        bound = U[F16] * want[0].abs() + (U[F16] + SINGLE) * want[1] + TINY[F16]
+        # entries below 2^-39 of their column's largest may be rounded away: that column is checked where there are none
+        columns = torch.arange(64, device="cuda") != 9
+        within(o[..., columns], want[0][..., columns], bound[..., columns], "o")
+        assert o.isfinite().all()
+        if large < 1e10:
+            within(o, want[0], bound + 2.0 ** -39 * large * 64, "o with the column")
+        assert abs(float(last[0, 0, 5, 9]) / large - 1) < 0.01       # no decay in this head
+
+
+@pytest.mark.parametrize("dk,dv", HALF_DIMS)
+def test_half_decay_grown_states(dk, dv):
+    """Without a decay, large keys and values: the state passes 65504 within some rows.  (Values that are all positive.)"""
+    b, t = 1, 600
+    q = rand(b, t, 1, dk, dtype=F16, seed=1, scale=2.0 ** -9)
+    k = rand(b, t, 1, dk, dtype=F16, seed=2).abs() * 16
+    v = rand(b, t, 1, dv, dtype=F16, seed=3).abs() * 64
+    ld = torch.zeros(1, device="cuda")
+    o, last = S.decay_attention_forward(q, k, v, ld)
+    want = decay_exact(q, k, v, ld, None)
+    assert float(want["state"][0].abs().amax()) > 2e5 and float(want["o"][0].abs().amax()) < 60000
+    within(last, want["state"][0], SINGLE * want["state"][1], "state")
+    within(o, want["o"][0], U[F16] * want["o"][0].abs() + (U[F16] + SINGLE) * want["o"][1] + TINY[F16], "o")
+
+
+@pytest.mark.parametrize("dk,dv", HALF_DIMS)
+def test_half_decay_large_and_small_products_of_rows(dk, dv):
+    """Products of two rows beyond 65504, and below float16's smallest step."""
+    check_half_decay(2, 130, 2, dk, dv, [-0.3, -0.01], scale=1.0, q=50.0, k=50.0, v=2.0 ** -9, g=2.0 ** -9)
+    check_half_decay(2, 130, 2, dk, dv, [-0.3, -0.01], q=2.0 ** -14, k=2.0 ** -8, v=500.0, g=2.0 ** -6)
