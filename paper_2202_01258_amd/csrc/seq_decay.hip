@@ -3,13 +3,13 @@
 // include/qd_seq.h.
 //
 // One recurrence serves every direction.  With rows x, y of DK and z of DV elements,
-//   M_i = a M_{i-1} + y_i^T z_i,   out_i = factor x_i M_i:
-//   o:  (x, y, z) = (q, k, v),   M the state S;
-//   dq: (do, v, k),              M = S^T;
-//   dv: (k, q, do), rows reversed, M = R = sum a^(t-s) q_t^T do_t + the state's gradient;
-//   dk: (v, do, q), rows reversed, M = R^T.
+//   M_i = a M_{i-1} + f y_i^T z_i,   out_i = g x_i M_i:
+//   o:  (x, y, z) = (q, k, v),   M the state S,                  f = 1, g = scale;
+//   dq: (do, v, k),              M = S^T,                        f = 1, g = scale;
+//   dv: (k, q, do), rows reversed, M = R = scale sum a^(t-s) q_t^T do_t + the state's gradient, f = scale, g = 1;
+//   dk: (v, do, q), rows reversed, M = R^T,                      f = scale, g = 1.
 // A chunk of 64 rows is
-//   out = ((x y^T) . a^(i-j) [j <= i]) z + a^(i+1) x M,   M <- a^64 M + (a^(63-j) y)^T z,
+//   out = f g ((x y^T) . a^(i-j) [j <= i]) z + g a^(i+1) x M,   M <- a^64 M + f y^T (a^(63-j) z),
 // all products on the matrix cores, the state in registers.  By its bytes (each
 // row read and written once) the recurrence is bound by memory.
 #include "seq_common.hpp"
@@ -31,8 +31,7 @@ struct Role {
   const float* init;     // the state before the first row [b][h][dim_k][dim_v] of the caller's sides, or null
   float* last;           // the state after the last row, or null
   float* states;         // [b][h][segment][DK][DV]: each segment's own sum, then the state before it
-  float factor;          // of the outputs
-  float init_factor, last_factor;
+  float sums, outputs;   // the factors f of what is summed and g of the outputs
   bool reversed;         // rows from the last to the first
   bool swapped;          // init and last are [dim_z][dim_x] (the transpose of M)
 };
@@ -67,7 +66,7 @@ template <int N> struct State {
   }
   // Buffer loads, all under way at once: an element outside is read as 0, without a branch
   // (with one, each load was waited for by itself).
-  __device__ void load(const float* p, int rows, int cols, int col, bool swapped, float factor) {
+  __device__ void load(const float* p, int rows, int cols, int col, bool swapped) {
     const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, kBufferSize, kBufferFlags);
     const uint32_t step = swapped ? 4 : 4 * cols, base = swapped ? col * 4 * rows : col * 4;
 #pragma unroll
@@ -78,8 +77,6 @@ template <int N> struct State {
         const uint32_t at = row < rows && col < cols ? base + row * step : kOutside;
         m[t][i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer, at, 0, 0));
       }
-#pragma unroll
-    for (int t = 0; t < N; ++t) m[t] *= factor;
   }
   __device__ void store(float* p, int rows, int cols, int col, bool swapped, float factor) const {
 #pragma unroll
@@ -93,8 +90,8 @@ template <int N> struct State {
 };
 
 // How many numbers of 16 bits carry an fp32 one: the state is fp32, so its
-// summands a^(63-j) y_j z_j keep 24 bits in bfloat16, 22 in float16 (y is exact;
-// z a^(63-j) is split).
+// summands f a^(63-j) y_j z_j keep 24 bits in bfloat16, 22 in float16 (y is exact;
+// f z a^(63-j) is split).
 template <class T> struct Terms;
 template <> struct Terms<bf16> { static constexpr int n = 3; };
 template <> struct Terms<half> { static constexpr int n = 2; };
@@ -135,7 +132,7 @@ __global__ __launch_bounds__(kDecayBlock<DV>, kScaled<T> && DK + DV <= kEarly ? 
   SEQ_SHARED T sx[OUT ? kChunk * DK : 8], sy[kChunk * DK], sz[kChunk * DV];
   SEQ_SHARED T sp[OUT ? kChunk * kChunk : 8];
   SEQ_SHARED T sm[OUT && SHARE == 2 ? WAVES * OWN * 2 * 64 * 8 : 8];
-  SEQ_SHARED float s_age[kChunk];            // a^(rows - 1 - j) of the chunk's rows
+  SEQ_SHARED float s_age[kChunk];            // f a^(rows - 1 - j) of the chunk's rows
   // what takes products with the state back (each share's columns), and the powers of products of rows (each row's halves)
   SEQ_SHARED float s_state[OUT && kScaled<T> ? SHARE * DV : 4], s_rows[OUT && kScaled<T> ? 2 * kChunk : 4];
   const Role& role = a.role[blockIdx.z];
@@ -156,9 +153,9 @@ __global__ __launch_bounds__(kDecayBlock<DV>, kScaled<T> && DK + DV <= kEarly ? 
   st.first = part * OWN;
   float* mine = role.states + (list * a.segments + blockIdx.y) * (DK * DV);
   if (OUT && a.segments > 1)
-    st.load(mine, DK, DV, col, false, 1.0f);
+    st.load(mine, DK, DV, col, false);
   else if (OUT && role.init)
-    st.load(role.init + list * a.dim_x * a.dim_z, a.dim_x, a.dim_z, col, role.swapped, role.init_factor);
+    st.load(role.init + list * a.dim_x * a.dim_z, a.dim_x, a.dim_z, col, role.swapped);
   else
     st.zero();
 
@@ -168,12 +165,13 @@ __global__ __launch_bounds__(kDecayBlock<DV>, kScaled<T> && DK + DV <= kEarly ? 
     if (OUT) rx.init(at<T>(role.x, b, turn, h), sign * role.x.t, a.dim_x);
     ry.init(at<T>(role.y, b, turn, h), sign * role.y.t, a.dim_x);
     rz.init(at<T>(role.z, b, turn, h), sign * role.z.t, a.dim_z);
-    // factor a^(i-j) of a wave's products of rows, 0 for j > i: the same in every chunk
+    // f g a^(i-j) of a wave's products of rows, 0 for j > i: the same in every chunk
+    const float both = role.sums * role.outputs;
     float fade[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int gap = (wave == 1 ? 32 : 0) + (lane & 31) - c_row(r);
-      fade[r] = gap >= 0 ? role.factor * decay_power(lambda, gap) : 0.0f;
+      fade[r] = gap >= 0 ? both * decay_power(lambda, gap) : 0.0f;
     }
     auto fetch = [&](int row0) {
       if (row0 >= end) return;
@@ -191,7 +189,7 @@ __global__ __launch_bounds__(kDecayBlock<DV>, kScaled<T> && DK + DV <= kEarly ? 
       ry.store(sy);
       rz.store(sz);
       if (threadIdx.x < kChunk)
-        s_age[threadIdx.x] = (int)threadIdx.x < count ? decay_power(lambda, count - 1 - threadIdx.x) : 0.0f;
+        s_age[threadIdx.x] = (int)threadIdx.x < count ? role.sums * decay_power(lambda, count - 1 - threadIdx.x) : 0.0f;
       // The products of rows and the state are rounded to the tensors' type for the
       // output's products: as much as the output's own rounding.  Float16 also brings each
       // column of the state, and each row of a quarter of the products of rows, to its
@@ -264,7 +262,7 @@ __global__ __launch_bounds__(kDecayBlock<DV>, kScaled<T> && DK + DV <= kEarly ? 
         };
         auto output = [&](int ib) {
           const int i = ib * 32 + (lane & 31);
-          const float reach = role.factor * decay_power(lambda, i + 1 - less);
+          const float reach = role.outputs * decay_power(lambda, i + 1 - less);
           f32x16 o = f32x16{};
           if constexpr (kScaled<T>) {
             // Each share and each half has powers of its own.
@@ -327,7 +325,7 @@ __global__ __launch_bounds__(kDecayBlock<DV>, kScaled<T> && DK + DV <= kEarly ? 
       const float age = decay_power(lambda, count - less);
 #pragma unroll
       for (int t = 0; t < OWN; ++t) st.m[t] *= age;
-      // z a^(63-j) of a lane's 8 rows in step ks
+      // f z a^(63-j) of a lane's 8 rows in step ks
       auto summand = [&](int ks, float* v) {
         const int j = 16 * ks + 8 * (lane >> 5);
         const f32x4 w0 = *reinterpret_cast<const f32x4*>(s_age + j), w1 = *reinterpret_cast<const f32x4*>(s_age + j + 4);
@@ -395,7 +393,7 @@ __global__ __launch_bounds__(kDecayBlock<DV>, kScaled<T> && DK + DV <= kEarly ? 
     return;
   }
   if (a.segments == 1 && role.last) {
-    const float f = role.last_factor * (role.reversed && n > 0 ? decay_power(lambda, 1) : 1.0f);
+    const float f = role.reversed && n > 0 ? decay_power(lambda, 1) : 1.0f;
     st.store(role.last + list * a.dim_x * a.dim_z, a.dim_x, a.dim_z, col, role.swapped, f);
   }
   // rows past the end
@@ -426,7 +424,7 @@ template <int DK, int DV, int PARTS> __global__ __launch_bounds__(256) void k_de
   const float lambda = decay_rate(a.log_decay, h);
   const bool real = row < a.dim_x && col < a.dim_z;
   const int64_t outer = list * a.dim_x * a.dim_z + (role.swapped ? col * a.dim_x + row : row * a.dim_z + col);
-  float m = role.init && real ? role.init_factor * role.init[outer] : 0.0f;
+  float m = role.init && real ? role.init[outer] : 0.0f;
   const int per = (a.segments + PARTS - 1) / PARTS;
   // rows of segments s .. s + many - 1; one less where the first of reversed rows is among them
   auto fade = [&](int s, int many) {
@@ -459,7 +457,7 @@ template <int DK, int DV, int PARTS> __global__ __launch_bounds__(256) void k_de
     }
   }
   if (role.last && real && part == PARTS - 1)
-    role.last[outer] = m * role.last_factor * (role.reversed && n > 0 ? decay_power(lambda, 1) : 1.0f);
+    role.last[outer] = m * (role.reversed && n > 0 ? decay_power(lambda, 1) : 1.0f);
 }
 
 // ---------------------------------------------------------------------------
@@ -629,7 +627,7 @@ extern "C" qds_status qds_decay_forward(const qds_decay_config* c, qds_view q, q
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
   if (c->length > 0 && (!near_rows(q) || !near_rows(k) || !near_rows(v))) return QDS_ERR_UNSUPPORTED;
   DecayArgs a = decay_args(c, segment_plan(c, 1), lengths, log_decay);
-  a.role[0] = Role{view(q), view(k), view(v), view(o), state_in, state_out, (float*)workspace, c->scale, 1.0f, 1.0f, false, false};
+  a.role[0] = Role{view(q), view(k), view(v), view(o), state_in, state_out, (float*)workspace, 1.0f, c->scale, false, false};
   run(c, a, 1, stream);
   return launch_status();
 }
@@ -661,11 +659,9 @@ extern "C" qds_status qds_decay_backward(const qds_decay_config* c, qds_view dou
   const SegmentPlan p = segment_plan(c, 3);
   const uint64_t each = state_bytes(c, p.segments) / sizeof(float);
   float* ws = (float*)workspace;
-  // R is formed without the scale; the state's gradient enters it divided by the scale.
-  const float back = 1.0f / c->scale;
-  const Role rq{view(dout), view(v), view(k), view(dq), state_in, nullptr, ws, c->scale, 1.0f, 1.0f, false, true};
-  const Role rk{view(v), view(dout), view(q), view(dk), dstate_out, nullptr, ws + each, c->scale, back, 1.0f, true, true};
-  const Role rv{view(k), view(q), view(dout), view(dv), dstate_out, dstate_in, ws + 2 * each, c->scale, back, c->scale, true, false};
+  const Role rq{view(dout), view(v), view(k), view(dq), state_in, nullptr, ws, 1.0f, c->scale, false, true};
+  const Role rk{view(v), view(dout), view(q), view(dk), dstate_out, nullptr, ws + each, c->scale, 1.0f, true, true};
+  const Role rv{view(k), view(q), view(dout), view(dv), dstate_out, dstate_in, ws + 2 * each, c->scale, 1.0f, true, false};
   DecayArgs a = decay_args(c, p, lengths, log_decay);
   if (c->dim_k == c->dim_v) {
     a.role[0] = rq, a.role[1] = rk, a.role[2] = rv;

@@ -160,3 +160,20 @@ def test_half_decay_large_and_small_products_of_rows(dk, dv):
     """Products of two rows beyond 65504, and below float16's smallest step."""
     check_half_decay(2, 130, 2, dk, dv, [-0.3, -0.01], scale=1.0, q=50.0, k=50.0, v=2.0 ** -9, g=2.0 ** -9)
     check_half_decay(2, 130, 2, dk, dv, [-0.3, -0.01], q=2.0 ** -14, k=2.0 ** -8, v=500.0, g=2.0 ** -6)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_decay_small_scale(dtype):
+    """A scale so small that a state's gradient divided by it has no fp32 number."""
+    scale = 2.0 ** -20
+    q, k, v, g = (rand(1, 90, 2, 64, dtype=dtype, seed=i) for i in range(4))
+    ld = torch.tensor([-0.1, 0.0], device="cuda")
+    dstate = rand(1, 2, 64, 64, seed=6, scale=2.0 ** 112)
+    k[:], v[:] = k * 2.0 ** -10, v * 2.0 ** -10
+    got = S.decay_attention_backward(g, q, k, v, ld, None, dstate, scale=scale)
+    want = decay_exact(q, k, v, ld, None, g, dstate, scale)
+    within(got[3], want["dstate"][0], SINGLE * want["dstate"][1], "dstate")
+    if dtype == BF16:
+        for name, x in zip(("dk", "dv"), got[1:3]):
+            y, size = want[name]
+            within(x, y, U[dtype] * y.abs() + (U[dtype] + SINGLE) * size, name)
