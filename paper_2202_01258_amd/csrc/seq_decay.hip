@@ -21,9 +21,13 @@ constexpr int kChunk = 64;
 constexpr int kEarly = 128;
 
 // a^n for lambda = log2(a).  `lambda` is kept finite (decay_rate), so that a^0 is 1
-// for a = 0, too; below the bound a^1 is 0 already.
+// for a = 0, too; below the bound a^1 is 0 already.  Not-a-number stays (fmaxf would
+// make it the bound).
 __device__ inline float decay_power(float lambda, float n) { return fast_exp2(lambda * n); }
-__device__ inline float decay_rate(const float* log_decay, int h) { return fmaxf(log_decay[h] * kLog2e, -1.0e4f); }
+__device__ inline float decay_rate(const float* log_decay, int h) {
+  const float lambda = log_decay[h] * kLog2e;
+  return lambda < -1.0e4f ? -1.0e4f : lambda;
+}
 
 // One direction of the recurrence.
 struct Role {

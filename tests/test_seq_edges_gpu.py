@@ -177,3 +177,25 @@ def test_decay_small_scale(dtype):
         for name, x in zip(("dk", "dv"), got[1:3]):
             y, size = want[name]
             within(x, y, U[dtype] * y.abs() + (U[dtype] + SINGLE) * size, name)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("t", [5, 700])
+def test_decay_that_is_not_a_number(dtype, t):
+    """A head whose decay is not-a-number gives not-a-number; the others do not see it."""
+    q, k, v = (rand(1, t, 3, 64, dtype=dtype, seed=i) for i in range(3))
+    good, bad = torch.tensor([-0.1, -0.2, -0.3], device="cuda"), torch.tensor([-0.1, math.nan, -0.3], device="cuda")
+    s = rand(1, 3, 64, 64, seed=4)
+    want = S.decay_attention_forward(q, k, v, good, s) + S.decay_attention_backward(v, q, k, v, good, s, s)
+    got = S.decay_attention_forward(q, k, v, bad, s) + S.decay_attention_backward(v, q, k, v, bad, s, s)
+    for i, (x, y) in enumerate(zip(got, want)):
+        x, y = (z if z.shape == s.shape else z.transpose(1, 2) for z in (x, y))
+        assert torch.equal(x[:, ::2], y[:, ::2]), i
+        if i not in (3, 4):          # dk and dv of the last row meet no decay
+            assert x[:, 1].isnan().all(), i
+        else:
+            assert x[:, 1, :-1].isnan().all(), i
+    o, last = S.decay_attention_step(q[:, 0], k[:, 0], v[:, 0], bad, s.clone())
+    o2, last2 = S.decay_attention_step(q[:, 0], k[:, 0], v[:, 0], good, s.clone())
+    assert o[:, 1].isnan().all() and last[:, 1].isnan().all()
+    assert torch.equal(o[:, ::2], o2[:, ::2]) and torch.equal(last[:, ::2], last2[:, ::2])
