@@ -290,6 +290,10 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 constexpr int kFill = 512;       // workgroups that fill the card: two per compute unit
 
+// A launch has fewer than 2^32 threads in a dimension: HIP takes a larger grid without an
+// error and leaves workgroups out.
+constexpr uint32_t most_blocks(int threads) { return 0xffffffffu / (uint32_t)threads; }
+
 inline qds_status launch_status() {
   return hipGetLastError() == hipSuccess ? QDS_OK : QDS_ERR_HIP;
 }

@@ -5,6 +5,8 @@
 // forward and again backward, against some ten operations.  A row is read once
 // and stays in registers between its sum and its use: one wave holds a row of up
 // to 64 lanes * 32 elements, four waves one of up to four times that.
+#include <algorithm>
+
 #include "seq_common.hpp"
 
 namespace seq {
@@ -112,6 +114,7 @@ struct ForwardArgs {
   int32_t width;
   float eps;
   bool w32;
+  int64_t first;    // the launch's first row
 };
 
 enum { kPlain = 0, kFp8Row = 1, kFp8Group = 2 };
@@ -125,7 +128,7 @@ __global__ __launch_bounds__(kBlock) void k_norm(ForwardArgs a) {
   __shared__ float part[8];
   constexpr int ROWS = kBlock / TPR;
   const int lane = threadIdx.x % TPR;
-  const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+  const int64_t row = a.first + (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
   if (TPR <= 64 && row >= a.rows) return;      // no barrier below for rows that waves hold
   const T* x = (const T*)a.x + row * a.x_stride;
   const T* r = a.r ? (const T*)a.r + row * a.r_stride : nullptr;
@@ -213,7 +216,7 @@ __global__ __launch_bounds__(kBlock) void k_norm(ForwardArgs a) {
 template <class T, int MODE>
 __global__ __launch_bounds__(kBlock) void k_norm_any(ForwardArgs a) {
   __shared__ float part[8];
-  const int64_t row = blockIdx.x;
+  const int64_t row = a.first + blockIdx.x;
   const T* x = (const T*)a.x + row * a.x_stride;
   const T* r = a.r ? (const T*)a.r + row * a.r_stride : nullptr;
   auto at = [&](int c) { return to_f32(x[c]) + (r ? to_f32(r[c]) : 0.0f); };
@@ -456,16 +459,28 @@ template <class T, class F> bool with_shape(int width, F&& f) {
   return width % (16 / sizeof(T)) ? with_lanes<T, true>(width, f) : with_lanes<T, false>(width, f);
 }
 
-template <class T, int MODE> void forward(const ForwardArgs& a, hipStream_t s) {
-  const bool held = with_shape<T>(a.width, [&](auto V, auto NV, auto TPR, auto TAIL) {
+// One launch for as many rows as one takes workgroups for, another for what is left.
+template <class F> void over_rows(ForwardArgs a, int rows_per_block, F&& launch) {
+  const int64_t step = (int64_t)most_blocks(kBlock) * rows_per_block;
+  for (a.first = 0; a.first < a.rows; a.first += step)
+    launch(a, (uint32_t)ceil_div(std::min(a.rows - a.first, step), rows_per_block));
+}
+
+template <class T, int MODE> void forward(const ForwardArgs& args, hipStream_t s) {
+  auto any = [&] {
+    over_rows(args, 1, [&](const ForwardArgs& a, uint32_t grid) { k_norm_any<T, MODE><<<grid, kBlock, 0, s>>>(a); });
+  };
+  const bool held = with_shape<T>(args.width, [&](auto V, auto NV, auto TPR, auto TAIL) {
     constexpr int v = decltype(V)::value, nv = decltype(NV)::value, tpr = decltype(TPR)::value;
     constexpr bool tail = decltype(TAIL)::value;
     if constexpr (MODE != kFp8Group || (tpr >= 128 / v && !tail))
-      k_norm<T, v, nv, tpr, tail, MODE><<<ceil_div(a.rows, kBlock / tpr), kBlock, 0, s>>>(a);
+      over_rows(args, kBlock / tpr, [&](const ForwardArgs& a, uint32_t grid) {
+        k_norm<T, v, nv, tpr, tail, MODE><<<grid, kBlock, 0, s>>>(a);
+      });
     else
-      k_norm_any<T, MODE><<<a.rows, kBlock, 0, s>>>(a);
+      any();
   });
-  if (!held) k_norm_any<T, MODE><<<a.rows, kBlock, 0, s>>>(a);
+  if (!held) any();
 }
 
 template <int MODE> qds_status run_forward(const qds_norm_config* c, const ForwardArgs& a, void* stream) {
@@ -512,7 +527,7 @@ extern "C" qds_status qds_residual_norm(const qds_norm_config* c, const void* x,
   if (c->group != 0) return QDS_ERR_INVALID_ARG;
   if (c->rows > 0 && (!x || !weight || !y || !h || !rstd)) return QDS_ERR_INVALID_ARG;
   const ForwardArgs a{x, residual, weight, y, h, rstd, x_stride, residual_stride, c->rows,
-                      c->width, c->eps, c->weight_dtype == QDS_F32};
+                      c->width, c->eps, c->weight_dtype == QDS_F32, 0};
   return run_forward<kPlain>(c, a, stream);
 }
 
@@ -524,7 +539,7 @@ extern "C" qds_status qds_residual_norm_fp8(const qds_norm_config* c, const void
   if (st != QDS_OK) return st;
   if (c->rows > 0 && (!x || !weight || !q || !scale || !h)) return QDS_ERR_INVALID_ARG;
   const ForwardArgs a{x, residual, weight, q, h, scale, x_stride, residual_stride, c->rows,
-                      c->width, c->eps, c->weight_dtype == QDS_F32};
+                      c->width, c->eps, c->weight_dtype == QDS_F32, 0};
   return c->group ? run_forward<kFp8Group>(c, a, stream) : run_forward<kFp8Row>(c, a, stream);
 }
 

@@ -199,3 +199,35 @@ def test_decay_that_is_not_a_number(dtype, t):
     o2, last2 = S.decay_attention_step(q[:, 0], k[:, 0], v[:, 0], good, s.clone())
     assert o[:, 1].isnan().all() and last[:, 1].isnan().all()
     assert torch.equal(o[:, ::2], o2[:, ::2]) and torch.equal(last[:, ::2], last2[:, ::2])
+
+
+# ---------------------------------------------------------------------------
+# Very many rows
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,width,dtype", [((1 << 24) + 3, 4, BF16), ((1 << 24) + 3, 1, F32), ((1 << 28) + 5, 8, BF16)])
+def test_norm_of_very_many_rows(rows, width, dtype):
+    """More rows than one launch has workgroups of."""
+    pattern = rand(4099, width, dtype=dtype, seed=1)          # a prime: pieces of a grid do not repeat it
+    x = pattern.repeat((rows + 4098) // 4099, 1)[:rows]
+    w = (1 + 0.2 * rand(width, seed=2))
+    at = torch.cat([torch.arange(3000), torch.arange(1 << 24, (1 << 24) + 3), torch.arange(rows - 3000, rows)]).cuda()
+    few = x[at]
+    y, h, rstd = S.residual_norm_forward(x, None, w)
+    for a, b in zip((y, h, rstd), S.residual_norm_forward(few, None, w)):
+        assert torch.equal(a[at], b)
+    ey = norm_exact(few, None, w)[2]
+    within(y[at], ey, (U[dtype] + SINGLE) * ey.abs(), "y")
+    del y
+    q, scale, _ = S.residual_norm_fp8(x, None, w)
+    q2, scale2, _ = S.residual_norm_fp8(few, None, w)
+    assert torch.equal(q[at].view(torch.uint8), q2.view(torch.uint8)) and torch.equal(scale[at], scale2)
+    del q, scale
+    dx, dw = S.residual_norm_backward(x, None, h, rstd, w)
+    dx2, _ = S.residual_norm_backward(few, None, h[at], rstd[at], w)
+    assert torch.equal(dx[at], dx2)
+    n = rstd[:, None].double()
+    step, want = 1 << 22, torch.zeros(width, dtype=torch.float64, device="cuda")
+    for i in range(0, rows, step):
+        want += (x[i:i + step].double() * h[i:i + step].double() * n[i:i + step]).sum(0)
+    # all terms are positive here; a thread adds up to rows / (512 * its share) of them in fp32
+    within(dw, want, (SINGLE + rows / 512 * 2.0 ** -24) * want, "dweight")
