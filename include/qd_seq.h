@@ -46,7 +46,8 @@ typedef enum {
   QDS_OK = 0,
   QDS_ERR_INVALID_ARG = 1,          /* bad config field, null or misaligned pointer */
   QDS_ERR_WORKSPACE_TOO_SMALL = 2,  /* workspace shorter than needed                */
-  QDS_ERR_UNSUPPORTED = 4,          /* valid but not built (e.g. head dimension)    */
+  QDS_ERR_UNSUPPORTED = 4,          /* valid but not built (e.g. head dimension), or */
+                                    /*   a launch of 2^32 threads or more            */
   QDS_ERR_HIP = 5                   /* a HIP runtime or launch error                */
 } qds_status;
 

@@ -532,7 +532,7 @@ qds_status validate(const qds_decay_config* c) {
   if (c->dim_k < 1 || c->dim_v < 1) return QDS_ERR_INVALID_ARG;
   if (c->dim_k % 8 || c->dim_v % 8 || c->dim_k > 128 || c->dim_v > 128) return QDS_ERR_UNSUPPORTED;
   if (!(c->scale > 0.0f) || c->scale > 3.0e38f) return QDS_ERR_INVALID_ARG;
-  if ((int64_t)c->batch * c->heads > (1 << 24)) return QDS_ERR_UNSUPPORTED;
+  if ((int64_t)c->batch * c->heads > most_blocks(256)) return QDS_ERR_UNSUPPORTED;      // workgroups of 256 threads
   return QDS_OK;
 }
 

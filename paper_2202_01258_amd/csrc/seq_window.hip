@@ -807,10 +807,7 @@ qds_status validate(const qds_window_config* c) {
   if (c->window < 1 || c->sinks < 0 || (int64_t)c->window + c->sinks >= (1 << 30) || c->length >= (1 << 30))
     return QDS_ERR_INVALID_ARG;
   if (!(c->scale > 0.0f) || c->scale > 3.0e38f) return QDS_ERR_INVALID_ARG;
-  // the kernels' grids and their item numbers stay below 2^31
-  if ((int64_t)c->batch * c->heads > (1 << 24) ||
-      (int64_t)c->batch * c->heads * (ceil_div(c->length, 64) + 1) > (1ll << 30))
-    return QDS_ERR_UNSUPPORTED;
+  if ((int64_t)c->batch * c->heads > most_blocks(kBlock)) return QDS_ERR_UNSUPPORTED;      // the step's grid
   return QDS_OK;
 }
 
@@ -846,6 +843,12 @@ bool spread(const qds_window_config* c, const int32_t* lengths) {
 int shared_heads(const qds_window_config* c) {
   const int group = c->heads / c->kv_heads;
   return group % 4 == 0 ? 2 : group % 2 == 0 ? 1 : 0;
+}
+
+// Workgroups of the kernels over queries.
+int64_t query_grid(const qds_window_config* c) {
+  const int share = shared_heads(c);
+  return (int64_t)c->batch * (c->heads >> share) * ceil_div(c->length, kForwardRows >> share);
 }
 
 WindowArgs window_args(const qds_window_config* c, const int32_t* lengths) {
@@ -944,12 +947,13 @@ extern "C" qds_status qds_window_forward(const qds_window_config* c, qds_view q,
   const qds_status st = validate(c);
   if (st != QDS_OK) return st;
   if (c->batch == 0 || c->length == 0) return QDS_OK;
+  if (query_grid(c) > most_blocks(kBlock)) return QDS_ERR_UNSUPPORTED;
   if (!usable(q) || !usable(k) || !usable(v) || !usable(o) || !lse) return QDS_ERR_INVALID_ARG;
   if (!near_rows(k) || !near_rows(v)) return QDS_ERR_UNSUPPORTED;
   WindowArgs a = window_args(c, lengths);
   a.q = view(q), a.k = view(k), a.v = view(v), a.o = view(o), a.lse = lse;
   const int blocks = (int)ceil_div(c->length, kForwardRows >> a.share);
-  const int grid = c->batch * (c->heads >> a.share) * blocks;
+  const uint32_t grid = (uint32_t)query_grid(c);
   with_type(c->dtype, c->dim, [&](auto t, auto d) {
     k_window_forward<decltype(t), decltype(d)::value><<<grid, kBlock, 0, (hipStream_t)stream>>>(a, blocks);
   });
@@ -960,8 +964,14 @@ extern "C" qds_status qds_window_backward_workspace(const qds_window_config* c, 
   const qds_status st = validate(c);
   if (st != QDS_OK) return st;
   if (!bytes) return QDS_ERR_INVALID_ARG;
+  const KeyPlan p = key_plan(c);
+  const int64_t lists = (int64_t)c->batch * c->kv_heads;
+  const int64_t joined = (p.first_cut > 1 ? p.first : 0) + (p.band_cut > 1 ? p.blocks - p.first : 0);
+  if (query_grid(c) > most_blocks(kBlock) || lists * p.items > most_blocks(kBlock) ||
+      lists * joined * (kKeyRows / 8) > most_blocks(kBlock))         // the join: 8 rows or more a workgroup
+    return QDS_ERR_UNSUPPORTED;
   const uint64_t delta = align_up((uint64_t)c->batch * c->heads * c->length * sizeof(float));
-  *bytes = delta + align_up(key_parts(c, key_plan(c)));
+  *bytes = delta + align_up(key_parts(c, p));
   return QDS_OK;
 }
 
@@ -987,12 +997,11 @@ extern "C" qds_status qds_window_backward(const qds_window_config* c, qds_view d
   const KeyPlan plan = key_plan(c);
   const int blocks = (int)ceil_div(c->length, kForwardRows >> a.share);
   const int lists = c->batch * c->kv_heads;
-  if ((int64_t)lists * plan.items > 0x7fffffff) return QDS_ERR_UNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
   with_type(c->dtype, c->dim, [&](auto t, auto d) {
     using T = decltype(t);
     constexpr int DC = decltype(d)::value, DP = padded(DC);
-    k_window_dq<T, DC><<<c->batch * (c->heads >> a.share) * blocks, kBlock, 0, s>>>(a, blocks);
+    k_window_dq<T, DC><<<(uint32_t)query_grid(c), kBlock, 0, s>>>(a, blocks);
     k_window_dkdv<T, DC><<<lists * plan.items, kBlock, 0, s>>>(a, plan, parts);
     const int from = plan.first_cut > 1 ? 0 : plan.first, to = plan.band_cut > 1 ? plan.blocks : plan.first;
     if (to > from) {

@@ -80,3 +80,43 @@ def test_empty_calls(lib):
     done = subprocess.run([sys.executable, "-c", EMPTY.format(root=ROOT, tests=os.path.join(ROOT, "tests"))],
                           capture_output=True, text=True)
     assert done.returncode == 0 and "all answered" in done.stdout, (done.returncode, done.stderr)
+
+
+# -- a launch has fewer than 2^32 threads in a dimension; HIP takes more without an error
+# and leaves workgroups out, so that outputs would stay unwritten
+def window_calls(lib, c):
+    v = view()
+    return {"forward": lib.qds_window_forward(C.byref(c), v, v, v, None, v, P, None),
+            "backward": lib.qds_window_backward(C.byref(c), *[v] * 5, P, None, *[v] * 3, P, 1 << 62, None),
+            "query": bytes_of(lib.qds_window_backward_workspace, c)[0]}
+
+
+@pytest.mark.parametrize("over", [
+    dict(batch=16, heads=4, kv_heads=1, length=1 << 25), dict(batch=1 << 12, heads=1, kv_heads=1, length=1 << 19),
+    dict(batch=1 << 24, heads=1, kv_heads=1, length=1), dict(batch=1 << 11, heads=2, kv_heads=1, length=1 << 19, dim=128)])
+def test_window_refuses_more_work_than_a_launch_takes(lib, over):
+    assert set(window_calls(lib, window(**over)).values()) == {S.ERR_UNSUPPORTED}
+
+
+@pytest.mark.parametrize("over", [
+    dict(batch=16, heads=4, kv_heads=1, length=(1 << 25) - 32), dict(batch=(1 << 12) - 1, heads=1, kv_heads=1, length=1 << 19, sinks=0),
+    dict(batch=(1 << 24) - 1, heads=1, kv_heads=1, length=1, sinks=0)])
+def test_window_takes_what_a_launch_takes(lib, over):
+    assert bytes_of(lib.qds_window_backward_workspace, window(**over))[0] == S.OK
+
+
+def test_steps_have_no_length(lib):
+    """The step does not use `length`, so nothing is refused for it."""
+    assert bytes_of(lib.qds_window_step_workspace, window(batch=64, length=(1 << 30) - 1))[0] == S.OK
+    for batch, status in (((1 << 24) - 1, S.OK), (1 << 24, S.ERR_UNSUPPORTED)):
+        assert bytes_of(lib.qds_window_step_workspace, window(batch=batch, heads=1, kv_heads=1))[0] == status
+
+
+def test_decay_refuses_more_work_than_a_launch_takes(lib):
+    for batch, status in (((1 << 24) - 1, S.OK), (1 << 24, S.ERR_UNSUPPORTED)):
+        c, v = decay(batch=batch, heads=1), view()
+        assert bytes_of(lib.qds_decay_forward_workspace, c)[0] == status
+        assert bytes_of(lib.qds_decay_backward_workspace, c)[0] == status
+        if status != S.OK:
+            assert lib.qds_decay_forward(C.byref(c), v, v, v, P, None, None, v, P, P, 1 << 40, None) == status
+            assert lib.qds_decay_step(C.byref(c), v, v, v, P, P, v, P, None) == status
