@@ -24,8 +24,8 @@ DEPS = SRC + [os.path.join(HERE, "csrc", f) for f in ("qd_device.hpp", "qd_kerne
 SEQ_LIB = os.path.join(HERE, "libqdseq.so")
 SEQ_SRC = [os.path.join(HERE, "csrc", f) for f in ("seq_norm.hip", "seq_window.hip",
                                                    "seq_decay.hip")]
-SEQ_DEPS = SEQ_SRC + [os.path.join(HERE, "csrc", "seq_common.hpp"),
-                      os.path.join(ROOT, "include", "qd_seq.h")]
+SEQ_DEPS = SEQ_SRC + [os.path.join(HERE, "csrc", f) for f in ("seq_common.hpp", "seq_plan.hpp")] + [
+    os.path.join(ROOT, "include", "qd_seq.h")]
 ARCH = os.environ.get("QD_OFFLOAD_ARCH", "gfx950")
 
 

@@ -17,6 +17,7 @@
 #include <cstdint>
 
 #include "../../include/qd_seq.h"
+#include "seq_plan.hpp"
 
 namespace seq {
 
@@ -288,8 +289,6 @@ __device__ inline int spread_order(int id, int count, int per_list) {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-constexpr int kFill = 512;       // workgroups that fill the card: two per compute unit
-
 // A launch has fewer than 2^32 threads in a dimension: HIP takes a larger grid without an
 // error and leaves workgroups out.
 constexpr uint32_t most_blocks(int threads) { return 0xffffffffu / (uint32_t)threads; }
@@ -298,7 +297,6 @@ inline qds_status launch_status() {
   return hipGetLastError() == hipSuccess ? QDS_OK : QDS_ERR_HIP;
 }
 
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline uint64_t align_up(uint64_t x) { return (x + 255) / 256 * 256; }
 
 }  // namespace seq

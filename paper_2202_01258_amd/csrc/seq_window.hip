@@ -328,27 +328,6 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blo
   }
 }
 
-// How the key blocks' work is cut.  A block of first tokens is seen by every
-// later row, one of the band by about window + 128 rows of each head of the
-// group: the former are cut into more pieces, so that no workgroup has far more
-// to do than the others; both into more where there are few blocks.  Pieces of
-// one block leave fp32 sums that k_window_dkdv_join adds in their order.
-constexpr int kKeyRows = 32 * kWaves;
-struct KeyPlan {
-  int32_t blocks, first;            // key blocks per key head; those that hold first tokens
-  int32_t first_cut, band_cut;      // pieces of each kind
-  int32_t items;                    // workgroups per key head
-};
-
-struct KeyItem {
-  int block, piece, cut;
-};
-__device__ inline KeyItem key_item(const KeyPlan& p, int x) {
-  if (x < p.first * p.first_cut) return {x / p.first_cut, x % p.first_cut, p.first_cut};
-  x -= p.first * p.first_cut;
-  return {p.first + x / p.band_cut, x % p.band_cut, p.band_cut};
-}
-
 // A wave has 32 keys, a unit is 32 query rows of one head.  Scores have queries as
 // rows and keys as columns of the C tile, so that both the weights and the score
 // gradients are operands of the sums over queries as they are.  Keys stay in
@@ -360,7 +339,7 @@ __device__ inline KeyItem key_item(const KeyPlan& p, int x) {
 template <class T, int DC>
 __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan plan, float* parts) {
   constexpr int DP = padded(DC);
-  constexpr int QT = 32;
+  constexpr int QT = kUnitRows;
   constexpr bool V_LDS = DP == 128;
   SEQ_SHARED T sq[2][QT * DP], sg[2][QT * DP], sv[V_LDS ? kKeyRows * DP : 8];
   SEQ_SHARED float s_lse[2][QT], s_delta[2][QT];
@@ -380,15 +359,9 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan
   f32x16 dk[DC / 32], dv[DC / 32];
 #pragma unroll
   for (int d = 0; d < DC / 32; ++d) dk[d] = dv[d] = f32x16{};
-  // the rows that see this block, in tiles of 32, for each head of the group
-  int unit = 0, stop = 0, per_head = 1;
-  if (j0 < n) {
-    const int64_t last = j0 < sinks ? n - 1 : min((int64_t)n - 1, (int64_t)j0 + kKeyRows - 1 + window - 1);
-    per_head = (int)((last - j0) / QT) + 1;
-    const int64_t units = (int64_t)per_head * group;
-    unit = (int)(units * item.piece / item.cut);
-    stop = (int)(units * (item.piece + 1) / item.cut);
-  }
+  const KeyUnits units = key_units(item, window, sinks, n, group);
+  const int per_head = units.per_head, stop = units.end;
+  int unit = units.begin;
   if (unit < stop) {
     x8<T> k[DC / 16], v[V_LDS ? 1 : DC / 16];
     load_rows<T, DC>(k, at<T>(a.k, b, j, hk), j < n, a.dim);
@@ -493,8 +466,8 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan
       }
     }
   } else {
-    // [item][dk, dv][row][DP]
-    float* to = parts + (int64_t)id * (2 * kKeyRows * DP) + (wave * 32 + (lane & 31)) * DP;
+    // [list][sum][dk, dv][row][DP]
+    float* to = parts + ((int64_t)head * plan.sums + item.sum) * (2 * kKeyRows * DP) + (wave * 32 + (lane & 31)) * DP;
 #pragma unroll
     for (int d = 0; d < DC / 32; ++d)
 #pragma unroll
@@ -515,17 +488,13 @@ __global__ __launch_bounds__(kBlock) void k_window_dkdv_join(WindowArgs a, KeyPl
   constexpr int ROWS = kBlock * 4 / DP;
   const int head = blockIdx.x / per_head, x = blockIdx.x % per_head;
   const int hk = head % a.kv_heads, b = head / a.kv_heads;
-  const int from = plan.first_cut > 1 ? 0 : plan.first;       // the cut blocks
-  const int block = from + x / (kKeyRows / ROWS);
+  const int block = cut_from(plan) + x / (kKeyRows / ROWS);
   const int row = (x % (kKeyRows / ROWS)) * ROWS + threadIdx.x / (DP / 4);
   const int col = threadIdx.x % (DP / 4) * 4;
   const int j = block * kKeyRows + row;
   if (j >= a.length || col >= a.dim) return;
-  const bool is_first = block < plan.first;
-  const int cut = is_first ? plan.first_cut : plan.band_cut;
-  const int item = is_first ? block * plan.first_cut
-                            : plan.first * plan.first_cut + (block - plan.first) * plan.band_cut;
-  const float* p = parts + ((int64_t)head * plan.items + item) * (2 * kKeyRows * DP) + row * DP + col;
+  const int cut = block < plan.first ? plan.first_cut : plan.band_cut;
+  const float* p = parts + ((int64_t)head * plan.sums + key_sums(plan, block)) * (2 * kKeyRows * DP) + row * DP + col;
   f32x4 dk = f32x4{}, dv = f32x4{};
 #pragma unroll 4
   for (int s = 0; s < cut; ++s) {
@@ -882,37 +851,6 @@ template <class F> void with_type(int dtype, int dim, F&& f) {
   else with_columns<half>(dim, f);
 }
 
-KeyPlan key_plan(const qds_window_config* c) {
-  KeyPlan p{};
-  const int64_t group = c->heads / c->kv_heads, lists = (int64_t)c->batch * c->kv_heads;
-  const int64_t sinks = c->sinks < c->length ? c->sinks : c->length;
-  p.blocks = (int32_t)ceil_div(c->length, kKeyRows);
-  p.first = (int32_t)ceil_div(sinks, kKeyRows);
-  const int64_t all = ceil_div(c->length, 32);                                        // tiles that see a first block
-  int64_t band = ceil_div((int64_t)c->window + kKeyRows, 32);                         // ... and one of the band
-  if (band > all) band = all;
-  // pieces of equal size that give about kFill workgroups, but of no less than 16 tiles
-  // (the sequence's last blocks are seen by fewer tiles, 4 more from each to the one before;
-  // counted as a whole band they left causal blocks whole, of which the first has twice the
-  // mean: 16384 rows, 16 heads of 128 over 4, whole window, forward and backward 6.6 ms; 5.1 so)
-  const int64_t bands = p.blocks - p.first, short_bands = std::min(bands, band / 4);
-  const int64_t seen = (bands - short_bands) * band + 2 * short_bands * (short_bands + 1);
-  const int64_t total = (p.first * all + seen) * group * lists;
-  int64_t piece = ceil_div(total, kFill);
-  if (piece < 16) piece = 16;
-  if (piece > band * group) piece = band * group;
-  if (piece < 1) piece = 1;                                                           // no rows: nothing to cut
-  p.first_cut = (int32_t)ceil_div(all * group, piece);
-  p.band_cut = (int32_t)ceil_div(band * group, piece);
-  p.items = p.first * p.first_cut + (p.blocks - p.first) * p.band_cut;
-  return p;
-}
-uint64_t key_parts(const qds_window_config* c, const KeyPlan& p) {
-  if (p.first_cut == 1 && p.band_cut == 1) return 0;
-  const uint64_t dp = c->dim <= 64 ? 64 : 128;
-  return (uint64_t)c->batch * c->kv_heads * p.items * 2 * kKeyRows * dp * sizeof(float);
-}
-
 struct StepPlan {
   int32_t tiles, cut, range;
 };
@@ -966,12 +904,12 @@ extern "C" qds_status qds_window_backward_workspace(const qds_window_config* c, 
   if (!bytes) return QDS_ERR_INVALID_ARG;
   const KeyPlan p = key_plan(c);
   const int64_t lists = (int64_t)c->batch * c->kv_heads;
-  const int64_t joined = (p.first_cut > 1 ? p.first : 0) + (p.band_cut > 1 ? p.blocks - p.first : 0);
+  const int64_t joined = cut_to(p) - cut_from(p);
   if (query_grid(c) > most_blocks(kBlock) || lists * p.items > most_blocks(kBlock) ||
       lists * joined * (kKeyRows / 8) > most_blocks(kBlock))         // the join: 8 rows or more a workgroup
     return QDS_ERR_UNSUPPORTED;
   const uint64_t delta = align_up((uint64_t)c->batch * c->heads * c->length * sizeof(float));
-  *bytes = delta + align_up(key_parts(c, p));
+  *bytes = delta + align_up(key_sums_bytes(c, p));
   return QDS_OK;
 }
 
@@ -1003,9 +941,8 @@ extern "C" qds_status qds_window_backward(const qds_window_config* c, qds_view d
     constexpr int DC = decltype(d)::value, DP = padded(DC);
     k_window_dq<T, DC><<<(uint32_t)query_grid(c), kBlock, 0, s>>>(a, blocks);
     k_window_dkdv<T, DC><<<lists * plan.items, kBlock, 0, s>>>(a, plan, parts);
-    const int from = plan.first_cut > 1 ? 0 : plan.first, to = plan.band_cut > 1 ? plan.blocks : plan.first;
-    if (to > from) {
-      const int per_head = (to - from) * (kKeyRows / (kBlock * 4 / DP));
+    if (cut_to(plan) > cut_from(plan)) {
+      const int per_head = (cut_to(plan) - cut_from(plan)) * (kKeyRows / (kBlock * 4 / DP));
       k_window_dkdv_join<T, DP><<<(uint32_t)lists * per_head, kBlock, 0, s>>>(a, plan, per_head, parts);
     }
   });

@@ -2,6 +2,7 @@
 scratch memory and work items that it plans."""
 import ctypes as C
 import os
+import shutil
 import subprocess
 import sys
 
@@ -120,3 +121,58 @@ def test_decay_refuses_more_work_than_a_launch_takes(lib):
         if status != S.OK:
             assert lib.qds_decay_forward(C.byref(c), v, v, v, P, None, None, v, P, P, 1 << 40, None) == status
             assert lib.qds_decay_step(C.byref(c), v, v, v, P, P, v, P, None) == status
+
+
+# -- the backward pass over keys: its work items, and the sums that cut blocks leave
+@pytest.fixture(scope="module")
+def replay(tmp_path_factory):
+    if shutil.which("g++") is None:
+        pytest.skip("g++ not available")
+    exe = tmp_path_factory.mktemp("plan") / "replay"
+    src = os.path.join(ROOT, "tests", "helpers", "seq_plan_replay.cpp")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", src, "-o", str(exe)], check=True)
+
+    def run(configs):
+        """(items, sums, first_cut, band_cut) of each (batch, length, heads, kv_heads, dim, window, sinks)."""
+        out = subprocess.run([str(exe)] + [str(x) for c in configs for x in c], capture_output=True, text=True)
+        assert out.returncode == 0, out.stdout[-400:]
+        return [tuple(map(int, line.split())) for line in out.stdout.splitlines()]
+
+    return run
+
+
+LENGTHS = [0, 1, 31, 64, 127, 128, 129, 300, 1000, 4096, 5001]
+
+
+@pytest.mark.parametrize("window", [1, 33, 250, 1024, 1 << 20])
+@pytest.mark.parametrize("sinks", [0, 1, 128, 129, 700, 1 << 20])
+def test_work_items_cover_everything_once(replay, window, sinks):
+    replay([(b, t, heads, kv, 64, window, sinks) for t in LENGTHS
+            for b, heads, kv in ((0, 1, 1), (1, 1, 1), (2, 8, 2), (3, 6, 1), (64, 16, 16), (600, 4, 4))])
+
+
+def backward_bytes(lib, c):
+    """Scratch memory beside a float per row and query head."""
+    st, need = bytes_of(lib.qds_window_backward_workspace, c)
+    assert st == S.OK
+    delta = c.batch * c.heads * c.length * 4
+    return need - (delta + 255) // 256 * 256
+
+
+def of(c):
+    return (c.batch, c.length, c.heads, c.kv_heads, c.dim, c.window, c.sinks)
+
+
+def test_scratch_memory_is_for_cut_blocks_only(lib, replay):
+    """Blocks that are not cut write their gradients themselves."""
+    wide = dict(batch=2, length=8192, heads=16, kv_heads=16, dim=128, window=1024)
+    assert backward_bytes(lib, window(**wide, sinks=0)) == 0
+    assert backward_bytes(lib, window(batch=64, length=16384, heads=8, kv_heads=8, dim=128, window=1024, sinks=0)) == 0
+    configs = [window(**wide, sinks=16), window(**wide, sinks=0), window(batch=1, length=3000, window=64, sinks=0),
+               window(batch=1, length=3000, window=64, sinks=300), window(batch=1, length=20000, window=2000, sinks=1)]
+    for c, (items, sums, first_cut, band_cut) in zip(configs, replay([of(c) for c in configs])):
+        columns = 64 if c.dim <= 64 else 128
+        want = c.batch * c.kv_heads * sums * 2 * 128 * columns * 4
+        assert backward_bytes(lib, c) == (want + 255) // 256 * 256
+        if c.sinks == 0:
+            assert first_cut == 1
