@@ -87,9 +87,15 @@ inline KeyPlan key_plan(const qds_window_config* c) {
   const int64_t total = (p.first * all + seen) * group * lists;
   int64_t piece = ceil_div(total, kFill);
   if (piece < 16) piece = 16;
-  if (piece > band * group) piece = band * group;
-  if (piece < 1) piece = 1;                                                           // no rows: nothing to cut
-  p.first_cut = p.first > 0 ? (int32_t)ceil_div(all * group, piece) : 1;
+  // A first block in pieces as long as a block of the band, which then end with the others,
+  // but of no less than a quarter of what a place on the card has to do: lists that fill the card
+  // many times over even out by themselves, as first blocks begin first.  All sums together then
+  // belong to some 8 kFill pieces at most, whatever the number of lists.  Backward, us, in pieces of
+  // the band's length | so: 64 x 4096 rows, 16 heads of 128, window 256, one first token: 5030 | 4650 (5.65 GB of
+  // sums | none);  256 x 1000, 8 heads of 64, window 64, one: 1448 | 1107;  32 x 2048, 8 heads of 64, 128,
+  // 300: 562 | 430;  64 x 4096, 8 heads of 64, 16, 4096: 16000 | 4670.
+  const int64_t first_piece = std::min(piece, std::max(band * group, piece / 4));
+  p.first_cut = p.first > 0 ? (int32_t)ceil_div(all * group, first_piece) : 1;
   p.band_cut = bands > 0 ? (int32_t)ceil_div(band * group, piece) : 1;
   p.items = (int32_t)(p.first * p.first_cut + bands * p.band_cut);
   p.sums = (p.first_cut > 1 ? p.first * p.first_cut : 0) + (p.band_cut > 1 ? (int32_t)bands * p.band_cut : 0);

@@ -2,6 +2,7 @@
 scratch memory and work items that it plans."""
 import ctypes as C
 import os
+import random
 import shutil
 import subprocess
 import sys
@@ -176,3 +177,26 @@ def test_scratch_memory_is_for_cut_blocks_only(lib, replay):
         assert backward_bytes(lib, c) == (want + 255) // 256 * 256
         if c.sinks == 0:
             assert first_cut == 1
+
+
+@pytest.mark.parametrize("shape", [
+    dict(batch=64, length=4096, heads=16, kv_heads=16, dim=128, window=256, sinks=1),
+    dict(batch=256, length=1000, heads=8, kv_heads=8, dim=64, window=64, sinks=1),
+    dict(batch=64, length=4096, heads=8, kv_heads=8, dim=64, window=16, sinks=4096)])
+def test_first_blocks_stay_whole_where_lists_fill_the_card(lib, shape):
+    assert backward_bytes(lib, window(**shape)) == 0
+
+
+def test_scratch_memory_does_not_grow_with_the_lists(replay):
+    """Pieces that leave sums: at most ten for each of the 512 places of the card.  (A first block's pieces
+    are a quarter of a place's share of the work or more, rounded down to no less than a fifth; a block is
+    cut into less than twice as many as that gives.)"""
+    rng = random.Random(5)
+    size = lambda most: int(2 ** rng.uniform(0, most))  # noqa: E731
+    configs = []
+    for _ in range(1500):
+        kv, group = rng.choice([1, 1, 2, 4, 8, 16]), rng.choice([1, 1, 2, 3, 8])
+        configs.append((size(10), size(13), kv * group, kv, 64, size(14), rng.choice([0, 1, size(14)])))
+    for i in range(0, len(configs), 300):
+        for c, (_, sums, _, _) in zip(configs[i:], replay(configs[i:i + 300])):
+            assert c[0] * c[3] * sums <= 10 * 512, c
