@@ -56,7 +56,10 @@ enum { QDS_F32 = 0, QDS_BF16 = 1, QDS_F16 = 2 };
 
 /* A tensor of rows per batch element and head: element (b, t, h, d) is
  * data[b * stride[0] + t * stride[1] + h * stride[2] + d].  Strides are in
- * elements; any sign or order, also 0. */
+ * elements; any sign or order, also 0; multiples of 8, as data is of 16 bytes.
+ * Rows that are read by tiles (keys and values, and all inputs of a backward pass
+ * or of the decay attention) are less than 2^23 elements apart; others are
+ * QDS_ERR_UNSUPPORTED. */
 typedef struct {
   void* data;
   int64_t stride[3];

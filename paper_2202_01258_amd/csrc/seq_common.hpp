@@ -146,8 +146,10 @@ inline bool usable(const qds_view& v, bool rows = true) {
   return v.data && aligned16(v.data) && v.stride[0] % 8 == 0 && v.stride[2] % 8 == 0 &&
          (!rows || v.stride[1] % 8 == 0);
 }
-// Tiles of 64 rows are addressed with 31 bits from their first row.
-inline bool near_rows(const qds_view& v) {
+// Tiles of 64 rows are addressed with 31 bits from their first row.  A single row's stride
+// means nothing; it is set to 0.
+inline bool near_rows(qds_view& v, int length) {
+  if (length < 2) v.stride[1] = 0;
   return v.stride[1] < (1 << 23) && v.stride[1] > -(1 << 23);
 }
 

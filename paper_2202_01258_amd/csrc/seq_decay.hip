@@ -629,7 +629,7 @@ extern "C" qds_status qds_decay_forward(const qds_decay_config* c, qds_view q, q
   if (c->length > 0 && (!usable(q) || !usable(k) || !usable(v) || !usable(o))) return QDS_ERR_INVALID_ARG;
   if (need && (!workspace || ((uintptr_t)workspace & 255))) return QDS_ERR_INVALID_ARG;
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
-  if (c->length > 0 && (!near_rows(q) || !near_rows(k) || !near_rows(v))) return QDS_ERR_UNSUPPORTED;
+  if (c->length > 0 && (!near_rows(q, c->length) || !near_rows(k, c->length) || !near_rows(v, c->length))) return QDS_ERR_UNSUPPORTED;
   DecayArgs a = decay_args(c, segment_plan(c, 1), lengths, log_decay);
   a.role[0] = Role{view(q), view(k), view(v), view(o), state_in, state_out, (float*)workspace, 1.0f, c->scale, false, false};
   run(c, a, 1, stream);
@@ -659,7 +659,7 @@ extern "C" qds_status qds_decay_backward(const qds_decay_config* c, qds_view dou
     return QDS_ERR_INVALID_ARG;
   if (need && (!workspace || ((uintptr_t)workspace & 255))) return QDS_ERR_INVALID_ARG;
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
-  if (c->length > 0 && (!near_rows(dout) || !near_rows(q) || !near_rows(k) || !near_rows(v))) return QDS_ERR_UNSUPPORTED;
+  if (c->length > 0 && (!near_rows(dout, c->length) || !near_rows(q, c->length) || !near_rows(k, c->length) || !near_rows(v, c->length))) return QDS_ERR_UNSUPPORTED;
   const SegmentPlan p = segment_plan(c, 3);
   const uint64_t each = state_bytes(c, p.segments) / sizeof(float);
   float* ws = (float*)workspace;

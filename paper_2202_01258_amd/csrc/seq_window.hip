@@ -894,7 +894,7 @@ extern "C" qds_status qds_window_forward(const qds_window_config* c, qds_view q,
   if (c->batch == 0 || c->length == 0) return QDS_OK;
   if (query_grid(c) > most_blocks(kBlock)) return QDS_ERR_UNSUPPORTED;
   if (!usable(q) || !usable(k) || !usable(v) || !usable(o) || !lse) return QDS_ERR_INVALID_ARG;
-  if (!near_rows(k) || !near_rows(v)) return QDS_ERR_UNSUPPORTED;
+  if (!near_rows(k, c->length) || !near_rows(v, c->length)) return QDS_ERR_UNSUPPORTED;
   WindowArgs a = window_args(c, lengths);
   a.q = view(q), a.k = view(k), a.v = view(v), a.o = view(o), a.lse = lse;
   const int blocks = (int)ceil_div(c->length, kForwardRows >> a.share);
@@ -933,7 +933,7 @@ extern "C" qds_status qds_window_backward(const qds_window_config* c, qds_view d
       !usable(dk) || !usable(dv) || !lse || !workspace || ((uintptr_t)workspace & 255))
     return QDS_ERR_INVALID_ARG;
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
-  if (!near_rows(q) || !near_rows(k) || !near_rows(v) || !near_rows(dout)) return QDS_ERR_UNSUPPORTED;
+  if (!near_rows(q, c->length) || !near_rows(k, c->length) || !near_rows(v, c->length) || !near_rows(dout, c->length)) return QDS_ERR_UNSUPPORTED;
   WindowArgs a = window_args(c, lengths);
   a.q = view(q), a.k = view(k), a.v = view(v), a.o = view(o), a.dout = view(dout);
   a.dq = view(dq), a.dk = view(dk), a.dv = view(dv), a.lse = const_cast<float*>(lse);

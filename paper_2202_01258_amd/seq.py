@@ -20,7 +20,7 @@ is enqueued on torch's current stream of the tensors' device, nothing waits for
 the GPU, and there is no fallback.  Tensors are used on that stream alone; a
 tensor made on another stream has to be synchronised with it first, as for any
 torch operation.  Attention takes bfloat16 or float16 tensors whose rows start
-at multiples of 16 bytes; others are copied first.
+at multiples of 16 bytes and are less than 2^23 elements apart; others are copied first.
 """
 from __future__ import annotations
 
@@ -150,10 +150,13 @@ def _on_gpu(t, name):
         raise RuntimeError(f"{name}: libqdseq needs tensors on a GPU, not on {t.device}")
 
 
+_FAR = 1 << 23                                     # elements; the kernels take rows that are nearer
+
+
 def _rows(t):
-    """`t` with contiguous, 16-byte aligned rows: itself, or a copy."""
+    """`t` with contiguous, 16-byte aligned rows that are near enough: itself, or a copy."""
     s = t.stride()
-    if s[-1] == 1 and t.data_ptr() % 16 == 0:
+    if s[-1] == 1 and t.data_ptr() % 16 == 0 and (len(s) == 3 or -_FAR < s[1] < _FAR or t.shape[1] < 2):
         for x in s[:-1]:
             if x % 8:
                 break

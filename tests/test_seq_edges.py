@@ -200,3 +200,25 @@ def test_scratch_memory_does_not_grow_with_the_lists(replay):
     for i in range(0, len(configs), 300):
         for c, (_, sums, _, _) in zip(configs[i:], replay(configs[i:i + 300])):
             assert c[0] * c[3] * sums <= 10 * 512, c
+
+
+# -- rows far apart (the binding copies such tensors)
+def test_rows_too_far_apart_are_refused(lib):
+    v, far = view(), view(P, (8, 1 << 23, 8))
+    c = window()
+    for i in (1, 2):
+        a = [v, v, v]
+        a[i] = far
+        assert lib.qds_window_forward(C.byref(c), *a, None, v, P, None) == S.ERR_UNSUPPORTED
+    for i in range(4):
+        a = [v] * 5
+        a[i] = far
+        assert lib.qds_window_backward(C.byref(c), *a, P, None, *[v] * 3, P, 1 << 40, None) == S.ERR_UNSUPPORTED
+    c = decay()
+    for i in range(3):
+        a = [v] * 3
+        a[i] = far
+        assert lib.qds_decay_forward(C.byref(c), *a, P, None, None, v, P, P, 1 << 40, None) == S.ERR_UNSUPPORTED
+    # a single row's stride means nothing: such a call is refused for other reasons only
+    c = decay(length=1)
+    assert lib.qds_decay_forward(C.byref(c), far, far, far, P, None, None, view(None), P, P, 1 << 40, None) == S.ERR_INVALID_ARG

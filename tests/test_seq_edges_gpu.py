@@ -231,3 +231,34 @@ def test_norm_of_very_many_rows(rows, width, dtype):
         want += (x[i:i + step].double() * h[i:i + step].double() * n[i:i + step]).sum(0)
     # all terms are positive here; a thread adds up to rows / (512 * its share) of them in fp32
     within(dw, want, (SINGLE + rows / 512 * 2.0 ** -24) * want, "dweight")
+
+
+# ---------------------------------------------------------------------------
+# Rows far apart
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("apart", [(1 << 23) - 8, 1 << 23, (1 << 23) + 64])
+def test_rows_far_apart(apart):
+    """Rows that are slices of a long time-major record: the same results as close together."""
+    b, t, h, d = 2, 70, 2, 64
+    big = torch.zeros(t, apart, dtype=BF16, device="cuda")
+    q, k, v = (rand(b, t, h, d, dtype=BF16, seed=i) for i in range(3))
+    n = b * h * d
+    far = []
+    for i, x in enumerate((q, k, v)):
+        y = big[:, i * n:(i + 1) * n].view(t, b, h, d).transpose(0, 1)
+        y.copy_(x)
+        far.append(y)
+    ld = torch.tensor([-0.1, -0.01], device="cuda")
+    o, lse = S.window_attention_forward(q, k, v, 20, 1)
+    want = (o, lse) + S.window_attention_backward(v, q, k, v, o, lse, 20, 1)
+    got = S.window_attention_forward(*far, 20, 1) + S.window_attention_backward(far[2], *far, o, lse, 20, 1)
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+    want = S.decay_attention_forward(q, k, v, ld) + S.decay_attention_backward(v, q, k, v, ld)
+    got = S.decay_attention_forward(*far, ld) + S.decay_attention_backward(far[2], *far, ld)
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+    # a single row has no distance to another
+    one = [x[:, 3:4] for x in far]
+    want = S.window_attention_forward(q[:, 3:4], k[:, 3:4], v[:, 3:4], 20, 1)
+    assert torch.equal(S.window_attention_forward(*one, 20, 1)[0], want[0])
