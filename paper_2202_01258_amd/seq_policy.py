@@ -163,7 +163,8 @@ class Rollout:
     @torch.no_grad()
     def prompt(self, tokens, lengths=None):
         """Takes in the first tokens [batch, n, width] of each episode at once
-        (`lengths`: how many of them each has); the next `step` continues them."""
+        (`lengths`: how many of them each has, clamped to 0 .. n); the next `step`
+        continues them."""
         p, stream, add = self.policy, None, tokens
         n = tokens.shape[1]
         for i in range(2 * p.blocks):
@@ -176,7 +177,7 @@ class Rollout:
                 o, last = seq.decay_attention_forward(q, k, v, p.log_decay, lengths=lengths)
                 self.state[i // 2].copy_(last)
             add = o.flatten(-2) @ self.out[i]
-        self.pos.copy_(torch.full_like(self.pos, n) if lengths is None else lengths)
+        self.pos.copy_(torch.full_like(self.pos, n) if lengths is None else lengths.clamp(0, n))
 
 
 def fit(policy, desc, states, actions, iterations=200, batch=64, lr=2e-3, seed=0):
