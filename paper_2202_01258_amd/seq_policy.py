@@ -133,7 +133,7 @@ class Rollout:
         self.state = [torch.zeros(batch, p.heads, p.dim, p.dim, device=dev) for _ in range(p.blocks)]
         self.qkv = [w.detach().to(low) for w in p.qkv]
         self.out = [w.detach().to(low) for w in p.out]
-        self.norm = [w.detach() for w in p.norm]
+        self.norm = [w.detach().clone() for w in p.norm]
         self.head = p.head.detach().to(low)
 
     @torch.no_grad()
