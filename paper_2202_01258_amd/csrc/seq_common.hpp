@@ -270,25 +270,6 @@ template <class T> __device__ inline void store_column(T* row, int dt, const f32
   }
 }
 
-// Workgroups that follow each other go round the card's eight XCDs, each with an L2
-// cache of its own.  This puts the `per_list` items of a list, which read the same
-// keys, on one XCD: lists are dealt to the XCDs in turn where their number allows
-// (so that episodes of different lengths even out), else in contiguous pieces.
-constexpr int kXcds = 8;
-__device__ inline int xcd_order(int id, int count, int per_list) {
-  const int x = id % kXcds, y = id / kXcds;
-  if (count / per_list % kXcds == 0) return (y / per_list * kXcds + x) * per_list + y % per_list;
-  const int per = count / kXcds, rest = count % kXcds;
-  return x * per + min(x, rest) + y;
-}
-
-// The same with every list on every XCD: the items are dealt one of each list in turn,
-// and one list further from item to item, so that a list's neighbours go round the XCDs.
-__device__ inline int spread_order(int id, int count, int per_list) {
-  const uint32_t lists = (uint32_t)(count / per_list), y = (uint32_t)id / lists;
-  return (int)(((uint32_t)id + y) % lists * (uint32_t)per_list + y);
-}
-
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // A launch has fewer than 2^32 threads in a dimension: HIP takes a larger grid without an

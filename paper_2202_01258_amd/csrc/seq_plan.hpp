@@ -1,6 +1,6 @@
-// seq_plan.hpp -- how the window attention's backward pass over keys is cut into
-// workgroups.  Plain C++: the kernels and the host side use it, and it can be replayed
-// without a GPU.
+// seq_plan.hpp -- in which order the window attention's workgroups take their work, and how
+// its backward pass over keys is cut into workgroups.  Plain C++: the kernels and the host
+// side use it, and it can be replayed without a GPU.
 #pragma once
 
 #include <algorithm>
@@ -21,6 +21,29 @@ constexpr int kKeyRows = 128;          // keys of a block, which a workgroup has
 constexpr int kUnitRows = 32;          // query rows of a unit of its work, of one head
 
 SEQ_BOTH int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Workgroups that follow each other go round the card's eight XCDs, each with an L2
+// cache of its own.  This puts the `per_list` items of a list, which read the same
+// keys, on one XCD: lists are dealt to the XCDs in turn where their number allows
+// (so that episodes of different lengths even out), else in contiguous pieces.
+constexpr int kXcds = 8;
+SEQ_BOTH int xcd_order(int id, int count, int per_list) {
+  const int x = id % kXcds, y = id / kXcds;
+  if (count / per_list % kXcds == 0) return (y / per_list * kXcds + x) * per_list + y % per_list;
+  const int per = count / kXcds, rest = count % kXcds;
+  return x * per + (x < rest ? x : rest) + y;
+}
+
+// The same with every list on every XCD: the items are dealt one of each list in turn,
+// and one list further from item to item, so that a list's neighbours go round the XCDs.
+SEQ_BOTH int spread_order(int id, int count, int per_list) {
+  const uint32_t lists = (uint32_t)(count / per_list), y = (uint32_t)id / lists;
+  return (int)(((uint32_t)id + y) % lists * (uint32_t)per_list + y);
+}
+
+SEQ_BOTH int item_order(bool spread, int id, int count, int per_list) {
+  return spread ? spread_order(id, count, per_list) : xcd_order(id, count, per_list);
+}
 
 // A block of first tokens is seen by every later row, one of the band by about
 // window + 128 rows of each head of the group: the former are cut into more pieces, so
@@ -49,6 +72,21 @@ SEQ_BOTH KeyItem key_item(const KeyPlan& p, int x) {
   if (!is_first) x -= p.first * p.first_cut;
   const int cut = is_first ? p.first_cut : p.band_cut, block = (is_first ? 0 : p.first) + x / cut, piece = x % cut;
   return {block, piece, cut, key_sums(p, block) + piece};
+}
+
+// The list (one batch element's key head) of workgroup `id` of `count`, and its place there.
+// All lists' first blocks come first: one that is not cut, as the lists fill the card many
+// times over, has the most to do and must not be what begins last (64 x 4096 rows, 16 heads of
+// 128, window 256, one first token, backward: 5.7 ms in the lists' order, 4.65 so).
+struct KeyWork {
+  int list, x;
+};
+SEQ_BOTH KeyWork key_work(const KeyPlan& p, bool spread, int id, int count) {
+  const int long_items = p.first * p.first_cut, longs = count / p.items * long_items;
+  const bool is_long = id < longs;
+  const int per_list = is_long ? long_items : p.items - long_items, before = is_long ? 0 : longs;
+  const int at = item_order(spread, id - before, is_long ? longs : count - longs, per_list);
+  return {at / per_list, at % per_list + (is_long ? 0 : long_items)};
 }
 
 // The cut blocks of a key head are blocks from .. to - 1.

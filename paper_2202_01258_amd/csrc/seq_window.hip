@@ -24,11 +24,10 @@ struct WindowArgs {
   int32_t share;                      // log2 of the query heads of a group that a workgroup has; see shared_heads()
 };
 
-// The item of workgroup `id` of `count` where each list (one batch element's key head) has per_list.
-__device__ inline int item_of(const WindowArgs& a, int id, int count, int per_list) {
-  return a.spread ? spread_order(id, count, per_list) : xcd_order(id, count, per_list);
+// The item of this workgroup where each list (one batch element's key head) has per_list.
+__device__ inline int item_of(const WindowArgs& a, int per_list) {
+  return item_order(a.spread, blockIdx.x, gridDim.x, per_list);
 }
-__device__ inline int item_of(const WindowArgs& a, int per_list) { return item_of(a, blockIdx.x, gridDim.x, per_list); }
 
 __device__ inline int rows_of(const WindowArgs& a, int b) {
   if (!a.lengths) return a.length;
@@ -347,15 +346,9 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan
   const int lane = threadIdx.x & 63, wave = wave_index();
   Lanes<DP> place;
   const int group = a.heads / a.kv_heads;
-  // All lists' first blocks come first: one that is not cut, as the lists fill the card many
-  // times over, has the most to do and must not be what begins last (64 x 4096 rows, 16 heads of 128,
-  // window 256, one first token, backward: 5.7 ms in the lists' order, 4.65 so).
-  const int long_items = plan.first * plan.first_cut, longs = gridDim.x / plan.items * long_items;
-  const bool is_long = (int)blockIdx.x < longs;
-  const int per_list = is_long ? long_items : plan.items - long_items;
-  const int id = is_long ? item_of(a, blockIdx.x, longs, per_list) : item_of(a, blockIdx.x - longs, gridDim.x - longs, per_list);
-  const int head = id / per_list;             // b * kv_heads + hk
-  const KeyItem item = key_item(plan, id % per_list + (is_long ? 0 : long_items));
+  const KeyWork work = key_work(plan, a.spread, blockIdx.x, gridDim.x);
+  const int head = work.list;                 // b * kv_heads + hk
+  const KeyItem item = key_item(plan, work.x);
   const int hk = head % a.kv_heads, b = head / a.kv_heads;
   const int n = rows_of(a, b), window = a.window, sinks = a.sinks;
   const int j0 = item.block * kKeyRows, w0 = j0 + 32 * wave;

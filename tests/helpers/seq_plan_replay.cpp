@@ -39,6 +39,16 @@ static int check(const qds_window_config& c) {
     if ((int)of[b].size() != of[b][0].cut) return wrong("pieces", b, (int)of[b].size());
     if ((of[b][0].cut > 1) != (b >= cut_from(p) && b < cut_to(p))) return wrong("join", b, of[b][0].cut);
   }
+  // every workgroup of the grid has an item of its own, in both orders
+  const int lists = c.batch * c.kv_heads, grid = lists * p.items;
+  for (int spread = 0; spread < 2 && grid <= 1 << 20; ++spread) {
+    std::vector<char> seen(grid, 0);
+    for (int id = 0; id < grid; ++id) {
+      const KeyWork w = key_work(p, spread, id, grid);
+      if (w.list < 0 || w.list >= lists || w.x < 0 || w.x >= p.items) return wrong("work", id, w.list);
+      if (seen[w.list * p.items + w.x]++) return wrong("work taken twice", id, w.list);
+    }
+  }
   // the pieces of a block share out the rows that see it, for every length of an episode
   for (int n : {c.length, c.length - 1, c.length / 2, c.length / 3 + 1, 65, 1, 0}) {
     if (n < 0 || n > c.length) continue;
