@@ -93,11 +93,6 @@ __device__ inline float sum_halves(float x) {
 
 template <class T> __device__ inline T shfl_xor(T v, int mask) { return __shfl_xor(v, mask, 64); }
 
-__device__ inline float wave_sum(float x) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) x += shfl_xor(x, m);
-  return x;
-}
 __device__ inline float wave_max(float x) {
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) x = fmaxf(x, shfl_xor(x, m));

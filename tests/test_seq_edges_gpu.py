@@ -262,3 +262,23 @@ def test_rows_far_apart(apart):
     one = [x[:, 3:4] for x in far]
     want = S.window_attention_forward(q[:, 3:4], k[:, 3:4], v[:, 3:4], 20, 1)
     assert torch.equal(S.window_attention_forward(*one, 20, 1)[0], want[0])
+
+
+# ---------------------------------------------------------------------------
+# Steps
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dk,dv", [(64, 64), (128, 128), (40, 72)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_decay_every_step(dk, dv, dtype):
+    """An episode token by token: the definition's output and state at each of them."""
+    b, t, h = 3, 12, 2
+    q, k, v = (rand(b, t, h, d, dtype=dtype, seed=i) for i, d in enumerate((dk, dk, dv)))
+    ld = torch.tensor([-0.5, -0.01], device="cuda")
+    s = rand(b, h, dk, dv, seed=4)
+    first = s.clone()
+    for i in range(t):
+        o, _ = S.decay_attention_step(q[:, i], k[:, i], v[:, i], ld, s)
+        want = decay_exact(q[:, :i + 1], k[:, :i + 1], v[:, :i + 1], ld, first)
+        x, size = want["o"][0][:, -1], want["o"][1][:, -1]
+        within(o, x, U[dtype] * x.abs() + SINGLE * size + TINY[dtype], f"o of row {i}")
+        within(s, want["state"][0], SINGLE * want["state"][1], f"state after row {i}")
