@@ -55,6 +55,7 @@ struct KeyPlan {
   int32_t first_cut, band_cut;      // pieces of each kind
   int32_t items;                    // workgroups per key head
   int32_t sums;                     // those that leave sums
+  bool ahead;                       // first blocks begin before all others
 };
 
 // Workgroup x of a key head.
@@ -75,18 +76,19 @@ SEQ_BOTH KeyItem key_item(const KeyPlan& p, int x) {
 }
 
 // The list (one batch element's key head) of workgroup `id` of `count`, and its place there.
-// All lists' first blocks come first: one that is not cut, as the lists fill the card many
-// times over, has the most to do and must not be what begins last (64 x 4096 rows, 16 heads of
-// 128, window 256, one first token, backward: 5.7 ms in the lists' order, 4.65 so).
+// Where a piece of a first block is longer than two blocks of the band, all lists' first blocks
+// come first: what has the most to do must not be what begins last (64 x 4096 rows, 16 heads of
+// 128, window 256, one first token, backward: 5.7 ms in the lists' order, 4.65 so).  Spread
+// lists begin with them anyway.
 struct KeyWork {
   int list, x;
 };
 SEQ_BOTH KeyWork key_work(const KeyPlan& p, bool spread, int id, int count) {
-  const int long_items = p.first * p.first_cut, longs = count / p.items * long_items;
+  const int ahead = p.ahead && !spread ? p.first * p.first_cut : 0, longs = count / p.items * ahead;
   const bool is_long = id < longs;
-  const int per_list = is_long ? long_items : p.items - long_items, before = is_long ? 0 : longs;
+  const int per_list = is_long ? ahead : p.items - ahead, before = is_long ? 0 : longs;
   const int at = item_order(spread, id - before, is_long ? longs : count - longs, per_list);
-  return {at / per_list, at % per_list + (is_long ? 0 : long_items)};
+  return {at / per_list, at % per_list + (is_long ? 0 : ahead)};
 }
 
 // The cut blocks of a key head are blocks from .. to - 1.
@@ -127,7 +129,7 @@ inline KeyPlan key_plan(const qds_window_config* c) {
   if (piece < 16) piece = 16;
   // A first block in pieces as long as a block of the band, which then end with the others,
   // but of no less than a quarter of what a place on the card has to do: lists that fill the card
-  // many times over even out by themselves, as first blocks begin first.  All sums together then
+  // many times over even out by themselves, as first blocks then begin first.  All sums together then
   // belong to some 8 kFill pieces at most, whatever the number of lists.  Backward, us, in pieces of
   // the band's length | so: 64 x 4096 rows, 16 heads of 128, window 256, one first token: 5030 | 4650 (5.65 GB of
   // sums | none);  256 x 1000, 8 heads of 64, window 64, one: 1448 | 1107;  32 x 2048, 8 heads of 64, 128,
@@ -135,6 +137,7 @@ inline KeyPlan key_plan(const qds_window_config* c) {
   const int64_t first_piece = std::min(piece, std::max(band * group, piece / 4));
   p.first_cut = p.first > 0 ? (int32_t)ceil_div(all * group, first_piece) : 1;
   p.band_cut = bands > 0 ? (int32_t)ceil_div(band * group, piece) : 1;
+  p.ahead = p.first > 0 && first_piece > 2 * band * group;
   p.items = (int32_t)(p.first * p.first_cut + bands * p.band_cut);
   p.sums = (p.first_cut > 1 ? p.first * p.first_cut : 0) + (p.band_cut > 1 ? (int32_t)bands * p.band_cut : 0);
   return p;
