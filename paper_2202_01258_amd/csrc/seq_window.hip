@@ -91,7 +91,8 @@ __device__ inline void hide(f32x16& s, int i, int j0, int window, int sinks, boo
 // its columns), so a query's maximum and sum are over a lane's own registers and one exchange with
 // lane l ^ 32, and the weights are the B operand of o^T = v^T p^T as they are.
 // Bound by the issue of matrix and vector instructions together: 32768 rows, 16 heads
-// of 128 over 4 key heads, window 4096, bfloat16 take 1.09 to 1.19 ms between cards, 890 to 970 TFLOP/s.  The next
+// of 128 over 4 key heads, window 4096, bfloat16 take 1.09 to 1.19 ms between cards, 890 to 970 TFLOP/s (after an
+// idle stretch the first launches take up to 1.48 and the twelfth 1.18: 1.23 to 1.28 in the middle).  The next
 // tile's scores beside this tile's weights do not fit the registers of two waves on a
 // SIMD (292 spills), and with one wave took 2.11 ms beside 1.07.
 constexpr int kForwardRows = 32 * kWaves;
@@ -227,11 +228,12 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_forward(WindowArgs a, int 
 // are then over a workgroup's own loop, in a fixed order.
 
 // dq of the same rows as the forward pass has; also writes delta.  2 x 8192 rows,
-// 16 heads of 128, window 1024, bfloat16: 255 to 264 us between cards (the forward pass takes 193 to 199).
+// 16 heads of 128, window 1024, bfloat16: 251 to 264 us between cards (the forward pass takes 190 to 199).
 //
 // delta is formed from o as stored, so it carries o's rounding; the score gradients
 // are rounded to the tensors' type for their product, relative to each of them.  In
-// float16 those below 2^-24 vanish: a loss is scaled there as for any float16 gradient.
+// float16 those below 2^-24 vanish and those beyond 65504 are infinite: a loss is scaled there
+// as for any float16 gradient.
 template <class T, int DC>
 __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blocks) {
   constexpr int DP = padded(DC);
@@ -334,8 +336,10 @@ __global__ __launch_bounds__(kBlock, 2) void k_window_dq(WindowArgs a, int q_blo
 // registers; values do for 64 columns, and are read from LDS for 128, where the
 // registers that two waves on a SIMD leave each other are 160 for keys and sums.
 // Two waves with values in LDS take 400 us where one with all in registers takes 490
-// (2 x 8192 rows, 16 heads of 128, window 1024, bfloat16; 388 to 404 now, between cards).  The weights and
-// the score gradients are rounded as in the other two kernels.
+// (2 x 8192 rows, 16 heads of 128, window 1024, bfloat16; 386 to 404 now, between cards).  For heads of up to 64
+// no other unit has been timed: 32 ragged episodes of 1000 rows, 8 heads of 64 over 2, window 250, float16 take 64 us, of
+// which waves wait 45% and the matrix units work 15%.  The weights and the score gradients are rounded as in the other two
+// kernels.
 template <class T, int DC>
 __global__ __launch_bounds__(kBlock, 2) void k_window_dkdv(WindowArgs a, KeyPlan plan, float* parts) {
   constexpr int DP = padded(DC);

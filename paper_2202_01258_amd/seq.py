@@ -477,6 +477,11 @@ def decay_attention_forward(q, k, v, log_decay, state=None, lengths=None, scale=
     gradient for it.  `state` (float32 [batch, heads, dim_k, dim_v]) is S
     before the first row, 0 if None; `lengths` as for window_attention.
 
+    Nothing is read from behind a length.  Before it, k and v have to be finite:
+    a row that is not may make up to 63 rows before it not-a-number as well
+    (their weight of 0 times infinity), in the same batch element and head.
+    States may hold any float32 numbers, in float16, too.
+
     Returns o and the state after the last row."""
     cfg, ref, size = _decay_setup(q, k, v, log_decay, scale, True, "qds_decay_forward_workspace")
     state = _state("state", state, cfg, q)
