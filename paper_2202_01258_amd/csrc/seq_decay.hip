@@ -95,7 +95,8 @@ template <int N> struct State {
 
 // How many numbers of 16 bits carry an fp32 one: the state is fp32, so its
 // summands f a^(63-j) y_j z_j keep 24 bits in bfloat16, 22 in float16 (y is exact;
-// f z a^(63-j) is split).
+// f z a^(63-j) is split).  Of a float16 y below its normal range the matrix instruction's sums
+// keep 2^-24 of what 2^-14 would have given: for y = 2^-24 the relative error is 5e-5.
 template <class T> struct Terms;
 template <> struct Terms<bf16> { static constexpr int n = 3; };
 template <> struct Terms<half> { static constexpr int n = 2; };

@@ -1,5 +1,5 @@
 """The sequence operators on the GPU at the edges of what they accept: no rows,
-values far from 1, very many rows, rows far apart.
+values far from 1, very many rows, rows far apart, tensors beyond 2^31 elements.
 
 Tolerances as in test_seq_gpu.py: bounds worked out element by element from
 the kernels' roundings, against definitions in 64 bits.
@@ -11,7 +11,7 @@ import pytest
 torch = pytest.importorskip("torch")
 
 from paper_2202_01258_amd import seq as S  # noqa: E402
-from test_seq_gpu import BF16, F16, F32, SINGLE, TINY, U, decay_exact, norm_exact, qkv, rand, within  # noqa: E402
+from test_seq_gpu import BF16, F16, F32, SINGLE, TINY, U, decay_exact, norm_exact, rand, window_exact, within  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -282,3 +282,78 @@ def test_decay_every_step(dk, dv, dtype):
         x, size = want["o"][0][:, -1], want["o"][1][:, -1]
         within(o, x, U[dtype] * x.abs() + SINGLE * size + TINY[dtype], f"o of row {i}")
         within(s, want["state"][0], SINGLE * want["state"][1], f"state after row {i}")
+
+
+# ---------------------------------------------------------------------------
+# Tensors of more than 2^31 elements
+# ---------------------------------------------------------------------------
+BIG = (1, (1 << 18) + 64, 64, 128)                 # rows x 64 heads of 128
+
+
+def big(seed, scale=1.0):
+    x = torch.empty(BIG, dtype=BF16, device="cuda")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    for h in range(0, BIG[2], 16):
+        x[:, :, h:h + 16] = torch.randn(1, BIG[1], 16, BIG[3], generator=g, device="cuda") * scale
+    return x
+
+
+def tail(x, rows=512):
+    """The last rows of the first and the last head."""
+    return x[:, -rows:, [0, -1]].contiguous()
+
+
+def test_window_beyond_31_bits():
+    """The last rows and heads of a long sequence see what is in their window alone."""
+    q, k, v, g = (big(i) for i in range(4))
+    assert q.numel() > 1 << 31
+    o, lse = S.window_attention_forward(q, k, v, 64)
+    grads = S.window_attention_backward(g, q, k, v, o, lse, 64)
+    want = window_exact(*(tail(x) for x in (q, k, v)), 64, 0, g=tail(g))
+    for name, got in zip(("o", "dq", "dk", "dv"), (o,) + grads):
+        x, e = want[name]
+        within(tail(got, 256), x[:, 256:], e[:, 256:], name)
+    within(lse[:, [0, -1], -256:], want["lse"][0][..., 256:], want["lse"][1][..., 256:], "lse")
+
+
+def test_decay_beyond_31_bits():
+    """The same for a decay after which rows 256 back are below fp32's share of a sum (e^-128)."""
+    q, k, v, g = (big(i) for i in range(4))
+    ld = torch.full((BIG[2],), -0.5, device="cuda")
+    o, last = S.decay_attention_forward(q, k, v, ld)
+    grads = S.decay_attention_backward(g, q, k, v, ld)
+    want = decay_exact(*(tail(x) for x in (q, k, v)), ld[:2], None, g=tail(g))
+    u = U[BF16]
+    for name, got in zip(("o", "dq", "dk", "dv"), (o,) + grads[:3]):
+        x, size = (y[:, 256:] for y in want[name])
+        within(tail(got, 256), x, u * x.abs() + (u + SINGLE) * size, name)
+    within(last[:, [0, -1]], want["state"][0], SINGLE * want["state"][1], "state")
+
+
+@pytest.mark.parametrize("window,sinks", [((1 << 20) + 5, 11)])
+def test_window_step_beyond_31_bits(window, sinks):
+    """A ring of more than 2^31 elements, read at its far end."""
+    b, hq, hkv, d = 3, 12, 6, 128
+    kc, vc = S.window_cache(b, hkv, d, window, sinks, BF16)
+    assert kc.numel() > 1 << 31
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    for x in (kc, vc):
+        for i in range(b):
+            x[i] = torch.randn(x.shape[1:], generator=g, device="cuda", dtype=F32).to(BF16)
+    q, k, v = (rand(b, h, d, dtype=BF16, seed=i) for i, h in enumerate((hq, hkv, hkv)))
+    pos = [window + sinks + 7, 5, 3 * window]
+    kept = [(kc[i].clone(), vc[i].clone()) for i in range(b)]
+    o = S.window_attention_step(q, k, v, kc, vc, torch.tensor(pos, dtype=torch.int32, device="cuda"), window, sinks)
+    for i, p in enumerate(pos):
+        slot = p if p < sinks else sinks + (p - sinks) % window
+        for new, old, row in ((kc[i], kept[i][0], k[i]), (vc[i], kept[i][1], v[i])):
+            old[:, slot] = row
+            assert torch.equal(new, old)
+        n = min(p + 1, window + sinks)
+        for h in (0, hq - 1):
+            K, V = (x[h * hkv // hq, :n].double() for x in kept[i])
+            w = torch.softmax(K @ q[i, h].double() * d ** -0.5, 0)
+            want, size = w @ V, w @ V.abs()
+            within(o[i, h], want, U[BF16] * want.abs() + (U[BF16] + SINGLE) * size, f"o {i} {h}")
