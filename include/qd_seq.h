@@ -13,7 +13,12 @@
  *     descriptor's) stay visible, with its gradient, and its single-token form
  *     over a ring cache;
  *   - linear attention with a decay for each head, by chunks, with its
- *     gradient, and its recurrent form for single tokens.
+ *     gradient, and its recurrent form for single tokens;
+ *   - a selective block: a short causal convolution and the selective state
+ *     space scan behind it, each with its gradient and its form for single
+ *     tokens; the norms before and after a block's branch with the branch's gate
+ *     and the residual's scale; dropout from a counter, whose mask is never
+ *     stored.
  *
  * Conventions for every entry point (those of qd.h):
  *   - Plain C types only.  `stream` is a hipStream_t passed as void*; work is
@@ -204,6 +209,165 @@ qds_status qds_decay_backward(const qds_decay_config* c, qds_view dout, qds_view
 qds_status qds_decay_step(const qds_decay_config* c, qds_view q, qds_view k, qds_view v,
                           const float* log_decay, const float* state_in, qds_view o,
                           float* state_out, void* stream);
+
+/* Rows of a tensor without heads: element (b, t, d) is
+ * data[b * stride[0] + t * stride[1] + d].  Strides are in elements, of any size,
+ * sign or order, also 0 for inputs; data is aligned to its elements. */
+typedef struct {
+  void* data;
+  int64_t stride[2];
+} qds_rows;
+
+/* ------------------------------------------------------------------------
+ * Short causal convolution over rows, for each column by itself
+ *
+ *   p_t = bias + sum_k weight[k] x_{t - taps + 1 + k};  y_t = p_t, or silu(p_t)
+ *
+ * Rows before the first are the state's: state [batch][taps - 1][width] of dtype,
+ * contiguous, holds the taps - 1 rows before it, the oldest first.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  uint32_t abi_version;   /* QDS_ABI_VERSION                                        */
+  int32_t dtype;          /* QDS_*: x, y, states and their gradients                */
+  int32_t weight_dtype;   /* QDS_F32 or dtype: weight, bias and their gradients     */
+  int32_t batch;          /* >= 0                                                   */
+  int32_t length;         /* rows per batch element, >= 0, < 2^30; unused by the step */
+  int32_t width;          /* columns, 1 .. 2^20                                     */
+  int32_t taps;           /* 1 .. 8                                                 */
+  int32_t silu;           /* 0: y = p;  1: y = p / (1 + e^-p)                       */
+} qds_conv_config;
+
+/* weight [taps][width], bias [width] or null, contiguous.  lengths [batch] int32
+ * gives each element's rows n (clamped to 0 .. length; null: all `length`); rows
+ * from n on are not read and get y = 0.  state_in null: 0.  state_out (may be
+ * null; not state_in): the taps - 1 rows before row n. */
+qds_status qds_causal_conv(const qds_conv_config* c, qds_rows x, const void* weight, const void* bias,
+                           const void* state_in, const int32_t* lengths, qds_rows y, void* state_out,
+                           void* stream);
+
+/* dx (0 from row n on), dweight, dbias (may be null) and dstate_in (may be null)
+ * from dy, dstate_out (null: 0) and what the forward call saw. */
+qds_status qds_causal_conv_backward_workspace(const qds_conv_config* c, uint64_t* bytes);
+qds_status qds_causal_conv_backward(const qds_conv_config* c, qds_rows dy, qds_rows x, const void* weight,
+                                    const void* bias, const void* state_in, const void* dstate_out,
+                                    const int32_t* lengths, qds_rows dx, void* dweight, void* dbias,
+                                    void* dstate_in, void* workspace, uint64_t workspace_bytes,
+                                    void* stream);
+
+/* One row of each batch element (stride[1] unused); state_out may be state_in. */
+qds_status qds_causal_conv_step(const qds_conv_config* c, qds_rows x, const void* weight, const void* bias,
+                                const void* state_in, qds_rows y, void* state_out, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Selective state space scan
+ *
+ *   dt = log(1 + e^(delta + bias));  h_t[n] = e^(dt a[n]) h_{t-1}[n] + dt u_t b_t[n]
+ *   y_t = sum_n c_t[n] h_t[n] + skip u_t;  o_t = y_t, or y_t silu(gate_t)
+ *
+ * for each column by itself; b and c are shared by the columns.  State h is
+ * [batch][width][states] fp32.  All arithmetic is fp32.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  uint32_t abi_version;   /* QDS_ABI_VERSION                                        */
+  int32_t dtype;          /* QDS_*: u, delta, b, c, gate, o and their gradients     */
+  int32_t batch;          /* >= 0                                                   */
+  int32_t length;         /* rows per batch element, >= 0, < 2^30; unused by the step */
+  int32_t width;          /* columns, 1 .. 2^20                                     */
+  int32_t states;         /* 1 .. 32 (more: QDS_ERR_UNSUPPORTED)                    */
+} qds_scan_config;
+
+/* u, delta, gate, o: rows of `width`; b, c: rows of `states`.  a [width][states]
+ * fp32; skip and bias [width] fp32 or null (0); gate.data null: o = y.  lengths as
+ * for the convolution.  state_in null: 0.  state_out (may be null, or state_in):
+ * h after row n - 1.  marks (null unless a backward pass follows, which needs
+ * them; 256-byte aligned): states that the backward pass starts from, *bytes as
+ * its size query gives. */
+qds_status qds_selective_scan_marks(const qds_scan_config* c, uint64_t* bytes);
+qds_status qds_selective_scan_workspace(const qds_scan_config* c, uint64_t* bytes);
+qds_status qds_selective_scan(const qds_scan_config* c, qds_rows u, qds_rows delta, const float* a,
+                              qds_rows b, qds_rows cc, const float* skip, qds_rows gate, const float* bias,
+                              const float* state_in, const int32_t* lengths, qds_rows o, float* state_out,
+                              void* marks, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Gradients from do and dstate_out (null: 0).  du, ddelta, dgate: rows of `width`
+ * (0 from row n on; dgate as gate); db, dc: rows of `states`, likewise; da, dskip,
+ * dbias (the last two may be null) and dstate_in (may be null, or dstate_out) fp32. */
+qds_status qds_selective_scan_backward_workspace(const qds_scan_config* c, uint64_t* bytes);
+qds_status qds_selective_scan_backward(const qds_scan_config* c, qds_rows dout, qds_rows u, qds_rows delta,
+                                       const float* a, qds_rows b, qds_rows cc, const float* skip,
+                                       qds_rows gate, const float* bias, const void* marks,
+                                       const float* dstate_out, const int32_t* lengths, qds_rows du,
+                                       qds_rows ddelta, float* da, qds_rows db, qds_rows dc, float* dskip,
+                                       qds_rows dgate, float* dbias, float* dstate_in, void* workspace,
+                                       uint64_t workspace_bytes, void* stream);
+
+/* One row of each batch element (stride[1] unused); state_out may be state_in. */
+qds_status qds_selective_scan_step(const qds_scan_config* c, qds_rows u, qds_rows delta, const float* a,
+                                   qds_rows b, qds_rows cc, const float* skip, qds_rows gate,
+                                   const float* bias, const float* state_in, qds_rows o, float* state_out,
+                                   void* stream);
+
+/* ------------------------------------------------------------------------
+ * Norms before and after a block's branch, its gate, the residual's scale
+ *
+ *   n = x (mean(x^2) + eps)^(-1/2) branch_weight            the norm behind the branch
+ *   h = residual_scale residual + silu(gate) n              (without a gate: ... + n)
+ *   y = h (mean(h^2) + eps)^(-1/2) weight                   the norm in front of the next
+ *
+ * Sums are in fp32 and y comes from h before it is rounded.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  uint32_t abi_version;   /* QDS_ABI_VERSION                                        */
+  int32_t dtype;          /* QDS_*: x, gate, residual, y, h and their gradients     */
+  int32_t weight_dtype;   /* QDS_F32 or dtype: both weights and their gradients     */
+  int32_t width;          /* elements per row, 1 .. 2^20                            */
+  int64_t rows;           /* >= 0, < 2^31                                           */
+  float eps;              /* >= 0; unused by the backward pass                      */
+  float residual_scale;   /* finite                                                 */
+} qds_branch_config;
+
+/* y, h [rows][width] of dtype and rstds [2][rows] fp32 (of x, of h), contiguous.
+ * Inputs have a row stride in elements; gate may be null. */
+qds_status qds_branch_norm(const qds_branch_config* c, const void* x, int64_t x_stride, const void* gate,
+                           int64_t gate_stride, const void* residual, int64_t residual_stride,
+                           const void* branch_weight, const void* weight, void* y, void* h, float* rstds,
+                           void* stream);
+
+/* dx, dgate (null without a gate), dresidual [rows][width], dbranch_weight and
+ * dweight [width] from dy and dh (the gradient that reaches h by other ways; may
+ * be null).  h is formed again from x, gate and residual. */
+qds_status qds_branch_norm_backward_workspace(const qds_branch_config* c, uint64_t* bytes);
+qds_status qds_branch_norm_backward(const qds_branch_config* c, const void* dy, int64_t dy_stride,
+                                    const void* dh, int64_t dh_stride, const void* x, int64_t x_stride,
+                                    const void* gate, int64_t gate_stride, const void* residual,
+                                    int64_t residual_stride, const float* rstds, const void* branch_weight,
+                                    const void* weight, void* dx, void* dgate, void* dresidual,
+                                    void* dbranch_weight, void* dweight, void* workspace,
+                                    uint64_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Dropout from a counter
+ *
+ *   y = residual + (draw >= threshold ? x / (1 - threshold / 2^16) : 0)
+ *
+ * Element i (of the contiguous tensor) belongs to group i / 8.  A group's draws are
+ * the eight 16-bit halves of one Philox4x32-10 block, words in order, low halves
+ * first: key = rng[0] (low word, high word), counter = (group, site, rng[1] low
+ * word, high word).  rng is read on the device, so a captured call draws anew where
+ * the program has changed it between replays.  The backward pass is the same call on
+ * the gradient, without a residual.
+ * ------------------------------------------------------------------------ */
+typedef struct {
+  uint32_t abi_version;   /* QDS_ABI_VERSION                                        */
+  int32_t dtype;          /* QDS_*: x, residual, y                                  */
+  int64_t elements;       /* 0 .. 2^34                                              */
+  uint32_t threshold;     /* 0 .. 65535: 2^16 times the probability of a zero       */
+  uint32_t site;          /* which of a program's dropouts this is                  */
+} qds_dropout_config;
+
+/* x, y, residual (may be null): contiguous; y may be x or residual. */
+qds_status qds_dropout(const qds_dropout_config* c, const void* x, const void* residual,
+                       const int64_t* rng, void* y, void* stream);
 
 const char* qds_status_str(qds_status status);
 

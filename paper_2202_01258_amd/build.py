@@ -23,8 +23,10 @@ DEPS = SRC + [os.path.join(HERE, "csrc", f) for f in ("qd_device.hpp", "qd_kerne
     os.path.join(ROOT, "include", "qd.h")]
 SEQ_LIB = os.path.join(HERE, "libqdseq.so")
 SEQ_SRC = [os.path.join(HERE, "csrc", f) for f in ("seq_norm.hip", "seq_window.hip",
-                                                   "seq_decay.hip")]
-SEQ_DEPS = SEQ_SRC + [os.path.join(HERE, "csrc", f) for f in ("seq_common.hpp", "seq_plan.hpp")] + [
+                                                   "seq_decay.hip", "seq_conv.hip", "seq_scan.hip",
+                                                   "seq_scan_backward.hip", "seq_branch.hip", "seq_dropout.hip")]
+SEQ_DEPS = SEQ_SRC + [os.path.join(HERE, "csrc", f) for f in ("seq_common.hpp", "seq_plan.hpp", "seq_rows.hpp",
+                                                                  "seq_scan.hpp")] + [
     os.path.join(ROOT, "include", "qd_seq.h")]
 ARCH = os.environ.get("QD_OFFLOAD_ARCH", "gfx950")
 

@@ -8,6 +8,7 @@
 #include <algorithm>
 
 #include "seq_common.hpp"
+#include "seq_rows.hpp"
 
 namespace seq {
 namespace {
@@ -16,48 +17,6 @@ constexpr int kBlock = 256;
 constexpr float kFp8Max = 448.0f;
 constexpr float kFp8Floor = 0x1p-100f;   // a smaller maximum would make 448 / maximum overflow
 constexpr int kBackwardBlocks = 512;     // two workgroups per compute unit, each with its own dweight
-
-template <class T> __device__ inline float to_f32(T x) { return (float)x; }
-template <class T> __device__ inline T from_f32(float x) { return (T)x; }
-
-// VEC consecutive elements, 16 bytes, at any alignment: rows of odd widths start
-// anywhere.  Where VEC does not divide the width (TAIL), a row's last lane takes its
-// last VEC elements, some of which its neighbour has as well: both store the same
-// values, and only the neighbour counts them in sums.  That leaves no branch around
-// the accesses (a branch per element at the row's end let each load wait for the
-// one before: 32000 x 1024 then took 141 us in place of 95).
-template <class T, int VEC> struct Pack { T v[VEC]; };
-
-template <class T, int VEC> __device__ inline void load(float* out, const T* p) {
-  Pack<T, VEC> e;
-  __builtin_memcpy(&e, p, sizeof(e));
-#pragma unroll
-  for (int i = 0; i < VEC; ++i) out[i] = to_f32(e.v[i]);
-}
-template <class T, int VEC> __device__ inline void store(T* p, const float* in) {
-  Pack<T, VEC> e;
-#pragma unroll
-  for (int i = 0; i < VEC; ++i) e.v[i] = from_f32<T>(in[i]);
-  __builtin_memcpy(p, &e, sizeof(e));
-}
-// The weight is fp32 or of the tensors' type.
-template <class T, int VEC> __device__ inline void load_weight(float* out, const void* w, bool w32, int col) {
-  if (w32) {
-    const float* p = (const float*)w + col;
-    if constexpr (VEC == 8) {
-      load<float, 4>(out, p);
-      load<float, 4>(out + 4, p + 4);
-    } else {
-      load<float, VEC>(out, p);
-    }
-  } else {
-    load<T, VEC>(out, (const T*)w + col);
-  }
-}
-// Where the pack of a lane at column `col` (inside the row) starts.
-template <int VEC, bool TAIL> __device__ inline int pack_at(int col, int width) {
-  return TAIL ? min(col, width - VEC) : col;
-}
 
 // Sum over the lanes that share a row: part of a wave, a wave, or the workgroup.
 // `part` has a place per wave; two calls that follow each other use different ones.
@@ -439,7 +398,6 @@ qds_status validate(const qds_norm_config* c) {
 // for each, 127238 rows of 128 took 47 us; with 16 lanes, 20 us.
 // fp32 rows beyond 4096 take eight packs of four: 9947 x 4697 forward and backward
 // 299 us, read again for each use 668.
-template <int V> using Int = std::integral_constant<int, V>;
 template <class T, bool TAIL, class F> bool with_lanes(int width, F&& f) {
   constexpr int V = 16 / sizeof(T);
   const Int<TAIL> tail{};

@@ -1,0 +1,222 @@
+// seq_scan.hpp -- what the forward and backward kernels of the selective scan share.
+//
+// A column's states are split among the four lanes of a quad, S each, so a wave has 16
+// columns.  Rows are taken K at a time: lane q of a quad does what is done once for a row
+// and column (step size, products, gate) for rows q, q + 4, ..., and gives it to the
+// others by lane moves; rows of b and c, which all columns share, come through LDS.  An
+// episode may be cut into segments that run side by side: a first pass forms what each
+// segment leaves behind when it starts from zero, a short scan joins them, and the main
+// pass starts each segment from its true state.
+#pragma once
+
+#include <algorithm>
+
+#include "seq_common.hpp"
+#include "seq_rows.hpp"
+
+namespace seq {
+
+constexpr int kScanStates = 32;                  // at most
+
+// Rows of a block.  The backward pass starts from the state in front of a block ("mark")
+// and keeps 2 K S numbers of it in registers.
+template <int S> constexpr int kScanRows = S <= 4 ? 16 : 8;
+
+struct Rows {
+  char* p;
+  int64_t b, t;                                  // strides in elements
+};
+inline Rows rows(const qds_rows& r) { return Rows{(char*)r.data, r.stride[0], r.stride[1]}; }
+template <class T> __device__ inline T* row_of(const Rows& r, int64_t b, int64_t t) {
+  return (T*)r.p + b * r.b + t * r.t;
+}
+
+struct ScanArgs {
+  Rows u, delta, b, c, gate, o, dout, du, ddelta, db, dc, dgate;
+  const float *a, *skip, *bias, *first, *dlast;
+  float *last, *dfirst, *da, *dskip, *dbias;
+  float* marks;                                  // [batch][blocks][width][4 S]
+  float* seg_state;                              // [batch][segs][width][4 S]: left behind by a segment, then what it starts from
+  float* seg_time;                               // [batch][segs][width]: sum of a segment's steps
+  float* rows_part;                              // [batch][length][column blocks][2][4 S]: shares of db and dc
+  float* cols_part;                              // [shares][width][4 S]: of da
+  float* ends_part;                              // [shares][2][width]: of dskip and dbias
+  const int32_t* lengths;
+  int32_t batch, length, width, states, seg, segs, blocks, col_blocks, shares;
+};
+__device__ inline int rows_in(const ScanArgs& a, int64_t b) {
+  return a.lengths ? min(max(a.lengths[b], 0), a.length) : a.length;
+}
+
+// The value of lane J of this lane's quad, of lane q ^ 1, of lane q ^ 2.
+template <int CTRL> __device__ inline float lane_move(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+template <int J> __device__ inline float quad_lane(float v) { return lane_move<J * 0x55>(v); }
+__device__ inline float quad_sum(float v) {
+  v += lane_move<0xB1>(v);
+  return v + lane_move<0x4E>(v);
+}
+// Four rows' values in four lanes: lane q gets row q's sum over the quad.
+__device__ inline float quad_rows(const float* v, int q) {
+  const bool odd = q & 1, high = q & 2;
+  const float a = (odd ? v[1] : v[0]) + lane_move<0xB1>(odd ? v[0] : v[1]);
+  const float b = (odd ? v[3] : v[2]) + lane_move<0xB1>(odd ? v[2] : v[3]);
+  return (high ? b : a) + lane_move<0x4E>(high ? a : b);
+}
+
+// log(1 + e^x) to an ulp or two for any x: log(1 + e) is formed as log(w) e / (w - 1) with
+// w = 1 + e as rounded, which takes w's rounding back where e is small.
+struct Step {
+  float dt, slope;                               // and its derivative, sigmoid(x)
+};
+__device__ inline Step softplus(float x) {
+  const float e = fast_exp2(-kLog2e * fabsf(x)), w = 1.0f + e, back = w - 1.0f;
+  const float log1 = back == 0.0f ? e : kLn2 * fast_log2(w) * e * __builtin_amdgcn_rcpf(back);
+  const float r = __builtin_amdgcn_rcpf(w);
+  return Step{(x > 0.0f ? x : 0.0f) + log1, x > 0.0f ? r : e * r};
+}
+
+// a in units of log 2, finite: rows behind an episode have dt = 0 and must leave the state alone.
+__device__ inline float rate(float a) {
+  const float x = a * kLog2e;
+  return x < -0x1.fffffep127f ? -0x1.fffffep127f : x > 0x1.fffffep127f ? 0x1.fffffep127f : x;
+}
+
+// S neighbouring floats, aligned to them all where S allows.
+template <int S> struct alignas(S * 4 > 16 ? 16 : S * 4) Floats { float v[S]; };
+template <int S> __device__ inline void load_floats(float* out, const float* p) {
+  const Floats<S> f = *reinterpret_cast<const Floats<S>*>(p);
+#pragma unroll
+  for (int s = 0; s < S; ++s) out[s] = f.v[s];
+}
+template <int S> __device__ inline void store_floats(float* p, const float* in) {
+  Floats<S> f;
+#pragma unroll
+  for (int s = 0; s < S; ++s) f.v[s] = in[s];
+  *reinterpret_cast<Floats<S>*>(p) = f;
+}
+// One number by a buffer access: a scalar base, the lane's offset and a scalar offset in bytes.
+// From kOutside on a load gives 0 and a store does nothing.
+template <class T> __device__ inline T get(const char* base, uint32_t lane_at, uint32_t at) {
+  const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, kBufferSize, kBufferFlags);
+  if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(buffer, lane_at, at, 0));
+  else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(buffer, lane_at, at, 0));
+}
+template <class T> __device__ inline void put(char* base, uint32_t lane_at, uint32_t at, T v) {
+  const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, kBufferSize, kBufferFlags);
+  if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), buffer, lane_at, at, 0);
+  else __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, v), buffer, lane_at, at, 0);
+}
+
+// The lane's states of column `at` in a tensor of the caller's, [..][width][states]; `p` is the
+// same for the wave.
+template <int S> __device__ inline void load_states(float* out, const float* p, int at, int q, int states) {
+#pragma unroll
+  for (int s = 0; s < S; ++s)
+    out[s] = get<float>((const char*)p, p && q * S + s < states ? (at * states + q * S) * 4u : kOutside, s * 4);
+}
+template <int S> __device__ inline void store_states(float* p, int at, int q, int states, bool in, const float* v) {
+#pragma unroll
+  for (int s = 0; s < S; ++s) put<float>((char*)p, in && q * S + s < states ? (at * states + q * S) * 4u : kOutside, s * 4, v[s]);
+}
+
+// A tensor's rows t + q, t + 4 + q, ... at a lane's column: the rows of an episode as a scalar
+// base, so that an access costs no 64-bit arithmetic in vector registers.  Rows are from 0 to
+// 2^23 elements apart.
+template <class T> struct Track {
+  char* p;
+  uint32_t step, lane_at;                        // bytes: from row to row, and the lane's
+  __device__ void init(const Rows& r, int64_t b, int q, int at) {
+    p = r.p + b * r.b * (int64_t)sizeof(T);
+    step = (uint32_t)r.t * sizeof(T);
+    lane_at = q * step + at * (uint32_t)sizeof(T);
+  }
+  __device__ T load(int t, int i, bool in) const { return get<T>(p + (int64_t)t * step, in ? lane_at : kOutside, 4 * i * step); }
+  __device__ void store(int t, int i, bool in, float v) const { put<T>(p + (int64_t)t * step, in ? lane_at : kOutside, 4 * i * step, from_f32<T>(v)); }
+};
+
+// K rows of b and c on their way to LDS: [K][2][4 S], what is behind `end` or the states is 0.
+template <class T, int S, int BLOCK> struct StagedRows {
+  static constexpr int N = 4 * S, K = kScanRows<S>, ALL = K * 2 * N, EACH = (ALL + BLOCK - 1) / BLOCK;
+  static_assert(K * N % 64 == 0, "a wave has rows of b or of c, not of both");
+  T v[EACH];
+  __device__ void load(const ScanArgs& a, int64_t b, int t, int end) {
+    const int wave = wave_index() * 64;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int id = threadIdx.x + i * BLOCK, row = id / N % K, n = id % N;
+      const Rows& from = wave + i * BLOCK < K * N ? a.b : a.c;
+      const uint32_t step = (uint32_t)from.t * sizeof(T);
+      const bool in = id < ALL && t + row < end && n < a.states;
+      v[i] = get<T>(from.p + (b * from.b) * (int64_t)sizeof(T) + (int64_t)t * step, in ? row * step + n * (uint32_t)sizeof(T) : kOutside, 0);
+    }
+  }
+  __device__ void store(float* lds) const {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int id = threadIdx.x + i * BLOCK;
+      if (id < ALL) lds[id / N % K * 2 * N + id / (K * N) * N + id % N] = to_f32(v[i]);
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+inline qds_status validate_scan(const qds_scan_config* c, bool step) {
+  if (!c || c->abi_version != QDS_ABI_VERSION) return QDS_ERR_INVALID_ARG;
+  if (c->dtype < QDS_F32 || c->dtype > QDS_F16) return QDS_ERR_INVALID_ARG;
+  if (c->batch < 0 || (!step && (c->length < 0 || c->length >= (1 << 30)))) return QDS_ERR_INVALID_ARG;
+  if (c->width < 1 || c->width > (1 << 20) || c->states < 1) return QDS_ERR_INVALID_ARG;
+  if (c->states > kScanStates) return QDS_ERR_UNSUPPORTED;
+  return QDS_OK;
+}
+// Rows that a scan reads or writes are from 0 to 2^23 elements apart (a single row's stride
+// means nothing and is set to 0).
+inline bool near_rows(qds_rows& r, int length) {
+  if (length < 2) r.stride[1] = 0;
+  return !r.data || (r.stride[1] >= 0 && r.stride[1] < (1 << 23));
+}
+inline int lane_states(const qds_scan_config* c) { return c->states <= 4 ? 1 : c->states <= 8 ? 2 : c->states <= 16 ? 4 : 8; }
+inline int block_rows(const qds_scan_config* c) { return lane_states(c) == 8 ? kScanRows<8> : kScanRows<4>; }
+inline int block_count(const qds_scan_config* c) { return (int)ceil_div(c->length, block_rows(c)); }
+
+// Rows of a segment and their number, for a kernel that wants `waves` waves.
+struct Cut {
+  int seg, segs;
+};
+inline Cut cut(const qds_scan_config* c, int64_t waves, int least) {
+  const int64_t whole = std::max<int64_t>(1, (int64_t)c->batch * ceil_div(c->width, 16));
+  const int64_t want = std::max<int64_t>(1, waves / whole);
+  const int k = block_rows(c);
+  int64_t seg = std::max<int64_t>(least, ceil_div(c->length, want));
+  seg = ceil_div(seg, k) * k;
+  return Cut{(int)seg, (int)std::max<int64_t>(1, ceil_div(c->length, seg))};
+}
+
+template <class F> void scan_instance(const qds_scan_config* c, F&& f) {
+  auto with_type = [&](auto S) {
+    if (c->dtype == QDS_F32) f(float(), S);
+    else if (c->dtype == QDS_BF16) f(bf16(), S);
+    else f(half(), S);
+  };
+  switch (lane_states(c)) {
+    case 1: return with_type(Int<1>{});
+    case 2: return with_type(Int<2>{});
+    case 4: return with_type(Int<4>{});
+    default: return with_type(Int<8>{});
+  }
+}
+
+inline ScanArgs scan_args(const qds_scan_config* c) {
+  ScanArgs a{};
+  a.batch = c->batch;
+  a.length = c->length;
+  a.width = c->width;
+  a.states = c->states;
+  a.blocks = block_count(c);
+  return a;
+}
+
+}  // namespace seq

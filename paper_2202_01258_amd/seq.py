@@ -8,12 +8,16 @@ elites, or rolled out in their place.  Its blocks are made of
   residual_norm        root-mean-square norm with the residual's addition
   window_attention     attention over a sliding window whose first tokens stay visible
   decay_attention      linear attention with a decay for each head
+  causal_conv          a short convolution over the rows, for each column
+  selective_scan       a state space scan whose steps and inputs the tokens choose
+  branch_norm          the norms after and before a block with its gate and the residual's scale
+  dropout              from a counter: its mask is never stored
 
 Each is differentiable under torch's autograd.  The calls below them are the
 plain ones: `*_forward` and `*_backward` for programs that keep their own
 tape, `residual_norm_fp8` for an 8-bit output, and `window_attention_step`
-(with `window_cache` and `window_cache_fill`) and `decay_attention_step` for
-rollouts, one token at a time.
+(with `window_cache` and `window_cache_fill`), `decay_attention_step`,
+`causal_conv_step` and `selective_scan_step` for rollouts, one token at a time.
 
 Argument marshalling only: outputs and scratch memory are torch tensors, work
 is enqueued on torch's current stream of the tensors' device, nothing waits for
@@ -21,6 +25,9 @@ the GPU, and there is no fallback.  Tensors are used on that stream alone; a
 tensor made on another stream has to be synchronised with it first, as for any
 torch operation.  Attention takes bfloat16 or float16 tensors whose rows start
 at multiples of 16 bytes and are less than 2^23 elements apart; others are copied first.
+The other operators take float32, too, and rows of any alignment; they copy tensors whose
+columns are apart (the scan those with rows 2^23 elements apart or more, dropout those
+that are not contiguous).
 """
 from __future__ import annotations
 
@@ -42,6 +49,11 @@ EXPORTS = ["qds_residual_norm", "qds_residual_norm_fp8", "qds_residual_norm_back
            "qds_window_backward", "qds_window_step_workspace", "qds_window_step",
            "qds_window_cache_fill", "qds_decay_forward_workspace", "qds_decay_forward",
            "qds_decay_backward_workspace", "qds_decay_backward", "qds_decay_step",
+           "qds_causal_conv", "qds_causal_conv_backward_workspace", "qds_causal_conv_backward",
+           "qds_causal_conv_step", "qds_selective_scan_marks", "qds_selective_scan_workspace",
+           "qds_selective_scan", "qds_selective_scan_backward_workspace",
+           "qds_selective_scan_backward", "qds_selective_scan_step", "qds_branch_norm",
+           "qds_branch_norm_backward_workspace", "qds_branch_norm_backward", "qds_dropout",
            "qds_status_str"]
 
 
@@ -67,6 +79,33 @@ class QdsDecayConfig(C.Structure):
     _fields_ = [("abi_version", C.c_uint32), ("dtype", C.c_int32), ("batch", C.c_int32),
                 ("length", C.c_int32), ("heads", C.c_int32), ("dim_k", C.c_int32),
                 ("dim_v", C.c_int32), ("scale", C.c_float)]
+
+
+class QdsRows(C.Structure):
+    # stride[0], stride[1] of the C struct
+    _fields_ = [("data", C.c_void_p), ("stride_b", C.c_int64), ("stride_t", C.c_int64)]
+
+
+class QdsConvConfig(C.Structure):
+    _fields_ = [("abi_version", C.c_uint32), ("dtype", C.c_int32), ("weight_dtype", C.c_int32),
+                ("batch", C.c_int32), ("length", C.c_int32), ("width", C.c_int32),
+                ("taps", C.c_int32), ("silu", C.c_int32)]
+
+
+class QdsScanConfig(C.Structure):
+    _fields_ = [("abi_version", C.c_uint32), ("dtype", C.c_int32), ("batch", C.c_int32),
+                ("length", C.c_int32), ("width", C.c_int32), ("states", C.c_int32)]
+
+
+class QdsBranchConfig(C.Structure):
+    _fields_ = [("abi_version", C.c_uint32), ("dtype", C.c_int32), ("weight_dtype", C.c_int32),
+                ("width", C.c_int32), ("rows", C.c_int64), ("eps", C.c_float),
+                ("residual_scale", C.c_float)]
+
+
+class QdsDropoutConfig(C.Structure):
+    _fields_ = [("abi_version", C.c_uint32), ("dtype", C.c_int32), ("elements", C.c_int64),
+                ("threshold", C.c_uint32), ("site", C.c_uint32)]
 
 
 class SeqError(RuntimeError):
@@ -104,6 +143,23 @@ def lib():
         L.qds_decay_backward_workspace.argtypes = [D, B]
         L.qds_decay_backward.argtypes = [D, V, V, V, V, P, P, P, P, V, V, V, P, P, U, P]
         L.qds_decay_step.argtypes = [D, V, V, V, P, P, V, P, P]
+        R, K, S = QdsRows, C.POINTER(QdsConvConfig), C.POINTER(QdsScanConfig)
+        L.qds_causal_conv.argtypes = [K, R, P, P, P, P, R, P, P]
+        L.qds_causal_conv_backward_workspace.argtypes = [K, B]
+        L.qds_causal_conv_backward.argtypes = [K, R, R, P, P, P, P, P, R, P, P, P, P, U, P]
+        L.qds_causal_conv_step.argtypes = [K, R, P, P, P, R, P, P]
+        L.qds_selective_scan_marks.argtypes = [S, B]
+        L.qds_selective_scan_workspace.argtypes = [S, B]
+        L.qds_selective_scan.argtypes = [S, R, R, P, R, R, P, R, P, P, P, R, P, P, P, U, P]
+        L.qds_selective_scan_backward_workspace.argtypes = [S, B]
+        L.qds_selective_scan_backward.argtypes = [S, R, R, R, P, R, R, P, R, P, P, P, P, R, R, P, R, R, P, R, P,
+                                                  P, P, U, P]
+        L.qds_selective_scan_step.argtypes = [S, R, R, P, R, R, P, R, P, P, R, P, P]
+        L.qds_branch_norm.argtypes = [C.POINTER(QdsBranchConfig), P, I, P, I, P, I, P, P, P, P, P, P]
+        L.qds_branch_norm_backward_workspace.argtypes = [C.POINTER(QdsBranchConfig), B]
+        L.qds_branch_norm_backward.argtypes = [C.POINTER(QdsBranchConfig), P, I, P, I, P, I, P, I, P, I, P, P, P,
+                                               P, P, P, P, P, P, U, P]
+        L.qds_dropout.argtypes = [C.POINTER(QdsDropoutConfig), P, P, P, P, P]
         L.qds_status_str.argtypes = [C.c_int]
         L.qds_status_str.restype = C.c_char_p
         for name in EXPORTS[:-1]:
@@ -541,6 +597,365 @@ def decay_attention_step(q, k, v, log_decay, state, scale=None, out_state=None):
 
 
 # ---------------------------------------------------------------------------
+# Short causal convolution
+# ---------------------------------------------------------------------------
+def _columns(t):
+    """`t` with contiguous columns: itself, or a copy."""
+    return t if t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
+
+
+def _near(t):
+    """`t` with contiguous columns and rows that are near enough for the scan: itself, or a copy."""
+    t = _columns(t)
+    return t if t.dim() < 3 or t.stride(1) < _FAR or t.shape[1] < 2 else t.clone(memory_format=torch.contiguous_format)
+
+
+_NO_ROWS = QdsRows(None, 0, 0)
+
+
+def _row_view(t):
+    """A [batch, rows, width] or [batch, width] tensor as qds_rows."""
+    if t is None:
+        return _NO_ROWS
+    s = t.stride()
+    return QdsRows(t.data_ptr(), s[0], s[1] if len(s) == 3 else 0)
+
+
+def _sig(t):
+    return None if t is None else (t.shape, t.dtype, t.device)
+
+
+def _written(name, t, ref, shape, dtype):
+    """A state that a step writes."""
+    _like(name, t, ref, shape, dtype)
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous")
+
+
+def _conv_setup(x, weight, bias, silu, rows, query=None):
+    """Checks x [batch, rows, width] (or without rows), weight and bias, and makes the plan."""
+    key = ("conv", x.shape, x.dtype, x.device, _sig(weight), _sig(bias), silu, rows, query)
+    plan = _plans.get(key)
+    if plan is not None:
+        return plan
+    _on_gpu(x, "x")
+    code = _code(x, "x")
+    if x.dim() != (3 if rows else 2) or x.shape[-1] < 1:
+        raise ValueError("x: [batch, rows, width]" if rows else "x: [batch, width]")
+    width = x.shape[-1]
+    wcode = _code(weight, "weight")
+    if wcode != F32 and wcode != code:
+        raise ValueError(f"weight is {weight.dtype}: float32 or x's {x.dtype}")
+    if weight.device != x.device or weight.dim() != 2 or weight.shape[1] != width or not 1 <= weight.shape[0] <= 8:
+        raise ValueError(f"weight: [taps, {width}] on {x.device}, of 1 to 8 taps")
+    if bias is not None:
+        _like("bias", bias, weight, (width,))
+    return _remember(key, _plan(QdsConvConfig, query, code, wcode, x.shape[0], x.shape[1] if rows else 0, width,
+                                weight.shape[0], int(bool(silu))))
+
+
+def _conv_state(name, t, c, ref):
+    if t is None:
+        return None
+    _like(name, t, ref, (c.batch, c.taps - 1, c.width))
+    return t.contiguous()
+
+
+def causal_conv_forward(x, weight, bias=None, state=None, lengths=None, silu: bool = True):
+    """p_t = bias + sum_k weight[k] x_{t - taps + 1 + k} for each column of x [batch, rows,
+    width]; y = p sigmoid(p), or p without `silu`.  `weight` [taps, width] (1 to 8 taps) and
+    `bias` [width] are float32 or of x's type.  `state` [batch, taps - 1, width] (x's type)
+    holds the rows before the first, the oldest first; None: 0.  `lengths` (int32 [batch]):
+    rows of each batch element; what is behind them is not read and gets 0.
+
+    Returns y and the state behind the last row."""
+    c, cfg, _ = _conv_setup(x, weight, bias, silu, True)
+    state = _conv_state("state", state, c, x)
+    lengths = _lengths(lengths, c.batch, x)
+    x, weight, bias = _columns(x), weight.contiguous(), None if bias is None else bias.contiguous()
+    y, last = x.new_empty(x.shape), x.new_empty((c.batch, c.taps - 1, c.width))
+    with _on(x):
+        _check(lib().qds_causal_conv(cfg, _row_view(x), weight.data_ptr(), _ptr(bias), _ptr(state), _ptr(lengths),
+                                     _row_view(y), last.data_ptr(), _stream(x)), "qds_causal_conv")
+    return y, last
+
+
+def causal_conv_backward(dy, x, weight, bias=None, state=None, dlast=None, lengths=None, silu: bool = True):
+    """Gradients from those of y and of the last state (`dlast`; None: 0): returns dx, dweight,
+    dbias (None without a bias) and that of the first state (also where `state` is None)."""
+    c, cfg, size = _conv_setup(x, weight, bias, silu, True, "qds_causal_conv_backward_workspace")
+    _like("dy", dy, x, x.shape)
+    state, dlast = _conv_state("state", state, c, x), _conv_state("dlast", dlast, c, x)
+    lengths = _lengths(lengths, c.batch, x)
+    dy, x, weight = _columns(dy), _columns(x), weight.contiguous()
+    bias = None if bias is None else bias.contiguous()
+    dx, dfirst = x.new_empty(x.shape), x.new_empty((c.batch, c.taps - 1, c.width))
+    dw, db = weight.new_empty(weight.shape), None if bias is None else bias.new_empty(bias.shape)
+    with _on(x):
+        ws = _scratch(size, x)
+        _check(lib().qds_causal_conv_backward(
+            cfg, _row_view(dy), _row_view(x), weight.data_ptr(), _ptr(bias), _ptr(state), _ptr(dlast), _ptr(lengths),
+            _row_view(dx), dw.data_ptr(), _ptr(db), dfirst.data_ptr(), _ptr(ws), size, _stream(x)),
+            "qds_causal_conv_backward")
+    return dx, dw, db, dfirst
+
+
+def causal_conv_step(x, weight, bias, state, silu: bool = True, out_state=None):
+    """One row x [batch, width] of each batch element.  Writes the new state into `out_state`
+    (by default into `state` itself) and returns y [batch, width] and that state."""
+    c, cfg, _ = _conv_setup(x, weight, bias, silu, False)
+    out_state = state if out_state is None else out_state
+    shape = (c.batch, c.taps - 1, c.width)
+    _written("state", state, x, shape, x.dtype)
+    if out_state is not state:
+        _written("out_state", out_state, x, shape, x.dtype)
+    x, weight, bias = _columns(x), weight.contiguous(), None if bias is None else bias.contiguous()
+    y = x.new_empty(x.shape)
+    with _on(x):
+        _check(lib().qds_causal_conv_step(cfg, _row_view(x), weight.data_ptr(), _ptr(bias), state.data_ptr(),
+                                          _row_view(y), out_state.data_ptr(), _stream(x)), "qds_causal_conv_step")
+    return y, out_state
+
+
+# ---------------------------------------------------------------------------
+# Selective state space scan
+# ---------------------------------------------------------------------------
+def _scan_setup(u, delta, a, b, c, skip, gate, bias, rows, query=None):
+    key = ("scan", u.shape, u.dtype, u.device, _sig(delta), _sig(a), _sig(b), _sig(c), _sig(skip), _sig(gate),
+           _sig(bias), rows, query)
+    plan = _plans.get(key)
+    if plan is not None:
+        return plan
+    _on_gpu(u, "u")
+    code = _code(u, "u")
+    if u.dim() != (3 if rows else 2) or u.shape[-1] < 1:
+        raise ValueError("u: [batch, rows, width]" if rows else "u: [batch, width]")
+    width = u.shape[-1]
+    if a.dim() != 2 or not 1 <= a.shape[1] <= 32:
+        raise ValueError(f"a: [{width}, states], of 1 to 32 states")
+    _like("a", a, u, (width, a.shape[1]), torch.float32)
+    _like("delta", delta, u, u.shape)
+    _like("b", b, u, (*u.shape[:-1], a.shape[1]))
+    _like("c", c, u, b.shape)
+    if gate is not None:
+        _like("gate", gate, u, u.shape)
+    for name, t in (("skip", skip), ("bias", bias)):
+        if t is not None:
+            _like(name, t, u, (width,), torch.float32)
+    return _remember(key, _plan(QdsScanConfig, query, code, u.shape[0], u.shape[1] if rows else 0, width, a.shape[1]))
+
+
+def _scan_state(name, t, cfg, ref):
+    if t is None:
+        return None
+    _like(name, t, ref, (cfg.batch, cfg.width, cfg.states), torch.float32)
+    return t.contiguous()
+
+
+def _dense(t):
+    return None if t is None else t.contiguous()
+
+
+def selective_scan_forward(u, delta, a, b, c, skip=None, gate=None, bias=None, state=None, lengths=None,
+                           keep: bool = False):
+    """dt = log(1 + e^(delta + bias)), h_t[n] = e^(dt a[n]) h_{t-1}[n] + dt u_t b_t[n],
+    y_t = sum_n c_t[n] h_t[n] + skip u_t for each column of u and delta [batch, rows, width],
+    with b and c [batch, rows, states] (1 to 32 states) for all columns; o = y gate
+    sigmoid(gate), or y without a gate (u's shape).  `a` [width, states], `skip` and `bias`
+    [width] are float32, and so is `state` [batch, width, states], h before the first row (None:
+    0).  `lengths` as for causal_conv_forward.  All arithmetic is float32.
+
+    Rows that are not finite reach the rows behind them (those of b and c in every column), as
+    in the definition.
+
+    Returns o, the state behind the last row, and with `keep` what selective_scan_backward
+    needs of this pass (else None)."""
+    args = (u, delta, a, b, c, skip, gate, bias, True)
+    cfg, ref, size = _scan_setup(*args, "qds_selective_scan_workspace")
+    state = _scan_state("state", state, cfg, u)
+    lengths = _lengths(lengths, cfg.batch, u)
+    u, delta, b, c = _near(u), _near(delta), _near(b), _near(c)
+    a, skip, bias, gate = a.contiguous(), _dense(skip), _dense(bias), None if gate is None else _near(gate)
+    o = u.new_empty(u.shape)
+    last = u.new_empty((cfg.batch, cfg.width, cfg.states), dtype=torch.float32)
+    with _on(u):
+        ws = _scratch(size, u)
+        marks = u.new_empty(_scan_setup(*args, "qds_selective_scan_marks")[2], dtype=torch.uint8) if keep else None
+        _check(lib().qds_selective_scan(
+            ref, _row_view(u), _row_view(delta), a.data_ptr(), _row_view(b), _row_view(c), _ptr(skip), _row_view(gate),
+            _ptr(bias), _ptr(state), _ptr(lengths), _row_view(o), last.data_ptr(), _ptr(marks), _ptr(ws), size,
+            _stream(u)), "qds_selective_scan")
+    return o, last, marks
+
+
+def selective_scan_backward(do, u, delta, a, b, c, marks, skip=None, gate=None, bias=None, dlast=None, lengths=None):
+    """Gradients from those of o and of the last state (`dlast`; None: 0), with what the forward
+    call saw and kept: returns du, ddelta, da, db, dc, dskip, dgate, dbias (None for those that
+    are) and that of the first state."""
+    args = (u, delta, a, b, c, skip, gate, bias, True)
+    cfg, ref, size = _scan_setup(*args, "qds_selective_scan_backward_workspace")
+    _like("do", do, u, u.shape)
+    _like("marks", marks, u, (_scan_setup(*args, "qds_selective_scan_marks")[2],), torch.uint8)
+    dlast = _scan_state("dlast", dlast, cfg, u)
+    lengths = _lengths(lengths, cfg.batch, u)
+    do, u, delta, b, c = _near(do), _near(u), _near(delta), _near(b), _near(c)
+    a, skip, bias, gate = a.contiguous(), _dense(skip), _dense(bias), None if gate is None else _near(gate)
+    du, ddelta, da = u.new_empty(u.shape), u.new_empty(u.shape), a.new_empty(a.shape)
+    db, dc = b.new_empty(b.shape), c.new_empty(c.shape)
+    dgate = None if gate is None else u.new_empty(u.shape)
+    dskip, dbias = (None if t is None else t.new_empty(t.shape) for t in (skip, bias))
+    dfirst = a.new_empty((cfg.batch, cfg.width, cfg.states))
+    with _on(u):
+        ws = _scratch(size, u)
+        _check(lib().qds_selective_scan_backward(
+            ref, _row_view(do), _row_view(u), _row_view(delta), a.data_ptr(), _row_view(b), _row_view(c), _ptr(skip),
+            _row_view(gate), _ptr(bias), marks.data_ptr(), _ptr(dlast), _ptr(lengths), _row_view(du),
+            _row_view(ddelta), da.data_ptr(), _row_view(db), _row_view(dc), _ptr(dskip), _row_view(dgate), _ptr(dbias),
+            dfirst.data_ptr(), _ptr(ws), size, _stream(u)), "qds_selective_scan_backward")
+    return du, ddelta, da, db, dc, dskip, dgate, dbias, dfirst
+
+
+def selective_scan_step(u, delta, a, b, c, state, skip=None, gate=None, bias=None, out_state=None):
+    """One row of each batch element: u, delta, gate [batch, width], b, c [batch, states].
+    Writes the new state into `out_state` (by default into `state` itself) and returns
+    o [batch, width] and that state."""
+    cfg, ref, _ = _scan_setup(u, delta, a, b, c, skip, gate, bias, False)
+    out_state = state if out_state is None else out_state
+    shape = (cfg.batch, cfg.width, cfg.states)
+    _written("state", state, u, shape, torch.float32)
+    if out_state is not state:
+        _written("out_state", out_state, u, shape, torch.float32)
+    u, delta, b, c = _columns(u), _columns(delta), _columns(b), _columns(c)
+    a, skip, bias, gate = a.contiguous(), _dense(skip), _dense(bias), None if gate is None else _columns(gate)
+    o = u.new_empty(u.shape)
+    with _on(u):
+        _check(lib().qds_selective_scan_step(
+            ref, _row_view(u), _row_view(delta), a.data_ptr(), _row_view(b), _row_view(c), _ptr(skip), _row_view(gate),
+            _ptr(bias), state.data_ptr(), _row_view(o), out_state.data_ptr(), _stream(u)), "qds_selective_scan_step")
+    return o, out_state
+
+
+# ---------------------------------------------------------------------------
+# Norms after and before a block, its gate, the residual's scale
+# ---------------------------------------------------------------------------
+def _branch_setup(x, gate, residual, branch_weight, weight, residual_scale, eps, query=None):
+    key = ("branch", x.shape, x.dtype, x.device, _sig(gate), _sig(residual), _sig(branch_weight), _sig(weight),
+           residual_scale, eps, query)
+    plan = _plans.get(key)
+    if plan is not None:
+        return plan
+    _on_gpu(x, "x")
+    code = _code(x, "x")
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError("x has no columns")
+    width = x.shape[-1]
+    _like("residual", residual, x, x.shape)
+    if gate is not None:
+        _like("gate", gate, x, x.shape)
+    if weight.device != x.device or weight.shape != (width,):
+        raise ValueError(f"weight: [{width}] on {x.device}")
+    wcode = _code(weight, "weight")
+    if wcode != F32 and wcode != code:
+        raise ValueError(f"weight is {weight.dtype}: float32 or x's {x.dtype}")
+    _like("branch_weight", branch_weight, weight, (width,))
+    return _remember(key, _plan(QdsBranchConfig, query, code, wcode, width, x.numel() // width, eps, residual_scale))
+
+
+def branch_norm_forward(x, gate, residual, branch_weight, weight, residual_scale: float = 1.0, eps: float = 1e-6):
+    """The end of a block and the norm in front of the next, over the last dimension:
+    n = x (mean(x^2) + eps)^(-1/2) branch_weight, h = residual_scale residual + gate sigmoid(gate) n
+    (`gate` None: + n), y = h (mean(h^2) + eps)^(-1/2) weight.  x, gate and residual have one
+    shape and type; both weights are float32 or of x's type.
+
+    Returns y, h (x's type and shape) and the factors of both norms (float32 [2, ...])."""
+    _, cfg, _ = _branch_setup(x, gate, residual, branch_weight, weight, residual_scale, eps)
+    width = x.shape[-1]
+    x2, r2, g2 = _norm_rows(x, width), _norm_rows(residual, width), None if gate is None else _norm_rows(gate, width)
+    w1, w2 = branch_weight.contiguous(), weight.contiguous()
+    y, h = x.new_empty(x.shape), x.new_empty(x.shape)
+    rstds = x.new_empty((2, *x.shape[:-1]), dtype=torch.float32)
+    with _on(x):
+        _check(lib().qds_branch_norm(
+            cfg, x2.data_ptr(), x2.stride(0), _ptr(g2), 0 if g2 is None else g2.stride(0), r2.data_ptr(), r2.stride(0),
+            w1.data_ptr(), w2.data_ptr(), y.data_ptr(), h.data_ptr(), rstds.data_ptr(), _stream(x)), "qds_branch_norm")
+    return y, h, rstds
+
+
+def branch_norm_backward(dy, dh, x, gate, residual, rstds, branch_weight, weight, residual_scale: float = 1.0):
+    """Gradients from those of y and of h (`dh` may be None), with what the forward call saw and
+    gave: returns dx, dgate (None without a gate), dresidual, dbranch_weight and dweight."""
+    c, cfg, size = _branch_setup(x, gate, residual, branch_weight, weight, residual_scale, 0.0,
+                                 "qds_branch_norm_backward_workspace")
+    _like("dy", dy, x, x.shape)
+    _like("rstds", rstds, x, (2, *x.shape[:-1]), torch.float32)
+    x2, r2, dy2 = _norm_rows(x, c.width), _norm_rows(residual, c.width), _norm_rows(dy, c.width)
+    g2 = dh2 = None
+    if gate is not None:
+        g2 = _norm_rows(gate, c.width)
+    if dh is not None:
+        _like("dh", dh, x, x.shape)
+        dh2 = _norm_rows(dh, c.width)
+    rstds, w1, w2 = rstds.contiguous(), branch_weight.contiguous(), weight.contiguous()
+    dx, dr, dg = x.new_empty(x.shape), x.new_empty(x.shape), None if gate is None else x.new_empty(x.shape)
+    dw1, dw2 = weight.new_empty(weight.shape), weight.new_empty(weight.shape)
+    with _on(x):
+        ws = _scratch(size, x)
+        _check(lib().qds_branch_norm_backward(
+            cfg, dy2.data_ptr(), dy2.stride(0), _ptr(dh2), 0 if dh2 is None else dh2.stride(0), x2.data_ptr(),
+            x2.stride(0), _ptr(g2), 0 if g2 is None else g2.stride(0), r2.data_ptr(), r2.stride(0), rstds.data_ptr(),
+            w1.data_ptr(), w2.data_ptr(), dx.data_ptr(), _ptr(dg), dr.data_ptr(), dw1.data_ptr(), dw2.data_ptr(),
+            _ptr(ws), size, _stream(x)), "qds_branch_norm_backward")
+    return dx, dg, dr, dw1, dw2
+
+
+# ---------------------------------------------------------------------------
+# Dropout from a counter
+# ---------------------------------------------------------------------------
+def dropout_rng(seed: int, step: int = 0, device="cuda:0"):
+    """The state of a program's dropouts: int64 [seed, step] on the device.  The program adds 1
+    to the step after each backward pass; a captured graph reads it at each replay."""
+    return torch.tensor([seed, step], dtype=torch.int64, device=device)
+
+
+def _dropout_setup(x, rng, p, site, residual):
+    key = ("dropout", x.shape, x.dtype, x.device, _sig(rng), p, site, _sig(residual))
+    plan = _plans.get(key)
+    if plan is not None:
+        return plan
+    _on_gpu(x, "x")
+    code = _code(x, "x")
+    if not 0.0 <= p < 1.0 or int(p * 65536 + 0.5) > 65535:
+        raise ValueError(f"p: a probability below 1 - 2^-17, not {p}")
+    if not 0 <= site < 1 << 32:
+        raise ValueError(f"site: 0 to 2^32 - 1, not {site}")
+    _like("rng", rng, x, (2,), torch.int64)
+    if residual is not None:
+        _like("residual", residual, x, x.shape)
+    cfg = QdsDropoutConfig(ABI_VERSION, code, x.numel(), int(p * 65536 + 0.5), site)
+    return _remember(key, (cfg, C.byref(cfg)))
+
+
+def dropout_forward(x, rng, p: float, site: int = 0, residual=None):
+    """y = residual + (x / (1 - p) where kept, else 0), without `residual` the latter alone.
+    Which elements are kept (each with probability 1 - p, in steps of 2^-16) follows from `rng`
+    (dropout_rng), `site` (a number for each dropout of a program) and the element's place in x
+    alone; no mask is stored."""
+    _, cfg = _dropout_setup(x, rng, p, site, residual)
+    x, residual, rng = x.contiguous(), _dense(residual), rng.contiguous()
+    y = x.new_empty(x.shape)
+    with _on(x):
+        _check(lib().qds_dropout(cfg, x.data_ptr(), _ptr(residual), rng.data_ptr(), y.data_ptr(), _stream(x)),
+               "qds_dropout")
+    return y
+
+
+def dropout_backward(dy, rng, p: float, site: int = 0):
+    """The gradient of x from that of y, with the forward call's rng, p and site (the residual's
+    gradient is dy)."""
+    return dropout_forward(dy, rng, p, site)
+
+
+# ---------------------------------------------------------------------------
 # Under autograd
 # ---------------------------------------------------------------------------
 _functions = None
@@ -605,7 +1020,77 @@ def _autograd():
                                                           ctx.scale)
             return dq, dk, dv, None, None if state is None else dfirst, None, None
 
-    _functions = (ResidualNorm, WindowAttention, DecayAttention)
+    class CausalConv(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, state, lengths, silu):
+            y, last = causal_conv_forward(x, weight, bias, state, lengths, silu)
+            ctx.save_for_backward(x, weight, bias, state, lengths)
+            ctx.silu = silu
+            ctx.set_materialize_grads(False)
+            return y, last
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dy, dlast):
+            x, weight, bias, state, lengths = ctx.saved_tensors
+            if dy is None:
+                dy = torch.zeros_like(x)
+            dx, dw, db, dfirst = causal_conv_backward(dy, x, weight, bias, state, dlast, lengths, ctx.silu)
+            return dx, dw, db, None if state is None else dfirst, None, None
+
+    class SelectiveScan(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, u, delta, a, b, c, skip, gate, bias, state, lengths):
+            o, last, marks = selective_scan_forward(u, delta, a, b, c, skip, gate, bias, state, lengths, keep=True)
+            ctx.save_for_backward(u, delta, a, b, c, skip, gate, bias, lengths, marks)
+            ctx.has_state = state is not None
+            ctx.set_materialize_grads(False)
+            return o, last
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, do, dlast):
+            u, delta, a, b, c, skip, gate, bias, lengths, marks = ctx.saved_tensors
+            if do is None:
+                do = torch.zeros_like(u)
+            du, ddelta, da, db, dc, dskip, dgate, dbias, dfirst = selective_scan_backward(
+                do, u, delta, a, b, c, marks, skip, gate, bias, dlast, lengths)
+            return du, ddelta, da, db, dc, dskip, dgate, dbias, dfirst if ctx.has_state else None, None
+
+    class BranchNorm(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, gate, residual, branch_weight, weight, residual_scale, eps):
+            y, h, rstds = branch_norm_forward(x, gate, residual, branch_weight, weight, residual_scale, eps)
+            ctx.save_for_backward(x, gate, residual, rstds, branch_weight, weight)
+            ctx.residual_scale = residual_scale
+            ctx.set_materialize_grads(False)
+            return y, h
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dy, dh):
+            x, gate, residual, rstds, branch_weight, weight = ctx.saved_tensors
+            if dy is None:
+                dy = torch.zeros_like(x)
+            return (*branch_norm_backward(dy, dh, x, gate, residual, rstds, branch_weight, weight,
+                                          ctx.residual_scale), None, None)
+
+    class Dropout(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, rng, p, site, residual):
+            ctx.save_for_backward(rng)
+            ctx.how = (p, site, residual is not None)
+            return dropout_forward(x, rng, p, site, residual)
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dy):
+            (rng,) = ctx.saved_tensors            # raises where the program has changed it since
+            p, site, has_residual = ctx.how
+            dx = dropout_backward(dy, rng, p, site) if ctx.needs_input_grad[0] else None
+            return dx, None, None, None, dy if has_residual else None
+
+    _functions = (ResidualNorm, WindowAttention, DecayAttention, CausalConv, SelectiveScan, BranchNorm, Dropout)
     return _functions
 
 
@@ -624,3 +1109,24 @@ def decay_attention(q, k, v, log_decay, state=None, lengths=None, scale=None):
     if log_decay.requires_grad:
         raise ValueError("log_decay is a constant of the layer: it has no gradient")
     return _autograd()[2].apply(q, k, v, log_decay, state, lengths, scale)
+
+
+def causal_conv(x, weight, bias=None, state=None, lengths=None, silu: bool = True):
+    """causal_conv_forward under autograd: returns y and the last state."""
+    return _autograd()[3].apply(x, weight, bias, state, lengths, silu)
+
+
+def selective_scan(u, delta, a, b, c, skip=None, gate=None, bias=None, state=None, lengths=None):
+    """selective_scan_forward under autograd: returns o and the last state."""
+    return _autograd()[4].apply(u, delta, a, b, c, skip, gate, bias, state, lengths)
+
+
+def branch_norm(x, gate, residual, branch_weight, weight, residual_scale: float = 1.0, eps: float = 1e-6):
+    """branch_norm_forward under autograd: returns y and h."""
+    return _autograd()[5].apply(x, gate, residual, branch_weight, weight, residual_scale, eps)
+
+
+def dropout(x, rng, p: float, site: int = 0, residual=None):
+    """dropout_forward under autograd: returns y.  `rng` has to be unchanged until the backward
+    pass is done (a changed one raises)."""
+    return _autograd()[6].apply(x, rng, p, site, residual)
