@@ -276,8 +276,9 @@ typedef struct {
   int32_t states;         /* 1 .. 32 (more: QDS_ERR_UNSUPPORTED)                    */
 } qds_scan_config;
 
-/* u, delta, gate, o: rows of `width`; b, c: rows of `states`.  a [width][states]
- * fp32; skip and bias [width] fp32 or null (0); gate.data null: o = y.  lengths as
+/* u, delta, gate: rows of `width`; b, c: rows of `states`; from 0 to 2^23
+ * elements apart (else QDS_ERR_UNSUPPORTED).  o [batch][length][width], contiguous.
+ * a [width][states] fp32; skip and bias [width] fp32 or null (0); gate.data null: o = y.  lengths as
  * for the convolution.  state_in null: 0.  state_out (may be null, or state_in):
  * h after row n - 1.  marks (null unless a backward pass follows, which needs
  * them; 256-byte aligned): states that the backward pass starts from, *bytes as
@@ -286,25 +287,26 @@ qds_status qds_selective_scan_marks(const qds_scan_config* c, uint64_t* bytes);
 qds_status qds_selective_scan_workspace(const qds_scan_config* c, uint64_t* bytes);
 qds_status qds_selective_scan(const qds_scan_config* c, qds_rows u, qds_rows delta, const float* a,
                               qds_rows b, qds_rows cc, const float* skip, qds_rows gate, const float* bias,
-                              const float* state_in, const int32_t* lengths, qds_rows o, float* state_out,
+                              const float* state_in, const int32_t* lengths, void* o, float* state_out,
                               void* marks, void* workspace, uint64_t workspace_bytes, void* stream);
 
-/* Gradients from do and dstate_out (null: 0).  du, ddelta, dgate: rows of `width`
- * (0 from row n on; dgate as gate); db, dc: rows of `states`, likewise; da, dskip,
- * dbias (the last two may be null) and dstate_in (may be null, or dstate_out) fp32. */
+/* Gradients from do and dstate_out (null: 0), contiguous: du, ddelta, dgate (null
+ * without a gate) [batch][length][width] and db, dc [batch][length][states] of dtype,
+ * 0 from row n on; da, dskip, dbias (the last two may be null) and dstate_in (may be
+ * null, or dstate_out) fp32. */
 qds_status qds_selective_scan_backward_workspace(const qds_scan_config* c, uint64_t* bytes);
 qds_status qds_selective_scan_backward(const qds_scan_config* c, qds_rows dout, qds_rows u, qds_rows delta,
                                        const float* a, qds_rows b, qds_rows cc, const float* skip,
                                        qds_rows gate, const float* bias, const void* marks,
-                                       const float* dstate_out, const int32_t* lengths, qds_rows du,
-                                       qds_rows ddelta, float* da, qds_rows db, qds_rows dc, float* dskip,
-                                       qds_rows dgate, float* dbias, float* dstate_in, void* workspace,
+                                       const float* dstate_out, const int32_t* lengths, void* du,
+                                       void* ddelta, float* da, void* db, void* dc, float* dskip,
+                                       void* dgate, float* dbias, float* dstate_in, void* workspace,
                                        uint64_t workspace_bytes, void* stream);
 
 /* One row of each batch element (stride[1] unused); state_out may be state_in. */
 qds_status qds_selective_scan_step(const qds_scan_config* c, qds_rows u, qds_rows delta, const float* a,
                                    qds_rows b, qds_rows cc, const float* skip, qds_rows gate,
-                                   const float* bias, const float* state_in, qds_rows o, float* state_out,
+                                   const float* bias, const float* state_in, void* o, float* state_out,
                                    void* stream);
 
 /* ------------------------------------------------------------------------

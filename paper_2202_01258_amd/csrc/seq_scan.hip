@@ -11,10 +11,11 @@ constexpr int kBlock = 256, kColumns = kBlock / 4;
 
 // One segment of 64 columns.  LOCAL: what the segment leaves behind when it starts from
 // zero, and the sum of its steps; otherwise outputs, marks and the last state.
-template <class T, int S, bool LOCAL> __global__ __launch_bounds__(kBlock) void k_scan(ScanArgs a) {
-  constexpr int K = kScanRows<S>, N = 4 * S, QUADS = K / 4;
+template <class T, int S, bool LOCAL, bool GATE> __global__ __launch_bounds__(kBlock) void k_scan(ScanArgs a) {
+  constexpr int K = kStageRows<S>, MARK = kScanRows<S>, N = 4 * S, QUADS = K / 4;
   SEQ_SHARED float bc[2][K * 2 * N];
   const int q = threadIdx.x & 3;
+  const Quad quad(q);
   const uint32_t item = blockIdx.x / (uint32_t)a.col_blocks;
   const int col = (blockIdx.x % (uint32_t)a.col_blocks) * kColumns + (threadIdx.x >> 2);
   const bool real = col < a.width;
@@ -38,45 +39,48 @@ template <class T, int S, bool LOCAL> __global__ __launch_bounds__(kBlock) void 
     load_states<S>(h, a.first ? a.first + b * a.width * a.states : nullptr, at, q, a.states);
   }
   float time = 0.0f;
+  Track<T> out(a.o, (int64_t)a.length * a.width, a.width, b, begin, q, at, real);
   if (begin < live) {
-    T u[QUADS], d[QUADS], z[QUADS];
-    Track<T> tu, td, tz, to;
-    tu.init(a.u, b, q, at);
-    td.init(a.delta, b, q, at);
-    if (!LOCAL) {
-      tz.init(a.gate, b, q, at);
-      to.init(a.o, b, q, at);
-    }
-    StagedRows<T, S, kBlock> rows;
+    uint32_t u[QUADS], d[QUADS], z[QUADS];
+    Track<T> tu(a.u, b, begin, q, at, real), td(a.delta, b, begin, q, at, real), tz(a.gate, b, begin, q, at, real);
+    StagedRows<T, S, K, kBlock> rows(a, b, begin);
+    float* marks = a.marks + (b * a.blocks + begin / MARK) * a.width * N;
     auto fetch = [&](int t) {
+      const Left left{live - t - q - 1};
 #pragma unroll
       for (int i = 0; i < QUADS; ++i) {
-        const bool in = t + 4 * i + q < live;
-        u[i] = tu.load(t, i, in);
-        d[i] = td.load(t, i, in);
-        if (!LOCAL && a.gate.p) z[i] = tz.load(t, i, in);
+        u[i] = tu.load(i, left);
+        d[i] = td.load(i, left);
+        if (GATE) z[i] = tz.load(i, left);
       }
-      rows.load(a, b, t, live);
+      rows.load(live - t);
+      tu.move(K);
+      td.move(K);
+      if (GATE) tz.move(K);
+      rows.move(K);
     };
     fetch(begin);
     rows.store(bc[0]);
     __syncthreads();
     int buffer = 0;
     for (int t = begin; t < live; t += K) {
+      const Left left{live - t - q - 1};
       float dt[QUADS], uu[QUADS], zz[QUADS];
 #pragma unroll
       for (int i = 0; i < QUADS; ++i) {
-        const bool in = t + 4 * i + q < live;
-        dt[i] = in ? softplus(to_f32(d[i]) + bias).dt : 0.0f;
-        uu[i] = to_f32(u[i]);
-        if (!LOCAL && a.gate.p) zz[i] = to_f32(z[i]);
+        dt[i] = left.keep(i, softplus(number<T>(d[i]) + bias).dt);
+        uu[i] = number<T>(u[i]);
+        if (GATE) zz[i] = number<T>(z[i]);
       }
       const bool more = t + K < live;
       if (more) fetch(t + K);
-      if (!LOCAL && a.marks && real) store_floats<S>(a.marks + ((b * a.blocks + t / K) * a.width + at) * N + q * S, h);
       const float* lds = bc[buffer] + q * S;
 #pragma unroll
       for (int i = 0; i < QUADS; ++i) {
+        if (!LOCAL && a.marks && 4 * i % MARK == 0) {
+          if (real && t + 4 * i < live) store_floats<S>(marks + (uint32_t)(at * N + q * S), h);
+          marks += (int64_t)a.width * N;
+        }
         const float x = dt[i] * uu[i];
         float y[4];
         auto row = [&](auto J) {
@@ -85,11 +89,10 @@ template <class T, int S, bool LOCAL> __global__ __launch_bounds__(kBlock) void 
           float bv[S], cv[S];
           load_floats<S>(bv, lds + (4 * i + j) * 2 * N);
           if (!LOCAL) load_floats<S>(cv, lds + (4 * i + j) * 2 * N + N);
-          y[j] = 0.0f;
 #pragma unroll
           for (int s = 0; s < S; ++s) {
             h[s] = fmaf(fast_exp2(dtj * rates[s]), h[s], xj * bv[s]);
-            if (!LOCAL) y[j] = fmaf(h[s], cv[s], y[j]);
+            if (!LOCAL) y[j] = s == 0 ? h[s] * cv[s] : fmaf(h[s], cv[s], y[j]);
           }
         };
         row(Int<0>{});
@@ -99,11 +102,12 @@ template <class T, int S, bool LOCAL> __global__ __launch_bounds__(kBlock) void 
         if (LOCAL) {
           time += dt[i];
         } else {
-          float o = fmaf(skip, uu[i], quad_rows(y, q));
-          if (a.gate.p) o *= zz[i] * sigmoid(zz[i]);
-          to.store(t, i, real && t + 4 * i + q < live, o);
+          float o = fmaf(skip, uu[i], quad_rows(y, quad));
+          if (GATE) o *= zz[i] * sigmoid(zz[i]);
+          out.store(i, left, o);
         }
       }
+      if (!LOCAL) out.move(K);
       if (more) {
         rows.store(bc[buffer ^ 1]);
         __syncthreads();
@@ -116,9 +120,11 @@ template <class T, int S, bool LOCAL> __global__ __launch_bounds__(kBlock) void 
     if (real) store_floats<S>(a.seg_state + place, h);
     if (real && q == 0) a.seg_time[(b * a.segs + seg) * a.width + at] = time;
   } else {
-    Track<T> to;
-    to.init(a.o, b, q, at);
-    for (int t = max(begin, live); t < end; t += 4) to.store(t, 0, real && t + q < end, 0.0f);
+    out = Track<T>(a.o, (int64_t)a.length * a.width, a.width, b, max(begin, live), q, at, real);
+    for (int t = max(begin, live); t < end; t += 4) {
+      out.store(0, Left{end - t - q - 1}, 0.0f);
+      out.move(4);
+    }
     if (seg == a.segs - 1 && a.last) store_states<S>(a.last + b * a.width * a.states, at, q, a.states, real, h);
   }
 }
@@ -178,15 +184,21 @@ template <class T, int S> __global__ __launch_bounds__(kBlock) void k_scan_step(
       const float z = to_f32(row_of<T>(a.gate, b, 0)[at]);
       o *= z * sigmoid(z);
     }
-    row_of<T>(a.o, b, 0)[at] = from_f32<T>(o);
+    ((T*)a.o)[column] = from_f32<T>(o);
   }
 }
 
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-constexpr int64_t kWaves = 2048;
-constexpr int kLeastRows = 64;
+#ifndef KW
+#define KW 8192
+#endif
+constexpr int64_t kWaves = KW;
+#ifndef KL
+#define KL 64
+#endif
+constexpr int kLeastRows = KL;
 
 Cut forward_cut(const qds_scan_config* c) { return cut(c, kWaves, kLeastRows); }
 uint64_t state_bytes(const qds_scan_config* c, int segs) {
@@ -223,14 +235,14 @@ extern "C" qds_status qds_selective_scan_workspace(const qds_scan_config* c, uin
 
 extern "C" qds_status qds_selective_scan(const qds_scan_config* c, qds_rows u, qds_rows delta, const float* a_,
                                          qds_rows b, qds_rows cc, const float* skip, qds_rows gate, const float* bias,
-                                         const float* state_in, const int32_t* lengths, qds_rows o, float* state_out,
+                                         const float* state_in, const int32_t* lengths, void* o, float* state_out,
                                          void* marks, void* workspace, uint64_t workspace_bytes, void* stream) {
   uint64_t need = 0;
   const qds_status st = qds_selective_scan_workspace(c, &need);
   if (st != QDS_OK) return st;
   if (c->batch == 0) return QDS_OK;
-  if (!a_ || (c->length > 0 && (!u.data || !delta.data || !b.data || !cc.data || !o.data))) return QDS_ERR_INVALID_ARG;
-  for (qds_rows* r : {&u, &delta, &b, &cc, &gate, &o})
+  if (!a_ || (c->length > 0 && (!u.data || !delta.data || !b.data || !cc.data || !o))) return QDS_ERR_INVALID_ARG;
+  for (qds_rows* r : {&u, &delta, &b, &cc, &gate})
     if (!near_rows(*r, c->length)) return QDS_ERR_UNSUPPORTED;
   if (((uintptr_t)marks & 255) || (need > 0 && (!workspace || ((uintptr_t)workspace & 255)))) return QDS_ERR_INVALID_ARG;
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
@@ -241,7 +253,7 @@ extern "C" qds_status qds_selective_scan(const qds_scan_config* c, qds_rows u, q
   a.b = rows(b);
   a.c = rows(cc);
   a.gate = rows(gate);
-  a.o = rows(o);
+  a.o = o;
   a.a = a_;
   a.skip = skip;
   a.bias = bias;
@@ -262,22 +274,23 @@ extern "C" qds_status qds_selective_scan(const qds_scan_config* c, qds_rows u, q
     constexpr int L = decltype(S)::value;
     const uint32_t across = (uint32_t)(a.batch * a.col_blocks);
     if (a.segs > 1) {
-      k_scan<T, L, true><<<across * (a.segs - 1), kBlock, 0, s>>>(a);
+      k_scan<T, L, true, false><<<across * (a.segs - 1), kBlock, 0, s>>>(a);
       k_scan_join<4 * L><<<(uint32_t)ceil_div((int64_t)a.batch * a.width * 4 * L, kBlock), kBlock, 0, s>>>(a);
     }
-    k_scan<T, L, false><<<across * a.segs, kBlock, 0, s>>>(a);
+    if (gate.data) k_scan<T, L, false, true><<<across * a.segs, kBlock, 0, s>>>(a);
+    else k_scan<T, L, false, false><<<across * a.segs, kBlock, 0, s>>>(a);
   });
   return launch_status();
 }
 
 extern "C" qds_status qds_selective_scan_step(const qds_scan_config* c, qds_rows u, qds_rows delta, const float* a_,
                                               qds_rows b, qds_rows cc, const float* skip, qds_rows gate,
-                                              const float* bias, const float* state_in, qds_rows o, float* state_out,
+                                              const float* bias, const float* state_in, void* o, float* state_out,
                                               void* stream) {
   const qds_status st = validate_scan(c, true);
   if (st != QDS_OK) return st;
   if (c->batch == 0) return QDS_OK;
-  if (!a_ || !u.data || !delta.data || !b.data || !cc.data || !o.data || !state_in || !state_out) return QDS_ERR_INVALID_ARG;
+  if (!a_ || !u.data || !delta.data || !b.data || !cc.data || !o || !state_in || !state_out) return QDS_ERR_INVALID_ARG;
   const int64_t columns = (int64_t)c->batch * c->width;
   if (columns >= (1 << 30)) return QDS_ERR_UNSUPPORTED;
   ScanArgs a = scan_args(c);
@@ -286,7 +299,7 @@ extern "C" qds_status qds_selective_scan_step(const qds_scan_config* c, qds_rows
   a.b = rows(b);
   a.c = rows(cc);
   a.gate = rows(gate);
-  a.o = rows(o);
+  a.o = o;
   a.a = a_;
   a.skip = skip;
   a.bias = bias;

@@ -20,7 +20,12 @@ constexpr int kScanStates = 32;                  // at most
 
 // Rows of a block.  The backward pass starts from the state in front of a block ("mark")
 // and keeps 2 K S numbers of it in registers.
-template <int S> constexpr int kScanRows = S <= 4 ? 16 : 8;
+#ifndef BK
+#define BK 8
+#endif
+template <int S> constexpr int kScanRows = S <= 4 ? BK : 8;
+// Rows whose b and c the forward pass has in LDS.
+template <int S> constexpr int kStageRows = S <= 4 ? 16 : 8;
 
 struct Rows {
   char* p;
@@ -32,7 +37,8 @@ template <class T> __device__ inline T* row_of(const Rows& r, int64_t b, int64_t
 }
 
 struct ScanArgs {
-  Rows u, delta, b, c, gate, o, dout, du, ddelta, db, dc, dgate;
+  Rows u, delta, b, c, gate, dout;
+  void *o, *du, *ddelta, *dgate, *db, *dc;       // contiguous
   const float *a, *skip, *bias, *first, *dlast;
   float *last, *dfirst, *da, *dskip, *dbias;
   float* marks;                                  // [batch][blocks][width][4 S]
@@ -52,17 +58,31 @@ __device__ inline int rows_in(const ScanArgs& a, int64_t b) {
 template <int CTRL> __device__ inline float lane_move(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
-template <int J> __device__ inline float quad_lane(float v) { return lane_move<J * 0x55>(v); }
+// A moved number is used by S instructions: kept from being merged into each of them, where it
+// would make each take the time of a move (4.4 cycles against 2.7).
+template <int J> __device__ inline float quad_lane(float v) {
+  float r = lane_move<J * 0x55>(v);
+  asm("" : "+v"(r));
+  return r;
+}
 __device__ inline float quad_sum(float v) {
   v += lane_move<0xB1>(v);
   return v + lane_move<0x4E>(v);
 }
-// Four rows' values in four lanes: lane q gets row q's sum over the quad.
-__device__ inline float quad_rows(const float* v, int q) {
-  const bool odd = q & 1, high = q & 2;
-  const float a = (odd ? v[1] : v[0]) + lane_move<0xB1>(odd ? v[0] : v[1]);
-  const float b = (odd ? v[3] : v[2]) + lane_move<0xB1>(odd ? v[2] : v[3]);
-  return (high ? b : a) + lane_move<0x4E>(high ? a : b);
+// a where the mask's bits are set, b elsewhere; a select by a mask in scalar registers takes longer.
+__device__ inline float pick(uint32_t mask, float a, float b) {
+  return __uint_as_float(__builtin_amdgcn_bitop3_b32(mask, __float_as_uint(a), __float_as_uint(b), 0xca));
+}
+// Four rows' values in four lanes: lane q gets row q's sum over the quad.  odd and high: all bits
+// set where bit 0 and bit 1 of q are.
+struct Quad {
+  uint32_t odd, high;
+  __device__ explicit Quad(int q) : odd(q & 1 ? ~0u : 0), high(q & 2 ? ~0u : 0) {}
+};
+__device__ inline float quad_rows(const float* v, Quad m) {
+  const float a = pick(m.odd, v[1], v[0]) + lane_move<0xB1>(pick(m.odd, v[0], v[1]));
+  const float b = pick(m.odd, v[3], v[2]) + lane_move<0xB1>(pick(m.odd, v[2], v[3]));
+  return pick(m.high, b, a) + lane_move<0x4E>(pick(m.high, a, b));
 }
 
 // log(1 + e^x) to an ulp or two for any x: log(1 + e) is formed as log(w) e / (w - 1) with
@@ -98,10 +118,17 @@ template <int S> __device__ inline void store_floats(float* p, const float* in) 
 }
 // One number by a buffer access: a scalar base, the lane's offset and a scalar offset in bytes.
 // From kOutside on a load gives 0 and a store does nothing.
-template <class T> __device__ inline T get(const char* base, uint32_t lane_at, uint32_t at) {
+template <class T> __device__ inline uint32_t get_bits(const char* base, uint32_t lane_at, uint32_t at) {
   const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, kBufferSize, kBufferFlags);
-  if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(buffer, lane_at, at, 0));
-  else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(buffer, lane_at, at, 0));
+  if constexpr (sizeof(T) == 4) return __builtin_amdgcn_raw_buffer_load_b32(buffer, lane_at, at, 0);
+  else return __builtin_amdgcn_raw_buffer_load_b16(buffer, lane_at, at, 0);
+}
+// The number that was loaded, a register each until here: left to itself the compiler joins two
+// 16-bit numbers in one register as soon as they are loaded, and so waits for memory there.
+template <class T> __device__ inline float number(uint32_t bits) {
+  asm volatile("" : "+v"(bits));
+  if constexpr (sizeof(T) == 4) return __uint_as_float(bits);
+  else return to_f32(__builtin_bit_cast(T, (uint16_t)bits));
 }
 template <class T> __device__ inline void put(char* base, uint32_t lane_at, uint32_t at, T v) {
   const auto buffer = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, kBufferSize, kBufferFlags);
@@ -114,49 +141,81 @@ template <class T> __device__ inline void put(char* base, uint32_t lane_at, uint
 template <int S> __device__ inline void load_states(float* out, const float* p, int at, int q, int states) {
 #pragma unroll
   for (int s = 0; s < S; ++s)
-    out[s] = get<float>((const char*)p, p && q * S + s < states ? (at * states + q * S) * 4u : kOutside, s * 4);
+    out[s] = __uint_as_float(get_bits<float>((const char*)p, p && q * S + s < states ? (at * states + q * S) * 4u : kOutside, s * 4));
 }
 template <int S> __device__ inline void store_states(float* p, int at, int q, int states, bool in, const float* v) {
 #pragma unroll
   for (int s = 0; s < S; ++s) put<float>((char*)p, in && q * S + s < states ? (at * states + q * S) * 4u : kOutside, s * 4, v[s]);
 }
 
-// A tensor's rows t + q, t + 4 + q, ... at a lane's column: the rows of an episode as a scalar
-// base, so that an access costs no 64-bit arithmetic in vector registers.  Rows are from 0 to
-// 2^23 elements apart.
-template <class T> struct Track {
-  char* p;
-  uint32_t step, lane_at;                        // bytes: from row to row, and the lane's
-  __device__ void init(const Rows& r, int64_t b, int q, int at) {
-    p = r.p + b * r.b * (int64_t)sizeof(T);
-    step = (uint32_t)r.t * sizeof(T);
-    lane_at = q * step + at * (uint32_t)sizeof(T);
-  }
-  __device__ T load(int t, int i, bool in) const { return get<T>(p + (int64_t)t * step, in ? lane_at : kOutside, 4 * i * step); }
-  __device__ void store(int t, int i, bool in, float v) const { put<T>(p + (int64_t)t * step, in ? lane_at : kOutside, 4 * i * step, from_f32<T>(v)); }
+// Which of a block's rows q, q + 4, ... an episode still has: rows left, less one, counted from a
+// lane's first.  Below 0 from a row on, where the sign bit makes an offset kOutside.
+struct Left {
+  int x;
+  __device__ int at(int i) const { return x - 4 * i; }
+  __device__ float keep(int i, float v) const { return __uint_as_float(__float_as_uint(v) & ~(uint32_t)(at(i) >> 31)); }
+  __device__ uint32_t offset(int i, uint32_t lane_at) const { return lane_at | ((uint32_t)at(i) & kOutside); }
 };
 
-// K rows of b and c on their way to LDS: [K][2][4 S], what is behind `end` or the states is 0.
-template <class T, int S, int BLOCK> struct StagedRows {
-  static constexpr int N = 4 * S, K = kScanRows<S>, ALL = K * 2 * N, EACH = (ALL + BLOCK - 1) / BLOCK;
-  static_assert(K * N % 64 == 0, "a wave has rows of b or of c, not of both");
-  T v[EACH];
-  __device__ void load(const ScanArgs& a, int64_t b, int t, int end) {
+// A tensor's rows t + q, t + 4 + q, ... at a lane's column, t a scalar that goes up or down: an
+// access costs one vector instruction beside it and no 64-bit arithmetic.  Rows are from 0 to
+// 2^23 elements apart.  Columns that are not real are outside.
+template <class T> struct Track {
+  char* p;                                       // of row t
+  uint32_t step, lane_at;                        // bytes: from row to row, and the lane's
+  __device__ Track(const void* base, int64_t batch_stride, int64_t row_stride, int64_t b, int t, int q, int at, bool real) {
+    step = (uint32_t)row_stride * sizeof(T);
+    p = (char*)base + b * batch_stride * (int64_t)sizeof(T) + (int64_t)t * step;
+    lane_at = real ? q * step + at * (uint32_t)sizeof(T) : kOutside;
+  }
+  __device__ Track(const Rows& r, int64_t b, int t, int q, int at, bool real) : Track(r.p, r.b, r.t, b, t, q, at, real) {}
+  __device__ void move(int rows) { p += (int64_t)rows * step; }
+  // a multiple of the step, formed where it is needed: scalar registers are short, too
+  __device__ uint32_t ahead(int i) const {
+    uint32_t s = step;
+    if (i > 0) asm volatile("" : "+s"(s));
+    return 4 * i * s;
+  }
+  __device__ uint32_t load(int i, Left left) const { return get_bits<T>(p, left.offset(i, lane_at), ahead(i)); }
+  __device__ void store(int i, Left left, float v) const { put<T>(p, left.offset(i, lane_at), ahead(i), from_f32<T>(v)); }
+};
+
+// K rows of b and c on their way to LDS: [K][2][4 S], what is behind the episode or the states is 0.
+// A wave has rows of b or of c, not of both, so that its base is a scalar.
+template <class T, int S, int K, int BLOCK> struct StagedRows {
+  static constexpr int N = 4 * S, PART = (K * N + 63) / 64 * 64, EACH = (2 * PART + BLOCK - 1) / BLOCK;
+  const char* p[EACH];
+  uint32_t step[EACH], lane_at[EACH];
+  uint32_t v[EACH];
+  __device__ StagedRows(const ScanArgs& a, int64_t b, int t) {
     const int wave = wave_index() * 64;
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      const int id = threadIdx.x + i * BLOCK, row = id / N % K, n = id % N;
-      const Rows& from = wave + i * BLOCK < K * N ? a.b : a.c;
-      const uint32_t step = (uint32_t)from.t * sizeof(T);
-      const bool in = id < ALL && t + row < end && n < a.states;
-      v[i] = get<T>(from.p + (b * from.b) * (int64_t)sizeof(T) + (int64_t)t * step, in ? row * step + n * (uint32_t)sizeof(T) : kOutside, 0);
+      const int k = (threadIdx.x + i * BLOCK) % PART;
+      const bool first = wave + i * BLOCK < PART;
+      const int64_t stride = first ? a.b.t : a.c.t, batch = first ? a.b.b : a.c.b;
+      step[i] = (uint32_t)stride * sizeof(T);
+      p[i] = (first ? a.b.p : a.c.p) + b * batch * (int64_t)sizeof(T) + (int64_t)t * step[i];
+      lane_at[i] = k < K * N && k % N < a.states ? k / N * step[i] + k % N * (uint32_t)sizeof(T) : kOutside;
     }
+  }
+  __device__ void load(int rows) {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      int k = (threadIdx.x + i * BLOCK) % PART;
+      asm volatile("" : "+v"(k));                // its row is not kept
+      v[i] = get_bits<T>(p[i], lane_at[i] | ((uint32_t)(rows - 1 - k / N) & kOutside), 0);
+    }
+  }
+  __device__ void move(int rows) {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) p[i] += (int64_t)rows * step[i];
   }
   __device__ void store(float* lds) const {
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
-      const int id = threadIdx.x + i * BLOCK;
-      if (id < ALL) lds[id / N % K * 2 * N + id / (K * N) * N + id % N] = to_f32(v[i]);
+      const int id = threadIdx.x + i * BLOCK, k = id % PART;
+      if (id < 2 * PART && k < K * N) lds[(k / N * 2 + id / PART) * N + k % N] = number<T>(v[i]);
     }
   }
 };

@@ -13,8 +13,8 @@ constexpr int kJoinBlock = 256;
 //   dh = m_t + dy_t c_t;  m_{t-1} = e^(dt_t a) dh.
 // One segment of 64 columns from its last row to its first, from zero: what it leaves to
 // the segment before, and the sum of its steps.
-template <class T, int S> __global__ __launch_bounds__(256) void k_scan_back(ScanArgs a) {
-  constexpr int K = kScanRows<S>, N = 4 * S, QUADS = K / 4, BLOCK = 256;
+template <class T, int S, bool GATE> __global__ __launch_bounds__(256) void k_scan_back(ScanArgs a) {
+  constexpr int K = kStageRows<S>, N = 4 * S, QUADS = K / 4, BLOCK = 256;
   SEQ_SHARED float bc[2][K * 2 * N];
   const int q = threadIdx.x & 3, blocks = (a.width + 63) / 64;
   const uint32_t item = blockIdx.x / (uint32_t)blocks;
@@ -33,35 +33,39 @@ template <class T, int S> __global__ __launch_bounds__(256) void k_scan_back(Sca
   }
   const float bias = a.bias ? a.bias[at] : 0.0f;
   if (begin < live) {
-    T d[QUADS], g[QUADS], z[QUADS];
-    Track<T> td, tg, tz;
-    td.init(a.delta, b, q, at);
-    tg.init(a.dout, b, q, at);
-    tz.init(a.gate, b, q, at);
-    StagedRows<T, S, BLOCK> rows;
+    uint32_t d[QUADS], g[QUADS], z[QUADS];
+    const int last = begin + (live - 1 - begin) / K * K;
+    Track<T> td(a.delta, b, last, q, at, real), tg(a.dout, b, last, q, at, real), tz(a.gate, b, last, q, at, real);
+    StagedRows<T, S, K, BLOCK> rows(a, b, last);
     auto fetch = [&](int t) {
+      const Left left{live - t - q - 1};
 #pragma unroll
       for (int i = 0; i < QUADS; ++i) {
-        const bool in = t + 4 * i + q < live;
-        d[i] = td.load(t, i, in);
-        g[i] = tg.load(t, i, in);
-        if (a.gate.p) z[i] = tz.load(t, i, in);
+        d[i] = td.load(i, left);
+        g[i] = tg.load(i, left);
+        if (GATE) z[i] = tz.load(i, left);
       }
-      rows.load(a, b, t, live);
+      rows.load(live - t);
+      td.move(-K);
+      tg.move(-K);
+      if (GATE) tz.move(-K);
+      rows.move(-K);
     };
-    const int last = begin + (live - 1 - begin) / K * K;
     fetch(last);
     rows.store(bc[0]);
     __syncthreads();
     int buffer = 0;
     for (int t = last; t >= begin; t -= K) {
+      const Left left{live - t - q - 1};
       float dt[QUADS], dy[QUADS];
 #pragma unroll
       for (int i = 0; i < QUADS; ++i) {
-        const bool in = t + 4 * i + q < live;
-        dt[i] = in ? softplus(to_f32(d[i]) + bias).dt : 0.0f;
-        dy[i] = to_f32(g[i]);
-        if (a.gate.p) dy[i] *= to_f32(z[i]) * sigmoid(to_f32(z[i]));
+        dt[i] = left.keep(i, softplus(number<T>(d[i]) + bias).dt);
+        dy[i] = number<T>(g[i]);
+        if (GATE) {
+          const float zz = number<T>(z[i]);
+          dy[i] *= zz * sigmoid(zz);
+        }
         time += dt[i];
       }
       const bool more = t > begin;
@@ -114,42 +118,86 @@ template <int N> __global__ __launch_bounds__(kJoinBlock) void k_scan_back_join(
   a.seg_state[(b * a.segs * a.width + at) * N + n] = x;
 }
 
-// Sums of 16 values over the wave's 16 columns (lane bits 2 to 5): halves of the values go to
-// halves of the lanes, so each step adds half as many numbers as the one before.  The lane
-// gets the sum of value 8 bit5 + 4 bit4 + 2 bit3 + bit2.
-__device__ inline float sum_columns(const float* v) {
-  float w[8], z[4], p[2];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 8]), false, false);
-    w[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+// Sums over a wave's 16 columns of four rows' terms of db and dc, through LDS: each lane leaves
+// its S terms of a row where they are read by two lanes for each (row, b or c, states of a lane),
+// eight columns each.  Added in registers, by moves between lanes, they took 87 cycles of a
+// wave's row; here it is two writes, two reads and ten additions.
+template <int S> struct ColumnSums {
+  static constexpr int N = 4 * S;
+  static constexpr int PAD = 68 * S;             // 64 lanes, and as much as sets the rows' reads in other banks
+  float* own;                                    // [4 rows][2][68][S]
+  __device__ explicit ColumnSums(float* lds) : own(lds) {}
+  __device__ void leave(int row, int which, const float* v) const {
+    store_floats<S>(own + (row * 2 + which) * PAD + (threadIdx.x & 63) * S, v);
   }
+  // The reads of a join, to be waited for as late as possible; then the sums, to part[row][2][4 S].
+  struct Reads {
+    float v[8][S];
+    int to;
+  };
+  __device__ Reads read() const {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    int l = threadIdx.x & 63;
+    asm volatile("" : "+v"(l));                  // what follows from it is not kept from call to call
+    const int half = l & 1, q = (l >> 1) & 3, which = (l >> 3) & 1, row = l >> 4;
+    const int from = (row * 2 + which) * PAD + (half * 32 + q) * S;
+    Reads r;
+    r.to = row * 2 * N + which * N + q * S;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(w[i]), __float_as_uint(w[i + 4]), false, false);
-    z[i] = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    for (int i = 0; i < 8; ++i) load_floats<S>(r.v[i], own + from + i * 4 * S);
+    return r;
   }
-  const bool three = threadIdx.x & 8, two = threadIdx.x & 4;
+  __device__ static void join(const Reads& r, float* part) {
+    float sum[S];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) p[i] = (three ? z[i + 2] : z[i]) + lane_move<0x128>(three ? z[i] : z[i + 2]);   // lane ^ 8
-  return (two ? p[1] : p[0]) + lane_move<0x1B>(lane_move<0x141>(two ? p[0] : p[1]));                          // lane ^ 4 = (lane ^ 7) ^ 3
-}
+    for (int s = 0; s < S; ++s) {
+      sum[s] = ((r.v[0][s] + r.v[1][s]) + (r.v[2][s] + r.v[3][s])) + ((r.v[4][s] + r.v[5][s]) + (r.v[6][s] + r.v[7][s]));
+      sum[s] += lane_move<0xB1>(sum[s]);
+    }
+    if ((threadIdx.x & 1) == 0) store_floats<S>(part + r.to, sum);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+};
+
+// A thread's column and quarter of its states, formed anew at each call: offsets that only the
+// ends of an episode need are not kept in registers throughout.
+struct Place {
+  int q, at;
+  bool real;
+  __device__ Place(int width, int first) {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    q = t & 3;
+    at = first + (t >> 2);
+    real = at < width;
+    at = real ? at : width - 1;
+  }
+};
 
 // All gradients.  A workgroup has COLS columns and goes through every `shares`-th segment, each
 // from its last block of rows to its first: a block's states and decays are formed again from
 // its mark and kept in registers for the way back.
-template <class T, int S, int COLS> __global__ __launch_bounds__(COLS * 4) void k_scan_backward(ScanArgs a) {
+#ifndef MW
+#define MW 2
+#endif
+template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS * 4, S <= 4 ? MW : 2) void k_scan_backward(ScanArgs a) {
   constexpr int K = kScanRows<S>, N = 4 * S, QUADS = K / 4, BLOCK = COLS * 4, WAVES = BLOCK / 64;
   constexpr bool KEEP = S <= 4;                                     // decays for the way back; else they are formed again
-  constexpr int GROUP = 8 / S;                                      // rows whose sums over columns are formed together
   SEQ_SHARED float bc[2][K * 2 * N];
-  SEQ_SHARED float part[2][WAVES][K * 2 * N];
-  const int q = threadIdx.x & 3, wave = wave_index();
+  // one place only where LDS is short: a barrier more keeps its readers and writers apart
+  constexpr int PARTS = S <= 4 ? 2 : 1;
+  SEQ_SHARED float part[PARTS][WAVES][K * 2 * N];
+  SEQ_SHARED float terms[WAVES][4 * 2 * ColumnSums<S>::PAD];
+  const int wave = wave_index();
+  const ColumnSums<S> sums(terms[wave]);
   const int block = blockIdx.x % (uint32_t)a.col_blocks;
   const uint32_t share = blockIdx.x / (uint32_t)a.col_blocks;
-  const int col = block * COLS + (threadIdx.x >> 2);
-  const bool real = col < a.width;
-  const int at = real ? col : a.width - 1;
+  const Place place(a.width, block * COLS);
+  const int q = place.q, at = place.at;
+  const bool real = place.real;
+  const Quad quad(q);
   float rates[S], da[S], dskip = 0.0f, dbias = 0.0f;
   load_states<S>(rates, a.a, at, q, a.states);
 #pragma unroll
@@ -158,95 +206,112 @@ template <class T, int S, int COLS> __global__ __launch_bounds__(COLS * 4) void 
     da[s] = 0.0f;
   }
   const float bias = a.bias ? a.bias[at] : 0.0f, skip = a.skip ? a.skip[at] : 0.0f;
-  // where this lane's sums over columns go: value (row, b or c, state) of a group of rows
-  const int value = ((threadIdx.x >> 5) & 1) * 8 + ((threadIdx.x >> 4) & 1) * 4 + ((threadIdx.x >> 3) & 1) * 2 + ((threadIdx.x >> 2) & 1);
-  const int target = value / (2 * S) * 2 * N + (value / S % 2) * N + q * S + value % S;
   int buffer = 0;
   const uint32_t items = (uint32_t)(a.batch * a.segs);
   for (uint32_t item = share; item < items; item += a.shares) {
     const int64_t b = item / (uint32_t)a.segs;
     const int seg = (int)(item % (uint32_t)a.segs);
     const int n = rows_in(a, b), begin = seg * a.seg, end = min(begin + a.seg, a.length), live = min(end, n);
-    Track<T> tu, td, tz, tg, tdu, tdd, tdz;
-    tu.init(a.u, b, q, at);
-    td.init(a.delta, b, q, at);
-    tg.init(a.dout, b, q, at);
-    tdu.init(a.du, b, q, at);
-    tdd.init(a.ddelta, b, q, at);
-    tz.init(a.gate, b, q, at);
-    tdz.init(a.dgate, b, q, at);
     float m[S];
-    if (a.segs > 1) load_floats<S>(m, a.seg_state + (b * a.segs + seg) * a.width * N + (uint32_t)(at * N + q * S));
-    else load_states<S>(m, a.dlast ? a.dlast + b * a.width * a.states : nullptr, at, q, a.states);
+    const Place entry(a.width, block * COLS);
+    if (a.segs > 1) load_floats<S>(m, a.seg_state + (b * a.segs + seg) * a.width * N + (uint32_t)(entry.at * N + entry.q * S));
+    else load_states<S>(m, a.dlast ? a.dlast + b * a.width * a.states : nullptr, entry.at, entry.q, a.states);
 #pragma unroll
     for (int s = 0; s < S; ++s) m[s] = real ? m[s] : 0.0f;           // columns that are not real add nothing to db and dc
     if (begin < live) {
-      T u[QUADS], d[QUADS], z[QUADS], g[QUADS];
+      uint32_t u[QUADS], d[QUADS], z[QUADS], g[QUADS];
       float first[S];
-      StagedRows<T, S, BLOCK> rows;
+      const int last = begin + (live - 1 - begin) / K * K;
+      Track<T> tu(a.u, b, last, q, at, real), td(a.delta, b, last, q, at, real), tg(a.dout, b, last, q, at, real),
+          tz(a.gate, b, last, q, at, real);
+      StagedRows<T, S, K, BLOCK> rows(a, b, last);
+      const float* mark = a.marks + (b * a.blocks + last / K) * a.width * N;
       auto fetch = [&](int t) {
+        const Left left{live - t - q - 1};
 #pragma unroll
         for (int i = 0; i < QUADS; ++i) {
-          const bool in = real && t + 4 * i + q < live;
-          u[i] = tu.load(t, i, in);
-          d[i] = td.load(t, i, in);
-          g[i] = tg.load(t, i, in);
-          if (a.gate.p) z[i] = tz.load(t, i, in);
+          u[i] = tu.load(i, left);
+          d[i] = td.load(i, left);
+          g[i] = tg.load(i, left);
+          if (GATE) z[i] = tz.load(i, left);
         }
-        load_floats<S>(first, a.marks + (b * a.blocks + t / K) * a.width * N + (uint32_t)(at * N + q * S));
-        rows.load(a, b, t, live);
+        load_floats<S>(first, mark + (uint32_t)(at * N + q * S));
+        rows.load(live - t);
+        tu.move(-K);
+        td.move(-K);
+        tg.move(-K);
+        if (GATE) tz.move(-K);
+        rows.move(-K);
+        mark -= (int64_t)a.width * N;
       };
-      const int last = begin + (live - 1 - begin) / K * K;
+      const int64_t whole = (int64_t)a.length * a.width;
+      Track<T> du(a.du, whole, a.width, b, last, q, at, real);          // ddelta and dgate lie alike
+      char *ddelta = (char*)a.ddelta + (du.p - (char*)a.du), *dgate = (char*)a.dgate + (du.p - (char*)a.du);
+      float* to = a.rows_part + ((b * a.length + last) * a.col_blocks + block) * 2 * N;
       fetch(last);
       rows.store(bc[buffer]);
       __syncthreads();
       for (int t = last; t >= begin; t -= K) {
+        const Left left{live - t - q - 1};
         const float* lds = bc[buffer] + q * S;
         float h[K + 1][S], e[KEEP ? K : 1][S];                      // h[r]: in front of row r; e[r]: its decay
         float dt[QUADS], slope[QUADS], uu[QUADS], dy[QUADS];
+        float kb[KEEP ? K : 1][S], kc[KEEP ? K : 1][S];             // the block's b and c, where registers allow
+        if (KEEP) {
+#pragma unroll
+          for (int k = 0; k < K; ++k) {
+            load_floats<S>(kb[k], lds + k * 2 * N);
+            load_floats<S>(kc[k], lds + k * 2 * N + N);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
         for (int s = 0; s < S; ++s) h[0][s] = real ? first[s] : 0.0f;
 #pragma unroll
         for (int i = 0; i < QUADS; ++i) {
-          const int r = t + 4 * i + q;
-          const bool in = real && r < live;
-          const Step step = softplus(to_f32(d[i]) + bias);
-          dt[i] = in ? step.dt : 0.0f;
+          const Step step = softplus(number<T>(d[i]) + bias);
+          dt[i] = left.keep(i, real ? step.dt : 0.0f);
           slope[i] = step.slope;
-          uu[i] = to_f32(u[i]);
+          uu[i] = number<T>(u[i]);
           const float x = dt[i] * uu[i];
           float y[4];
           auto row = [&](auto J) {
-            constexpr int j = decltype(J)::value, k = j;
+            constexpr int j = decltype(J)::value;
+            const int k = 4 * i + j;
             const float dtj = quad_lane<j>(dt[i]), xj = quad_lane<j>(x);
             float bv[S], cv[S];
-            load_floats<S>(bv, lds + (4 * i + k) * 2 * N);
-            load_floats<S>(cv, lds + (4 * i + k) * 2 * N + N);
-            y[j] = 0.0f;
+            if (!KEEP) load_floats<S>(bv, lds + k * 2 * N);
+            if (!KEEP && GATE) load_floats<S>(cv, lds + k * 2 * N + N);
+#pragma unroll
+            for (int s = 0; KEEP && s < S; ++s) {
+              bv[s] = kb[k][s];
+              cv[s] = kc[k][s];
+            }
 #pragma unroll
             for (int s = 0; s < S; ++s) {
               const float decay = fast_exp2(dtj * rates[s]);
               if (KEEP) e[4 * i + j][s] = decay;
               h[4 * i + j + 1][s] = fmaf(decay, h[4 * i + j][s], xj * bv[s]);
-              y[j] = fmaf(h[4 * i + j + 1][s], cv[s], y[j]);
+              if (GATE) y[j] = s == 0 ? h[4 * i + j + 1][s] * cv[s] : fmaf(h[4 * i + j + 1][s], cv[s], y[j]);
             }
           };
           row(Int<0>{});
           row(Int<1>{});
           row(Int<2>{});
           row(Int<3>{});
-          const float out = to_f32(g[i]);
+          const float out = number<T>(g[i]);
           dy[i] = out;
-          if (a.gate.p) {
-            const float zz = to_f32(z[i]), s = sigmoid(zz);
+          if (GATE) {
+            const float zz = number<T>(z[i]), s = sigmoid(zz);
             dy[i] = out * (zz * s);
-            const float yy = fmaf(skip, uu[i], quad_rows(y, q));
-            tdz.store(t, i, in, out * yy * silu_slope(zz, s));
+            const float yy = fmaf(skip, uu[i], quad_rows(y, quad));
+            put<T>(dgate, left.offset(i, du.lane_at), du.ahead(i), from_f32<T>(out * yy * silu_slope(zz, s)));
           }
-          __builtin_amdgcn_sched_barrier(0);     // no reads of later rows before these are done: registers are short
+          asm volatile("" : "+v"(slope[i]));     // now, not where it is used: its parts take more registers
+          __builtin_amdgcn_sched_barrier(0);     // no reads of later rows before these are done
         }
         const bool more = t > begin;
-        float sums[16];
+        if (KEEP && more) fetch(t - K);
         // b and c are read and steps are moved again: kept from above they would take as many
         // registers as the states
         int again = q * S;
@@ -254,6 +319,8 @@ template <class T, int S, int COLS> __global__ __launch_bounds__(COLS * 4) void 
         lds = bc[buffer] + again;
 #pragma unroll
         for (int i = 0; i < QUADS; ++i) asm volatile("" : "+v"(dt[i]));
+        Left rest = left;
+        asm volatile("" : "+v"(rest.x));
 #pragma unroll
         for (int i = QUADS - 1; i >= 0; --i) {
           const float x = dt[i] * uu[i];
@@ -262,37 +329,42 @@ template <class T, int S, int COLS> __global__ __launch_bounds__(COLS * 4) void 
             constexpr int j = decltype(J)::value;
             const float dtj = quad_lane<j>(dt[i]), xj = quad_lane<j>(x), dyj = quad_lane<j>(dy[i]);
             const int k = 4 * i + j;
-            float bv[S], cv[S];
-            load_floats<S>(bv, lds + k * 2 * N);
-            load_floats<S>(cv, lds + k * 2 * N + N);
-            along[j] = te[j] = 0.0f;
+            float bv[S], cv[S], tb[S], tc[S];
+            if (!KEEP) load_floats<S>(bv, lds + k * 2 * N);
+            if (!KEEP) load_floats<S>(cv, lds + k * 2 * N + N);
+#pragma unroll
+            for (int s = 0; KEEP && s < S; ++s) {
+              bv[s] = kb[k][s];
+              cv[s] = kc[k][s];
+            }
 #pragma unroll
             for (int s = 0; s < S; ++s) {
               const float dh = fmaf(dyj, cv[s], m[s]);
-              sums[k % GROUP * 2 * S + s] = dh * xj;
-              sums[k % GROUP * 2 * S + S + s] = dyj * h[k + 1][s];
-              along[j] = fmaf(dh, bv[s], along[j]);
+              tb[s] = dh * xj;
+              tc[s] = dyj * h[k + 1][s];
+              along[j] = s == 0 ? dh * bv[s] : fmaf(dh, bv[s], along[j]);
               m[s] = dh * (KEEP ? e[k][s] : fast_exp2(dtj * rates[s]));
               const float f = m[s] * h[k][s];
               da[s] = fmaf(f, dtj, da[s]);
-              te[j] = fmaf(f, rates[s], te[j]);
+              te[j] = s == 0 ? f * rates[s] : fmaf(f, rates[s], te[j]);
             }
-            if (k % GROUP == 0) part[buffer][wave][k * 2 * N + target] = sum_columns(sums);
+            sums.leave(j, 0, tb);
+            sums.leave(j, 1, tc);
           };
           row(Int<3>{});
           row(Int<2>{});
           row(Int<1>{});
           row(Int<0>{});
-          const float db = quad_rows(along, q), dtime = quad_rows(te, q) * kLn2;
-          const int r = t + 4 * i + q;
-          const float ddelta = fmaf(db, uu[i], dtime) * slope[i];
-          const bool in = real && r < live;
+          __builtin_amdgcn_sched_barrier(0);
+          const auto reads = sums.read();
+          const float db = quad_rows(along, quad), dtime = quad_rows(te, quad) * kLn2;
+          const float raw = rest.keep(i, fmaf(db, uu[i], dtime) * slope[i]);
           dskip = fmaf(dy[i], uu[i], dskip);               // both are 0 behind the episode
-          dbias += in ? ddelta : 0.0f;
-          tdu.store(t, i, in, fmaf(db, dt[i], skip * dy[i]));
-          tdd.store(t, i, in, ddelta);
-          // the next block's loads, where half of this one's states are no longer needed
-          if (i == QUADS / 2 && more) fetch(t - K);
+          dbias += raw;
+          du.store(i, rest, fmaf(db, dt[i], skip * dy[i]));
+          put<T>(ddelta, rest.offset(i, du.lane_at), du.ahead(i), from_f32<T>(raw));
+          sums.join(reads, part[buffer % PARTS][wave] + 4 * i * 2 * N);
+          if (!KEEP && i == QUADS / 2 && more) fetch(t - K);          // where some states are no longer needed
           __builtin_amdgcn_sched_barrier(0);
         }
         if (more) rows.store(bc[buffer ^ 1]);
@@ -304,28 +376,38 @@ template <class T, int S, int COLS> __global__ __launch_bounds__(COLS * 4) void 
           if (k < K * 2 * N && r < live) {
             float sum = 0.0f;
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) sum += part[buffer][w][k];
-            a.rows_part[((b * a.length + r) * a.col_blocks + block) * 2 * N + k % (2 * N)] = sum;
+            for (int w = 0; w < WAVES; ++w) sum += part[buffer % PARTS][w][k];
+            to[(int64_t)(k / (2 * N)) * a.col_blocks * 2 * N + k % (2 * N)] = sum;
           }
         }
+        du.move(-K);
+        ddelta -= (int64_t)K * du.step;
+        dgate -= (int64_t)K * du.step;
+        to -= (int64_t)K * a.col_blocks * 2 * N;
+        if (PARTS == 1) __syncthreads();
         buffer ^= 1;
       }
     }
-    if (seg == 0 && a.dfirst) store_states<S>(a.dfirst + b * a.width * a.states, at, q, a.states, real, m);
+    const Place exit(a.width, block * COLS);
+    if (seg == 0 && a.dfirst) store_states<S>(a.dfirst + b * a.width * a.states, exit.at, exit.q, a.states, exit.real, m);
+    Track<T> dead(a.du, (int64_t)a.length * a.width, a.width, b, max(begin, live), exit.q, exit.at, exit.real);
     for (int t = max(begin, live); t < end; t += 4) {
-      const bool in = real && t + q < end;
-      tdu.store(t, 0, in, 0.0f);
-      tdd.store(t, 0, in, 0.0f);
-      if (a.gate.p) tdz.store(t, 0, in, 0.0f);
+      const Left left{end - t - exit.q - 1};
+      const int64_t here = dead.p - (char*)a.du;
+      dead.store(0, left, 0.0f);
+      put<T>((char*)a.ddelta + here, left.offset(0, dead.lane_at), 0, from_f32<T>(0.0f));
+      if (GATE) put<T>((char*)a.dgate + here, left.offset(0, dead.lane_at), 0, from_f32<T>(0.0f));
+      dead.move(4);
     }
   }
-  if (!real) return;
-  store_floats<S>(a.cols_part + ((int64_t)share * a.width + at) * N + q * S, da);
   dskip = quad_sum(dskip);
   dbias = quad_sum(dbias);
-  if (q == 0) {
-    a.ends_part[((int64_t)share * 2) * a.width + at] = dskip;
-    a.ends_part[((int64_t)share * 2 + 1) * a.width + at] = dbias;
+  const Place end(a.width, block * COLS);
+  if (!end.real) return;
+  store_floats<S>(a.cols_part + ((int64_t)share * a.width + end.at) * N + end.q * S, da);
+  if (end.q == 0) {
+    a.ends_part[(int64_t)share * 2 * a.width + end.at] = dskip;
+    a.ends_part[((int64_t)share * 2 + 1) * a.width + end.at] = dbias;
   }
 }
 
@@ -341,7 +423,7 @@ template <class T, int N> __global__ __launch_bounds__(kJoinBlock) void k_scan_r
 #pragma unroll 4
     for (int i = 0; i < a.col_blocks; ++i) sum += a.rows_part[(row * a.col_blocks + i) * 2 * N + k];
   }
-  (k < N ? row_of<T>(a.db, b, t) : row_of<T>(a.dc, b, t))[n] = from_f32<T>(sum);
+  ((T*)(k < N ? a.db : a.dc))[row * a.states + n] = from_f32<T>(sum);
 }
 
 // da, dskip and dbias: 64 numbers per workgroup, sixteen waves each add every sixteenth share.
@@ -386,10 +468,19 @@ template <int N> __global__ __launch_bounds__(64 * kJoinWaves) void k_scan_colum
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-constexpr int64_t kWaves = 2048;
-constexpr int kLeastRows = 64;
+#ifndef KW
+#define KW 2048
+#endif
+constexpr int64_t kWaves = KW;
+#ifndef KL
+#define KL 64
+#endif
+constexpr int kLeastRows = KL;
 constexpr int64_t kWorkgroups = 1024;       // each leaves a share of da
-constexpr int kCols = 128;
+#ifndef BC
+#define BC 64
+#endif
+constexpr int kCols = BC;
 
 struct Plan {
   Cut parts;
@@ -442,20 +533,20 @@ extern "C" qds_status qds_selective_scan_backward_workspace(const qds_scan_confi
 extern "C" qds_status qds_selective_scan_backward(const qds_scan_config* c, qds_rows dout, qds_rows u, qds_rows delta,
                                                   const float* a_, qds_rows b, qds_rows cc, const float* skip,
                                                   qds_rows gate, const float* bias, const void* marks,
-                                                  const float* dstate_out, const int32_t* lengths, qds_rows du,
-                                                  qds_rows ddelta, float* da, qds_rows db, qds_rows dc, float* dskip,
-                                                  qds_rows dgate, float* dbias, float* dstate_in, void* workspace,
+                                                  const float* dstate_out, const int32_t* lengths, void* du,
+                                                  void* ddelta, float* da, void* db, void* dc, float* dskip,
+                                                  void* dgate, float* dbias, float* dstate_in, void* workspace,
                                                   uint64_t workspace_bytes, void* stream) {
   uint64_t need = 0;
   const qds_status st = qds_selective_scan_backward_workspace(c, &need);
   if (st != QDS_OK) return st;
   if (!a_ || !da || !workspace || ((uintptr_t)workspace & 255)) return QDS_ERR_INVALID_ARG;
   if (c->batch > 0 && c->length > 0 &&
-      (!dout.data || !u.data || !delta.data || !b.data || !cc.data || !marks || !du.data || !ddelta.data || !db.data ||
-       !dc.data || (gate.data && !dgate.data) || ((uintptr_t)marks & 255)))
+      (!dout.data || !u.data || !delta.data || !b.data || !cc.data || !marks || !du || !ddelta || !db || !dc ||
+       (gate.data && !dgate) || ((uintptr_t)marks & 255)))
     return QDS_ERR_INVALID_ARG;
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
-  for (qds_rows* r : {&dout, &u, &delta, &b, &cc, &gate, &du, &ddelta, &db, &dc, &dgate})
+  for (qds_rows* r : {&dout, &u, &delta, &b, &cc, &gate})
     if (!near_rows(*r, c->length)) return QDS_ERR_UNSUPPORTED;
   const Plan p = plan_of(c);
   ScanArgs a = scan_args(c);
@@ -465,11 +556,11 @@ extern "C" qds_status qds_selective_scan_backward(const qds_scan_config* c, qds_
   a.c = rows(cc);
   a.gate = rows(gate);
   a.dout = rows(dout);
-  a.du = rows(du);
-  a.ddelta = rows(ddelta);
-  a.db = rows(db);
-  a.dc = rows(dc);
-  a.dgate = rows(dgate);
+  a.du = du;
+  a.ddelta = ddelta;
+  a.db = db;
+  a.dc = dc;
+  a.dgate = dgate;
   a.a = a_;
   a.skip = skip;
   a.bias = bias;
@@ -496,10 +587,14 @@ extern "C" qds_status qds_selective_scan_backward(const qds_scan_config* c, qds_
     constexpr int L = decltype(S)::value, N = 4 * L;
     if (c->batch > 0) {
       if (a.segs > 1) {
-        k_scan_back<T, L><<<(uint32_t)(c->batch * ceil_div(c->width, 64) * (a.segs - 1)), 256, 0, s>>>(a);
+        const uint32_t grid = (uint32_t)(c->batch * ceil_div(c->width, 64) * (a.segs - 1));
+        if (gate.data) k_scan_back<T, L, true><<<grid, 256, 0, s>>>(a);
+        else k_scan_back<T, L, false><<<grid, 256, 0, s>>>(a);
         k_scan_back_join<N><<<(uint32_t)ceil_div((int64_t)c->batch * c->width * N, kJoinBlock), kJoinBlock, 0, s>>>(a);
       }
-      k_scan_backward<T, L, kCols><<<(uint32_t)(a.col_blocks * a.shares), kCols * 4, 0, s>>>(a);
+      const uint32_t grid = (uint32_t)(a.col_blocks * a.shares);
+      if (gate.data) k_scan_backward<T, L, kCols, true><<<grid, kCols * 4, 0, s>>>(a);
+      else k_scan_backward<T, L, kCols, false><<<grid, kCols * 4, 0, s>>>(a);
       if (c->length > 0)
         k_scan_rows_join<T, N><<<(uint32_t)ceil_div((int64_t)c->batch * c->length * 2 * N, kJoinBlock), kJoinBlock, 0, s>>>(a);
     }

@@ -150,11 +150,11 @@ def lib():
         L.qds_causal_conv_step.argtypes = [K, R, P, P, P, R, P, P]
         L.qds_selective_scan_marks.argtypes = [S, B]
         L.qds_selective_scan_workspace.argtypes = [S, B]
-        L.qds_selective_scan.argtypes = [S, R, R, P, R, R, P, R, P, P, P, R, P, P, P, U, P]
+        L.qds_selective_scan.argtypes = [S, R, R, P, R, R, P, R, P, P, P, P, P, P, P, U, P]
         L.qds_selective_scan_backward_workspace.argtypes = [S, B]
-        L.qds_selective_scan_backward.argtypes = [S, R, R, R, P, R, R, P, R, P, P, P, P, R, R, P, R, R, P, R, P,
+        L.qds_selective_scan_backward.argtypes = [S, R, R, R, P, R, R, P, R, P, P, P, P, P, P, P, P, P, P, P, P,
                                                   P, P, U, P]
-        L.qds_selective_scan_step.argtypes = [S, R, R, P, R, R, P, R, P, P, R, P, P]
+        L.qds_selective_scan_step.argtypes = [S, R, R, P, R, R, P, R, P, P, P, P, P]
         L.qds_branch_norm.argtypes = [C.POINTER(QdsBranchConfig), P, I, P, I, P, I, P, P, P, P, P, P]
         L.qds_branch_norm_backward_workspace.argtypes = [C.POINTER(QdsBranchConfig), B]
         L.qds_branch_norm_backward.argtypes = [C.POINTER(QdsBranchConfig), P, I, P, I, P, I, P, I, P, I, P, P, P,
@@ -783,7 +783,7 @@ def selective_scan_forward(u, delta, a, b, c, skip=None, gate=None, bias=None, s
         marks = u.new_empty(_scan_setup(*args, "qds_selective_scan_marks")[2], dtype=torch.uint8) if keep else None
         _check(lib().qds_selective_scan(
             ref, _row_view(u), _row_view(delta), a.data_ptr(), _row_view(b), _row_view(c), _ptr(skip), _row_view(gate),
-            _ptr(bias), _ptr(state), _ptr(lengths), _row_view(o), last.data_ptr(), _ptr(marks), _ptr(ws), size,
+            _ptr(bias), _ptr(state), _ptr(lengths), o.data_ptr(), last.data_ptr(), _ptr(marks), _ptr(ws), size,
             _stream(u)), "qds_selective_scan")
     return o, last, marks
 
@@ -809,8 +809,8 @@ def selective_scan_backward(do, u, delta, a, b, c, marks, skip=None, gate=None, 
         ws = _scratch(size, u)
         _check(lib().qds_selective_scan_backward(
             ref, _row_view(do), _row_view(u), _row_view(delta), a.data_ptr(), _row_view(b), _row_view(c), _ptr(skip),
-            _row_view(gate), _ptr(bias), marks.data_ptr(), _ptr(dlast), _ptr(lengths), _row_view(du),
-            _row_view(ddelta), da.data_ptr(), _row_view(db), _row_view(dc), _ptr(dskip), _row_view(dgate), _ptr(dbias),
+            _row_view(gate), _ptr(bias), marks.data_ptr(), _ptr(dlast), _ptr(lengths), du.data_ptr(),
+            ddelta.data_ptr(), da.data_ptr(), db.data_ptr(), dc.data_ptr(), _ptr(dskip), _ptr(dgate), _ptr(dbias),
             dfirst.data_ptr(), _ptr(ws), size, _stream(u)), "qds_selective_scan_backward")
     return du, ddelta, da, db, dc, dskip, dgate, dbias, dfirst
 
@@ -831,7 +831,7 @@ def selective_scan_step(u, delta, a, b, c, state, skip=None, gate=None, bias=Non
     with _on(u):
         _check(lib().qds_selective_scan_step(
             ref, _row_view(u), _row_view(delta), a.data_ptr(), _row_view(b), _row_view(c), _ptr(skip), _row_view(gate),
-            _ptr(bias), state.data_ptr(), _row_view(o), out_state.data_ptr(), _stream(u)), "qds_selective_scan_step")
+            _ptr(bias), state.data_ptr(), o.data_ptr(), out_state.data_ptr(), _stream(u)), "qds_selective_scan_step")
     return o, out_state
 
 

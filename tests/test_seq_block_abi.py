@@ -130,25 +130,25 @@ def test_scan_refusals(lib, over, status):
     c, r = scan(**over), rows()
     assert bytes_of(lib.qds_selective_scan_workspace, c)[0] == status
     assert bytes_of(lib.qds_selective_scan_backward_workspace, c)[0] == status
-    assert lib.qds_selective_scan(C.byref(c), r, r, P, r, r, P, r, P, P, None, r, P, P, P, 1 << 40, None) == status
-    assert lib.qds_selective_scan_backward(C.byref(c), r, r, r, P, r, r, P, r, P, P, P, None, r, r, P, r, r, P, r, P, P, P,
+    assert lib.qds_selective_scan(C.byref(c), r, r, P, r, r, P, r, P, P, None, P, P, P, P, 1 << 40, None) == status
+    assert lib.qds_selective_scan_backward(C.byref(c), r, r, r, P, r, r, P, r, P, P, P, None, P, P, P, P, P, P, P, P, P, P,
                                            1 << 40, None) == status
     if "length" not in over:
-        assert lib.qds_selective_scan_step(C.byref(c), r, r, P, r, r, P, r, P, P, r, P, None) == status
+        assert lib.qds_selective_scan_step(C.byref(c), r, r, P, r, r, P, r, P, P, P, P, None) == status
 
 
 def test_scan_refuses_pointers(lib):
     c, r = scan(batch=1, width=16), rows()
     st, need = bytes_of(lib.qds_selective_scan_workspace, c)
     assert st == S.OK and need > 0                    # few columns: their rows are cut into segments
-    ok = [C.byref(c), r, r, P, r, r, P, r, P, P, None, r, P, P, P, need, None]
+    ok = [C.byref(c), r, r, P, r, r, P, r, P, P, None, P, P, P, P, need, None]
     far, back = rows(strides=(1, 1 << 23)), rows(strides=(1, -64))
-    for i, bad in [(0, None), (1, NONE), (2, NONE), (3, None), (4, NONE), (5, NONE), (11, NONE), (13, P + 64), (14, None),
+    for i, bad in [(0, None), (1, NONE), (2, NONE), (3, None), (4, NONE), (5, NONE), (11, None), (13, P + 64), (14, None),
                    (14, P + 128)]:
         a = list(ok)
         a[i] = bad
         assert lib.qds_selective_scan(*a) == S.ERR_INVALID_ARG, i
-    for i in (1, 2, 4, 5, 7, 11):
+    for i in (1, 2, 4, 5, 7):
         for bad in (far, back):
             a = list(ok)
             a[i] = bad
@@ -156,21 +156,21 @@ def test_scan_refuses_pointers(lib):
     ok[15] = need - 1
     assert lib.qds_selective_scan(*ok) == S.ERR_WORKSPACE_TOO_SMALL
     st, need = bytes_of(lib.qds_selective_scan_backward_workspace, c)
-    ok = [C.byref(c), r, r, r, P, r, r, P, r, P, P, P, None, r, r, P, r, r, P, r, P, P, P, need, None]
-    for i, bad in [(1, NONE), (2, NONE), (3, NONE), (4, None), (5, NONE), (6, NONE), (10, None), (10, P + 16), (13, NONE),
-                   (14, NONE), (15, None), (16, NONE), (17, NONE), (19, NONE), (22, None), (22, P + 4)]:
+    ok = [C.byref(c), r, r, r, P, r, r, P, r, P, P, P, None, P, P, P, P, P, P, P, P, P, P, need, None]
+    for i, bad in [(1, NONE), (2, NONE), (3, NONE), (4, None), (5, NONE), (6, NONE), (10, None), (10, P + 16), (13, None),
+                   (14, None), (15, None), (16, None), (17, None), (19, None), (22, None), (22, P + 4)]:
         a = list(ok)
         a[i] = bad
         assert lib.qds_selective_scan_backward(*a) == S.ERR_INVALID_ARG, i
-    for i in (1, 2, 3, 5, 6, 8, 13, 14, 16, 17, 19):
+    for i in (1, 2, 3, 5, 6, 8):
         for bad in (far, back):
             a = list(ok)
             a[i] = bad
             assert lib.qds_selective_scan_backward(*a) == S.ERR_UNSUPPORTED, i
     ok[23] = need - 1
     assert lib.qds_selective_scan_backward(*ok) == S.ERR_WORKSPACE_TOO_SMALL
-    ok = [C.byref(c), r, r, P, r, r, P, r, P, P, r, P, None]
-    for i, bad in [(1, NONE), (2, NONE), (3, None), (4, NONE), (5, NONE), (9, None), (10, NONE), (11, None)]:
+    ok = [C.byref(c), r, r, P, r, r, P, r, P, P, P, P, None]
+    for i, bad in [(1, NONE), (2, NONE), (3, None), (4, NONE), (5, NONE), (9, None), (10, None), (11, None)]:
         a = list(ok)
         a[i] = bad
         assert lib.qds_selective_scan_step(*a) == S.ERR_INVALID_ARG, i
@@ -217,9 +217,9 @@ def test_dropout_refusals(lib):
 def test_empty_calls_launch_nothing(lib):
     assert lib.qds_causal_conv(C.byref(conv(batch=0)), NONE, P, None, None, None, NONE, None, None) == S.OK
     assert lib.qds_causal_conv_step(C.byref(conv(batch=0)), NONE, P, None, None, NONE, None, None) == S.OK
-    assert lib.qds_selective_scan(C.byref(scan(batch=0)), NONE, NONE, P, NONE, NONE, None, NONE, None, None, None, NONE, None,
+    assert lib.qds_selective_scan(C.byref(scan(batch=0)), NONE, NONE, P, NONE, NONE, None, NONE, None, None, None, None, None,
                                   None, None, 0, None) == S.OK
-    assert lib.qds_selective_scan_step(C.byref(scan(batch=0)), NONE, NONE, P, NONE, NONE, None, NONE, None, None, NONE, None,
+    assert lib.qds_selective_scan_step(C.byref(scan(batch=0)), NONE, NONE, P, NONE, NONE, None, NONE, None, None, None, None,
                                        None) == S.OK
     assert lib.qds_branch_norm(C.byref(branch(rows=0)), *[None, 0] * 3, *[None] * 6) == S.OK
     assert lib.qds_dropout(C.byref(dropout(elements=0)), None, None, None, None, None) == S.OK
