@@ -85,6 +85,7 @@ template <class T, int S, bool GATE> __global__ __launch_bounds__(256) void k_sc
         row(Int<2>{});
         row(Int<1>{});
         row(Int<0>{});
+        __builtin_amdgcn_sched_barrier(0);
       }
       if (more) {
         rows.store(bc[buffer ^ 1]);
