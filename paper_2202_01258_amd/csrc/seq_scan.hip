@@ -33,10 +33,11 @@ template <class T, int S, bool LOCAL, bool GATE> __global__ __launch_bounds__(kB
   if (LOCAL) {
 #pragma unroll
     for (int s = 0; s < S; ++s) h[s] = 0.0f;
-  } else if (a.segs > 1) {
-    load_floats<S>(h, a.seg_state + place);
+  } else if (a.joined) {
+    load_floats<S>(h, a.left_state + place);
   } else {
     load_states<S>(h, a.first ? a.first + b * a.width * a.states : nullptr, at, q, a.states);
+    follow<S, false>(h, a, rates, b, seg, at, q);
   }
   float time = 0.0f;
   Track<T> out(a.o, (int64_t)a.length * a.width, a.width, b, begin, q, at, real);
@@ -118,8 +119,8 @@ template <class T, int S, bool LOCAL, bool GATE> __global__ __launch_bounds__(kB
   }
   if (LOCAL) {
     time = quad_sum(time);
-    if (real) store_floats<S>(a.seg_state + place, h);
-    if (real && q == 0) a.seg_time[(b * a.segs + seg) * a.width + at] = time;
+    if (real) store_floats<S>(a.left_state + place, h);
+    if (real && q == 0) a.left_time[(b * a.segs + seg) * a.width + at] = time;
   } else {
     out = Track<T>(a.o, (int64_t)a.length * a.width, a.width, b, max(begin, live), q, at, real);
     for (int t = max(begin, live); t < end; t += 4) {
@@ -128,26 +129,6 @@ template <class T, int S, bool LOCAL, bool GATE> __global__ __launch_bounds__(kB
     }
     if (seg == a.segs - 1 && a.last) store_states<S>(a.last + b * a.width * a.states, at, q, a.states, real, h);
   }
-}
-
-// What each segment starts from: x = e^(a time) x + what the segment before left behind.
-template <int N> __global__ __launch_bounds__(kBlock) void k_scan_join(ScanArgs a) {
-  const int64_t id = (int64_t)blockIdx.x * kBlock + threadIdx.x, column = id / N;
-  const int n = (int)(id % N);
-  if (column >= (int64_t)a.batch * a.width) return;
-  const int64_t b = column / a.width;
-  const int at = (int)(column % a.width);
-  const bool in = n < a.states;
-  float x = in && a.first ? a.first[column * a.states + n] : 0.0f;
-  const float r = in ? rate(a.a[(int64_t)at * a.states + n]) : 0.0f;
-#pragma unroll 4
-  for (int seg = 0; seg < a.segs - 1; ++seg) {
-    const int64_t where = (b * a.segs + seg) * a.width + at;
-    const float left = a.seg_state[where * N + n], time = a.seg_time[where];
-    a.seg_state[where * N + n] = x;
-    x = fmaf(fast_exp2(r * time), x, left);
-  }
-  a.seg_state[((b * a.segs + a.segs - 1) * a.width + at) * N + n] = x;
 }
 
 // One row: the state is what is read and written, a lane's share in one access at any alignment
@@ -191,19 +172,16 @@ template <class T, int S, bool TAIL> __global__ __launch_bounds__(kBlock) void k
 #define KW 8192
 #endif
 constexpr int64_t kWaves = KW;
-#ifndef KL
-#define KL 64
-#endif
-constexpr int kLeastRows = KL;
+constexpr int kLeastRows = 64;
 
-Cut forward_cut(const qds_scan_config* c) { return cut(c, kWaves, kLeastRows); }
+Cut forward_cut(const qds_scan_config* c) { return cut(c, kWaves, kLeastRows, block_rows(c)); }
 uint64_t state_bytes(const qds_scan_config* c, int segs) {
   return align_up((uint64_t)c->batch * segs * c->width * 4 * lane_states(c) * sizeof(float));
 }
 bool fits(const qds_scan_config* c) {
   const int64_t workgroups = ceil_div(c->width, kColumns) * forward_cut(c).segs;
   return (int64_t)c->batch <= (int64_t)most_blocks(kBlock) / workgroups &&
-         (int64_t)c->batch * c->width <= (int64_t)most_blocks(kBlock) * 8;
+         (int64_t)c->batch * c->width <= (int64_t)most_blocks(kScanJoin) / 2;
 }
 
 }  // namespace
@@ -260,9 +238,13 @@ extern "C" qds_status qds_selective_scan(const qds_scan_config* c, qds_rows u, q
   a.seg = parts.seg;
   a.segs = parts.segs;
   a.col_blocks = (int)ceil_div(c->width, kColumns);
+  a.piece = a.seg;
+  a.pieces = a.segs;
+  a.ratio = 1;
+  a.joined = a.pieces > kFewPieces;
   if (a.segs > 1) {
-    a.seg_state = (float*)workspace;
-    a.seg_time = (float*)((char*)workspace + state_bytes(c, a.segs));
+    a.left_state = (float*)workspace;
+    a.left_time = (float*)((char*)workspace + state_bytes(c, a.segs));
   }
   hipStream_t s = (hipStream_t)stream;
   scan_instance(c, [&](auto type, auto S) {
@@ -271,7 +253,7 @@ extern "C" qds_status qds_selective_scan(const qds_scan_config* c, qds_rows u, q
     const uint32_t across = (uint32_t)(a.batch * a.col_blocks);
     if (a.segs > 1) {
       k_scan<T, L, true, false><<<across * (a.segs - 1), kBlock, 0, s>>>(a);
-      k_scan_join<4 * L><<<(uint32_t)ceil_div((int64_t)a.batch * a.width * 4 * L, kBlock), kBlock, 0, s>>>(a);
+      if (a.joined) k_scan_join<4 * L, false><<<(uint32_t)ceil_div((int64_t)a.batch * a.width * 4 * L, 16), kScanJoin, 0, s>>>(a);
     }
     if (gate.data) k_scan<T, L, false, true><<<across * a.segs, kBlock, 0, s>>>(a);
     else k_scan<T, L, false, false><<<across * a.segs, kBlock, 0, s>>>(a);

@@ -5,8 +5,9 @@
 // and column (step size, products, gate) for rows q, q + 4, ..., and gives it to the
 // others by lane moves; rows of b and c, which all columns share, come through LDS.  An
 // episode may be cut into segments that run side by side: a first pass forms what each
-// segment leaves behind when it starts from zero, a short scan joins them, and the main
-// pass starts each segment from its true state.
+// segment leaves behind when it starts from zero, and the main pass starts each segment from
+// its true state, which follows from what all segments in front of it left (the main pass
+// works that out where they are few, a scan between the two where they are many).
 #pragma once
 
 #include <algorithm>
@@ -42,13 +43,16 @@ struct ScanArgs {
   const float *a, *skip, *bias, *first, *dlast;
   float *last, *dfirst, *da, *dskip, *dbias;
   float* marks;                                  // [batch][blocks][width][4 S]
-  float* seg_state;                              // [batch][segs][width][4 S]: left behind by a segment, then what it starts from
-  float* seg_time;                               // [batch][segs][width]: sum of a segment's steps
+  float* left_state;                             // [batch][pieces][width][4 S]: left behind by a piece; after a scan, what it starts from
+  float* left_time;                              // [batch][pieces][width]: sum of a piece's steps
   float* rows_part;                              // [batch][length][column blocks][2][4 S]: shares of db and dc
   float* cols_part;                              // [shares][width][4 S]: of da
   float* ends_part;                              // [shares][2][width]: of dskip and dbias
   const int32_t* lengths;
-  int32_t batch, length, width, states, seg, segs, blocks, col_blocks, shares;
+  int32_t batch, length, width, states, blocks, col_blocks, shares;
+  int32_t seg, segs;                             // rows of a segment of the main pass; segments
+  int32_t piece, pieces, ratio;                  // rows of a piece of the first pass; pieces; pieces of a segment
+  bool joined;                                   // a scan has run
 };
 __device__ inline int rows_in(const ScanArgs& a, int64_t b) {
   return a.lengths ? min(max(a.lengths[b], 0), a.length) : a.length;
@@ -241,18 +245,80 @@ inline int lane_states(const qds_scan_config* c) { return c->states <= 4 ? 1 : c
 inline int block_rows(const qds_scan_config* c) { return lane_states(c) == 8 ? kScanRows<8> : kScanRows<4>; }
 inline int block_count(const qds_scan_config* c) { return (int)ceil_div(c->length, block_rows(c)); }
 
+// What all pieces before `until` leave together when the first starts from x (the pieces in their
+// order, or from the last one backwards).
+template <int S, bool BACK> __device__ inline void follow(float* x, const ScanArgs& a, const float* rates, int64_t b, int until, int at, int q) {
+  constexpr int N = 4 * S;
+  const int first = BACK ? a.pieces - 1 : 0, count = BACK ? a.pieces - until : until;
+  const float* state = a.left_state + (b * a.pieces + first) * a.width * N + (uint32_t)(at * N + q * S);
+  const float* time = a.left_time + (b * a.pieces + first) * a.width + at;
+#pragma unroll 4
+  for (int i = 0; i < count; ++i) {
+    const int64_t to = (int64_t)(BACK ? -i : i) * a.width;
+    float left[S];
+    load_floats<S>(left, state + to * N);
+    const float t = time[to];
+#pragma unroll
+    for (int s = 0; s < S; ++s) x[s] = fmaf(fast_exp2(t * rates[s]), x[s], left[s]);
+  }
+}
+
+// The same for many pieces: puts what each starts from in its place.  Sixteen states per workgroup, whose
+// pieces are dealt to sixteen groups of threads: each forms what its share does to any x, then, from
+// what the groups before it do, what its own pieces start from.
+constexpr int kScanJoin = 256;
+template <int N, bool BACK> __global__ __launch_bounds__(kScanJoin) void k_scan_join(ScanArgs a) {
+  __shared__ float shares[2][16][16];
+  const int i = threadIdx.x & 15, group = threadIdx.x >> 4;
+  const int64_t id = (int64_t)blockIdx.x * 16 + i, column = id / N, all = (int64_t)a.batch * a.width;
+  const int n = (int)(id % N);
+  const bool real = column < all, in = real && n < a.states;
+  const int64_t b = real ? column / a.width : 0;
+  const int at = real ? (int)(column % a.width) : 0;
+  const float r = in ? rate(a.a[(int64_t)at * a.states + n]) : 0.0f;
+  // pieces with something left behind, in their order; one more starts behind the last
+  const int count = BACK ? a.pieces - a.ratio : a.pieces - 1, share = (count + 15) / 16;
+  const int from = min(group * share, count), to = min(from + share, count);
+  auto place = [&](int k) { return (b * a.pieces + (BACK ? a.pieces - 1 - k : k)) * a.width + at; };
+  float decay = 1.0f, left = 0.0f;
+  if (real) {
+#pragma unroll 4
+    for (int k = from; k < to; ++k) {
+      const int64_t where = place(k);
+      const float e = fast_exp2(r * a.left_time[where]);
+      left = fmaf(e, left, a.left_state[where * N + n]);
+      decay *= e;
+    }
+  }
+  shares[0][group][i] = decay;
+  shares[1][group][i] = left;
+  __syncthreads();
+  if (!real) return;
+  const float* first = BACK ? a.dlast : a.first;
+  float x = in && first ? first[column * a.states + n] : 0.0f;
+  for (int g = 0; g < group; ++g) x = fmaf(shares[0][g][i], x, shares[1][g][i]);
+#pragma unroll 4
+  for (int k = from; k < to; ++k) {
+    const int64_t where = place(k);
+    const float gone = a.left_state[where * N + n], time = a.left_time[where];
+    a.left_state[where * N + n] = x;
+    x = fmaf(fast_exp2(r * time), x, gone);
+  }
+  if (to == count && (from < to || group == 0)) a.left_state[place(count) * N + n] = x;
+}
+
 // Rows of a segment and their number, for a kernel that wants `waves` waves.
 struct Cut {
   int seg, segs;
 };
-inline Cut cut(const qds_scan_config* c, int64_t waves, int least) {
+inline Cut cut(const qds_scan_config* c, int64_t waves, int least, int unit) {
   const int64_t whole = std::max<int64_t>(1, (int64_t)c->batch * ceil_div(c->width, 16));
   const int64_t want = std::max<int64_t>(1, waves / whole);
-  const int k = block_rows(c);
   int64_t seg = std::max<int64_t>(least, ceil_div(c->length, want));
-  seg = ceil_div(seg, k) * k;
+  seg = ceil_div(seg, unit) * unit;
   return Cut{(int)seg, (int)std::max<int64_t>(1, ceil_div(c->length, seg))};
 }
+constexpr int kFewPieces = 16;                   // so many are followed by the main pass itself
 
 template <class F> void scan_instance(const qds_scan_config* c, F&& f) {
   auto with_type = [&](auto S) {

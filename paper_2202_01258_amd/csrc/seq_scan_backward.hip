@@ -11,8 +11,8 @@ constexpr int kJoinBlock = 256;
 
 // With m_t = e^(dt_{t+1} a) dh_{t+1}, what reaches row t from the rows behind it:
 //   dh = m_t + dy_t c_t;  m_{t-1} = e^(dt_t a) dh.
-// One segment of 64 columns from its last row to its first, from zero: what it leaves to
-// the segment before, and the sum of its steps.
+// One piece of 64 columns from its last row to its first, from zero: what it leaves to the
+// piece before, and the sum of its steps.
 template <class T, int S, bool GATE> __global__ __launch_bounds__(256) void k_scan_back(ScanArgs a) {
   constexpr int K = kStageRows<S>, N = 4 * S, QUADS = K / 4, BLOCK = 256;
   SEQ_SHARED float bc[2][K * 2 * N];
@@ -21,9 +21,10 @@ template <class T, int S, bool GATE> __global__ __launch_bounds__(256) void k_sc
   const int col = (blockIdx.x % (uint32_t)blocks) * 64 + (threadIdx.x >> 2);
   const bool real = col < a.width;
   const int at = real ? col : a.width - 1;
-  const int64_t b = item / (uint32_t)(a.segs - 1);
-  const int seg = 1 + (int)(item % (uint32_t)(a.segs - 1));       // nothing comes before the first segment
-  const int n = rows_in(a, b), begin = seg * a.seg, end = min(begin + a.seg, a.length), live = min(end, n);
+  const int runs = a.pieces - a.ratio;                            // no segment asks what the first one's pieces leave
+  const int64_t b = item / (uint32_t)runs;
+  const int piece = a.ratio + (int)(item % (uint32_t)runs);
+  const int n = rows_in(a, b), begin = piece * a.piece, end = min(begin + a.piece, a.length), live = min(end, n);
   float rates[S], m[S], time = 0.0f;
   load_states<S>(rates, a.a, at, q, a.states);
 #pragma unroll
@@ -95,28 +96,8 @@ template <class T, int S, bool GATE> __global__ __launch_bounds__(256) void k_sc
     }
   }
   time = quad_sum(time);
-  if (real) store_floats<S>(a.seg_state + ((b * a.segs + seg) * a.width + at) * N + q * S, m);
-  if (real && q == 0) a.seg_time[(b * a.segs + seg) * a.width + at] = time;
-}
-
-// What reaches each segment's last row from behind.
-template <int N> __global__ __launch_bounds__(kJoinBlock) void k_scan_back_join(ScanArgs a) {
-  const int64_t id = (int64_t)blockIdx.x * kJoinBlock + threadIdx.x, column = id / N;
-  const int n = (int)(id % N);
-  if (column >= (int64_t)a.batch * a.width) return;
-  const int64_t b = column / a.width;
-  const int at = (int)(column % a.width);
-  const bool in = n < a.states;
-  float x = in && a.dlast ? a.dlast[column * a.states + n] : 0.0f;
-  const float r = in ? rate(a.a[(int64_t)at * a.states + n]) : 0.0f;
-#pragma unroll 4
-  for (int seg = a.segs - 1; seg > 0; --seg) {
-    const int64_t where = (b * a.segs + seg) * a.width + at;
-    const float left = a.seg_state[where * N + n], time = a.seg_time[where];
-    a.seg_state[where * N + n] = x;
-    x = fmaf(fast_exp2(r * time), x, left);
-  }
-  a.seg_state[(b * a.segs * a.width + at) * N + n] = x;
+  if (real) store_floats<S>(a.left_state + ((b * a.pieces + piece) * a.width + at) * N + q * S, m);
+  if (real && q == 0) a.left_time[(b * a.pieces + piece) * a.width + at] = time;
 }
 
 // Sums over a wave's 16 columns of four rows' terms of db and dc, through LDS: each lane leaves
@@ -215,8 +196,13 @@ template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS
     const int n = rows_in(a, b), begin = seg * a.seg, end = min(begin + a.seg, a.length), live = min(end, n);
     float m[S];
     const Place entry(a.width, block * COLS);
-    if (a.segs > 1) load_floats<S>(m, a.seg_state + (b * a.segs + seg) * a.width * N + (uint32_t)(entry.at * N + entry.q * S));
-    else load_states<S>(m, a.dlast ? a.dlast + b * a.width * a.states : nullptr, entry.at, entry.q, a.states);
+    const int behind = min((seg + 1) * a.ratio, a.pieces);            // the first piece behind this segment
+    if (a.joined) {
+      load_floats<S>(m, a.left_state + (b * a.pieces + behind - 1) * a.width * N + (uint32_t)(entry.at * N + entry.q * S));
+    } else {
+      load_states<S>(m, a.dlast ? a.dlast + b * a.width * a.states : nullptr, entry.at, entry.q, a.states);
+      follow<S, true>(m, a, rates, b, behind, entry.at, entry.q);
+    }
 #pragma unroll
     for (int s = 0; s < S; ++s) m[s] = real ? m[s] : 0.0f;           // columns that are not real add nothing to db and dc
     if (begin < live) {
@@ -412,27 +398,26 @@ template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS
   }
 }
 
-// db and dc: each row's shares of the column blocks.
-template <class T, int N> __global__ __launch_bounds__(kJoinBlock) void k_scan_rows_join(ScanArgs a) {
-  const int64_t id = (int64_t)blockIdx.x * kJoinBlock + threadIdx.x, row = id / (2 * N);
-  const int k = (int)(id % (2 * N)), n = k % N;
-  if (row >= (int64_t)a.batch * a.length || n >= a.states) return;
-  const int64_t b = row / a.length;
-  const int t = (int)(row % a.length);
-  float sum = 0.0f;
-  if (t < rows_in(a, b)) {
+// The shares' sums, always in the same order: db and dc, a number a thread, in the first
+// `row_groups` workgroups; da, dskip and dbias in the others, 16 numbers each, whose shares are
+// dealt to 16 groups of threads.
+template <class T, int N> __global__ __launch_bounds__(kJoinBlock) void k_scan_sums(ScanArgs a, uint32_t row_groups) {
+  __shared__ float part[16][16];
+  if (blockIdx.x < row_groups) {
+    const int64_t id = (int64_t)blockIdx.x * kJoinBlock + threadIdx.x, row = id / (2 * N);
+    const int k = (int)(id % (2 * N)), n = k % N;
+    if (row >= (int64_t)a.batch * a.length || n >= a.states) return;
+    const int64_t b = row / a.length;
+    float sum = 0.0f;
+    if ((int)(row % a.length) < rows_in(a, b)) {
 #pragma unroll 4
-    for (int i = 0; i < a.col_blocks; ++i) sum += a.rows_part[(row * a.col_blocks + i) * 2 * N + k];
+      for (int i = 0; i < a.col_blocks; ++i) sum += a.rows_part[(row * a.col_blocks + i) * 2 * N + k];
+    }
+    ((T*)(k < N ? a.db : a.dc))[row * a.states + n] = from_f32<T>(sum);
+    return;
   }
-  ((T*)(k < N ? a.db : a.dc))[row * a.states + n] = from_f32<T>(sum);
-}
-
-// da, dskip and dbias: 64 numbers per workgroup, sixteen waves each add every sixteenth share.
-constexpr int kJoinWaves = 16;
-template <int N> __global__ __launch_bounds__(64 * kJoinWaves) void k_scan_columns_join(ScanArgs a) {
-  __shared__ float part[64 * kJoinWaves];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t id = (int64_t)blockIdx.x * 64 + lane, numbers = (int64_t)a.width * N, ends = (int64_t)a.width * 2;
+  const int lane = threadIdx.x & 15, group = threadIdx.x >> 4;
+  const int64_t id = (int64_t)(blockIdx.x - row_groups) * 16 + lane, numbers = (int64_t)a.width * N, ends = (int64_t)a.width * 2;
   const float* from = nullptr;
   int64_t step = 0;
   if (id < numbers) {
@@ -445,14 +430,14 @@ template <int N> __global__ __launch_bounds__(64 * kJoinWaves) void k_scan_colum
   float sum = 0.0f;
   if (from) {
 #pragma unroll 8
-    for (int i = wave; i < a.shares; i += kJoinWaves) sum += from[i * step];
+    for (int i = group; i < a.shares; i += 16) sum += from[i * step];
   }
-  part[threadIdx.x] = sum;
+  part[group][lane] = sum;
   __syncthreads();
-  if (wave != 0 || !from) return;
+  if (group != 0 || !from) return;
   sum = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kJoinWaves; ++i) sum += part[i * 64 + lane];
+  for (int i = 0; i < 16; ++i) sum += part[i][lane];
   if (id < numbers) {
     const int n = (int)(id % N);
     if (n < a.states) a.da[id / N * a.states + n] = sum;
@@ -469,14 +454,14 @@ template <int N> __global__ __launch_bounds__(64 * kJoinWaves) void k_scan_colum
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
+#ifndef KP
+#define KP 8192
+#endif
 #ifndef KW
 #define KW 2048
 #endif
-constexpr int64_t kWaves = KW;
-#ifndef KL
-#define KL 64
-#endif
-constexpr int kLeastRows = KL;
+constexpr int64_t kPieceWaves = KP, kWaves = KW;
+constexpr int kLeastRows = 64;
 constexpr int64_t kWorkgroups = 1024;       // each leaves a share of da
 #ifndef BC
 #define BC 64
@@ -484,14 +469,15 @@ constexpr int64_t kWorkgroups = 1024;       // each leaves a share of da
 constexpr int kCols = BC;
 
 struct Plan {
-  Cut parts;
+  Cut pieces, parts;
   int col_blocks, shares;
-  uint64_t seg_state, seg_time, rows_part, cols_part, ends_part, bytes;
+  uint64_t left_state, left_time, rows_part, cols_part, ends_part, bytes;
 };
 Plan plan_of(const qds_scan_config* c) {
   Plan p;
   const int64_t n = 4 * lane_states(c), rows = (int64_t)c->batch * c->length;
-  p.parts = cut(c, kWaves, kLeastRows);
+  p.pieces = cut(c, kPieceWaves, kLeastRows, block_rows(c));
+  p.parts = cut(c, kWaves, p.pieces.seg, p.pieces.seg);
   p.col_blocks = (int)ceil_div(c->width, kCols);
   const int64_t items = (int64_t)c->batch * p.parts.segs;
   p.shares = (int)std::max<int64_t>(1, std::min(items, std::max<int64_t>(1, kWorkgroups / p.col_blocks)));
@@ -501,9 +487,9 @@ Plan plan_of(const qds_scan_config* c) {
     at += align_up(floats * sizeof(float));
     return here;
   };
-  const uint64_t segments = p.parts.segs > 1 ? (uint64_t)items * c->width : 0;
-  p.seg_state = take(segments * n);
-  p.seg_time = take(segments);
+  const uint64_t left = p.parts.segs > 1 ? (uint64_t)c->batch * p.pieces.segs * c->width : 0;
+  p.left_state = take(left * n);
+  p.left_time = take(left);
   p.rows_part = take((uint64_t)rows * p.col_blocks * 2 * n);
   p.cols_part = take((uint64_t)p.shares * c->width * n);
   p.ends_part = take((uint64_t)p.shares * c->width * 2);
@@ -513,8 +499,8 @@ Plan plan_of(const qds_scan_config* c) {
 bool fits(const qds_scan_config* c) {
   const Plan p = plan_of(c);
   const int64_t most = most_blocks(kJoinBlock);
-  return (int64_t)c->batch <= most / (ceil_div(c->width, 64) * p.parts.segs) && (int64_t)c->batch * c->width <= most * 8 &&
-         (int64_t)c->batch * c->length <= most * 4;
+  return (int64_t)c->batch <= most / (ceil_div(c->width, 64) * p.pieces.segs) && (int64_t)c->batch * c->width <= most / 2 &&
+         (int64_t)c->batch * c->length <= most * 2;
 }
 
 }  // namespace
@@ -574,11 +560,16 @@ extern "C" qds_status qds_selective_scan_backward(const qds_scan_config* c, qds_
   a.marks = (float*)marks;
   a.seg = p.parts.seg;
   a.segs = p.parts.segs;
+  a.piece = p.pieces.seg;
+  a.pieces = p.pieces.segs;
+  a.ratio = p.parts.seg / p.pieces.seg;
+  a.joined = a.segs > 1 && a.pieces > kFewPieces;
+  if (a.segs == 1) a.ratio = a.pieces;
   a.col_blocks = p.col_blocks;
   a.shares = c->batch > 0 ? p.shares : 0;
   char* ws = (char*)workspace;
-  a.seg_state = (float*)(ws + p.seg_state);
-  a.seg_time = (float*)(ws + p.seg_time);
+  a.left_state = (float*)(ws + p.left_state);
+  a.left_time = (float*)(ws + p.left_time);
   a.rows_part = (float*)(ws + p.rows_part);
   a.cols_part = (float*)(ws + p.cols_part);
   a.ends_part = (float*)(ws + p.ends_part);
@@ -588,18 +579,18 @@ extern "C" qds_status qds_selective_scan_backward(const qds_scan_config* c, qds_
     constexpr int L = decltype(S)::value, N = 4 * L;
     if (c->batch > 0) {
       if (a.segs > 1) {
-        const uint32_t grid = (uint32_t)(c->batch * ceil_div(c->width, 64) * (a.segs - 1));
+        const uint32_t grid = (uint32_t)(c->batch * ceil_div(c->width, 64) * (a.pieces - a.ratio));
         if (gate.data) k_scan_back<T, L, true><<<grid, 256, 0, s>>>(a);
         else k_scan_back<T, L, false><<<grid, 256, 0, s>>>(a);
-        k_scan_back_join<N><<<(uint32_t)ceil_div((int64_t)c->batch * c->width * N, kJoinBlock), kJoinBlock, 0, s>>>(a);
+        if (a.joined) k_scan_join<N, true><<<(uint32_t)ceil_div((int64_t)c->batch * c->width * N, 16), kScanJoin, 0, s>>>(a);
       }
       const uint32_t grid = (uint32_t)(a.col_blocks * a.shares);
       if (gate.data) k_scan_backward<T, L, kCols, true><<<grid, kCols * 4, 0, s>>>(a);
       else k_scan_backward<T, L, kCols, false><<<grid, kCols * 4, 0, s>>>(a);
-      if (c->length > 0)
-        k_scan_rows_join<T, N><<<(uint32_t)ceil_div((int64_t)c->batch * c->length * 2 * N, kJoinBlock), kJoinBlock, 0, s>>>(a);
     }
-    k_scan_columns_join<N><<<(uint32_t)ceil_div((int64_t)c->width * (N + 2), 64), 64 * kJoinWaves, 0, s>>>(a);
+    const uint32_t row_groups = (uint32_t)ceil_div((int64_t)c->batch * c->length * 2 * N, kJoinBlock);
+    const uint32_t col_groups = (uint32_t)ceil_div((int64_t)c->width * (N + 2), 16);
+    k_scan_sums<T, N><<<row_groups + col_groups, kJoinBlock, 0, s>>>(a, row_groups);
   });
   return launch_status();
 }

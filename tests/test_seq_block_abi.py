@@ -231,8 +231,8 @@ def test_scratch_memory_stays_small(lib):
     c = scan(batch=32, length=1000, width=1024)
     need = bytes_of(lib.qds_selective_scan_backward_workspace, c)[1]
     assert need < 0.3 * 14 * 32 * 1000 * 1024
-    # one mark, [columns][states] fp32, for 16 rows
-    assert bytes_of(lib.qds_selective_scan_marks, c)[1] == 32 * 63 * 1024 * 16 * 4
+    # one mark, [columns][states] fp32, for 8 rows
+    assert bytes_of(lib.qds_selective_scan_marks, c)[1] == 32 * 125 * 1024 * 16 * 4
     assert bytes_of(lib.qds_causal_conv_backward_workspace, conv(batch=32, length=1000, width=1024))[1] <= 2048 * 5 * 128 * 4
 
 
