@@ -14,7 +14,11 @@ namespace seq {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kAhead = 4;                // rows whose loads are under way together
+// Columns a thread holds, and rows whose loads are under way together: few columns leave registers
+// for many waves.  16 bits, 32 x 1000 x 1024, forward and backward: two columns and eight rows
+// 88 us, four and four 98; fp32, 16 x 1000 x 777: 78 and 70.
+template <class T> constexpr int kVec = sizeof(T) == 2 ? 2 : 4;
+template <int VEC> constexpr int kRowsAhead = VEC == 2 ? 8 : 4;
 
 struct Rows {
   char* p;
@@ -77,18 +81,19 @@ template <class T, int VEC, int TAPS, bool TAIL> __global__ __launch_bounds__(kB
   }
   float w[TAPS][VEC], bias[VEC];
   load_weights<T, VEC, TAPS>(w, bias, a, at);
-  // rows t - TAPS + 1 .. t + kAhead - 1
-  float x[TAPS - 1 + kAhead][VEC];
+  constexpr int AHEAD = kRowsAhead<VEC>;
+  // rows t - TAPS + 1 .. t + AHEAD - 1
+  float x[TAPS - 1 + AHEAD][VEC];
   if (begin < live) {
 #pragma unroll
     for (int i = 0; i < TAPS - 1; ++i) load_row<T, VEC, TAPS>(x[i], a, b, begin - (TAPS - 1) + i, at);
   }
-  for (int t = begin; t < live; t += kAhead) {
+  for (int t = begin; t < live; t += AHEAD) {
     // a chunk's last rows may be fewer: those behind are read again as the last, and not stored
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) load<T, VEC>(x[TAPS - 1 + i], row_of<T>(a.x, b, min(t + i, live - 1)) + at);
+    for (int i = 0; i < AHEAD; ++i) load<T, VEC>(x[TAPS - 1 + i], row_of<T>(a.x, b, min(t + i, live - 1)) + at);
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
+    for (int i = 0; i < AHEAD; ++i) {
       float y[VEC];
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
@@ -102,7 +107,7 @@ template <class T, int VEC, int TAPS, bool TAIL> __global__ __launch_bounds__(kB
 #pragma unroll
     for (int i = 0; i < TAPS - 1; ++i)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) x[i][e] = x[i + kAhead][e];
+      for (int e = 0; e < VEC; ++e) x[i][e] = x[i + AHEAD][e];
   }
   const float zero[VEC] = {};
   for (int t = max(begin, live); t < end; ++t) store<T, VEC>(row_of<T>(a.y, b, t) + at, zero);
@@ -112,8 +117,8 @@ template <class T, int VEC, int TAPS, bool TAIL> __global__ __launch_bounds__(kB
 // A thread goes down its chunk and the taps - 1 rows behind it, whose g its last rows need.
 // A workgroup's threads hold `lanes` packs of columns, times kBlock / lanes chunks at a time;
 // it adds its threads' shares of dweight and leaves their sum for k_conv_dweight.
-template <class T, int VEC, int TAPS, bool TAIL> __global__ __launch_bounds__(kBlock) void k_conv_backward(ConvArgs a) {
-  constexpr int SUMS = (TAPS + 1) * VEC;
+template <class T, int VEC, int TAPS, bool TAIL, bool SILU> __global__ __launch_bounds__(kBlock) void k_conv_backward(ConvArgs a) {
+  constexpr int SUMS = (TAPS + 1) * VEC, AHEAD = kRowsAhead<VEC>;
   __shared__ float shares[kBlock / 2 * SUMS];
   const int lane = threadIdx.x & (a.lanes - 1), sub = threadIdx.x / (uint32_t)a.lanes, subs = kBlock / a.lanes;
   const int pack = blockIdx.x * a.lanes + lane;
@@ -155,21 +160,23 @@ template <class T, int VEC, int TAPS, bool TAIL> __global__ __launch_bounds__(kB
         for (int e = 0; e < VEC; ++e) g[i][e] = 0.0f;
 #pragma unroll
       for (int i = 1; i < TAPS; ++i) load_row<T, VEC, TAPS>(x[i], a, b, begin - TAPS + i, at);
-      for (int t0 = begin; t0 < stop; t0 += kAhead) {
-        float nx[kAhead][VEC], ny[kAhead][VEC];
-        if (n > 0) {
+      Pack<T, VEC> nx[AHEAD], ny[AHEAD];
+      auto fetch = [&](int t0) {
 #pragma unroll
-          for (int i = 0; i < kAhead; ++i) {
-            const int t = min(t0 + i, n - 1);
-            load<T, VEC>(nx[i], row_of<T>(a.x, b, t) + at);
-            load<T, VEC>(ny[i], row_of<T>(a.dy, b, t) + at);
-          }
+        for (int i = 0; i < AHEAD; ++i) {
+          const int t = max(min(t0 + i, n - 1), 0);
+          __builtin_memcpy(&nx[i], row_of<T>(a.x, b, t) + at, sizeof(nx[i]));
+          __builtin_memcpy(&ny[i], row_of<T>(a.dy, b, t) + at, sizeof(ny[i]));
         }
+      };
+      // INNER: all of the rows are the chunk's own
+      auto advance = [&](int t0, auto INNER) {
+        constexpr bool inner = decltype(INNER)::value;
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
+        for (int i = 0; i < AHEAD; ++i) {
           const int t = t0 + i;
-          if (t >= stop) break;
-          const bool in = t < n, own = t < live;
+          if (!inner && t >= stop) break;
+          const bool in = inner || t < n, own = inner || t < live;
           float v[VEC];
 #pragma unroll
           for (int e = 0; e < VEC; ++e) {
@@ -178,25 +185,40 @@ template <class T, int VEC, int TAPS, bool TAIL> __global__ __launch_bounds__(kB
               x[k][e] = x[k + 1][e];
               g[k][e] = g[k + 1][e];
             }
-            x[TAPS - 1][e] = in ? nx[i][e] : 0.0f;
-            float d = in ? ny[i][e] : 0.0f;
-            if (a.silu) {
+            x[TAPS - 1][e] = in ? to_f32(nx[i].v[e]) : 0.0f;
+            float d = in ? to_f32(ny[i].v[e]) : 0.0f;
+            if (SILU) {
               float p = bias[e];
 #pragma unroll
               for (int k = 0; k < TAPS; ++k) p = fmaf(w[k][e], x[k][e], p);
               d = in ? d * silu_slope(p, sigmoid(p)) : 0.0f;
             }
             g[TAPS - 1][e] = d;
-            const float mine = own ? d : 0.0f;
 #pragma unroll
-            for (int k = 0; k < TAPS; ++k) sum[k][e] = own ? fmaf(mine, x[k][e], sum[k][e]) : sum[k][e];
-            sum[TAPS][e] += mine;
-            v[e] = 0.0f;
+            for (int k = 0; k < TAPS; ++k) sum[k][e] = own ? fmaf(d, x[k][e], sum[k][e]) : sum[k][e];
+            sum[TAPS][e] += own ? d : 0.0f;
+            v[e] = w[0][e] * d;
 #pragma unroll
-            for (int k = 0; k < TAPS; ++k) v[e] = fmaf(w[k][e], g[TAPS - 1 - k][e], v[e]);
+            for (int k = 1; k < TAPS; ++k) v[e] = fmaf(w[k][e], g[TAPS - 1 - k][e], v[e]);
           }
-          if (t - TAPS + 1 >= from) out(t - TAPS + 1, v);
+          const int s = t - TAPS + 1;
+          if (s >= from) {
+            if (!inner || s < 0) out(s, v);
+            else store<T, VEC>(row_of<T>(a.dx, b, s) + at, v);      // no row of the last state yet
+          }
         }
+      };
+      int t0 = begin;
+      if (n > 0) fetch(t0);
+      while (t0 + AHEAD <= live) {
+        advance(t0, std::true_type{});
+        t0 += AHEAD;
+        fetch(t0);
+      }
+      while (t0 < stop) {
+        advance(t0, std::false_type{});
+        t0 += AHEAD;
+        if (n > 0 && t0 < stop) fetch(t0);
       }
     }
     const float zero[VEC] = {};
@@ -290,7 +312,7 @@ template <class T, int VEC, int TAPS, bool TAIL> __global__ __launch_bounds__(kB
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-constexpr int kShares = 2048;             // workgroups of the backward pass, each with a share of dweight
+constexpr int kShares = 2048;            // workgroups of the backward pass, each with a share of dweight
 
 qds_status validate(const qds_conv_config* c, bool step) {
   if (!c || c->abi_version != QDS_ABI_VERSION) return QDS_ERR_INVALID_ARG;
@@ -302,27 +324,26 @@ qds_status validate(const qds_conv_config* c, bool step) {
   return QDS_OK;
 }
 
-// Packs of four columns: of eight, a thread's rows, weights and sums leave too few registers
-// for waves that hide the loads.
-constexpr int kVec = 4;
-int pack_width(const qds_conv_config* c) { return c->width < kVec ? 1 : kVec; }
+int vec_of(const qds_conv_config* c) { return c->dtype == QDS_F32 ? kVec<float> : kVec<bf16>; }
+int pack_width(const qds_conv_config* c) { return c->width < vec_of(c) ? 1 : vec_of(c); }
 int packs_of(const qds_conv_config* c) { return (int)ceil_div(c->width, pack_width(c)); }
 
-template <int TAPS, class F> void with_pack(const qds_conv_config* c, F&& f) {
-  if (c->width < kVec) f(Int<1>{}, Int<TAPS>{}, std::false_type{});
-  else if (c->width % kVec) f(Int<kVec>{}, Int<TAPS>{}, std::true_type{});
-  else f(Int<kVec>{}, Int<TAPS>{}, std::false_type{});
+template <class T, int TAPS, class F> void with_pack(const qds_conv_config* c, F&& f) {
+  constexpr int V = kVec<T>;
+  if (c->width < V) f(Int<1>{}, Int<TAPS>{}, std::false_type{});
+  else if (c->width % V) f(Int<V>{}, Int<TAPS>{}, std::true_type{});
+  else f(Int<V>{}, Int<TAPS>{}, std::false_type{});
 }
-template <class F> void with_taps(const qds_conv_config* c, F&& f) {
+template <class T, class F> void with_taps(const qds_conv_config* c, F&& f) {
   switch (c->taps) {
-    case 1: return with_pack<1>(c, f);
-    case 2: return with_pack<2>(c, f);
-    case 3: return with_pack<3>(c, f);
-    case 4: return with_pack<4>(c, f);
-    case 5: return with_pack<5>(c, f);
-    case 6: return with_pack<6>(c, f);
-    case 7: return with_pack<7>(c, f);
-    default: return with_pack<8>(c, f);
+    case 1: return with_pack<T, 1>(c, f);
+    case 2: return with_pack<T, 2>(c, f);
+    case 3: return with_pack<T, 3>(c, f);
+    case 4: return with_pack<T, 4>(c, f);
+    case 5: return with_pack<T, 5>(c, f);
+    case 6: return with_pack<T, 6>(c, f);
+    case 7: return with_pack<T, 7>(c, f);
+    default: return with_pack<T, 8>(c, f);
   }
 }
 template <class F> void with_type(const qds_conv_config* c, F&& f) {
@@ -331,9 +352,10 @@ template <class F> void with_type(const qds_conv_config* c, F&& f) {
   else f(half());
 }
 
-// Rows per chunk: as many as leave the card some 2^17 threads, 8 to 64 (a chunk reads taps - 1 rows twice).
+// Rows per chunk, 8 to 64: as many as leave some 2^18 columns' chunks (a chunk reads taps - 1 rows
+// twice, and its loads wait for each other).
 int chunk_rows(const qds_conv_config* c) {
-  const int64_t cells = (int64_t)c->batch * c->length * packs_of(c);
+  const int64_t cells = (int64_t)c->batch * c->length * c->width;
   int rows = 64;
   while (rows > 8 && cells / rows < (1 << 18)) rows /= 2;
   return rows;
@@ -345,7 +367,7 @@ bool numbered(const qds_conv_config* c) { return (int64_t)c->batch * chunk_count
 // Packs side by side in a workgroup of the backward pass, and workgroups over the chunks.
 int lane_count(const qds_conv_config* c) {
   int lanes = 1;
-  while (lanes < 32 && lanes < packs_of(c)) lanes *= 2;
+  while (lanes < 64 && lanes < packs_of(c)) lanes *= 2;
   return lanes;
 }
 int share_count(const qds_conv_config* c) {
@@ -393,7 +415,7 @@ extern "C" qds_status qds_causal_conv(const qds_conv_config* c, qds_rows x, cons
   const int64_t blocks = ceil_div((int64_t)c->batch * a.chunks * a.packs, kBlock);
   hipStream_t s = (hipStream_t)stream;
   with_type(c, [&](auto type) {
-    with_taps(c, [&](auto V, auto K, auto TAIL) {
+    with_taps<decltype(type)>(c, [&](auto V, auto K, auto TAIL) {
       k_conv<decltype(type), decltype(V)::value, decltype(K)::value, decltype(TAIL)::value><<<(uint32_t)blocks, kBlock, 0, s>>>(a);
     });
   });
@@ -442,8 +464,11 @@ extern "C" qds_status qds_causal_conv_backward(const qds_conv_config* c, qds_row
   const dim3 join((uint32_t)ceil_div(a.width, 64), (uint32_t)(c->taps + 1));
   with_type(c, [&](auto type) {
     using T = decltype(type);
-    with_taps(c, [&](auto V, auto K, auto TAIL) {
-      k_conv_backward<T, decltype(V)::value, decltype(K)::value, decltype(TAIL)::value><<<grid, kBlock, 0, s>>>(a);
+    with_taps<T>(c, [&](auto V, auto K, auto TAIL) {
+      constexpr int v = decltype(V)::value, taps = decltype(K)::value;
+      constexpr bool tail = decltype(TAIL)::value;
+      if (c->silu) k_conv_backward<T, v, taps, tail, true><<<grid, kBlock, 0, s>>>(a);
+      else k_conv_backward<T, v, taps, tail, false><<<grid, kBlock, 0, s>>>(a);
     });
     k_conv_dweight<T><<<join, 64 * kJoinWaves, 0, s>>>(a, c->taps);
   });
@@ -467,7 +492,7 @@ extern "C" qds_status qds_causal_conv_step(const qds_conv_config* c, qds_rows x,
   const int64_t blocks = ceil_div((int64_t)c->batch * a.packs, kBlock);
   hipStream_t s = (hipStream_t)stream;
   with_type(c, [&](auto type) {
-    with_taps(c, [&](auto V, auto K, auto TAIL) {
+    with_taps<decltype(type)>(c, [&](auto V, auto K, auto TAIL) {
       k_conv_step<decltype(type), decltype(V)::value, decltype(K)::value, decltype(TAIL)::value><<<(uint32_t)blocks, kBlock, 0, s>>>(a);
     });
   });
