@@ -742,7 +742,9 @@ def _scan_setup(u, delta, a, b, c, skip, gate, bias, rows, query=None):
     for name, t in (("skip", skip), ("bias", bias)):
         if t is not None:
             _like(name, t, u, (width,), torch.float32)
-    return _remember(key, _plan(QdsScanConfig, query, code, u.shape[0], u.shape[1] if rows else 0, width, a.shape[1]))
+    fields = code, u.shape[0], u.shape[1] if rows else 0, width, a.shape[1]
+    marks = _plan(QdsScanConfig, "qds_selective_scan_marks", *fields)[2] if rows else 0
+    return _remember(key, (*_plan(QdsScanConfig, query, *fields), marks))
 
 
 def _scan_state(name, t, cfg, ref):
@@ -770,8 +772,7 @@ def selective_scan_forward(u, delta, a, b, c, skip=None, gate=None, bias=None, s
 
     Returns o, the state behind the last row, and with `keep` what selective_scan_backward
     needs of this pass (else None)."""
-    args = (u, delta, a, b, c, skip, gate, bias, True)
-    cfg, ref, size = _scan_setup(*args, "qds_selective_scan_workspace")
+    cfg, ref, size, room = _scan_setup(u, delta, a, b, c, skip, gate, bias, True, "qds_selective_scan_workspace")
     state = _scan_state("state", state, cfg, u)
     lengths = _lengths(lengths, cfg.batch, u)
     u, delta, b, c = _near(u), _near(delta), _near(b), _near(c)
@@ -780,7 +781,7 @@ def selective_scan_forward(u, delta, a, b, c, skip=None, gate=None, bias=None, s
     last = u.new_empty((cfg.batch, cfg.width, cfg.states), dtype=torch.float32)
     with _on(u):
         ws = _scratch(size, u)
-        marks = u.new_empty(_scan_setup(*args, "qds_selective_scan_marks")[2], dtype=torch.uint8) if keep else None
+        marks = u.new_empty(room, dtype=torch.uint8) if keep else None
         _check(lib().qds_selective_scan(
             ref, _row_view(u), _row_view(delta), a.data_ptr(), _row_view(b), _row_view(c), _ptr(skip), _row_view(gate),
             _ptr(bias), _ptr(state), _ptr(lengths), o.data_ptr(), last.data_ptr(), _ptr(marks), _ptr(ws), size,
@@ -792,10 +793,9 @@ def selective_scan_backward(do, u, delta, a, b, c, marks, skip=None, gate=None, 
     """Gradients from those of o and of the last state (`dlast`; None: 0), with what the forward
     call saw and kept: returns du, ddelta, da, db, dc, dskip, dgate, dbias (None for those that
     are) and that of the first state."""
-    args = (u, delta, a, b, c, skip, gate, bias, True)
-    cfg, ref, size = _scan_setup(*args, "qds_selective_scan_backward_workspace")
+    cfg, ref, size, room = _scan_setup(u, delta, a, b, c, skip, gate, bias, True, "qds_selective_scan_backward_workspace")
     _like("do", do, u, u.shape)
-    _like("marks", marks, u, (_scan_setup(*args, "qds_selective_scan_marks")[2],), torch.uint8)
+    _like("marks", marks, u, (room,), torch.uint8)
     dlast = _scan_state("dlast", dlast, cfg, u)
     lengths = _lengths(lengths, cfg.batch, u)
     do, u, delta, b, c = _near(do), _near(u), _near(delta), _near(b), _near(c)
@@ -819,7 +819,7 @@ def selective_scan_step(u, delta, a, b, c, state, skip=None, gate=None, bias=Non
     """One row of each batch element: u, delta, gate [batch, width], b, c [batch, states].
     Writes the new state into `out_state` (by default into `state` itself) and returns
     o [batch, width] and that state."""
-    cfg, ref, _ = _scan_setup(u, delta, a, b, c, skip, gate, bias, False)
+    cfg, ref, _, _ = _scan_setup(u, delta, a, b, c, skip, gate, bias, False)
     out_state = state if out_state is None else out_state
     shape = (cfg.batch, cfg.width, cfg.states)
     _written("state", state, u, shape, torch.float32)
