@@ -239,7 +239,7 @@ typedef struct {
 
 /* weight [taps][width], bias [width] or null, contiguous.  lengths [batch] int32
  * gives each element's rows n (clamped to 0 .. length; null: all `length`); rows
- * from n on are not read and get y = 0.  state_in null: 0.  state_out (may be
+ * from n on are not read and get y = 0.  y is not x.  state_in null: 0.  state_out (may be
  * null; not state_in): the taps - 1 rows before row n. */
 qds_status qds_causal_conv(const qds_conv_config* c, qds_rows x, const void* weight, const void* bias,
                            const void* state_in, const int32_t* lengths, qds_rows y, void* state_out,
@@ -279,7 +279,7 @@ typedef struct {
 /* u, delta, gate: rows of `width`; b, c: rows of `states`; from 0 to 2^23
  * elements apart (else QDS_ERR_UNSUPPORTED).  o [batch][length][width], contiguous.
  * a [width][states] fp32; skip and bias [width] fp32 or null (0); gate.data null: o = y.  lengths as
- * for the convolution.  state_in null: 0.  state_out (may be null, or state_in):
+ * for the convolution.  state_in null: 0.  state_out (may be null; not state_in):
  * h after row n - 1.  marks (null unless a backward pass follows, which needs
  * them; 256-byte aligned): states that the backward pass starts from, *bytes as
  * its size query gives. */
@@ -293,7 +293,8 @@ qds_status qds_selective_scan(const qds_scan_config* c, qds_rows u, qds_rows del
 /* Gradients from do and dstate_out (null: 0), contiguous: du, ddelta, dgate (null
  * without a gate) [batch][length][width] and db, dc [batch][length][states] of dtype,
  * 0 from row n on; da, dskip, dbias (the last two may be null) and dstate_in (may be
- * null, or dstate_out) fp32. */
+ * null; not dstate_out) fp32.  batch times length is at most 2^25 (else
+ * QDS_ERR_UNSUPPORTED). */
 qds_status qds_selective_scan_backward_workspace(const qds_scan_config* c, uint64_t* bytes);
 qds_status qds_selective_scan_backward(const qds_scan_config* c, qds_rows dout, qds_rows u, qds_rows delta,
                                        const float* a, qds_rows b, qds_rows cc, const float* skip,

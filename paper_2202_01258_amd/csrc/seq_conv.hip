@@ -401,7 +401,7 @@ extern "C" qds_status qds_causal_conv(const qds_conv_config* c, qds_rows x, cons
   if (!numbered(c)) return QDS_ERR_UNSUPPORTED;
   if (c->batch == 0) return QDS_OK;
   if (!weight || (c->length > 0 && (!x.data || !y.data))) return QDS_ERR_INVALID_ARG;
-  if (state_out && state_out == state_in) return QDS_ERR_INVALID_ARG;
+  if ((state_out && state_out == state_in) || (c->length > 0 && x.data == y.data)) return QDS_ERR_INVALID_ARG;
   ConvArgs a = args_of(c);
   a.x = rows(x);
   a.y = rows(y);

@@ -1,5 +1,11 @@
 // seq_scan.hip -- selective state space scan: forward and one row.  The C ABI is in
 // include/qd_seq.h, the layout of the work in seq_scan.hpp.
+//
+// Bound by the vector units.  A state of a row takes an exponential (8.2 cycles of a wave on a
+// SIMD), two products and an fma (2.7 each), its output another fma, where a column's row moves 8
+// bytes: at 16 states some 120 cycles for 16 columns (lane moves, softplus and gate included), four
+// times what memory takes for them.  1 x 65536 x 1024 bfloat16: 313 us for the outputs (183 cycles),
+// 245 us for the pieces in front of them.
 #include <algorithm>
 
 #include "seq_scan.hpp"
@@ -12,7 +18,7 @@ constexpr int kBlock = 256, kColumns = kBlock / 4;
 // One segment of 64 columns.  LOCAL: what the segment leaves behind when it starts from
 // zero, and the sum of its steps; otherwise outputs, marks and the last state.
 template <class T, int S, bool LOCAL, bool GATE> __global__ __launch_bounds__(kBlock) void k_scan(ScanArgs a) {
-  constexpr int K = kStageRows<S>, MARK = kScanRows<S>, N = 4 * S, QUADS = K / 4;
+  constexpr int K = kStageRows<S>, MARK = kScanRows, N = 4 * S, QUADS = K / 4;
   SEQ_SHARED float bc[2][K * 2 * N];
   const int q = threadIdx.x & 3;
   const Quad quad(q);
@@ -168,13 +174,13 @@ template <class T, int S, bool TAIL> __global__ __launch_bounds__(kBlock) void k
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-#ifndef KW
-#define KW 8192
-#endif
-constexpr int64_t kWaves = KW;
-constexpr int kLeastRows = 64;
+// Two waves on each SIMD do without cuts; fewer are cut to eight (one piece costs what 0.4 of a
+// main pass does).  16 states, bfloat16, 48 x 1000 x 1024: 239 us whole, 302 cut; 1 x 65536 x 1024: 634 us
+// cut for two waves, 522 for eight.
+constexpr int64_t kWhole = 2048, kWaves = 8192;
+constexpr int kLeastRows = 32;
 
-Cut forward_cut(const qds_scan_config* c) { return cut(c, kWaves, kLeastRows, block_rows(c)); }
+Cut forward_cut(const qds_scan_config* c) { return cut(c, whole_waves(c) >= kWhole ? 1 : kWaves, kLeastRows, kScanRows); }
 uint64_t state_bytes(const qds_scan_config* c, int segs) {
   return align_up((uint64_t)c->batch * segs * c->width * 4 * lane_states(c) * sizeof(float));
 }
@@ -193,7 +199,7 @@ extern "C" qds_status qds_selective_scan_marks(const qds_scan_config* c, uint64_
   const qds_status st = validate_scan(c, false);
   if (st != QDS_OK) return st;
   if (!bytes) return QDS_ERR_INVALID_ARG;
-  *bytes = state_bytes(c, block_count(c));
+  *bytes = state_bytes(c, mark_count(c));
   return QDS_OK;
 }
 
@@ -218,6 +224,7 @@ extern "C" qds_status qds_selective_scan(const qds_scan_config* c, qds_rows u, q
   if (!a_ || (c->length > 0 && (!u.data || !delta.data || !b.data || !cc.data || !o))) return QDS_ERR_INVALID_ARG;
   for (qds_rows* r : {&u, &delta, &b, &cc, &gate})
     if (!near_rows(*r, c->length)) return QDS_ERR_UNSUPPORTED;
+  if (state_out && state_out == state_in) return QDS_ERR_INVALID_ARG;      // all segments read one, the last writes the other
   if (((uintptr_t)marks & 255) || (need > 0 && (!workspace || ((uintptr_t)workspace & 255)))) return QDS_ERR_INVALID_ARG;
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
   ScanArgs a = scan_args(c);

@@ -19,13 +19,11 @@ namespace seq {
 
 constexpr int kScanStates = 32;                  // at most
 
-// Rows of a block.  The backward pass starts from the state in front of a block ("mark")
-// and keeps 2 K S numbers of it in registers.
-#ifndef BK
-#define BK 8
-#endif
-template <int S> constexpr int kScanRows = S <= 4 ? BK : 8;
-// Rows whose b and c the forward pass has in LDS.
+// Rows that the backward pass has at a time: it starts from the state in front of them ("mark"),
+// which the forward pass leaves, and keeps their states in registers.  With 16 rows the marks take half
+// the memory, but neither decays nor b and c fit beside the states.
+constexpr int kScanRows = 8;
+// Rows whose b and c the other passes have in LDS.
 template <int S> constexpr int kStageRows = S <= 4 ? 16 : 8;
 
 struct Rows {
@@ -242,8 +240,7 @@ inline bool near_rows(qds_rows& r, int length) {
   return !r.data || (r.stride[1] >= 0 && r.stride[1] < (1 << 23));
 }
 inline int lane_states(const qds_scan_config* c) { return c->states <= 4 ? 1 : c->states <= 8 ? 2 : c->states <= 16 ? 4 : 8; }
-inline int block_rows(const qds_scan_config* c) { return lane_states(c) == 8 ? kScanRows<8> : kScanRows<4>; }
-inline int block_count(const qds_scan_config* c) { return (int)ceil_div(c->length, block_rows(c)); }
+inline int mark_count(const qds_scan_config* c) { return (int)ceil_div(c->length, kScanRows); }
 
 // What all pieces before `until` leave together when the first starts from x (the pieces in their
 // order, or from the last one backwards).
@@ -307,18 +304,20 @@ template <int N, bool BACK> __global__ __launch_bounds__(kScanJoin) void k_scan_
   if (to == count && (from < to || group == 0)) a.left_state[place(count) * N + n] = x;
 }
 
+// Waves of a pass over whole episodes.
+inline int64_t whole_waves(const qds_scan_config* c) { return std::max<int64_t>(1, (int64_t)c->batch * ceil_div(c->width, 16)); }
+
 // Rows of a segment and their number, for a kernel that wants `waves` waves.
 struct Cut {
   int seg, segs;
 };
 inline Cut cut(const qds_scan_config* c, int64_t waves, int least, int unit) {
-  const int64_t whole = std::max<int64_t>(1, (int64_t)c->batch * ceil_div(c->width, 16));
-  const int64_t want = std::max<int64_t>(1, waves / whole);
+  const int64_t want = std::max<int64_t>(1, waves / whole_waves(c));
   int64_t seg = std::max<int64_t>(least, ceil_div(c->length, want));
   seg = ceil_div(seg, unit) * unit;
   return Cut{(int)seg, (int)std::max<int64_t>(1, ceil_div(c->length, seg))};
 }
-constexpr int kFewPieces = 16;                   // so many are followed by the main pass itself
+constexpr int kFewPieces = 32;                   // so many are followed by the main pass itself
 
 template <class F> void scan_instance(const qds_scan_config* c, F&& f) {
   auto with_type = [&](auto S) {
@@ -340,7 +339,7 @@ inline ScanArgs scan_args(const qds_scan_config* c) {
   a.length = c->length;
   a.width = c->width;
   a.states = c->states;
-  a.blocks = block_count(c);
+  a.blocks = mark_count(c);
   return a;
 }
 

@@ -1,5 +1,9 @@
 // seq_scan_backward.hip -- gradients of the selective state space scan.  The C ABI is in
 // include/qd_seq.h, the layout of the work in seq_scan.hpp.
+//
+// Bound by the vector units: 97 vector instructions for a row of 16 columns and 16 states, which
+// are issued 84% of the time (64 x 1000 x 1024 bfloat16, 809 us).  Two waves a SIMD is what the states
+// in registers leave; three, with fewer of them kept, took 1.07 of the time.
 #include <algorithm>
 
 #include "seq_scan.hpp"
@@ -161,11 +165,8 @@ struct Place {
 // All gradients.  A workgroup has COLS columns and goes through every `shares`-th segment, each
 // from its last block of rows to its first: a block's states and decays are formed again from
 // its mark and kept in registers for the way back.
-#ifndef MW
-#define MW 2
-#endif
-template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS * 4, S <= 4 ? MW : 2) void k_scan_backward(ScanArgs a) {
-  constexpr int K = kScanRows<S>, N = 4 * S, QUADS = K / 4, BLOCK = COLS * 4, WAVES = BLOCK / 64;
+template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS * 4, 2) void k_scan_backward(ScanArgs a) {
+  constexpr int K = kScanRows, N = 4 * S, QUADS = K / 4, BLOCK = COLS * 4, WAVES = BLOCK / 64;
   constexpr bool KEEP = S <= 4;                                     // decays for the way back; else they are formed again
   SEQ_SHARED float bc[2][K * 2 * N];
   // one place only where LDS is short: a barrier more keeps its readers and writers apart
@@ -454,19 +455,11 @@ template <class T, int N> __global__ __launch_bounds__(kJoinBlock) void k_scan_s
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-#ifndef KP
-#define KP 8192
-#endif
-#ifndef KW
-#define KW 2048
-#endif
-constexpr int64_t kPieceWaves = KP, kWaves = KW;
-constexpr int kLeastRows = 64;
+// The main pass holds two waves on each SIMD; the pieces of the first pass are shorter than its segments.
+constexpr int64_t kPieceWaves = 8192, kWaves = 2048;
+constexpr int kLeastRows = 32;
 constexpr int64_t kWorkgroups = 1024;       // each leaves a share of da
-#ifndef BC
-#define BC 64
-#endif
-constexpr int kCols = BC;
+constexpr int kCols = 64;
 
 struct Plan {
   Cut pieces, parts;
@@ -476,7 +469,7 @@ struct Plan {
 Plan plan_of(const qds_scan_config* c) {
   Plan p;
   const int64_t n = 4 * lane_states(c), rows = (int64_t)c->batch * c->length;
-  p.pieces = cut(c, kPieceWaves, kLeastRows, block_rows(c));
+  p.pieces = cut(c, kPieceWaves, kLeastRows, kScanRows);
   p.parts = cut(c, kWaves, p.pieces.seg, p.pieces.seg);
   p.col_blocks = (int)ceil_div(c->width, kCols);
   const int64_t items = (int64_t)c->batch * p.parts.segs;
@@ -532,6 +525,7 @@ extern "C" qds_status qds_selective_scan_backward(const qds_scan_config* c, qds_
       (!dout.data || !u.data || !delta.data || !b.data || !cc.data || !marks || !du || !ddelta || !db || !dc ||
        (gate.data && !dgate) || ((uintptr_t)marks & 255)))
     return QDS_ERR_INVALID_ARG;
+  if (dstate_in && dstate_in == dstate_out) return QDS_ERR_INVALID_ARG;
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
   for (qds_rows* r : {&dout, &u, &delta, &b, &cc, &gate})
     if (!near_rows(*r, c->length)) return QDS_ERR_UNSUPPORTED;

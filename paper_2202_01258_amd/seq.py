@@ -23,11 +23,15 @@ Argument marshalling only: outputs and scratch memory are torch tensors, work
 is enqueued on torch's current stream of the tensors' device, nothing waits for
 the GPU, and there is no fallback.  Tensors are used on that stream alone; a
 tensor made on another stream has to be synchronised with it first, as for any
-torch operation.  Attention takes bfloat16 or float16 tensors whose rows start
-at multiples of 16 bytes and are less than 2^23 elements apart; others are copied first.
-The other operators take float32, too, and rows of any alignment; they copy tensors whose
-columns are apart (the scan those with rows 2^23 elements apart or more, dropout those
-that are not contiguous).
+torch operation.  As for any autograd function, too, a backward pass is captured
+into a graph only while no eager graph of the same leaves lives: torch would wait
+for that one's stream within the capture.
+
+Attention takes bfloat16 or float16 tensors whose rows start at multiples of 16
+bytes and are less than 2^23 elements apart; others are copied first.  The other
+operators take float32, too, and rows of any alignment; they copy tensors whose
+columns are apart (the scan those with rows 2^23 elements apart or more, dropout
+those that are not contiguous).
 """
 from __future__ import annotations
 

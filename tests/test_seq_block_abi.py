@@ -90,7 +90,7 @@ CONV_BAD = [(dict(abi_version=0), S.ERR_INVALID_ARG), (dict(dtype=3), S.ERR_INVA
 @pytest.mark.parametrize("over,status", CONV_BAD)
 def test_conv_refusals(lib, over, status):
     c = conv(**over)
-    assert lib.qds_causal_conv(C.byref(c), rows(), P, P, P, None, rows(), P + 4096, None) == status
+    assert lib.qds_causal_conv(C.byref(c), rows(), P, P, P, None, rows(2 * P), P + 4096, None) == status
     assert bytes_of(lib.qds_causal_conv_backward_workspace, c)[0] == status
     if "length" not in over:
         assert lib.qds_causal_conv_step(C.byref(c), rows(), P, P, P, rows(), P, None) == status
@@ -98,8 +98,8 @@ def test_conv_refusals(lib, over, status):
 
 def test_conv_refuses_pointers(lib):
     c = conv()
-    ok = [C.byref(c), rows(), P, P, P, None, rows(), P + 4096, None]
-    for i, bad in [(0, None), (1, NONE), (2, None), (6, NONE), (7, P)]:
+    ok = [C.byref(c), rows(), P, P, P, None, rows(2 * P), P + 4096, None]
+    for i, bad in [(0, None), (1, NONE), (2, None), (6, NONE), (6, rows()), (7, P)]:     # y is not x, one state not the other
         a = list(ok)
         a[i] = bad
         assert lib.qds_causal_conv(*a) == S.ERR_INVALID_ARG
@@ -141,9 +141,9 @@ def test_scan_refuses_pointers(lib):
     c, r = scan(batch=1, width=16), rows()
     st, need = bytes_of(lib.qds_selective_scan_workspace, c)
     assert st == S.OK and need > 0                    # few columns: their rows are cut into segments
-    ok = [C.byref(c), r, r, P, r, r, P, r, P, P, None, P, P, P, P, need, None]
+    ok = [C.byref(c), r, r, P, r, r, P, r, P, P, None, P, P + 4096, P, P, need, None]
     far, back = rows(strides=(1, 1 << 23)), rows(strides=(1, -64))
-    for i, bad in [(0, None), (1, NONE), (2, NONE), (3, None), (4, NONE), (5, NONE), (11, None), (13, P + 64), (14, None),
+    for i, bad in [(0, None), (1, NONE), (2, NONE), (3, None), (4, NONE), (5, NONE), (11, None), (12, P), (13, P + 64), (14, None),
                    (14, P + 128)]:
         a = list(ok)
         a[i] = bad
@@ -156,9 +156,9 @@ def test_scan_refuses_pointers(lib):
     ok[15] = need - 1
     assert lib.qds_selective_scan(*ok) == S.ERR_WORKSPACE_TOO_SMALL
     st, need = bytes_of(lib.qds_selective_scan_backward_workspace, c)
-    ok = [C.byref(c), r, r, r, P, r, r, P, r, P, P, P, None, P, P, P, P, P, P, P, P, P, P, need, None]
+    ok = [C.byref(c), r, r, r, P, r, r, P, r, P, P, P, None, P, P, P, P, P, P, P, P, P + 4096, P, need, None]
     for i, bad in [(1, NONE), (2, NONE), (3, NONE), (4, None), (5, NONE), (6, NONE), (10, None), (10, P + 16), (13, None),
-                   (14, None), (15, None), (16, None), (17, None), (19, None), (22, None), (22, P + 4)]:
+                   (14, None), (15, None), (16, None), (17, None), (19, None), (21, P), (22, None), (22, P + 4)]:
         a = list(ok)
         a[i] = bad
         assert lib.qds_selective_scan_backward(*a) == S.ERR_INVALID_ARG, i
