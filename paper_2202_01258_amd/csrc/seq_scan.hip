@@ -18,7 +18,7 @@ constexpr int kBlock = 256, kColumns = kBlock / 4;
 // One segment of 64 columns.  LOCAL: what the segment leaves behind when it starts from
 // zero, and the sum of its steps; otherwise outputs, marks and the last state.
 template <class T, int S, bool LOCAL, bool GATE> __global__ __launch_bounds__(kBlock) void k_scan(ScanArgs a) {
-  constexpr int K = kStageRows<S>, MARK = kScanRows, N = 4 * S, QUADS = K / 4;
+  constexpr int K = kScanRows, N = 4 * S, QUADS = K / 4;
   SEQ_SHARED float bc[2][K * 2 * N];
   const int q = threadIdx.x & 3;
   const Quad quad(q);
@@ -51,7 +51,7 @@ template <class T, int S, bool LOCAL, bool GATE> __global__ __launch_bounds__(kB
     uint32_t u[QUADS], d[QUADS], z[QUADS];
     Track<T> tu(a.u, b, begin, q, at, real), td(a.delta, b, begin, q, at, real), tz(a.gate, b, begin, q, at, real);
     StagedRows<T, S, K, kBlock> rows(a, b, begin);
-    float* marks = a.marks + (b * a.blocks + begin / MARK) * a.width * N;
+    float* marks = a.marks + (b * a.blocks + begin / K) * a.width * N;
     auto fetch = [&](int t) {
       const Left left{live - t - q - 1};
 #pragma unroll
@@ -81,13 +81,13 @@ template <class T, int S, bool LOCAL, bool GATE> __global__ __launch_bounds__(kB
       }
       const bool more = t + K < live;
       if (more) fetch(t + K);
+      if (!LOCAL && a.marks) {
+        if (real) store_floats<S>(marks + (uint32_t)(at * N + q * S), h);
+        marks += (int64_t)a.width * N;
+      }
       const float* lds = bc[buffer] + q * S;
 #pragma unroll
       for (int i = 0; i < QUADS; ++i) {
-        if (!LOCAL && a.marks && 4 * i % MARK == 0) {
-          if (real && t + 4 * i < live) store_floats<S>(marks + (uint32_t)(at * N + q * S), h);
-          marks += (int64_t)a.width * N;
-        }
         const float x = dt[i] * uu[i];
         float y[4];
         auto row = [&](auto J) {

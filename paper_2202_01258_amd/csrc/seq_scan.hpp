@@ -23,9 +23,6 @@ constexpr int kScanStates = 32;                  // at most
 // which the forward pass leaves, and keeps their states in registers.  With 16 rows the marks take half
 // the memory, but neither decays nor b and c fit beside the states.
 constexpr int kScanRows = 8;
-// Rows whose b and c the other passes have in LDS.
-template <int S> constexpr int kStageRows = S <= 4 ? 16 : 8;
-
 struct Rows {
   char* p;
   int64_t b, t;                                  // strides in elements

@@ -18,7 +18,7 @@ constexpr int kJoinBlock = 256;
 // One piece of 64 columns from its last row to its first, from zero: what it leaves to the
 // piece before, and the sum of its steps.
 template <class T, int S, bool GATE> __global__ __launch_bounds__(256) void k_scan_back(ScanArgs a) {
-  constexpr int K = kStageRows<S>, N = 4 * S, QUADS = K / 4, BLOCK = 256;
+  constexpr int K = S <= 4 ? 16 : 8, N = 4 * S, QUADS = K / 4, BLOCK = 256;
   SEQ_SHARED float bc[2][K * 2 * N];
   const int q = threadIdx.x & 3, blocks = (a.width + 63) / 64;
   const uint32_t item = blockIdx.x / (uint32_t)blocks;
