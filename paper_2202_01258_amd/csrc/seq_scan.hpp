@@ -158,7 +158,7 @@ struct Left {
 
 // A tensor's rows t + q, t + 4 + q, ... at a lane's column, t a scalar that goes up or down: an
 // access costs one vector instruction beside it and no 64-bit arithmetic.  Rows are from 0 to
-// 2^23 elements apart.  Columns that are not real are outside.
+// less than 2^23 elements apart.  Columns that are not real are outside.
 template <class T> struct Track {
   char* p;                                       // of row t
   uint32_t step, lane_at;                        // bytes: from row to row, and the lane's
@@ -230,7 +230,7 @@ inline qds_status validate_scan(const qds_scan_config* c, bool step) {
   if (c->states > kScanStates) return QDS_ERR_UNSUPPORTED;
   return QDS_OK;
 }
-// Rows that a scan reads or writes are from 0 to 2^23 elements apart (a single row's stride
+// Rows that a scan reads are from 0 to less than 2^23 elements apart (a single row's stride
 // means nothing and is set to 0).
 inline bool near_rows(qds_rows& r, int length) {
   if (length < 2) r.stride[1] = 0;

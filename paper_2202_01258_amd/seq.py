@@ -796,7 +796,7 @@ def selective_scan_forward(u, delta, a, b, c, skip=None, gate=None, bias=None, s
 def selective_scan_backward(do, u, delta, a, b, c, marks, skip=None, gate=None, bias=None, dlast=None, lengths=None):
     """Gradients from those of o and of the last state (`dlast`; None: 0), with what the forward
     call saw and kept: returns du, ddelta, da, db, dc, dskip, dgate, dbias (None for those that
-    are) and that of the first state."""
+    are) and that of the first state.  batch times rows is at most 2^25."""
     cfg, ref, size, room = _scan_setup(u, delta, a, b, c, skip, gate, bias, True, "qds_selective_scan_backward_workspace")
     _like("do", do, u, u.shape)
     _like("marks", marks, u, (room,), torch.uint8)
@@ -1122,6 +1122,8 @@ def causal_conv(x, weight, bias=None, state=None, lengths=None, silu: bool = Tru
 
 def selective_scan(u, delta, a, b, c, skip=None, gate=None, bias=None, state=None, lengths=None):
     """selective_scan_forward under autograd: returns o and the last state."""
+    if not torch.is_grad_enabled():              # nothing is kept for a backward pass
+        return selective_scan_forward(u, delta, a, b, c, skip, gate, bias, state, lengths)[:2]
     return _autograd()[4].apply(u, delta, a, b, c, skip, gate, bias, state, lengths)
 
 

@@ -304,6 +304,20 @@ def test_scan_segments(rows, states):
     check_scan(3, rows, 9, states, F16, lengths=[rows - 1, 64, 65])
 
 
+@pytest.mark.parametrize("states", [4, 13, 16, 32])
+def test_scan_many_pieces(states):
+    """More pieces than the main pass follows by itself: a scan over them joins them."""
+    check_scan(1, 1057, 7, states, F32)
+    check_scan(2, 1400, 70, states, BF16, lengths=[1400, 1060])
+    check_scan(3, 1100, 5, states, F16, lengths=[0, 1, 1099])
+
+
+@pytest.mark.parametrize("states", [4, 16, 32])
+def test_scan_pieces_of_segments(states):
+    """Several pieces for each segment of the gradients' main pass, which ends inside them."""
+    check_scan(16, 300, 256, states, BF16, lengths=[300, 0, 1, 31, 32, 33, 63, 64, 65, 95, 96, 97, 128, 200, 299, 300])
+
+
 @pytest.mark.parametrize("how", LAYOUTS)
 def test_scan_layouts(how):
     check_scan(3, 40, 17, 16, BF16, how=how, lengths=[40, 7, 31])
@@ -724,6 +738,8 @@ def test_autograd_matches_the_plain_calls():
     marks = S.selective_scan_forward(*[s[k] for k in names], s["state"], lengths, keep=True)[2]
     want = S.selective_scan_backward(g["do"], *[s[k] for k in names[:5]], marks, *[s[k] for k in names[5:]], g["dlast"], lengths)
     assert same(got, want)
+    with torch.no_grad():
+        assert same(S.selective_scan(*[t[k] for k in names], t["state"], lengths), (o.detach(), last.detach()))
     o, _ = S.selective_scan(*[t[k] for k in names[:5]])
     assert len(torch.autograd.grad(o.sum(), [t[k] for k in names[:5]])) == 5
 
