@@ -5,7 +5,8 @@
 // in the program and the element's number, so the backward pass draws the same again.  Eight
 // elements share a Philox4x32-10 block (Salmon et al., "Parallel random numbers: as easy as 1, 2,
 // 3", SC 2011), 16 bits each: with 32 bits each, four elements would carry the block's ten
-// rounds, as many vector instructions as memory leaves time for.
+// rounds, as many vector instructions as memory leaves time for.  32000 x 1024 bfloat16: 30 us
+// (131 MB, 4.4 TB/s).
 #include "seq_common.hpp"
 #include "seq_rows.hpp"
 

@@ -5,7 +5,7 @@
 // SIMD), two products and an fma (2.7 each), its output another fma, where a column's row moves 8
 // bytes: at 16 states some 120 cycles for 16 columns (lane moves, softplus and gate included), four
 // times what memory takes for them.  1 x 65536 x 1024 bfloat16: 313 us for the outputs (183 cycles),
-// 245 us for the pieces in front of them.
+// 253 us for the pieces in front of them.
 #include <algorithm>
 
 #include "seq_scan.hpp"
@@ -176,7 +176,7 @@ template <class T, int S, bool TAIL> __global__ __launch_bounds__(kBlock) void k
 // ---------------------------------------------------------------------------
 // Two waves on each SIMD do without cuts; fewer are cut to eight (one piece costs what 0.4 of a
 // main pass does).  16 states, bfloat16, 48 x 1000 x 1024: 239 us whole, 302 cut; 1 x 65536 x 1024: 634 us
-// cut for two waves, 522 for eight.
+// cut for two waves, 522 for eight.  (Before b and c were staged by eight rows, which took 0.95 of that.)
 constexpr int64_t kWhole = 2048, kWaves = 8192;
 constexpr int kLeastRows = 32;
 
