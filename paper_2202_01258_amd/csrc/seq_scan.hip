@@ -26,9 +26,9 @@ template <class T, int S, bool LOCAL, bool GATE> __global__ __launch_bounds__(kB
   const int col = (blockIdx.x % (uint32_t)a.col_blocks) * kColumns + (threadIdx.x >> 2);
   const bool real = col < a.width;
   const int at = real ? col : a.width - 1;
-  const int runs = LOCAL ? a.segs - 1 : a.segs;            // nothing comes behind the last segment
-  const int64_t b = item / (uint32_t)runs;
-  const int seg = (int)(item % (uint32_t)runs);
+  const Item which(item, a.batch);                         // of LOCAL all but the last segments: nothing comes behind those
+  const int64_t b = which.b;
+  const int seg = which.part;
   const int n = rows_in(a, b), begin = seg * a.seg, end = min(begin + a.seg, a.length), live = min(end, n);
   float rates[S], h[S];
   load_states<S>(rates, a.a, at, q, a.states);

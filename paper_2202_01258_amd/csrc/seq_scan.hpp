@@ -49,9 +49,29 @@ struct ScanArgs {
   int32_t piece, pieces, ratio;                  // rows of a piece of the first pass; pieces; pieces of a segment
   bool joined;                                   // a scan has run
 };
+// A kernel's arguments, its only ones, read anew: what is needed once for an episode's part is
+// not kept in scalar registers.  Those are short: the backward pass kept 121 numbers in vector
+// registers' lanes, and took them out within its rows (32 x 1000 x 512 with 16 states, forward and
+// backward: 397 us, now 388).
+__device__ inline const ScanArgs& read_args() {
+  auto p = (const __attribute__((address_space(4))) ScanArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  return *(const ScanArgs*)p;
+}
 __device__ inline int rows_in(const ScanArgs& a, int64_t b) {
   return a.lengths ? min(max(a.lengths[b], 0), a.length) : a.length;
 }
+
+// Episodes' parts in the order in which workgroups start: all episodes' first ones, then all
+// second ones, another episode first each time.  Episodes have the early parts and may lack
+// the late ones, and workgroups of one compute unit (every 32nd of 64 columns') have parts of
+// several episodes.
+struct Item {
+  int64_t b;
+  int part;
+  __device__ Item(uint32_t item, int batch)
+      : b((item + item / (uint32_t)batch) % (uint32_t)batch), part((int)(item / (uint32_t)batch)) {}
+};
 
 // The value of lane J of this lane's quad, of lane q ^ 1, of lane q ^ 2.
 template <int CTRL> __device__ inline float lane_move(float v) {

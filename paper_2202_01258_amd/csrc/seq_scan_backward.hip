@@ -25,9 +25,9 @@ template <class T, int S, bool GATE> __global__ __launch_bounds__(256) void k_sc
   const int col = (blockIdx.x % (uint32_t)blocks) * 64 + (threadIdx.x >> 2);
   const bool real = col < a.width;
   const int at = real ? col : a.width - 1;
-  const int runs = a.pieces - a.ratio;                            // no segment asks what the first one's pieces leave
-  const int64_t b = item / (uint32_t)runs;
-  const int piece = a.ratio + (int)(item % (uint32_t)runs);
+  const Item which(item, a.batch);
+  const int64_t b = which.b;
+  const int piece = a.ratio + which.part;                         // no segment asks what the first one's pieces leave
   const int n = rows_in(a, b), begin = piece * a.piece, end = min(begin + a.piece, a.length), live = min(end, n);
   float rates[S], m[S], time = 0.0f;
   load_states<S>(rates, a.a, at, q, a.states);
@@ -165,7 +165,7 @@ struct Place {
 // All gradients.  A workgroup has COLS columns and goes through every `shares`-th segment, each
 // from its last block of rows to its first: a block's states and decays are formed again from
 // its mark and kept in registers for the way back.
-template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS * 4, 2) void k_scan_backward(ScanArgs a) {
+template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS * 4, 2) void k_scan_backward(ScanArgs args) {
   constexpr int K = kScanRows, N = 4 * S, QUADS = K / 4, BLOCK = COLS * 4, WAVES = BLOCK / 64;
   constexpr bool KEEP = S <= 4;                                     // decays for the way back; else they are formed again
   SEQ_SHARED float bc[2][K * 2 * N];
@@ -175,38 +175,45 @@ template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS
   SEQ_SHARED float terms[WAVES][4 * 2 * ColumnSums<S>::PAD];
   const int wave = wave_index();
   const ColumnSums<S> sums(terms[wave]);
-  const int block = blockIdx.x % (uint32_t)a.col_blocks;
-  const uint32_t share = blockIdx.x / (uint32_t)a.col_blocks;
-  const Place place(a.width, block * COLS);
+  const int block = blockIdx.x % (uint32_t)args.col_blocks;
+  const uint32_t share = blockIdx.x / (uint32_t)args.col_blocks;
+  const Place place(args.width, block * COLS);
   const int q = place.q, at = place.at;
   const bool real = place.real;
   const Quad quad(q);
   float rates[S], da[S], dskip = 0.0f, dbias = 0.0f;
-  load_states<S>(rates, a.a, at, q, a.states);
+  load_states<S>(rates, args.a, at, q, args.states);
 #pragma unroll
   for (int s = 0; s < S; ++s) {
     rates[s] = rate(rates[s]);
     da[s] = 0.0f;
   }
-  const float bias = a.bias ? a.bias[at] : 0.0f, skip = a.skip ? a.skip[at] : 0.0f;
+  const float bias = args.bias ? args.bias[at] : 0.0f, skip = args.skip ? args.skip[at] : 0.0f;
   int buffer = 0;
-  const uint32_t items = (uint32_t)(a.batch * a.segs);
-  for (uint32_t item = share; item < items; item += a.shares) {
-    const int64_t b = item / (uint32_t)a.segs;
-    const int seg = (int)(item % (uint32_t)a.segs);
+  uint32_t item = share;
+  while (true) {
+    const ScanArgs& a = read_args();
+    if (item >= (uint32_t)(a.batch * a.segs)) break;
+    const Item which(item, a.batch);
+    const int64_t b = which.b;
+    const int seg = which.part;
     const int n = rows_in(a, b), begin = seg * a.seg, end = min(begin + a.seg, a.length), live = min(end, n);
     float m[S];
-    const Place entry(a.width, block * COLS);
-    const int behind = min((seg + 1) * a.ratio, a.pieces);            // the first piece behind this segment
-    if (a.joined) {
-      load_floats<S>(m, a.left_state + (b * a.pieces + behind - 1) * a.width * N + (uint32_t)(entry.at * N + entry.q * S));
-    } else {
-      load_states<S>(m, a.dlast ? a.dlast + b * a.width * a.states : nullptr, entry.at, entry.q, a.states);
-      follow<S, true>(m, a, rates, b, behind, entry.at, entry.q);
-    }
+    auto enter = [&] {
+      const Place entry(a.width, block * COLS);
+      const int behind = min((seg + 1) * a.ratio, a.pieces);          // the first piece behind this segment
+      if (a.joined) {
+        load_floats<S>(m, a.left_state + (b * a.pieces + behind - 1) * a.width * N + (uint32_t)(entry.at * N + entry.q * S));
+      } else {
+        load_states<S>(m, a.dlast ? a.dlast + b * a.width * a.states : nullptr, entry.at, entry.q, a.states);
+        follow<S, true>(m, a, rates, b, behind, entry.at, entry.q);
+      }
 #pragma unroll
-    for (int s = 0; s < S; ++s) m[s] = real ? m[s] : 0.0f;           // columns that are not real add nothing to db and dc
-    if (begin < live) {
+      for (int s = 0; s < S; ++s) m[s] = real ? m[s] : 0.0f;         // columns that are not real add nothing to db and dc
+    };
+    if (begin >= live) {
+      if (seg == 0) enter();                                          // an episode without rows hands its gradient through
+    } else {
       uint32_t u[QUADS], d[QUADS], z[QUADS], g[QUADS];
       float first[S];
       const int last = begin + (live - 1 - begin) / K * K;
@@ -237,6 +244,7 @@ template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS
       char *ddelta = (char*)a.ddelta + (du.p - (char*)a.du), *dgate = (char*)a.dgate + (du.p - (char*)a.du);
       float* to = a.rows_part + ((b * a.length + last) * a.col_blocks + block) * 2 * N;
       fetch(last);
+      enter();                                   // while the first block is on its way
       rows.store(bc[buffer]);
       __syncthreads();
       for (int t = last; t >= begin; t -= K) {
@@ -376,18 +384,21 @@ template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS
         buffer ^= 1;
       }
     }
-    const Place exit(a.width, block * COLS);
-    if (seg == 0 && a.dfirst) store_states<S>(a.dfirst + b * a.width * a.states, exit.at, exit.q, a.states, exit.real, m);
-    Track<T> dead(a.du, (int64_t)a.length * a.width, a.width, b, max(begin, live), exit.q, exit.at, exit.real);
+    const ScanArgs& z = read_args();
+    item += z.shares;
+    const Place exit(z.width, block * COLS);
+    if (seg == 0 && z.dfirst) store_states<S>(z.dfirst + b * z.width * z.states, exit.at, exit.q, z.states, exit.real, m);
+    Track<T> dead(z.du, (int64_t)z.length * z.width, z.width, b, max(begin, live), exit.q, exit.at, exit.real);
     for (int t = max(begin, live); t < end; t += 4) {
       const Left left{end - t - exit.q - 1};
-      const int64_t here = dead.p - (char*)a.du;
+      const int64_t here = dead.p - (char*)z.du;
       dead.store(0, left, 0.0f);
-      put<T>((char*)a.ddelta + here, left.offset(0, dead.lane_at), 0, from_f32<T>(0.0f));
-      if (GATE) put<T>((char*)a.dgate + here, left.offset(0, dead.lane_at), 0, from_f32<T>(0.0f));
+      put<T>((char*)z.ddelta + here, left.offset(0, dead.lane_at), 0, from_f32<T>(0.0f));
+      if (GATE) put<T>((char*)z.dgate + here, left.offset(0, dead.lane_at), 0, from_f32<T>(0.0f));
       dead.move(4);
     }
   }
+  const ScanArgs& a = read_args();
   dskip = quad_sum(dskip);
   dbias = quad_sum(dbias);
   const Place end(a.width, block * COLS);
@@ -459,6 +470,11 @@ template <class T, int N> __global__ __launch_bounds__(kJoinBlock) void k_scan_s
 constexpr int64_t kPieceWaves = 8192, kWaves = 2048;
 constexpr int kLeastRows = 32;
 constexpr int64_t kWorkgroups = 1024;       // each leaves a share of da
+// Episodes of different lengths leave places: segments that are cut anyway are then shorter, down to
+// 128 rows, for four times the workgroups, which start where others have ended (forward and backward,
+// 32 episodes of up to 1000 rows x 512: 367 us, now 356; 24 of up to 1500 x 384: 382 and 337; episodes
+// of one length lose by it: 32 x 1000 x 512 397 and 424).
+constexpr int kRaggedRows = 128, kRaggedRounds = 4;
 constexpr int kCols = 64;
 
 struct Plan {
@@ -466,14 +482,16 @@ struct Plan {
   int col_blocks, shares;
   uint64_t left_state, left_time, rows_part, cols_part, ends_part, bytes;
 };
-Plan plan_of(const qds_scan_config* c) {
+Plan plan_of(const qds_scan_config* c, bool ragged) {
   Plan p;
   const int64_t n = 4 * lane_states(c), rows = (int64_t)c->batch * c->length;
   p.pieces = cut(c, kPieceWaves, kLeastRows, kScanRows);
   p.parts = cut(c, kWaves, p.pieces.seg, p.pieces.seg);
+  const int rounds = ragged && p.parts.segs > 1 ? kRaggedRounds : 1;
+  if (rounds > 1) p.parts = cut(c, rounds * kWaves, std::min(p.parts.seg, std::max(p.pieces.seg, kRaggedRows)), p.pieces.seg);
   p.col_blocks = (int)ceil_div(c->width, kCols);
   const int64_t items = (int64_t)c->batch * p.parts.segs;
-  p.shares = (int)std::max<int64_t>(1, std::min(items, std::max<int64_t>(1, kWorkgroups / p.col_blocks)));
+  p.shares = (int)std::max<int64_t>(1, std::min(items, std::max<int64_t>(1, rounds * kWorkgroups / p.col_blocks)));
   uint64_t at = 0;
   auto take = [&](uint64_t floats) {
     const uint64_t here = at;
@@ -490,7 +508,7 @@ Plan plan_of(const qds_scan_config* c) {
   return p;
 }
 bool fits(const qds_scan_config* c) {
-  const Plan p = plan_of(c);
+  const Plan p = plan_of(c, false);
   const int64_t most = most_blocks(kJoinBlock);
   return (int64_t)c->batch <= most / (ceil_div(c->width, 64) * p.pieces.segs) && (int64_t)c->batch * c->width <= most / 2 &&
          (int64_t)c->batch * c->length <= most * 2;
@@ -506,7 +524,7 @@ extern "C" qds_status qds_selective_scan_backward_workspace(const qds_scan_confi
   if (st != QDS_OK) return st;
   if (!bytes) return QDS_ERR_INVALID_ARG;
   if (!fits(c)) return QDS_ERR_UNSUPPORTED;
-  *bytes = plan_of(c).bytes;
+  *bytes = std::max(plan_of(c, false).bytes, plan_of(c, true).bytes);      // whether there are lengths is not known here
   return QDS_OK;
 }
 
@@ -529,7 +547,7 @@ extern "C" qds_status qds_selective_scan_backward(const qds_scan_config* c, qds_
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
   for (qds_rows* r : {&dout, &u, &delta, &b, &cc, &gate})
     if (!near_rows(*r, c->length)) return QDS_ERR_UNSUPPORTED;
-  const Plan p = plan_of(c);
+  const Plan p = plan_of(c, lengths != nullptr);
   ScanArgs a = scan_args(c);
   a.u = rows(u);
   a.delta = rows(delta);
