@@ -4,7 +4,7 @@
 // Bound by memory: with a gate, five rows move forward and eight backward, against some 20 and
 // 50 operations per element.  A row is read once and stays in registers: the two sums over
 // it follow each other (the second norm is of what the first one scales).  32000 x 1024 bfloat16:
-// forward 59 us (5.5 TB/s), backward 117 us (4.5 TB/s); 9973 x 777 float32: 27 and 53 us.
+// forward 59 us (5.5 TB/s), backward 115 us (4.6 TB/s); 9973 x 777 float32: 27 and 52 us.
 #include <algorithm>
 
 #include "seq_common.hpp"

@@ -4,8 +4,8 @@
 // Bound by the vector units.  A state of a row takes an exponential (8.2 cycles of a wave on a
 // SIMD), two products and an fma (2.7 each), its output another fma, where a column's row moves 8
 // bytes: at 16 states some 120 cycles for 16 columns (lane moves, softplus and gate included), four
-// times what memory takes for them.  1 x 65536 x 1024 bfloat16: 313 us for the outputs (183 cycles),
-// 253 us for the pieces in front of them.
+// times what memory takes for them.  1 x 65536 x 1024 bfloat16: 300 us for the outputs (176 cycles),
+// 243 us for the pieces in front of them.
 #include <algorithm>
 
 #include "seq_scan.hpp"

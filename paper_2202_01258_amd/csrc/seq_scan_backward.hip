@@ -2,7 +2,7 @@
 // include/qd_seq.h, the layout of the work in seq_scan.hpp.
 //
 // Bound by the vector units: 97 vector instructions for a row of 16 columns and 16 states, which
-// are issued 92% of the time (32 episodes of up to 1000 rows x 512 bfloat16, 232 us).  Two waves a SIMD is what the states
+// are issued 88% of the time (32 episodes of up to 1000 rows x 512 bfloat16, 176 us).  Two waves a SIMD is what the states
 // in registers leave; three, with fewer of them kept, took 1.07 of the time.
 #include <algorithm>
 
