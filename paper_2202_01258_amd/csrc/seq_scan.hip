@@ -277,7 +277,7 @@ extern "C" qds_status qds_selective_scan_step(const qds_scan_config* c, qds_rows
   if (c->batch == 0) return QDS_OK;
   if (!a_ || !u.data || !delta.data || !b.data || !cc.data || !o || !state_in || !state_out) return QDS_ERR_INVALID_ARG;
   const int64_t columns = (int64_t)c->batch * c->width;
-  if (columns >= (1 << 30)) return QDS_ERR_UNSUPPORTED;
+  if (ceil_div(columns, kColumns) > most_blocks(kBlock)) return QDS_ERR_UNSUPPORTED;
   ScanArgs a = scan_args(c);
   a.u = rows(u);
   a.delta = rows(delta);
