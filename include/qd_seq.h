@@ -277,7 +277,9 @@ typedef struct {
 } qds_scan_config;
 
 /* u, delta, gate: rows of `width`; b, c: rows of `states`; from 0 to less than
- * 2^23 elements apart (else QDS_ERR_UNSUPPORTED).  o [batch][length][width], contiguous.
+ * 2^23 elements apart (else QDS_ERR_UNSUPPORTED).  batch times ceil(width / 64) is less than
+ * 2^24, in the backward pass too, and batch times width at most 2^30 - 64 in the step (else
+ * QDS_ERR_UNSUPPORTED).  o [batch][length][width], contiguous.
  * a [width][states] fp32; skip and bias [width] fp32 or null (0); gate.data null: o = y.  lengths as
  * for the convolution.  state_in null: 0.  state_out (may be null; not state_in):
  * h after row n - 1.  marks (null unless a backward pass follows, which needs

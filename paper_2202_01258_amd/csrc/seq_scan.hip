@@ -185,9 +185,8 @@ uint64_t state_bytes(const qds_scan_config* c, int segs) {
   return align_up((uint64_t)c->batch * segs * c->width * 4 * lane_states(c) * sizeof(float));
 }
 bool fits(const qds_scan_config* c) {
-  const int64_t workgroups = ceil_div(c->width, kColumns) * forward_cut(c).segs;
-  return (int64_t)c->batch <= (int64_t)most_blocks(kBlock) / workgroups &&
-         (int64_t)c->batch * c->width <= (int64_t)most_blocks(kScanJoin) / 2;
+  const int segs = forward_cut(c).segs;
+  return (int64_t)c->batch <= (int64_t)most_blocks(kBlock) / (ceil_div(c->width, kColumns) * segs) && joinable(c, segs);
 }
 
 }  // namespace

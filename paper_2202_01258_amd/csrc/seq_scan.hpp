@@ -335,6 +335,10 @@ inline Cut cut(const qds_scan_config* c, int64_t waves, int least, int unit) {
   return Cut{(int)seg, (int)std::max<int64_t>(1, ceil_div(c->length, seg))};
 }
 constexpr int kFewPieces = 32;                   // so many are followed by the main pass itself
+// Whether the launch that joins more of them can be made: only few columns are cut so far.
+inline bool joinable(const qds_scan_config* c, int pieces) {
+  return pieces <= kFewPieces || ceil_div((int64_t)c->batch * c->width * 4 * lane_states(c), 16) <= most_blocks(kScanJoin);
+}
 
 template <class F> void scan_instance(const qds_scan_config* c, F&& f) {
   auto with_type = [&](auto S) {

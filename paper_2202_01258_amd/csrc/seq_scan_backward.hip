@@ -510,7 +510,7 @@ Plan plan_of(const qds_scan_config* c, bool ragged) {
 bool fits(const qds_scan_config* c) {
   const Plan p = plan_of(c, false);
   const int64_t most = most_blocks(kJoinBlock);
-  return (int64_t)c->batch <= most / (ceil_div(c->width, 64) * p.pieces.segs) && (int64_t)c->batch * c->width <= most / 2 &&
+  return (int64_t)c->batch <= most / (ceil_div(c->width, 64) * p.pieces.segs) && joinable(c, p.pieces.segs) &&
          (int64_t)c->batch * c->length <= most * 2;
 }
 
