@@ -1044,8 +1044,8 @@ def _autograd():
 
     class SelectiveScan(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, u, delta, a, b, c, skip, gate, bias, state, lengths):
-            o, last, marks = selective_scan_forward(u, delta, a, b, c, skip, gate, bias, state, lengths, keep=True)
+        def forward(ctx, u, delta, a, b, c, skip, gate, bias, state, lengths, keep):
+            o, last, marks = selective_scan_forward(u, delta, a, b, c, skip, gate, bias, state, lengths, keep)
             ctx.save_for_backward(u, delta, a, b, c, skip, gate, bias, lengths, marks)
             ctx.has_state = state is not None
             ctx.set_materialize_grads(False)
@@ -1059,7 +1059,7 @@ def _autograd():
                 do = torch.zeros_like(u)
             du, ddelta, da, db, dc, dskip, dgate, dbias, dfirst = selective_scan_backward(
                 do, u, delta, a, b, c, marks, skip, gate, bias, dlast, lengths)
-            return du, ddelta, da, db, dc, dskip, dgate, dbias, dfirst if ctx.has_state else None, None
+            return du, ddelta, da, db, dc, dskip, dgate, dbias, dfirst if ctx.has_state else None, None, None
 
     class BranchNorm(torch.autograd.Function):
         @staticmethod
@@ -1122,9 +1122,8 @@ def causal_conv(x, weight, bias=None, state=None, lengths=None, silu: bool = Tru
 
 def selective_scan(u, delta, a, b, c, skip=None, gate=None, bias=None, state=None, lengths=None):
     """selective_scan_forward under autograd: returns o and the last state."""
-    if not torch.is_grad_enabled():              # nothing is kept for a backward pass
-        return selective_scan_forward(u, delta, a, b, c, skip, gate, bias, state, lengths)[:2]
-    return _autograd()[4].apply(u, delta, a, b, c, skip, gate, bias, state, lengths)
+    keep = torch.is_grad_enabled()               # else there is no backward pass
+    return _autograd()[4].apply(u, delta, a, b, c, skip, gate, bias, state, lengths, keep)
 
 
 def branch_norm(x, gate, residual, branch_weight, weight, residual_scale: float = 1.0, eps: float = 1e-6):

@@ -6,6 +6,7 @@ import os
 import pytest
 
 torch = pytest.importorskip("torch")
+import torch.autograd.forward_ad as forward_ad  # noqa: E402
 
 from paper_2202_01258_amd import seq as S  # noqa: E402
 from test_seq_block_abi import P, bytes_of, rows, scan  # noqa: E402
@@ -38,3 +39,44 @@ def test_scan_takes_many_columns(lib, batch, length, width, status, states):
     c = scan(batch=batch, length=length, width=width, states=states)
     assert bytes_of(lib.qds_selective_scan_workspace, c)[0] == status
     assert bytes_of(lib.qds_selective_scan_backward_workspace, c)[0] == status
+
+
+# -- what the binding does without a GPU: the plain calls are stood in for
+@pytest.fixture
+def stand_ins(monkeypatch):
+    """The plain forward calls, giving new tensors of the right shapes as the library does; what
+    selective_scan_forward was asked to keep is returned."""
+    kept = []
+
+    def scan_forward(u, delta, a, b, c, skip=None, gate=None, bias=None, state=None, lengths=None, keep=False):
+        kept.append(keep)
+        return u.new_zeros(u.shape), u.new_zeros(u.shape[0], *a.shape), u.new_zeros(8) if keep else None
+
+    monkeypatch.setattr(S, "selective_scan_forward", scan_forward)
+    monkeypatch.setattr(S, "causal_conv_forward", lambda x, w, *_: (x.new_zeros(x.shape), x.new_zeros(x.shape[0], 3, x.shape[2])))
+    monkeypatch.setattr(S, "branch_norm_forward", lambda x, *_: (x.new_zeros(x.shape), x.new_zeros(x.shape), x.new_zeros(2, *x.shape[:-1])))
+    monkeypatch.setattr(S, "dropout_forward", lambda x, *_: x.new_zeros(x.shape))
+    return kept
+
+
+X, W, A, N = torch.ones(2, 5, 8), torch.ones(4, 8), torch.ones(8, 4), torch.ones(2, 5, 4)
+RNG = torch.zeros(2, dtype=torch.int64)
+
+
+@pytest.mark.parametrize("call", [lambda x: S.causal_conv(x, W), lambda x: S.selective_scan(x, X, A, N, N),
+                                  lambda x: S.selective_scan(X, X, A, N, N, gate=x), lambda x: S.branch_norm(x, None, X, W[0], W[0]),
+                                  lambda x: S.dropout(x, RNG, 0.5)])
+@pytest.mark.parametrize("mode", [torch.enable_grad, torch.no_grad])
+def test_forward_mode_is_refused(stand_ins, call, mode):
+    """There is no forward-mode derivative; torch.no_grad does not switch forward mode off, so a tangent
+    must not get lost there either."""
+    with forward_ad.dual_level(), mode():
+        with pytest.raises(NotImplementedError, match="jvp"):
+            call(forward_ad.make_dual(X, torch.ones_like(X)))
+
+
+def test_scan_keeps_nothing_without_gradients(stand_ins):
+    with torch.no_grad():
+        S.selective_scan(X.clone().requires_grad_(), X, A, N, N)
+    S.selective_scan(X.clone().requires_grad_(), X, A, N, N)
+    assert stand_ins == [False, True]
