@@ -1122,8 +1122,9 @@ def causal_conv(x, weight, bias=None, state=None, lengths=None, silu: bool = Tru
 
 def selective_scan(u, delta, a, b, c, skip=None, gate=None, bias=None, state=None, lengths=None):
     """selective_scan_forward under autograd: returns o and the last state."""
-    keep = torch.is_grad_enabled()               # else there is no backward pass
-    return _autograd()[4].apply(u, delta, a, b, c, skip, gate, bias, state, lengths, keep)
+    inputs = u, delta, a, b, c, skip, gate, bias, state
+    keep = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in inputs)     # else no backward pass
+    return _autograd()[4].apply(*inputs, lengths, keep)
 
 
 def branch_norm(x, gate, residual, branch_weight, weight, residual_scale: float = 1.0, eps: float = 1e-6):

@@ -60,6 +60,7 @@ def stand_ins(monkeypatch):
 
 
 X, W, A, N = torch.ones(2, 5, 8), torch.ones(4, 8), torch.ones(8, 4), torch.ones(2, 5, 4)
+NAMES = ("u", "delta", "a", "b", "c")
 RNG = torch.zeros(2, dtype=torch.int64)
 
 
@@ -80,3 +81,14 @@ def test_scan_keeps_nothing_without_gradients(stand_ins):
         S.selective_scan(X.clone().requires_grad_(), X, A, N, N)
     S.selective_scan(X.clone().requires_grad_(), X, A, N, N)
     assert stand_ins == [False, True]
+
+
+@pytest.mark.parametrize("which", ["u", "delta", "a", "b", "c", "skip", "gate", "bias", "state"])
+def test_scan_keeps_only_for_inputs_with_gradients(stand_ins, which):
+    """Frozen layers and evaluations with gradients on have no backward pass either."""
+    tensors = dict(u=X, delta=X, a=A, b=N, c=N, skip=W[0], gate=X, bias=W[0], state=torch.ones(2, 8, 4))
+    assert not S.selective_scan(**tensors, lengths=torch.ones(2, dtype=torch.int32))[0].requires_grad
+    tensors[which] = tensors[which].clone().requires_grad_()
+    assert S.selective_scan(**tensors)[0].requires_grad
+    assert S.selective_scan(**{k: v if k == which or k in NAMES else None for k, v in tensors.items()})[0].requires_grad
+    assert stand_ins == [False, True, True]
