@@ -167,6 +167,19 @@ template <int S> __device__ inline void store_states(float* p, int at, int q, in
   for (int s = 0; s < S; ++s) put<float>((char*)p, in && q * S + s < states ? (at * states + q * S) * 4u : kOutside, s * 4, v[s]);
 }
 
+// Which of a lane's states there are: four lanes may hold more.
+template <int S> struct Held {
+  int count;
+  __device__ Held(int q, int states) : count(states - q * S) {}
+  __device__ float keep(int s, float v) const { return s < count ? v : 0.0f; }
+};
+// Whether one of a wave's numbers is 2^EXPONENT or more, or not a number.
+template <int EXPONENT, class... F> __device__ inline bool any_from(F... v) {
+  uint32_t top = 0;
+  ((top = max(top, __float_as_uint(v) & 0x7fffffffu)), ...);
+  return __builtin_amdgcn_ballot_w64(top >= (EXPONENT + 127u) << 23) != 0;
+}
+
 // Which of a block's rows q, q + 4, ... an episode still has: rows left, less one, counted from a
 // lane's first.  Below 0 from a row on, where the sign bit makes an offset kOutside.
 struct Left {

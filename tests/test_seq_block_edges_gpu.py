@@ -58,3 +58,80 @@ def test_scan_of_more_than_2_to_the_23_columns():
     mag = (g["do"].double() * gate * torch.sigmoid(gate) * x[0].double()).abs().sum((0, 1))
     assert ((ends[0][5] + ends[1][5] - got[5]).abs() <= 1.001 * terms * mag).all()
     assert ((ends[0][7] + ends[1][7] - got[7]).abs() <= 1.01 * terms * got[1].double().abs().sum((0, 1))).all()
+
+
+def scan_pass(s, g):
+    """Outputs and gradients by name."""
+    x, kw = args(s)
+    o, last, marks = S.selective_scan_forward(*x, state=s["state"], keep=True, **kw)
+    got = S.selective_scan_backward(g["do"], *x, marks, dlast=g["dlast"], **kw)
+    return dict(zip(("o", "last", "du", "ddelta", "da", "db", "dc", "dskip", "dgate", "dbias", "dstate"), (o, last, *got)))
+
+
+def as_defined(got, want, roundings, what):
+    """Equal where the definition gives an infinity, within the bound where it gives a number; where it gives
+    none (infinities of both signs meet) anything may come."""
+    value, mag = want
+    known, infinite = ~value.isnan(), value.isinf()
+    v = got.double().cpu()
+    assert torch.equal(v[infinite], value[infinite]), (what, v[infinite], value[infinite])
+    finite = known & ~infinite
+    assert mag[finite].isfinite().all() and finite.any() + infinite.any() > 0, what
+    within(got.cpu()[finite], (value[finite], mag[finite]), roundings, what)
+
+
+def positive(batch, rows, width, states, dtype, seed=1):
+    """Inputs with every term of one sign, so that infinities add up to infinities."""
+    s, g = scan_inputs(batch, rows, width, states, dtype, seed)
+    s = {k: v if k in ("a", "delta", "bias") else v.abs() + 0.125 for k, v in s.items()}
+    return s, {k: v.abs() + 0.125 for k, v in g.items()}
+
+
+HELD = [4, 8, 16, 32]                               # states that four lanes hold without a place left
+
+
+@pytest.mark.parametrize("states", HELD)
+@pytest.mark.parametrize("which,value", [("u", float("inf")), ("u", -float("inf")), ("delta", float("inf")), ("do", float("inf"))])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_scan_of_infinities(states, which, value, dtype):
+    """What is behind an episode (20 rows, which are taken by eight) adds nothing where an
+    input, a step or a gradient is infinite."""
+    s, g = positive(2, 20, 18, states, dtype)
+    (s if which in s else g)[which][0, 11, 5] = value
+    want, top = D.scan(**{k: wide(v) for k, v in s.items()}, ends=[20, 20], do=wide(g["do"]), dlast=wide(g["dlast"]))
+    got = scan_pass(s, g)
+    top = float((torch.logaddexp(wide(s["delta"]) + wide(s["bias"]), torch.zeros(()).double())[..., None] * wide(s["a"]).abs())
+                .nan_to_num(posinf=0).max())
+    path = (16 + 6 * top) * 22
+    as_defined(got["o"], want["o"], path + states + 16, "o")
+    as_defined(got["last"], want["last"], path, "last")
+    if which == "delta":
+        return                                       # its gradient is the product of 0 and infinity
+    for name, n in (("du", states), ("ddelta", states), ("da", 40), ("db", 18), ("dc", 18), ("dskip", 40), ("dgate", states),
+                    ("dbias", states + 40), ("dstate", 0)):
+        as_defined(got[name], want[name], 2 * path + 32 + n, name)
+
+
+@pytest.mark.parametrize("states", HELD)
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_scan_ends_with_no_number(states, value):
+    """The last row's input is not finite: the gradient of a, to which the state behind it adds nothing, is."""
+    s, g = positive(3, 37, 18, states, F32)
+    ends = [20, 37, 3]
+    for i, n in enumerate(ends):
+        s["u"][i, n - 1, 5 + i] = value
+    got = scan_pass(dict(s, lengths=torch.tensor(ends, dtype=torch.int32, device="cuda")), g)
+    # each episode by itself and without rows behind it, whose gradients the definition would make 0 times infinity
+    sums = {"da": 92, "dskip": 60, "dbias": states + 60}
+    total = dict.fromkeys(sums, (0.0, 0.0))
+    for i, n in enumerate(ends):
+        one = {k: wide(v[i:i + 1, :n] if v.dim() == 3 and k != "state" else v[i:i + 1] if k == "state" else v) for k, v in s.items()}
+        want, top = D.scan(**one, ends=[n], do=wide(g["do"][i:i + 1, :n]), dlast=wide(g["dlast"][i:i + 1]))
+        path = 2 * (16 + 6 * top) * 39 + 32
+        for name, k in (("du", states), ("ddelta", states), ("db", 18), ("dc", 18), ("dgate", states)):
+            as_defined(got[name][i:i + 1, :n], want[name], path + k, name)
+        as_defined(got["dstate"][i:i + 1], want["dstate"], path, "dstate")
+        total = {k: (v + want[k][0], m + want[k][1]) for k, (v, m) in total.items()}
+    assert total["da"][0].isfinite().all()
+    for name, k in sums.items():
+        as_defined(got[name], total[name], path + k, name)
