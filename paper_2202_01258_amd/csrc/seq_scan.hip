@@ -17,7 +17,7 @@ constexpr int kBlock = 256, kColumns = kBlock / 4;
 
 // One segment of 64 columns.  LOCAL: what the segment leaves behind when it starts from
 // zero, and the sum of its steps; otherwise outputs, marks and the last state.
-template <class T, int S, bool LOCAL, bool GATE> __global__ __launch_bounds__(kBlock) void k_scan(ScanArgs a) {
+template <class T, int S, bool LOCAL, bool GATE, bool TAIL> __global__ __launch_bounds__(kBlock) void k_scan(ScanArgs a) {
   constexpr int K = kScanRows, N = 4 * S, QUADS = K / 4;
   SEQ_SHARED float bc[2][K * 2 * N];
   const int q = threadIdx.x & 3;
@@ -31,9 +31,8 @@ template <class T, int S, bool LOCAL, bool GATE> __global__ __launch_bounds__(kB
   const int seg = which.part;
   const int n = rows_in(a, b), begin = seg * a.seg, end = min(begin + a.seg, a.length), live = min(end, n);
   float rates[S], h[S];
-  load_states<S>(rates, a.a, at, q, a.states);
-#pragma unroll
-  for (int s = 0; s < S; ++s) rates[s] = rate(rates[s]);
+  load_rates<S>(rates, a, at, q);
+  const Held<S> held(q, a.states);
   const float bias = a.bias ? a.bias[at] : 0.0f, skip = a.skip ? a.skip[at] : 0.0f;
   const int64_t place = ((b * a.segs + seg) * a.width + at) * N + q * S;
   if (LOCAL) {
@@ -86,35 +85,41 @@ template <class T, int S, bool LOCAL, bool GATE> __global__ __launch_bounds__(kB
         marks += (int64_t)a.width * N;
       }
       const float* lds = bc[buffer] + q * S;
+      auto form = [&](auto CAREFUL) {
+        constexpr bool careful = decltype(CAREFUL)::value;
 #pragma unroll
-      for (int i = 0; i < QUADS; ++i) {
-        const float x = dt[i] * uu[i];
-        float y[4];
-        auto row = [&](auto J) {
-          constexpr int j = decltype(J)::value;
-          const float dtj = quad_lane<j>(dt[i]), xj = quad_lane<j>(x);
-          float bv[S], cv[S];
-          load_floats<S>(bv, lds + (4 * i + j) * 2 * N);
-          if (!LOCAL) load_floats<S>(cv, lds + (4 * i + j) * 2 * N + N);
+        for (int i = 0; i < QUADS; ++i) {
+          const float x = dt[i] * uu[i];
+          float y[4];
+          auto row = [&](auto J) {
+            constexpr int j = decltype(J)::value;
+            const float dtj = quad_lane<j>(dt[i]), xj = quad_lane<j>(x);
+            float bv[S], cv[S];
+            load_floats<S>(bv, lds + (4 * i + j) * 2 * N);
+            if (!LOCAL) load_floats<S>(cv, lds + (4 * i + j) * 2 * N + N);
 #pragma unroll
-          for (int s = 0; s < S; ++s) {
-            h[s] = fmaf(fast_exp2(dtj * rates[s]), h[s], xj * bv[s]);
-            if (!LOCAL) y[j] = s == 0 ? h[s] * cv[s] : fmaf(h[s], cv[s], y[j]);
+            for (int s = 0; s < S; ++s) {
+              h[s] = fmaf(fast_exp2(dtj * rates[s]), h[s], xj * bv[s]);
+              if (careful) h[s] = held.keep(s, h[s]);
+              if (!LOCAL) y[j] = s == 0 ? h[s] * cv[s] : fmaf(h[s], cv[s], y[j]);
+            }
+          };
+          row(Int<0>{});
+          row(Int<1>{});
+          row(Int<2>{});
+          row(Int<3>{});
+          if (LOCAL) {
+            time += dt[i];
+          } else {
+            float o = fmaf(skip, uu[i], quad_rows(y, quad));
+            if (GATE) o *= zz[i] * sigmoid(zz[i]);
+            out.store(i, left, o);
           }
-        };
-        row(Int<0>{});
-        row(Int<1>{});
-        row(Int<2>{});
-        row(Int<3>{});
-        if (LOCAL) {
-          time += dt[i];
-        } else {
-          float o = fmaf(skip, uu[i], quad_rows(y, quad));
-          if (GATE) o *= zz[i] * sigmoid(zz[i]);
-          out.store(i, left, o);
+          __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      };
+      if (TAIL && !LOCAL && any_from<128>(dt[0] * uu[0], dt[1] * uu[1])) form(std::true_type{});
+      else form(std::false_type{});
       if (!LOCAL) out.move(K);
       if (more) {
         rows.store(bc[buffer ^ 1]);
@@ -125,6 +130,7 @@ template <class T, int S, bool LOCAL, bool GATE> __global__ __launch_bounds__(kB
   }
   if (LOCAL) {
     time = quad_sum(time);
+    held.keep_all(h);
     if (real) store_floats<S>(a.left_state + place, h);
     if (real && q == 0) a.left_time[(b * a.segs + seg) * a.width + at] = time;
   } else {
@@ -253,16 +259,17 @@ extern "C" qds_status qds_selective_scan(const qds_scan_config* c, qds_rows u, q
     a.left_time = (float*)((char*)workspace + state_bytes(c, a.segs));
   }
   hipStream_t s = (hipStream_t)stream;
-  scan_instance(c, [&](auto type, auto S) {
+  scan_instance(c, [&](auto type, auto S, auto TAIL) {
     using T = decltype(type);
     constexpr int L = decltype(S)::value;
+    constexpr bool tail = decltype(TAIL)::value;
     const uint32_t across = (uint32_t)(a.batch * a.col_blocks);
     if (a.segs > 1) {
-      k_scan<T, L, true, false><<<across * (a.segs - 1), kBlock, 0, s>>>(a);
+      k_scan<T, L, true, false, false><<<across * (a.segs - 1), kBlock, 0, s>>>(a);
       if (a.joined) k_scan_join<4 * L, false><<<(uint32_t)ceil_div((int64_t)a.batch * a.width * 4 * L, 16), kScanJoin, 0, s>>>(a);
     }
-    if (gate.data) k_scan<T, L, false, true><<<across * a.segs, kBlock, 0, s>>>(a);
-    else k_scan<T, L, false, false><<<across * a.segs, kBlock, 0, s>>>(a);
+    if (gate.data) k_scan<T, L, false, true, tail><<<across * a.segs, kBlock, 0, s>>>(a);
+    else k_scan<T, L, false, false, tail><<<across * a.segs, kBlock, 0, s>>>(a);
   });
   return launch_status();
 }
@@ -290,11 +297,9 @@ extern "C" qds_status qds_selective_scan_step(const qds_scan_config* c, qds_rows
   a.first = state_in;
   a.last = state_out;
   hipStream_t s = (hipStream_t)stream;
-  scan_instance(c, [&](auto type, auto S) {
-    constexpr int L = decltype(S)::value;
+  scan_instance(c, [&](auto type, auto S, auto TAIL) {
     const uint32_t grid = (uint32_t)ceil_div(columns, kColumns);
-    if (a.states == 4 * L) k_scan_step<decltype(type), L, false><<<grid, kBlock, 0, s>>>(a);
-    else k_scan_step<decltype(type), L, true><<<grid, kBlock, 0, s>>>(a);
+    k_scan_step<decltype(type), decltype(S)::value, decltype(TAIL)::value><<<grid, kBlock, 0, s>>>(a);
   });
   return launch_status();
 }

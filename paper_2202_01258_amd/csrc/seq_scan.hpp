@@ -43,6 +43,7 @@ struct ScanArgs {
   float* rows_part;                              // [batch][length][column blocks][2][4 S]: shares of db and dc
   float* cols_part;                              // [shares][width][4 S]: of da
   float* ends_part;                              // [shares][2][width]: of dskip and dbias
+  float* saved;                                  // [threads of the main pass][2 S + 2]: of a block that is done again
   const int32_t* lengths;
   int32_t batch, length, width, states, blocks, col_blocks, shares;
   int32_t seg, segs;                             // rows of a segment of the main pass; segments
@@ -167,12 +168,26 @@ template <int S> __device__ inline void store_states(float* p, int at, int q, in
   for (int s = 0; s < S; ++s) put<float>((char*)p, in && q * S + s < states ? (at * states + q * S) * 4u : kOutside, s * 4, v[s]);
 }
 
-// Which of a lane's states there are: four lanes may hold more.
+// Four lanes may hold more states than there are.  Those that are not there are 0 wherever states meet
+// (their rate is -1, so that no step makes them anything else); b and c are 0 for them, which is
+// not enough beside an infinite input or gradient.  Kernels for such counts (TAIL) look for one in
+// each block of rows (13 states, 16 x 1000 x 1024: 397 us for a training pass, 385 without; outputs of 1 x
+// 16384 x 1024: 137 and 134); masks on each state would be some 8 of a row's 97 instructions.
 template <int S> struct Held {
-  int count;
+  int count;                                     // of the lane's states
   __device__ Held(int q, int states) : count(states - q * S) {}
   __device__ float keep(int s, float v) const { return s < count ? v : 0.0f; }
+  __device__ void keep_all(float* v) const {
+#pragma unroll
+    for (int s = 0; s < S; ++s) v[s] = keep(s, v[s]);
+  }
 };
+template <int S> __device__ inline void load_rates(float* out, const ScanArgs& a, int at, int q) {
+  load_states<S>(out, a.a, at, q, a.states);
+  const Held<S> held(q, a.states);
+#pragma unroll
+  for (int s = 0; s < S; ++s) out[s] = s < held.count ? rate(out[s]) : -1.0f;
+}
 // Whether one of a wave's numbers is 2^EXPONENT or more, or not a number.
 template <int EXPONENT, class... F> __device__ inline bool any_from(F... v) {
   uint32_t top = 0;
@@ -302,7 +317,7 @@ template <int N, bool BACK> __global__ __launch_bounds__(kScanJoin) void k_scan_
   const bool real = column < all, in = real && n < a.states;
   const int64_t b = real ? column / a.width : 0;
   const int at = real ? (int)(column % a.width) : 0;
-  const float r = in ? rate(a.a[(int64_t)at * a.states + n]) : 0.0f;
+  const float r = in ? rate(a.a[(int64_t)at * a.states + n]) : -1.0f;
   // pieces with something left behind, in their order; one more starts behind the last
   const int count = BACK ? a.pieces - a.ratio : a.pieces - 1, share = (count + 15) / 16;
   const int from = min(group * share, count), to = min(from + share, count);
@@ -354,10 +369,14 @@ inline bool joinable(const qds_scan_config* c, int pieces) {
 }
 
 template <class F> void scan_instance(const qds_scan_config* c, F&& f) {
+  auto with_tail = [&](auto type, auto S) {
+    if (c->states == 4 * decltype(S)::value) f(type, S, std::false_type{});
+    else f(type, S, std::true_type{});
+  };
   auto with_type = [&](auto S) {
-    if (c->dtype == QDS_F32) f(float(), S);
-    else if (c->dtype == QDS_BF16) f(bf16(), S);
-    else f(half(), S);
+    if (c->dtype == QDS_F32) with_tail(float(), S);
+    else if (c->dtype == QDS_BF16) with_tail(bf16(), S);
+    else with_tail(half(), S);
   };
   switch (lane_states(c)) {
     case 1: return with_type(Int<1>{});

@@ -30,12 +30,9 @@ template <class T, int S, bool GATE> __global__ __launch_bounds__(256) void k_sc
   const int piece = a.ratio + which.part;                         // no segment asks what the first one's pieces leave
   const int n = rows_in(a, b), begin = piece * a.piece, end = min(begin + a.piece, a.length), live = min(end, n);
   float rates[S], m[S], time = 0.0f;
-  load_states<S>(rates, a.a, at, q, a.states);
+  load_rates<S>(rates, a, at, q);
 #pragma unroll
-  for (int s = 0; s < S; ++s) {
-    rates[s] = rate(rates[s]);
-    m[s] = 0.0f;
-  }
+  for (int s = 0; s < S; ++s) m[s] = 0.0f;
   const float bias = a.bias ? a.bias[at] : 0.0f;
   if (begin < live) {
     uint32_t d[QUADS], g[QUADS], z[QUADS];
@@ -100,6 +97,7 @@ template <class T, int S, bool GATE> __global__ __launch_bounds__(256) void k_sc
     }
   }
   time = quad_sum(time);
+  Held<S>(q, a.states).keep_all(m);
   if (real) store_floats<S>(a.left_state + ((b * a.pieces + piece) * a.width + at) * N + q * S, m);
   if (real && q == 0) a.left_time[(b * a.pieces + piece) * a.width + at] = time;
 }
@@ -161,6 +159,20 @@ struct Place {
     at = real ? at : width - 1;
   }
 };
+
+// The largest magnitude of three; a number that is none does not count.
+__device__ inline float largest(float a, float b, float c) {
+  asm("v_max3_f32 %0, |%1|, |%2|, |%0|" : "+v"(a) : "v"(b), "v"(c));
+  return a;
+}
+
+// A place in memory for what a thread has of a block that is done again: gradients from behind, sums.
+using Saved = __attribute__((address_space(1))) float;
+template <int S> __device__ inline Saved* saved_at() {
+  Saved* p = (Saved*)read_args().saved + ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * (2 * S + 2);
+  asm volatile("" : "+v"(p));                    // what is saved is not kept in registers as well
+  return p;
+}
 
 // Whether a block's states and gradients may reach 2^127, its steps and inputs being below 2^16; states
 // whose rate is above 0 may.
@@ -249,7 +261,7 @@ template <class T, int S, bool GATE> __device__ inline void by_rows(uint32_t ite
 // All gradients.  A workgroup has COLS columns and goes through every `shares`-th segment, each
 // from its last block of rows to its first: a block's states and decays are formed again from
 // its mark and kept in registers for the way back.
-template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS * 4, 2) void k_scan_backward(ScanArgs args) {
+template <class T, int S, int COLS, bool GATE, bool TAIL> __global__ __launch_bounds__(COLS * 4, 2) void k_scan_backward(ScanArgs args) {
   constexpr int K = kScanRows, N = 4 * S, QUADS = K / 4, BLOCK = COLS * 4, WAVES = BLOCK / 64;
   constexpr bool KEEP = S <= 4;                                     // decays for the way back; else they are formed again
   SEQ_SHARED float bc[2][K * 2 * N];
@@ -266,12 +278,9 @@ template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS
   const bool real = place.real;
   const Quad quad(q);
   float rates[S], da[S], dskip = 0.0f, dbias = 0.0f;
-  load_states<S>(rates, args.a, at, q, args.states);
+  load_rates<S>(rates, args, at, q);
 #pragma unroll
-  for (int s = 0; s < S; ++s) {
-    rates[s] = rate(rates[s]);
-    da[s] = 0.0f;
-  }
+  for (int s = 0; s < S; ++s) da[s] = 0.0f;
   const float bias = args.bias ? args.bias[at] : 0.0f, skip = args.skip ? args.skip[at] : 0.0f;
   int buffer = 0;
   uint32_t item = share;
@@ -380,6 +389,32 @@ template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS
       for (; t >= begin; t -= K) {
         const Left left{live - t - q - 1};
         const float* lds = bc[buffer] + q * S;
+        // States that are not there take part with factors of 0, which is not enough beside infinities: a
+        // block that may come to any is done again, a row at a time.
+        float gd[QUADS], gu[QUADS], gg[QUADS], gz[QUADS];           // the numbers as they were read
+        bool odd = false;
+        if (TAIL) {
+          float top = bias;
+#pragma unroll
+          for (int i = 0; i < QUADS; ++i) {
+            gd[i] = number<T>(d[i]);
+            gu[i] = number<T>(u[i]);
+            gg[i] = number<T>(g[i]);
+            gz[i] = GATE ? number<T>(z[i]) : 0.0f;
+            top = largest(largest(top, gd[i], gu[i]), gg[i], gz[i]);
+          }
+          odd = __builtin_amdgcn_ballot_w64(top >= 0x1p60f) != 0;
+        }
+        if (odd) {
+          Saved* p = saved_at<S>();
+#pragma unroll
+          for (int s = 0; s < S; ++s) {
+            p[s] = m[s];
+            p[S + s] = da[s];
+          }
+          p[2 * S] = dskip;
+          p[2 * S + 1] = dbias;
+        }
         float h[K + 1][S], e[KEEP ? K : 1][S];                      // h[r]: in front of row r; e[r]: its decay
         float dt[QUADS], slope[QUADS], uu[QUADS], dy[QUADS];
         float kb[KEEP ? K : 1][S], kc[KEEP ? K : 1][S];             // the block's b and c, where registers allow
@@ -395,10 +430,11 @@ template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS
         for (int s = 0; s < S; ++s) h[0][s] = real ? first[s] : 0.0f;
 #pragma unroll
         for (int i = 0; i < QUADS; ++i) {
-          const Step step = softplus(number<T>(d[i]) + bias);
+          if (!TAIL) gd[i] = number<T>(d[i]);
+          const Step step = softplus(gd[i] + bias);
           dt[i] = left.keep(i, real ? step.dt : 0.0f);
           slope[i] = step.slope;
-          uu[i] = number<T>(u[i]);
+          uu[i] = TAIL ? gu[i] : number<T>(u[i]);
           const float x = dt[i] * uu[i];
           float y[4];
           auto row = [&](auto J) {
@@ -425,10 +461,10 @@ template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS
           row(Int<1>{});
           row(Int<2>{});
           row(Int<3>{});
-          const float out = number<T>(g[i]);
+          const float out = TAIL ? gg[i] : number<T>(g[i]);
           dy[i] = out;
           if (GATE) {
-            const float zz = number<T>(z[i]), s = sigmoid(zz);
+            const float zz = TAIL ? gz[i] : number<T>(z[i]), s = sigmoid(zz);
             dy[i] = out * (zz * s);
             const float yy = fmaf(skip, uu[i], quad_rows(y, quad));
             put<T>(dgate, left.offset(i, du.lane_at), du.ahead(i), from_f32<T>(out * yy * silu_slope(zz, s)));
@@ -492,6 +528,17 @@ template <class T, int S, int COLS, bool GATE> __global__ __launch_bounds__(COLS
           sums.join(reads, part[buffer % PARTS][wave] + 4 * i * 2 * N);
           if (!KEEP && i == QUADS / 2 && more) fetch(t - K);          // where some states are no longer needed
           __builtin_amdgcn_sched_barrier(0);
+        }
+        if (odd) {
+          const Saved* p = saved_at<S>();
+#pragma unroll
+          for (int s = 0; s < S; ++s) {
+            m[s] = p[s];
+            da[s] = p[S + s];
+          }
+          dskip = p[2 * S];
+          dbias = p[2 * S + 1];
+          by_rows<T, S, GATE>(item, t, block * COLS, lds, rates, bias, skip, m, da, dskip, dbias, sums, part[buffer % PARTS][wave]);
         }
         if (more) rows.store(bc[buffer ^ 1]);
         __syncthreads();
@@ -596,7 +643,7 @@ constexpr int kCols = 64;
 struct Plan {
   Cut pieces, parts;
   int col_blocks, shares;
-  uint64_t left_state, left_time, rows_part, cols_part, ends_part, bytes;
+  uint64_t left_state, left_time, rows_part, cols_part, ends_part, saved, bytes;
 };
 Plan plan_of(const qds_scan_config* c, bool ragged) {
   Plan p;
@@ -620,6 +667,7 @@ Plan plan_of(const qds_scan_config* c, bool ragged) {
   p.rows_part = take((uint64_t)rows * p.col_blocks * 2 * n);
   p.cols_part = take((uint64_t)p.shares * c->width * n);
   p.ends_part = take((uint64_t)p.shares * c->width * 2);
+  p.saved = take(c->states == n ? 0 : (uint64_t)p.shares * p.col_blocks * kCols * 4 * (2 * lane_states(c) + 2));
   p.bytes = at;
   return p;
 }
@@ -701,10 +749,12 @@ extern "C" qds_status qds_selective_scan_backward(const qds_scan_config* c, qds_
   a.rows_part = (float*)(ws + p.rows_part);
   a.cols_part = (float*)(ws + p.cols_part);
   a.ends_part = (float*)(ws + p.ends_part);
+  a.saved = (float*)(ws + p.saved);
   hipStream_t s = (hipStream_t)stream;
-  scan_instance(c, [&](auto type, auto S) {
+  scan_instance(c, [&](auto type, auto S, auto TAIL) {
     using T = decltype(type);
     constexpr int L = decltype(S)::value, N = 4 * L;
+    constexpr bool tail = decltype(TAIL)::value;
     if (c->batch > 0) {
       if (a.segs > 1) {
         const uint32_t grid = (uint32_t)(c->batch * ceil_div(c->width, 64) * (a.pieces - a.ratio));
@@ -713,8 +763,8 @@ extern "C" qds_status qds_selective_scan_backward(const qds_scan_config* c, qds_
         if (a.joined) k_scan_join<N, true><<<(uint32_t)ceil_div((int64_t)c->batch * c->width * N, 16), kScanJoin, 0, s>>>(a);
       }
       const uint32_t grid = (uint32_t)(a.col_blocks * a.shares);
-      if (gate.data) k_scan_backward<T, L, kCols, true><<<grid, kCols * 4, 0, s>>>(a);
-      else k_scan_backward<T, L, kCols, false><<<grid, kCols * 4, 0, s>>>(a);
+      if (gate.data) k_scan_backward<T, L, kCols, true, tail><<<grid, kCols * 4, 0, s>>>(a);
+      else k_scan_backward<T, L, kCols, false, tail><<<grid, kCols * 4, 0, s>>>(a);
     }
     const uint32_t row_groups = (uint32_t)ceil_div((int64_t)c->batch * c->length * 2 * N, kJoinBlock);
     const uint32_t col_groups = (uint32_t)ceil_div((int64_t)c->width * (N + 2), 16);

@@ -88,14 +88,15 @@ def positive(batch, rows, width, states, dtype, seed=1):
 
 
 HELD = [4, 8, 16, 32]                               # states that four lanes hold without a place left
+PLACES_LEFT = [1, 2, 3, 5, 7, 9, 12, 13, 15, 17, 24, 31]
 
 
-@pytest.mark.parametrize("states", HELD)
+@pytest.mark.parametrize("states", HELD + PLACES_LEFT)
 @pytest.mark.parametrize("which,value", [("u", float("inf")), ("u", -float("inf")), ("delta", float("inf")), ("do", float("inf"))])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_scan_of_infinities(states, which, value, dtype):
-    """What is behind an episode (20 rows, which are taken by eight) adds nothing where an
-    input, a step or a gradient is infinite."""
+    """What is behind an episode (20 rows, which are taken by eight) and places of states that are not
+    there add nothing where an input, a step or a gradient is infinite."""
     s, g = positive(2, 20, 18, states, dtype)
     (s if which in s else g)[which][0, 11, 5] = value
     want, top = D.scan(**{k: wide(v) for k, v in s.items()}, ends=[20, 20], do=wide(g["do"]), dlast=wide(g["dlast"]))
@@ -112,7 +113,7 @@ def test_scan_of_infinities(states, which, value, dtype):
         as_defined(got[name], want[name], 2 * path + 32 + n, name)
 
 
-@pytest.mark.parametrize("states", HELD)
+@pytest.mark.parametrize("states", HELD + PLACES_LEFT)
 @pytest.mark.parametrize("value", [float("inf"), float("nan")])
 def test_scan_ends_with_no_number(states, value):
     """The last row's input is not finite: the gradient of a, to which the state behind it adds nothing, is."""
@@ -135,3 +136,24 @@ def test_scan_ends_with_no_number(states, value):
     assert total["da"][0].isfinite().all()
     for name, k in sums.items():
         as_defined(got[name], total[name], path + k, name)
+
+
+@pytest.mark.parametrize("states", HELD + PLACES_LEFT)
+@pytest.mark.parametrize("which,row", [("u", 70), ("delta", 70), ("do", 70), ("u", 3), ("do", 66)])
+@pytest.mark.parametrize("rows,width", [(77, 9), (1057, 3)])
+def test_scan_of_infinities_in_segments(states, which, row, rows, width):
+    """The same through pieces, which leave their states to each other; slow decays, so that none of them
+    is 0 in float32."""
+    s, g = positive(1, rows, width, states, F32)
+    s["a"] = s["a"] * 2.0 ** -10
+    (s if which in s else g)[which][0, row, 1] = float("inf")
+    want, _ = D.scan(**{k: wide(v) for k, v in s.items()}, ends=[rows], do=wide(g["do"]), dlast=wide(g["dlast"]))
+    got = scan_pass(s, g)
+    path = (16 + 6) * (rows + 2)                      # dt |a| is below 1
+    as_defined(got["o"], want["o"], path + states + 16, "o")
+    as_defined(got["last"], want["last"], path, "last")
+    if which == "delta":
+        return
+    for name, n in (("du", states), ("ddelta", states), ("da", rows), ("db", width), ("dc", width), ("dskip", rows), ("dgate", states),
+                    ("dbias", states + rows), ("dstate", 0)):
+        as_defined(got[name], want[name], 2 * path + 32 + n, name)
