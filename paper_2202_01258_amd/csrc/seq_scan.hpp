@@ -287,6 +287,14 @@ inline bool near_rows(qds_rows& r, int length) {
 inline int lane_states(const qds_scan_config* c) { return c->states <= 4 ? 1 : c->states <= 8 ? 2 : c->states <= 16 ? 4 : 8; }
 inline int mark_count(const qds_scan_config* c) { return (int)ceil_div(c->length, kScanRows); }
 
+// The root of what rows with a sum of steps `time` multiply a state by: all of it need not be a float, and
+// what is 0 or infinite stays so.  Limited to where neither half is infinite or 0: beyond, a number
+// comes to infinity by 2^254, or to less than 2^-124 by 2^-252.  No rows: 1, whatever the rate.
+__device__ inline float half_decay(float time, float rate) {
+  const float half = fast_exp2(__builtin_amdgcn_fmed3f(0.5f * time * rate, -126.0f, 127.0f));
+  return time == 0.0f ? 1.0f : half;
+}
+
 // What all pieces before `until` leave together when the first starts from x (the pieces in their
 // order, or from the last one backwards).
 template <int S, bool BACK> __device__ inline void follow(float* x, const ScanArgs& a, const float* rates, int64_t b, int until, int at, int q) {
@@ -301,7 +309,10 @@ template <int S, bool BACK> __device__ inline void follow(float* x, const ScanAr
     load_floats<S>(left, state + to * N);
     const float t = time[to];
 #pragma unroll
-    for (int s = 0; s < S; ++s) x[s] = fmaf(fast_exp2(t * rates[s]), x[s], left[s]);
+    for (int s = 0; s < S; ++s) {
+      const float half = half_decay(t, rates[s]);
+      x[s] = fmaf(x[s] * half, half, left[s]);
+    }
   }
 }
 
@@ -322,29 +333,32 @@ template <int N, bool BACK> __global__ __launch_bounds__(kScanJoin) void k_scan_
   const int count = BACK ? a.pieces - a.ratio : a.pieces - 1, share = (count + 15) / 16;
   const int from = min(group * share, count), to = min(from + share, count);
   auto place = [&](int k) { return (b * a.pieces + (BACK ? a.pieces - 1 - k : k)) * a.width + at; };
-  float decay = 1.0f, left = 0.0f;
+  float time = 0.0f, left = 0.0f;
   if (real) {
 #pragma unroll 4
     for (int k = from; k < to; ++k) {
       const int64_t where = place(k);
-      const float e = fast_exp2(r * a.left_time[where]);
-      left = fmaf(e, left, a.left_state[where * N + n]);
-      decay *= e;
+      const float t = a.left_time[where], half = half_decay(t, r);
+      left = fmaf(left * half, half, a.left_state[where * N + n]);
+      time += t;
     }
   }
-  shares[0][group][i] = decay;
+  shares[0][group][i] = time;
   shares[1][group][i] = left;
   __syncthreads();
   if (!real) return;
   const float* first = BACK ? a.dlast : a.first;
   float x = in && first ? first[column * a.states + n] : 0.0f;
-  for (int g = 0; g < group; ++g) x = fmaf(shares[0][g][i], x, shares[1][g][i]);
+  for (int g = 0; g < group; ++g) {
+    const float half = half_decay(shares[0][g][i], r);
+    x = fmaf(x * half, half, shares[1][g][i]);
+  }
 #pragma unroll 4
   for (int k = from; k < to; ++k) {
     const int64_t where = place(k);
-    const float gone = a.left_state[where * N + n], time = a.left_time[where];
+    const float gone = a.left_state[where * N + n], half = half_decay(a.left_time[where], r);
     a.left_state[where * N + n] = x;
-    x = fmaf(fast_exp2(r * time), x, gone);
+    x = fmaf(x * half, half, gone);
   }
   if (to == count && (from < to || group == 0)) a.left_state[place(count) * N + n] = x;
 }

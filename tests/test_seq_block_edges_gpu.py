@@ -5,7 +5,7 @@ torch = pytest.importorskip("torch")
 
 from helpers import block_definitions as D  # noqa: E402
 from paper_2202_01258_amd import seq as S  # noqa: E402
-from test_seq_block_gpu import BF16, E32, F16, F32, TYPES, rand, same, scan_inputs, wide, within  # noqa: E402
+from test_seq_block_gpu import BF16, E32, F32, FLUSH, rand, same, scan_inputs, wide, within  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -68,7 +68,7 @@ def scan_pass(s, g):
     return dict(zip(("o", "last", "du", "ddelta", "da", "db", "dc", "dskip", "dgate", "dbias", "dstate"), (o, last, *got)))
 
 
-def as_defined(got, want, roundings, what):
+def as_defined(got, want, roundings, what, flush=FLUSH):
     """Equal where the definition gives an infinity, within the bound where it gives a number; where it gives
     none (infinities of both signs meet) anything may come."""
     value, mag = want
@@ -77,7 +77,7 @@ def as_defined(got, want, roundings, what):
     assert torch.equal(v[infinite], value[infinite]), (what, v[infinite], value[infinite])
     finite = known & ~infinite
     assert mag[finite].isfinite().all() and finite.any() + infinite.any() > 0, what
-    within(got.cpu()[finite], (value[finite], mag[finite]), roundings, what)
+    within(got.cpu()[finite], (value[finite], mag[finite]), roundings, what, flush)
 
 
 def positive(batch, rows, width, states, dtype, seed=1):
@@ -157,3 +157,73 @@ def test_scan_of_infinities_in_segments(states, which, row, rows, width):
     for name, n in (("du", states), ("ddelta", states), ("da", rows), ("db", width), ("dc", width), ("dskip", rows), ("dgate", states),
                     ("dbias", states + rows), ("dstate", 0)):
         as_defined(got[name], want[name], 2 * path + 32 + n, name)
+
+
+def steady(rows, states, step, rate, width=5):
+    """One episode whose states decay or grow by e^(step rate) a row."""
+    s, g = positive(1, rows, width, states, F32)
+    s["delta"], s["bias"] = torch.zeros_like(s["delta"]), torch.full_like(s["bias"], float(torch.expm1(torch.tensor(step).double()).log()))
+    return dict(s, a=torch.full_like(s["a"], rate)), g
+
+
+@pytest.mark.parametrize("rows,step,rate", [(40, 4.0, 1.0), (300, 4.0, 1.0), (1057, 1.0, 1.0), (1057, 4.0, 1.0), (300, 4.0, -1.0),
+                                            (1057, 1.0, -1.0), (1057, 4.0, -1.0), (300, 30.0, -3.0)])
+@pytest.mark.parametrize("states", [4, 13, 32])
+def test_scan_decays_beyond_the_range(rows, step, rate, states):
+    """Over a piece of an episode, or some of them, states grow or decay by more than float32 holds: what is 0
+    stays 0, what is infinite stays so, and what is small may grow."""
+    names = (("du", states), ("ddelta", states), ("da", rows), ("db", 5), ("dc", 5), ("dskip", rows), ("dgate", states),
+             ("dbias", states + rows), ("dstate", 0))
+    path = (16 + 6 * step * abs(rate)) * (rows + 2)
+
+    def check(s, g):
+        want, _ = D.scan(**{k: wide(v) for k, v in s.items()}, ends=[rows], do=wide(g["do"]), dlast=wide(g["dlast"]))
+        got = scan_pass(s, g)
+        as_defined(got["o"], want["o"], path + states + 16, "o")
+        as_defined(got["last"], want["last"], path, "last")
+        # Every term of da has a row's decay as a factor.  Where that is below 2^-126 (e^-90 = 2^-129.8), it is 0 in
+        # float32, and with it all of da: the bound is then the sum of its terms' magnitudes, 300 * 30 * h * dh * 2^-129.8.
+        lost = float(want["da"][1].max()) if step * rate < -87.3 else 0.0
+        # Where states grow, so do gradients on their way to the first row, beyond 2^128: in float32 those rows
+        # have infinities to be multiplied by zeros.  Rows within the range are compared: du = dt sum dh b + ..., of positive
+        # terms with b of at least 1/8 and dt of at least 1, so that a dh is at most 8 du, below 2^127.
+        du = want["du"][0].abs().amax(-1)[0]
+        held = (du < 2.0 ** 124) if rate > 0 else torch.ones(rows, dtype=torch.bool)
+        assert held.any()
+        for name, n in names:
+            v, w = got[name].cpu(), want[name]
+            if name in ("du", "ddelta", "db", "dc", "dgate"):
+                v, w = v[:, held], (w[0][:, held], w[1][:, held])
+            elif not held.all():
+                continue
+            as_defined(v, w, 2 * path + 32 + n, name, FLUSH + (lost if name == "da" else 0.0))
+        assert not got["du"].cpu()[:, held].isnan().any() and got["du"].cpu()[0, du > 2.0 ** 129].isinf().any(-1).all()
+
+    if step > 10:                                     # a row's decay is 0 in float32 by itself
+        return check(*steady(rows, states, step, rate))
+    # from 0 to the last rows' inputs, and from nothing behind to the first rows' gradients
+    s, g = steady(rows, states, step, rate)
+    s["state"] = torch.zeros_like(s["state"])
+    s["u"][:, :-3] = 0
+    g["do"], g["dlast"] = torch.zeros_like(g["do"]), torch.zeros_like(g["dlast"])
+    g["do"][:, -3:] = 1.0
+    check(s, g)
+    s, g = steady(rows, states, step, rate)
+    s["state"] = torch.zeros_like(s["state"])
+    s["u"][:, 3:] = 0
+    s["u"][:, :3] *= 0
+    g["do"][:, 3:] = 0
+    g["dlast"] = torch.zeros_like(g["dlast"])
+    check(s, g)
+    if rate < 0:                                      # infinite states and gradients
+        s, g = steady(rows, states, step, rate)
+        s["state"][0, 2] = float("inf")
+        check(s, g)
+        s, g = steady(rows, states, step, rate)
+        g["dlast"][0, 2] = float("inf")
+        check(s, g)
+    elif rows == 40:                                  # e^160 = 2^230.8
+        s, g = steady(rows, states, step, rate)
+        s["u"], s["state"] = torch.zeros_like(s["u"]), s["state"] * 2.0 ** -121
+        g["do"], g["dlast"] = torch.zeros_like(g["do"]), g["dlast"] * 2.0 ** -121
+        check(s, g)
