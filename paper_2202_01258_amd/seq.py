@@ -921,6 +921,13 @@ def dropout_rng(seed: int, step: int = 0, device="cuda:0"):
     return torch.tensor([seed, step], dtype=torch.int64, device=device)
 
 
+def dropout_threshold(p: float) -> int:
+    """2^16 times the probability of a zero; raises where that is not 0 to 65535."""
+    if not 0.0 <= p < 1.0 or int(p * 65536 + 0.5) > 65535:
+        raise ValueError(f"p: a probability below 1 - 2^-17, not {p}")
+    return int(p * 65536 + 0.5)
+
+
 def _dropout_setup(x, rng, p, site, residual):
     key = ("dropout", x.shape, x.dtype, x.device, _sig(rng), p, site, _sig(residual))
     plan = _plans.get(key)
@@ -928,14 +935,13 @@ def _dropout_setup(x, rng, p, site, residual):
         return plan
     _on_gpu(x, "x")
     code = _code(x, "x")
-    if not 0.0 <= p < 1.0 or int(p * 65536 + 0.5) > 65535:
-        raise ValueError(f"p: a probability below 1 - 2^-17, not {p}")
+    threshold = dropout_threshold(p)
     if not 0 <= site < 1 << 32:
         raise ValueError(f"site: 0 to 2^32 - 1, not {site}")
     _like("rng", rng, x, (2,), torch.int64)
     if residual is not None:
         _like("residual", residual, x, x.shape)
-    cfg = QdsDropoutConfig(ABI_VERSION, code, x.numel(), int(p * 65536 + 0.5), site)
+    cfg = QdsDropoutConfig(ABI_VERSION, code, x.numel(), threshold, site)
     return _remember(key, (cfg, C.byref(cfg)))
 
 

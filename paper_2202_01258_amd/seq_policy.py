@@ -96,6 +96,9 @@ class SequencePolicy(torch.nn.Module):
             raise ValueError(f"width {width}: heads ({heads}) times a multiple of 8")
         if not mixers or any(m not in ("window", "decay", "scan") for m in mixers):
             raise ValueError(f"mixers {mixers}: of window, decay and scan")
+        if not math.isfinite(residual_scale):
+            raise ValueError(f"residual_scale {residual_scale}: a finite number")
+        seq.dropout_threshold(dropout)       # refuses what the layers would
         self.width, self.heads, self.blocks, self.window, self.sinks = width, heads, blocks, window, 1
         self.dim = width // heads
         self.layers = list(mixers) * blocks
