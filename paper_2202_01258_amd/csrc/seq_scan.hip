@@ -74,7 +74,7 @@ template <class T, int S, bool LOCAL, bool GATE, bool TAIL> __global__ __launch_
       float dt[QUADS], uu[QUADS], zz[QUADS];
 #pragma unroll
       for (int i = 0; i < QUADS; ++i) {
-        dt[i] = left.keep(i, softplus(number<T>(d[i]) + bias).dt);
+        dt[i] = left.keep(i, softplus<T>(number<T>(d[i]) + bias).dt);
         uu[i] = number<T>(u[i]);
         if (GATE) zz[i] = number<T>(z[i]);
       }
@@ -159,7 +159,7 @@ template <class T, int S, bool TAIL> __global__ __launch_bounds__(kBlock) void k
   load<T, S>(bv, (const T*)row_of<T>(a.b, b, 0) + n);
   load<T, S>(cv, (const T*)row_of<T>(a.c, b, 0) + n);
   const float u = to_f32(row_of<T>(a.u, b, 0)[at]);
-  const float dt = softplus(to_f32(row_of<T>(a.delta, b, 0)[at]) + (a.bias ? a.bias[at] : 0.0f)).dt;
+  const float dt = softplus<T>(to_f32(row_of<T>(a.delta, b, 0)[at]) + (a.bias ? a.bias[at] : 0.0f)).dt;
 #pragma unroll
   for (int s = 0; s < S; ++s) {
     h[s] = fmaf(fast_exp2(dt * rate(r[s])), h[s], dt * u * bv[s]);

@@ -62,7 +62,7 @@ template <class T, int S, bool GATE> __global__ __launch_bounds__(256) void k_sc
       float dt[QUADS], dy[QUADS];
 #pragma unroll
       for (int i = 0; i < QUADS; ++i) {
-        dt[i] = left.keep(i, softplus(number<T>(d[i]) + bias).dt);
+        dt[i] = left.keep(i, softplus<T>(number<T>(d[i]) + bias).dt);
         dy[i] = number<T>(g[i]);
         if (GATE) {
           const float zz = number<T>(z[i]);
@@ -213,7 +213,7 @@ template <class T, int S, bool GATE> __device__ inline void by_rows(uint32_t ite
 #pragma unroll 1
     for (int r = 0; r <= k; ++r) {
       u = r < rows ? to_f32(row_of<T>(a.u, b, t + r)[at]) : 0.0f;
-      step = softplus(r < rows ? to_f32(row_of<T>(a.delta, b, t + r)[at]) + bias : 0.0f);
+      step = softplus<T>(r < rows ? to_f32(row_of<T>(a.delta, b, t + r)[at]) + bias : 0.0f);
       if (r >= rows) step.dt = 0.0f;
       load_floats<S>(bv, lds + r * 2 * N);
 #pragma unroll
@@ -431,7 +431,7 @@ template <class T, int S, int COLS, bool GATE, bool TAIL> __global__ __launch_bo
 #pragma unroll
         for (int i = 0; i < QUADS; ++i) {
           if (!TAIL) gd[i] = number<T>(d[i]);
-          const Step step = softplus(gd[i] + bias);
+          const Step step = softplus<T>(gd[i] + bias);
           dt[i] = left.keep(i, real ? step.dt : 0.0f);
           slope[i] = step.slope;
           uu[i] = TAIL ? gu[i] : number<T>(u[i]);

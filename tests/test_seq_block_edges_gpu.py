@@ -5,7 +5,7 @@ torch = pytest.importorskip("torch")
 
 from helpers import block_definitions as D  # noqa: E402
 from paper_2202_01258_amd import seq as S  # noqa: E402
-from test_seq_block_gpu import BF16, E32, F32, FLUSH, rand, same, scan_inputs, wide, within  # noqa: E402
+from test_seq_block_gpu import BF16, E32, F16, F32, FLUSH, rand, same, scan_inputs, wide, within  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -227,3 +227,25 @@ def test_scan_decays_beyond_the_range(rows, step, rate, states):
         s["u"], s["state"] = torch.zeros_like(s["u"]), s["state"] * 2.0 ** -121
         g["do"], g["dlast"] = torch.zeros_like(g["do"]), g["dlast"] * 2.0 ** -121
         check(s, g)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_scan_steps_by_themselves(dtype):
+    """log(1 + e^x) as the new state of a row with u = b = 1 and no state before it.  Roundings, in units of 2^-24:
+    the exponential, whose argument's own rounding is taken back, 2 and 1 for that; w = 1 + e, which moves log(w) / (w - 1) by
+    half of its 1; the logarithm and the reciprocal 2 each, log 2 and three products 1 each; the last sum 1: 13 in all
+    (a product with u and one with b are exact).  With 16-bit inputs the argument's rounding stays, 1 |x|, and that of
+    log2(e) as a float, 0.25 |x|; below e^-87, 2^-126, a step is 0."""
+    x = torch.cat([torch.linspace(-80.0, 80.0, 1 << 18), torch.linspace(-8.0, 1.0, 1 << 18), -torch.logspace(-30, 1.9, 1 << 16),
+                   torch.logspace(-30, 30, 1 << 16)]).to(dtype).cuda().view(-1, 1024)
+    if dtype == F16:
+        x = x.clamp(max=60000.0)
+    one = torch.ones(x.shape[0], 1, device="cuda", dtype=dtype)
+    a = torch.full((1024, 1), -1.0, device="cuda")
+    want = torch.logaddexp(x.double(), torch.zeros((), device="cuda").double())[..., None]
+    _, by_step = S.selective_scan_step(torch.ones_like(x), x, a, one, one, torch.zeros(*x.shape, 1, device="cuda"))
+    _, by_rows, _ = S.selective_scan_forward(torch.ones_like(x)[:, None], x[:, None], a, one[:, None], one[:, None])
+    for got in (by_step, by_rows):
+        off = (got.double() - want).abs() / want / E32
+        bound = 13 + (0.0 if dtype == F32 else 1.25) * x.double().abs()[..., None]
+        assert (off <= bound).all(), float((off / bound).max())
