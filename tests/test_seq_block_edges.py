@@ -92,3 +92,14 @@ def test_scan_keeps_only_for_inputs_with_gradients(stand_ins, which):
     assert S.selective_scan(**tensors)[0].requires_grad
     assert S.selective_scan(**{k: v if k == which or k in NAMES else None for k, v in tensors.items()})[0].requires_grad
     assert stand_ins == [False, True, True]
+
+
+def test_scan_scratch_memory(lib):
+    """Shares of db and dc, 2 * 16 floats for 64 columns of a row, are nearly all of it; of da, dskip and dbias there
+    is one for each of the 32 episodes, which are whole.  Counts that leave places in four lanes add what the threads
+    of 32 * 16 workgroups may save: 2 * 4 + 2 floats each."""
+    shares, rest = 32 * 1000 * 16 * 2 * 16 * 4, 32 * 1024 * (16 + 2) * 4
+    assert bytes_of(lib.qds_selective_scan_backward_workspace, scan(batch=32, length=1000, width=1024))[1] == shares + rest
+    saved = 32 * 16 * 256 * 10 * 4
+    assert bytes_of(lib.qds_selective_scan_backward_workspace,
+                    scan(batch=32, length=1000, width=1024, states=13))[1] == shares + rest + saved

@@ -249,3 +249,44 @@ def test_scan_steps_by_themselves(dtype):
         off = (got.double() - want).abs() / want / E32
         bound = 13 + (0.0 if dtype == F32 else 1.25) * x.double().abs()[..., None]
         assert (off <= bound).all(), float((off / bound).max())
+
+
+def test_norms_and_dropout_beyond_31_bits():
+    """Rows that start more than 2^31 elements into their tensors, inputs and outputs, each with numbers of its
+    own; dropout of more than 2^32 elements."""
+    big = torch.zeros((1 << 31) + (1 << 30), dtype=BF16, device="cuda")
+    w1, w2 = 1 + 0.2 * rand(700, seed=3), 1 + 0.2 * rand(700, seed=4)
+    for at in range(5):                               # x, gate, residual, dy, dh: one of them far, the others near
+        near = [rand(6, 700, dtype=BF16, seed=10 + i) for i in range(5)]
+        far = list(near)
+        far[at] = big.as_strided((6, 700), ((1 << 29) + 40, 1))
+        far[at].copy_(near[at])
+        out = []
+        for x, g, r, dy, dh in (near, far):
+            y, h, rstds = S.branch_norm_forward(x, g, r, w1, w2, 0.5)
+            out.append((y, h, rstds) + S.branch_norm_backward(dy, dh, x, g, r, rstds, w1, w2, 0.5))
+        assert same(*out), at
+    del big, far
+    rows = (1 << 21) + 8                              # of 1024: the last eight start at 2^31 and behind it
+    x = torch.randn(rows, 1024, device="cuda", dtype=BF16)
+    w = 1 + 0.2 * rand(1024, seed=5)
+    y, h, rstds = S.branch_norm_forward(x, x, x, w, w)
+    ty, th, trstds = S.branch_norm_forward(x[-8:], x[-8:], x[-8:], w, w)
+    assert torch.equal(y[-8:], ty) and torch.equal(h[-8:], th) and torch.equal(rstds[:, -8:], trstds)
+    assert not torch.equal(y[-8:], y[:8])
+    del y, h
+    got = S.branch_norm_backward(x, x, x, x, x, rstds, w, w)
+    tail = S.branch_norm_backward(*[x[-8:]] * 5, trstds, w, w)
+    assert all(torch.equal(got[i][-8:], tail[i]) for i in range(3))
+    del x, got
+    n = (1 << 32) + 4099
+    x = torch.ones(n, dtype=BF16, device="cuda")
+    rng, site, limit = S.dropout_rng(5, 6), 2, 16384
+    places = [(1 << 31) - 1000, (1 << 32) - 1000, n - 2000]
+    for i, at in enumerate(places):
+        x[at:at + 2000] = rand(2000, dtype=BF16, seed=20 + i)
+    y = S.dropout_forward(x, rng, limit / 65536, site, residual=x)
+    for at in places:
+        keep = torch.tensor([d >= limit for d in D.draws(range(at, at + 2000), 5, 6, site)])
+        v = wide(x[at:at + 2000])
+        within(y[at:at + 2000], (v + keep * v * (65536 / (65536 - limit)), v.abs() * (1 + 65536 / (65536 - limit))), 4, "y")
