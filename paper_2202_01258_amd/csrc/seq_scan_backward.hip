@@ -640,6 +640,8 @@ constexpr int64_t kWorkgroups = 1024;       // each leaves a share of da
 constexpr int kRaggedRows = 128, kRaggedRounds = 4;
 constexpr int kCols = 64;
 
+constexpr int64_t kMostRows = 1 << 25;      // of all episodes: k_scan_sums takes a workgroup for four of them at 32 states
+
 struct Plan {
   Cut pieces, parts;
   int col_blocks, shares;
@@ -675,7 +677,7 @@ bool fits(const qds_scan_config* c) {
   const Plan p = plan_of(c, false);
   const int64_t most = most_blocks(kJoinBlock);
   return (int64_t)c->batch <= most / (ceil_div(c->width, 64) * p.pieces.segs) && joinable(c, p.pieces.segs) &&
-         (int64_t)c->batch * c->length <= most * 2;
+         (int64_t)c->batch * c->length <= kMostRows;
 }
 
 }  // namespace

@@ -103,3 +103,13 @@ def test_scan_scratch_memory(lib):
     saved = 32 * 16 * 256 * 10 * 4
     assert bytes_of(lib.qds_selective_scan_backward_workspace,
                     scan(batch=32, length=1000, width=1024, states=13))[1] == shares + rest + saved
+
+
+@pytest.mark.parametrize("batch,length,status", [(1, 1 << 25, S.OK), (1 << 12, 1 << 13, S.OK), (3, 11184810, S.OK),
+                                                 (1, (1 << 25) + 1, S.ERR_UNSUPPORTED), (1 << 13, (1 << 12) + 1, S.ERR_UNSUPPORTED)])
+@pytest.mark.parametrize("states", [1, 16, 32])
+def test_scan_backward_takes_2_to_the_25_rows(lib, batch, length, status, states):
+    """batch times length as the header has it; the forward pass takes more."""
+    c = scan(batch=batch, length=length, states=states)
+    assert bytes_of(lib.qds_selective_scan_backward_workspace, c)[0] == status
+    assert bytes_of(lib.qds_selective_scan_workspace, c)[0] == S.OK

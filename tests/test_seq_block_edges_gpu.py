@@ -290,3 +290,16 @@ def test_norms_and_dropout_beyond_31_bits():
         keep = torch.tensor([d >= limit for d in D.draws(range(at, at + 2000), 5, 6, site)])
         v = wide(x[at:at + 2000])
         within(y[at:at + 2000], (v + keep * v * (65536 / (65536 - limit)), v.abs() * (1 + 65536 / (65536 - limit))), 4, "y")
+
+
+def test_scan_backward_of_2_to_the_25_rows():
+    """As many rows as the backward pass takes: its first and last episodes against the definition."""
+    batch, rows, states = 1 << 15, 1 << 10, 2
+    s, g = scan_inputs(batch, rows, 1, states, BF16)
+    got = scan_pass(s, g)
+    some = [0, batch - 1]
+    one = {k: wide(v[some]) if k in ("u", "delta", "b", "c", "gate", "state") else wide(v) for k, v in s.items()}
+    want, top = D.scan(**one, ends=[rows] * 2, do=wide(g["do"][some]), dlast=wide(g["dlast"][some]))
+    path = (16 + 6 * top) * (rows + 2)
+    for name, n in (("o", states), ("last", 0), ("du", states), ("ddelta", states), ("db", 1), ("dc", 1), ("dgate", states), ("dstate", 0)):
+        within(got[name][some], want[name], 2 * path + 32 + n, name)
