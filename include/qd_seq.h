@@ -30,6 +30,8 @@
  *     function gives; its content means nothing before or after the call.
  *   - Calls keep no state: they may run on any streams and threads, as long
  *     as calls that run at the same time have workspaces of their own.
+ *   - Outputs overlap neither inputs nor each other, except where a call says
+ *     that one may be another.
  *   - Results do not depend on timing: no sum is formed by atomics.
  *   - Empty tensors (no rows, batch 0, length 0) are valid and launch nothing,
  *     except that outputs that are sums over them are still written.
@@ -245,8 +247,8 @@ qds_status qds_causal_conv(const qds_conv_config* c, qds_rows x, const void* wei
                            const void* state_in, const int32_t* lengths, qds_rows y, void* state_out,
                            void* stream);
 
-/* dx (0 from row n on), dweight, dbias (may be null) and dstate_in (may be null)
- * from dy, dstate_out (null: 0) and what the forward call saw. */
+/* dx (0 from row n on; neither dy nor x), dweight, dbias (may be null) and dstate_in
+ * (may be null) from dy, dstate_out (null: 0) and what the forward call saw. */
 qds_status qds_causal_conv_backward_workspace(const qds_conv_config* c, uint64_t* bytes);
 qds_status qds_causal_conv_backward(const qds_conv_config* c, qds_rows dy, qds_rows x, const void* weight,
                                     const void* bias, const void* state_in, const void* dstate_out,
@@ -294,8 +296,8 @@ qds_status qds_selective_scan(const qds_scan_config* c, qds_rows u, qds_rows del
 
 /* Gradients from do and dstate_out (null: 0), contiguous: du, ddelta, dgate (null
  * without a gate) [batch][length][width] and db, dc [batch][length][states] of dtype,
- * 0 from row n on; da, dskip, dbias (the last two may be null) and dstate_in (may be
- * null; not dstate_out) fp32.  batch times length is at most 2^25 (else
+ * 0 from row n on, none of them an input; da, dskip, dbias (the last two may be null)
+ * and dstate_in (may be null; not dstate_out) fp32.  batch times length is at most 2^25 (else
  * QDS_ERR_UNSUPPORTED). */
 qds_status qds_selective_scan_backward_workspace(const qds_scan_config* c, uint64_t* bytes);
 qds_status qds_selective_scan_backward(const qds_scan_config* c, qds_rows dout, qds_rows u, qds_rows delta,

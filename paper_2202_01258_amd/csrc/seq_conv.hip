@@ -444,6 +444,8 @@ extern "C" qds_status qds_causal_conv_backward(const qds_conv_config* c, qds_row
   if (c->batch > 0 && c->length > 0 && (!dy.data || !x.data || !dx.data)) return QDS_ERR_INVALID_ARG;
   if (dstate_in && dstate_in == dstate_out) return QDS_ERR_INVALID_ARG;
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
+  // a chunk reads rows of the next one
+  if (dx.data && (dx.data == dy.data || dx.data == x.data)) return QDS_ERR_INVALID_ARG;
   ConvArgs a = args_of(c);
   a.x = rows(x);
   a.dy = rows(dy);

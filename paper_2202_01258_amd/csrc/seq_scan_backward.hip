@@ -713,6 +713,9 @@ extern "C" qds_status qds_selective_scan_backward(const qds_scan_config* c, qds_
   if (workspace_bytes < need) return QDS_ERR_WORKSPACE_TOO_SMALL;
   for (qds_rows* r : {&dout, &u, &delta, &b, &cc, &gate})
     if (!near_rows(*r, c->length)) return QDS_ERR_UNSUPPORTED;
+  for (const void* to : {du, ddelta, dgate})                                // blocks may be gone through again
+    for (const qds_rows& from : {dout, u, delta, gate})
+      if (to && to == from.data) return QDS_ERR_INVALID_ARG;
   const Plan p = plan_of(c, lengths != nullptr);
   ScanArgs a = scan_args(c);
   a.u = rows(u);

@@ -9,7 +9,7 @@ torch = pytest.importorskip("torch")
 import torch.autograd.forward_ad as forward_ad  # noqa: E402
 
 from paper_2202_01258_amd import seq as S  # noqa: E402
-from test_seq_block_abi import P, bytes_of, rows, scan  # noqa: E402
+from test_seq_block_abi import P, bytes_of, conv, rows, scan  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -113,3 +113,24 @@ def test_scan_backward_takes_2_to_the_25_rows(lib, batch, length, status, states
     c = scan(batch=batch, length=length, states=states)
     assert bytes_of(lib.qds_selective_scan_backward_workspace, c)[0] == status
     assert bytes_of(lib.qds_selective_scan_workspace, c)[0] == S.OK
+
+
+def test_backward_passes_refuse_gradients_in_place(lib):
+    """A gradient is written where other workgroups (the convolution's next rows) or a later look (the scan's
+    blocks that are gone through again) still read the inputs.  With no address that could be followed the call ends
+    at the check, or at the launch for want of a device."""
+    c = conv()
+    need = bytes_of(lib.qds_causal_conv_backward_workspace, c)[1]
+    for dy, x in ((2 * P, P), (P, 2 * P)):            # dx is at P
+        assert lib.qds_causal_conv_backward(C.byref(c), rows(dy), rows(x), P, P, P, P, None, rows(), P, P, P + 4096, P, need,
+                                            None) == S.ERR_INVALID_ARG
+    c = scan()
+    need = bytes_of(lib.qds_selective_scan_backward_workspace, c)[1]
+    for out in range(3):                              # du, ddelta, dgate
+        for place in range(4):                        # dout, u, delta, gate
+            do, u, delta, gate = [rows((16 + i) * P) for i in range(4)]
+            to = [(32 + i) * P for i in range(3)]
+            to[out] = (16 + place) * P
+            assert lib.qds_selective_scan_backward(
+                C.byref(c), do, u, delta, P, rows(), rows(), P, gate, P, P, P, None, to[0], to[1], 40 * P, 41 * P, 42 * P, 43 * P,
+                to[2], 44 * P, 45 * P, 46 * P, need, None) == S.ERR_INVALID_ARG
