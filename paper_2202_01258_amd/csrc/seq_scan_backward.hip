@@ -1,9 +1,10 @@
 // seq_scan_backward.hip -- gradients of the selective state space scan.  The C ABI is in
 // include/qd_seq.h, the layout of the work in seq_scan.hpp.
 //
-// Bound by the vector units: 97 vector instructions for a row of 16 columns and 16 states, which
-// are issued 88% of the time (32 episodes of up to 1000 rows x 512 bfloat16, 176 us).  Two waves a SIMD is what the states
-// in registers leave; three, with fewer of them kept, took 1.07 of the time.
+// Bound by the vector units: 97 vector instructions for a row of 16 columns and 16 states.  In 32 episodes of up
+// to 1000 rows x 512 bfloat16 (184 us under the tracer) they are issued in 88% of the time in which a SIMD has its two
+// waves, and in 73% of the kernel's: episodes that end leave places that are not filled.  Two waves a SIMD is what
+// the states in registers leave; three, with fewer of them kept, took 1.07 of the time.
 #include <algorithm>
 
 #include "seq_scan.hpp"
@@ -405,7 +406,7 @@ template <class T, int S, int COLS, bool GATE, bool TAIL> __global__ __launch_bo
           }
           odd = __builtin_amdgcn_ballot_w64(top >= 0x1p60f) != 0;
         }
-        if (odd) {
+        if (__builtin_expect(odd, 0)) {
           Saved* p = saved_at<S>();
 #pragma unroll
           for (int s = 0; s < S; ++s) {
@@ -529,7 +530,7 @@ template <class T, int S, int COLS, bool GATE, bool TAIL> __global__ __launch_bo
           if (!KEEP && i == QUADS / 2 && more) fetch(t - K);          // where some states are no longer needed
           __builtin_amdgcn_sched_barrier(0);
         }
-        if (odd) {
+        if (__builtin_expect(odd, 0)) {
           const Saved* p = saved_at<S>();
 #pragma unroll
           for (int s = 0; s < S; ++s) {
@@ -635,8 +636,10 @@ constexpr int kLeastRows = 32;
 constexpr int64_t kWorkgroups = 1024;       // each leaves a share of da
 // Episodes of different lengths leave places: segments that are cut anyway are then shorter, down to
 // 128 rows, for four times the workgroups, which start where others have ended (forward and backward,
-// 32 episodes of up to 1000 rows x 512: 367 us, now 356; 24 of up to 1500 x 384: 382 and 337; episodes
-// of one length lose by it: 32 x 1000 x 512 397 and 424).
+// without and with: 32 episodes of up to 1000 rows x 512 348 and 325 us, 24 of up to 1500 x 384 375 and 331).
+// The host does not know the lengths, only that there are some.  Where all are alike it may lose
+// (32 x 1000 x 512 385 and 411, 16 x 1000 x 1024 385 and 413) or gain (24 x 1500 x 384 398 and 367): a program whose
+// episodes are of one length gives none.
 constexpr int kRaggedRows = 128, kRaggedRounds = 4;
 constexpr int kCols = 64;
 
