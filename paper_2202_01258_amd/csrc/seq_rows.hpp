@@ -1,4 +1,4 @@
-// seq_rows.hpp -- rows of any width, alignment and stride in packs of 16 bytes, and the
+// seq_rows.hpp -- rows of any width, alignment and stride in packs of elements, and the
 // functions of one number that several kernels of libqdseq.so share.
 #pragma once
 
@@ -11,8 +11,8 @@ namespace seq {
 template <class T> __device__ inline float to_f32(T x) { return (float)x; }
 template <class T> __device__ inline T from_f32(float x) { return (T)x; }
 
-// VEC consecutive elements, 16 bytes, at any alignment: rows of odd widths start
-// anywhere.  Where VEC does not divide the width (TAIL), a row's last lane takes its
+// VEC consecutive elements, 16 bytes in the norms and 4 to 32 elsewhere, at any alignment: rows of odd
+// widths start anywhere.  Where VEC does not divide the width (TAIL), a row's last lane takes its
 // last VEC elements, some of which its neighbour has as well: both store the same
 // values, and only the neighbour counts them in sums.  That leaves no branch around
 // the accesses (a branch per element at the row's end let each load wait for the

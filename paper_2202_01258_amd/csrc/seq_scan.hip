@@ -2,10 +2,10 @@
 // include/qd_seq.h, the layout of the work in seq_scan.hpp.
 //
 // Bound by the vector units.  A state of a row takes an exponential (8.2 cycles of a wave on a
-// SIMD), two products and an fma (2.7 each), its output another fma, where a column's row moves 8
-// bytes: at 16 states some 120 cycles for 16 columns (lane moves, softplus and gate included), four
-// times what memory takes for them.  1 x 65536 x 1024 bfloat16: 300 us for the outputs (176 cycles),
-// 243 us for the pieces in front of them.
+// SIMD), two products and an fma (2.7 each), its output another fma: at 16 states 65 cycles for 16
+// columns of a piece's row and 76 of an output's.  With lane moves, transposes, softplus, gate, LDS reads and
+// accesses they take 143 and 176.  1 x 65536 x 1024 bfloat16: 490 us, where the bytes take 111; under the tracer, which
+// lengthens it to 556, 243 us for the pieces, 13 to join them and 300 for the outputs.
 #include <algorithm>
 
 #include "seq_scan.hpp"
@@ -180,9 +180,12 @@ template <class T, int S, bool TAIL> __global__ __launch_bounds__(kBlock) void k
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-// Two waves on each SIMD do without cuts; fewer are cut to eight (one piece costs what 0.4 of a
-// main pass does).  16 states, bfloat16, 48 x 1000 x 1024: 239 us whole, 302 cut; 1 x 65536 x 1024: 634 us
-// cut for two waves, 522 for eight.  (Before b and c were staged by eight rows, which took 0.95 of that.)
+// Two waves on each SIMD do without cuts; fewer are cut to eight (a pass over the pieces costs what 0.65 to
+// 0.8 of the main pass does).  Outputs of rows by 1000, bfloat16, whole and cut, in us, by waves:
+//   16 states  1024: 121, 121   1536: 163, 172   1792: 164, 199   2048: 165, 214   2304: 220, 246   3072: 224, 294
+//    4 states  1024:  89,  69   1536: 105, 100   1792: 111, 116   2048: 121, 131   2304: 151, 156   3072: 156, 192
+// so that 16 states could do without from 1536 on.  1 x 65536 x 1024: 634 us cut for two waves, 522 for eight.  (The
+// last two before b and c were staged by eight rows, which took 0.95 of that.)
 constexpr int64_t kWhole = 2048, kWaves = 8192;
 constexpr int kLeastRows = 32;
 

@@ -53,7 +53,7 @@ struct ScanArgs {
 // A kernel's arguments, its only ones, read anew: what is needed once for an episode's part is
 // not kept in scalar registers.  Those are short: the backward pass kept 121 numbers in vector
 // registers' lanes, and took them out within its rows (32 x 1000 x 512 with 16 states, forward and
-// backward: 397 us, now 388).
+// backward: 397 us so, 388 without).
 __device__ inline const ScanArgs& read_args() {
   auto p = (const __attribute__((address_space(4))) ScanArgs*)__builtin_amdgcn_kernarg_segment_ptr();
   asm volatile("" : "+s"(p));
@@ -180,7 +180,7 @@ template <int S> __device__ inline void store_states(float* p, int at, int q, in
 // Four lanes may hold more states than there are.  Those that are not there are 0 wherever states meet
 // (their rate is -1, so that no step makes them anything else); b and c are 0 for them, which is
 // not enough beside an infinite input or gradient.  Kernels for such counts (TAIL) look for one in
-// each block of rows (13 states, 16 x 1000 x 1024: 397 us for a training pass, 385 without; outputs of 1 x
+// each block of rows (13 states, 16 x 1000 x 1024: 395 us for a training pass, 385 without; outputs of 1 x
 // 16384 x 1024: 137 and 134); masks on each state would be some 8 of a row's 97 instructions.
 template <int S> struct Held {
   int count;                                     // of the lane's states
