@@ -772,7 +772,8 @@ def selective_scan_forward(u, delta, a, b, c, skip=None, gate=None, bias=None, s
     0).  `lengths` as for causal_conv_forward.  All arithmetic is float32.
 
     Rows that are not finite reach the rows behind them (those of b and c in every column), as
-    in the definition.
+    in the definition.  batch times width, each row of columns rounded up to a multiple of 64, is
+    below 2^30.
 
     Returns o, the state behind the last row, and with `keep` what selective_scan_backward
     needs of this pass (else None)."""
