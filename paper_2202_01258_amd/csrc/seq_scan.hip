@@ -182,8 +182,8 @@ template <class T, int S, bool TAIL> __global__ __launch_bounds__(kBlock) void k
 // ---------------------------------------------------------------------------
 // Two waves on each SIMD do without cuts; fewer are cut to eight (a pass over the pieces costs what 0.65 to
 // 0.8 of the main pass does).  Outputs of rows by 1000, bfloat16, whole and cut, in us, by waves:
-//   16 states  1024: 121, 121   1536: 163, 172   1792: 164, 199   2048: 165, 214   2304: 220, 246   3072: 224, 294
-//    4 states  1024:  89,  69   1536: 105, 100   1792: 111, 116   2048: 121, 131   2304: 151, 156   3072: 156, 192
+//   16 states  1024: 121, 121   1536: 163, 172   1792: 164, 199   2048: 165, 214   2304: 220, 246   4096: 280, 378
+//    4 states  1024:  89,  69   1536: 105, 100   1792: 111, 116   2048: 121, 131   2304: 151, 156   4096: 197, 245
 // so that 16 states could do without from 1536 on.  1 x 65536 x 1024: 634 us cut for two waves, 522 for eight.  (The
 // last two before b and c were staged by eight rows, which took 0.95 of that.)
 constexpr int64_t kWhole = 2048, kWaves = 8192;
