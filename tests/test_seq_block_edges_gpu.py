@@ -303,3 +303,68 @@ def test_scan_backward_of_2_to_the_25_rows():
     path = (16 + 6 * top) * (rows + 2)
     for name, n in (("o", states), ("last", 0), ("du", states), ("ddelta", states), ("db", 1), ("dc", 1), ("dgate", states), ("dstate", 0)):
         within(got[name][some], want[name], 2 * path + 32 + n, name)
+
+
+def check_pass(s, g, ends, width, states):
+    """A pass over finite numbers against the definition; no gate where there is none."""
+    batch, rows = s["u"].shape[:2]
+    w = {k: wide(v) for k, v in s.items() if v is not None}
+    if s["gate"] is None:
+        w["gate"] = torch.full((batch, rows, width), 1.2784645427610738).double()        # silu is 1 here
+    want, top = D.scan(**w, ends=ends, do=wide(g["do"]), dlast=wide(g["dlast"]))
+    got = scan_pass(dict(s, lengths=torch.tensor(ends, dtype=torch.int32, device="cuda")), g)
+    path = (16 + 6 * top) * (rows + 2)
+    within(got["o"], want["o"], path + states + 16, "o")
+    within(got["last"], want["last"], path, "last")
+    for name, n in (("du", states), ("ddelta", states), ("da", sum(ends)), ("db", width), ("dc", width), ("dskip", sum(ends)),
+                    ("dgate", states), ("dbias", states + sum(ends)), ("dstate", 0)):
+        if name == "dgate" and s["gate"] is None:
+            assert got[name] is None
+            continue
+        within(got[name], want[name], 2 * path + 32 + n, name)
+
+
+@pytest.mark.parametrize("states", [1, 4, 8, 13, 16, 24, 32])
+@pytest.mark.parametrize("dtype,gate", [(F32, True), (BF16, True), (F32, False)])
+@pytest.mark.parametrize("which", ["b", "u", "state", "a"])
+def test_scan_of_large_numbers(states, dtype, gate, which):
+    """Finite numbers that may become infinite take the careful way through a block: the last of an episode, or all
+    of them where four lanes have places left."""
+    batch, rows, width = 3, 45, 70
+    s, g = scan_inputs(batch, rows, width, states, dtype)
+    if which == "b":
+        s["b"], s["c"] = s["b"] * 2.0 ** 20, s["c"] * 2.0 ** -20
+    elif which == "u":
+        s["u"] = s["u"] * 2.0 ** 61
+    elif which == "state":
+        s["state"] = s["state"] * 2.0 ** 70
+    else:
+        s["a"] = s["a"].abs() * 2.0 ** -6             # states that grow
+    if not gate:
+        s["gate"] = None
+    check_pass(s, g, [rows, 12, 33], width, states)
+
+
+@pytest.mark.parametrize("states", [4, 13, 16, 32])
+def test_scan_careful_blocks_stay_by_themselves(states):
+    """More episodes than workgroups take at once: those whose last row is infinite change nothing in the others,
+    before or behind them in a workgroup's turn."""
+    batch, rows, width = 2200, 11, 70
+    s, g = scan_inputs(batch, rows, width, states, F32)
+    clean = scan_pass(s, g)
+    hit = torch.zeros(batch, dtype=torch.bool)
+    hit[[0, 1, 511, 512, 1023, 1024, 1500, 2199]] = True
+    s["u"][hit.cuda(), -1, 7] = float("inf")
+    got = scan_pass(s, g)
+    for name in ("o", "last", "du", "ddelta", "db", "dc", "dgate", "dstate"):
+        assert torch.equal(got[name].cpu()[~hit], clean[name].cpu()[~hit]), name
+    others = torch.arange(width) != 7
+    # the hit rows' own steps and skips have infinities of both signs as terms: dbias and dskip of column 7 are none of
+    # the numbers to look at; da is, as the row's decay meets the state in front of it
+    assert got["da"].isfinite().all() and got["dbias"].cpu()[others].isfinite().all() and got["dskip"].cpu()[others].isfinite().all()
+    # a column's gradient of a is its own: some of the others against the definition, for the careful way rounds elsewhere
+    some = [0, 6, 8, 63, 64, 69]
+    one = {k: wide(v[..., some] if k in ("u", "delta", "gate", "skip", "bias") else v[:, some] if k == "state" else v[some] if k == "a" else v)
+           for k, v in s.items()}
+    want, top = D.scan(**one, ends=[rows] * batch, do=wide(g["do"][..., some]), dlast=wide(g["dlast"][:, some]))
+    within(got["da"][some], want["da"], 2 * (16 + 6 * top) * (rows + 2) + 32 + batch * rows, "da")
